@@ -284,6 +284,71 @@ int lda_dense_table_noalloc(const int32_t* n_k_dev, int32_t K, int32_t V, double
                             uint32_t* dn_thr32_dev, int32_t* dn_alias_dev, uint64_t* dense_mass_dev,
                             int32_t* status_dev, void* cuda_stream);
 
+/* Operators on rows of logits or probabilities over V words (or topics): what a neural model of the same words needs beside the
+ * sampler -- a teacher's lists and a drafter's loss, and the draws that accept the drafter's tokens (the paper has no
+ * counterpart; the acceptance test is the one of Section 4.1 with an independence proposal).  They need no context: all pointers
+ * are DEVICE memory of the current GPU, the work is queued on `cuda_stream` (a cudaStream_t of that GPU, NULL = default stream),
+ * and the call returns without waiting for it.  Nothing is allocated and no state is kept, so calls on different streams and host
+ * threads may overlap, and a call may be captured into a graph.
+ *
+ *   dtype    LDA_F32, LDA_F16 or LDA_BF16: the rows' element type (aligned to an element)
+ *   rows     0 .. 2^31-1; 0 is legal and does nothing
+ *   V        1 .. LDA_ROW_MAX_V words per row, consecutive in memory
+ *   stride   elements from one row to the next, 0 .. 2^31 (0: the same row again); rows that are written need >= V
+ *
+ * LDA_EINVAL: NULL where a pointer is needed, unknown dtype, negative size, a misaligned row, a temperature outside [1e-6, 1e6];
+ * LDA_ERANGE: sizes beyond the limits; LDA_ECUDA: the launch failed.  The contents of DEVICE memory are not looked at by the
+ * call; the kernels read and write nothing outside the rows and lists that the arguments describe, whatever ids and offsets hold. */
+#define LDA_F32 0
+#define LDA_F16 1
+#define LDA_BF16 2
+#define LDA_ROW_MAX_V 1048576
+#define LDA_TOP_MAX 512
+
+/* The `top` (1..LDA_TOP_MAX) largest logits of every row: ids[rows][top] and values[rows][top] (element type of the logits), value
+ * descending, equal values by the lower word; NaN comes first.  Words at minus infinity are masked: they are never listed, and
+ * places that no word is left for have id -1 and value minus infinity.  lse[rows] (may be NULL): log sum_v exp(x_v / temperature);
+ * minus infinity for a row that is masked whole, NaN where a NaN is in the row. */
+int lda_top_logits(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride, int32_t top,
+                   double temperature, int32_t* ids_dev, void* values_dev, float* lse_dev, void* cuda_stream);
+
+/* Distillation from a teacher's top logits.  Per row the student's logits x, and a list of `top` (1..LDA_TOP_MAX) words ids with
+ * the teacher's logits values (type values_dtype; rows of both lie list_stride elements apart).  An id outside [0, V) is padding.
+ *   q = softmax(x / tau);   p_j = softmax(values / tau) over the list (teacher_lse NULL), or
+ *   p_j = exp(values_j / tau - teacher_lse) and P = max(0, 1 - sum p_j) for all words outside the list, whose q add up to Q
+ *   (teacher_lse[rows]: the teacher's log sum exp(x / tau) over its whole row, as lda_top_logits gives it)
+ *   loss = tau^2 ( sum_j p_j (log p_j - log q_{ids_j}) + P (log P - log Q) )
+ * Where the student has no mass outside the list the last term is left out.  A word that the list holds twice counts with both
+ * entries.  A row whose list holds nothing but padding has loss 0 and gradient 0. */
+int lda_distill_loss(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride,
+                     const int32_t* ids_dev, const void* values_dev, int values_dtype, int32_t top, int64_t list_stride,
+                     const float* teacher_lse_dev, double temperature, float* loss_dev, void* cuda_stream);
+
+/* Gradient of sum_r weights[r] loss[r] with respect to the student's logits (weights NULL: all 1), in the logits' element type,
+ * and the losses too if loss is not NULL.  A row of weight 0 has gradient 0, whatever its logits hold.  grad may be the logits
+ * themselves (same stride); any other overlap is not allowed. */
+int lda_distill_grad(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride,
+                     const int32_t* ids_dev, const void* values_dev, int values_dtype, int32_t top, int64_t list_stride,
+                     const float* teacher_lse_dev, double temperature, const float* weights_dev, float* loss_dev,
+                     void* grad_dev, int64_t grad_stride, void* cuda_stream);
+
+/* Verification of drafted tokens against the target's probabilities.  Sequence b has the drafts [offsets[b], offsets[b+1]) of
+ * drafts[n_drafts], its rows of draft_probs (n_drafts rows) at the same places, and one row more of target (n_drafts + n_seqs
+ * rows): rows offsets[b] + b .. offsets[b+1] + b, the last one behind its last draft.  Probabilities need not add up to 1.
+ *   - draft i is accepted iff accept_u[i] * q(x_i) < p(x_i), exactly (draft_probs NULL: q(x_i) = 1); a draft outside [0, V) is
+ *     not.  The leading accepted drafts stand.
+ *   - one token follows, drawn with draw_u[b] from the masses max(p - q, 0) of the first draft that was not accepted (draft_probs
+ *     NULL: p without that draft), or from p of the last row.  A mass is floor(2^42 x), x cut to [0, 1], NaN as 0; masses are
+ *     added up as whole numbers, and the token is the first whose running sum exceeds floor(total floor(2^32 u) / 2^32).  Rows
+ *     without any such mass are drawn from p itself, and where p has none either the token is -1.  (u: cut to [0, 1 - 2^-32].)
+ * tokens[n_drafts + n_seqs]: at the places of the sequence's target rows, the accepted drafts, the drawn token, then -1.
+ * accepted[n_seqs]: how many drafts stood.  Offsets that do not run upwards inside [0, n_drafts] give accepted = -1 and leave
+ * the sequence's tokens as they were; so are places that belong to no sequence. */
+int lda_verify_drafts(const int64_t* draft_offsets_dev, int64_t n_seqs, const int32_t* drafts_dev, int64_t n_drafts,
+                      const void* target_dev, int64_t target_stride, const void* draft_probs_dev, int64_t probs_stride,
+                      int dtype, int32_t V, const float* accept_u_dev, const float* draw_u_dev, int32_t* tokens_dev,
+                      int32_t* accepted_dev, void* cuda_stream);
+
 int lda_get_stats(lda_ctx* ctx, lda_stats* out);
 
 /* Message of the last failure on this context (library-owned, valid until the next call). */

@@ -18,12 +18,15 @@ from . import build as _build
 
 LDA_OK, LDA_EINVAL, LDA_ERANGE, LDA_ESTATE, LDA_ENOMEM, LDA_ECUDA, LDA_EINTERNAL = 0, -1, -2, -3, -4, -5, -6
 LDA_NK, LDA_NWK, LDA_NDK = 0, 1, 2
+LDA_F32, LDA_F16, LDA_BF16 = 0, 1, 2
+LDA_ROW_MAX_V, LDA_TOP_MAX = 1048576, 512
 
 EXPORTS = [
     "lda_create", "lda_set_stream", "lda_set_allocator", "lda_set_option", "lda_set_proposals", "lda_load_corpus", "lda_load_corpus_device",
     "lda_set_shard", "lda_word_counts_to_dense", "lda_word_counts_from_dense", "lda_init", "lda_set_assignments", "lda_set_assignments_u16", "lda_sweep", "lda_gibbs_sweep", "lda_loglik", "lda_get_counts",
     "lda_get_assignments", "lda_get_assignments_u16", "lda_get_assignments_async", "lda_get_assignments_u16_async", "lda_wait", "lda_get_tables", "lda_get_stats", "lda_last_error", "lda_destroy",
     "lda_dense_table_noalloc",
+    "lda_top_logits", "lda_distill_loss", "lda_distill_grad", "lda_verify_drafts",
 ]
 
 
@@ -99,6 +102,11 @@ def load_library(path: str | None = None):
     L.lda_get_tables.argtypes = [vp, vp, vp, i64, vp, vp, vp, C.POINTER(u64)]
     L.lda_get_stats.argtypes = [vp, C.POINTER(lda_stats)]
     L.lda_dense_table_noalloc.argtypes = [vp, i32, i32, dbl, vp, vp, vp, vp, vp]
+    L.lda_top_logits.argtypes = [vp, C.c_int, i64, i32, i64, i32, dbl, vp, vp, vp, vp]
+    lists = [vp, C.c_int, i64, i32, i64, vp, vp, C.c_int, i32, i64, vp, dbl]
+    L.lda_distill_loss.argtypes = lists + [vp, vp]
+    L.lda_distill_grad.argtypes = lists + [vp, vp, vp, i64, vp]
+    L.lda_verify_drafts.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, C.c_int, i32, vp, vp, vp, vp, vp]
     L.lda_last_error.argtypes = [vp]
     L.lda_last_error.restype = C.c_char_p
     L.lda_destroy.argtypes = [vp]
@@ -280,6 +288,33 @@ def lda_dense_table_noalloc(n_k_ptr, K, V, beta, dn_thr32_ptr, dn_alias_ptr, den
         C.c_void_p(n_k_ptr), K, V, beta, C.c_void_p(dn_thr32_ptr), C.c_void_p(dn_alias_ptr),
         C.c_void_p(dense_mass_ptr), C.c_void_p(status_ptr) if status_ptr else None,
         C.c_void_p(cuda_stream) if cuda_stream else None)
+
+
+# Operators on rows (raw DEVICE pointers or None; queued on ``cuda_stream``, the launch status is returned).  ``rows`` has
+# them for torch tensors.
+
+def lda_top_logits(logits_ptr, dtype, rows, V, row_stride, top, temperature, ids_ptr, values_ptr, lse_ptr=None, cuda_stream=None):
+    return load_library().lda_top_logits(logits_ptr, dtype, rows, V, row_stride, top, temperature, ids_ptr, values_ptr, lse_ptr,
+                                         cuda_stream)
+
+
+def lda_distill_loss(logits_ptr, dtype, rows, V, row_stride, ids_ptr, values_ptr, values_dtype, top, list_stride, teacher_lse_ptr,
+                     temperature, loss_ptr, cuda_stream=None):
+    return load_library().lda_distill_loss(logits_ptr, dtype, rows, V, row_stride, ids_ptr, values_ptr, values_dtype, top,
+                                           list_stride, teacher_lse_ptr, temperature, loss_ptr, cuda_stream)
+
+
+def lda_distill_grad(logits_ptr, dtype, rows, V, row_stride, ids_ptr, values_ptr, values_dtype, top, list_stride, teacher_lse_ptr,
+                     temperature, weights_ptr, loss_ptr, grad_ptr, grad_stride, cuda_stream=None):
+    return load_library().lda_distill_grad(logits_ptr, dtype, rows, V, row_stride, ids_ptr, values_ptr, values_dtype, top,
+                                           list_stride, teacher_lse_ptr, temperature, weights_ptr, loss_ptr, grad_ptr,
+                                           grad_stride, cuda_stream)
+
+
+def lda_verify_drafts(offsets_ptr, n_seqs, drafts_ptr, n_drafts, target_ptr, target_stride, probs_ptr, probs_stride, dtype, V,
+                      accept_u_ptr, draw_u_ptr, tokens_ptr, accepted_ptr, cuda_stream=None):
+    return load_library().lda_verify_drafts(offsets_ptr, n_seqs, drafts_ptr, n_drafts, target_ptr, target_stride, probs_ptr,
+                                            probs_stride, dtype, V, accept_u_ptr, draw_u_ptr, tokens_ptr, accepted_ptr, cuda_stream)
 
 
 def lda_get_stats(h):

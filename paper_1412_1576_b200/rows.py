@@ -1,0 +1,205 @@
+"""Operators on rows of logits or probabilities, for callers that hold torch tensors.
+
+What a neural model of the sampler's words needs beside the sampler: a teacher's lists (``top_logits``), a drafter's loss
+against them (``distill_loss``, ``distill_loss_and_grad``), and the test that accepts the drafter's tokens (``verify_drafts``).
+Argument checks and outputs only: the work is done by the entry points of the same purpose in ``include/lda_b200.h``, queued on
+the current stream of the tensors' device.  There is no fallback: tensors that are not on a GPU are refused.
+"""
+
+from __future__ import annotations
+
+import torch
+
+from . import binding as _b
+
+_DTYPES = {torch.float32: _b.LDA_F32, torch.float16: _b.LDA_F16, torch.bfloat16: _b.LDA_BF16}
+
+
+def _rows(x, name):
+    """Checks a matrix whose rows are consecutive in memory; returns (dtype code, rows, V, row stride)."""
+    code = _DTYPES.get(x.dtype)
+    if code is None:
+        raise TypeError(f"{name}: float32, float16 or bfloat16 is needed, not {x.dtype}")
+    if x.dim() != 2 or x.shape[1] < 1:
+        raise ValueError(f"{name}: a matrix with at least one column is needed, not {tuple(x.shape)}")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise ValueError(f"{name}: the words of a row must be consecutive in memory")
+    return code, x.shape[0], x.shape[1], x.stride(0)
+
+
+def _vector(x, name, dtype, n, device):
+    if x.dtype != dtype:
+        raise TypeError(f"{name}: {dtype} is needed, not {x.dtype}")
+    if x.dim() != 1 or x.shape[0] != n:
+        raise ValueError(f"{name}: {n} values are needed, not {tuple(x.shape)}")
+    if n > 1 and x.stride(0) != 1:
+        raise ValueError(f"{name}: must be contiguous")
+    _here(x, name, device)
+    return x.data_ptr()
+
+
+def _here(x, name, device):
+    if x.device != device:
+        raise ValueError(f"{name}: on {x.device}, the rows are on {device}")
+
+
+def _cuda(x, name):
+    if not x.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor is needed (there is no CPU fallback)")
+    return x.device
+
+
+def _call(fn, device, *args):
+    """One library call on the device's current stream."""
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, stream)
+    if rc:
+        raise _b.LdaError(rc, fn.__name__)
+
+
+def top_logits(logits, top: int, temperature: float = 1.0):
+    """The `top` largest logits of every row: (ids int32 [rows, top], values [rows, top], lse float32 [rows]).
+
+    Values descend, equal ones by the lower word.  Words at minus infinity are masked: never listed, and places that no word
+    is left for have id -1 and value minus infinity.  ``lse`` is log sum exp(x / temperature) of the whole row.
+    """
+    device = _cuda(logits, "logits")
+    code, rows, V, stride = _rows(logits, "logits")
+    if not 1 <= top <= _b.LDA_TOP_MAX:
+        raise ValueError(f"top: 1 to {_b.LDA_TOP_MAX}, not {top}")
+    ids = torch.empty((rows, top), dtype=torch.int32, device=device)
+    values = torch.empty((rows, top), dtype=logits.dtype, device=device)
+    lse = torch.empty(rows, dtype=torch.float32, device=device)
+    _call(_b.lda_top_logits, device, logits.data_ptr(), code, rows, V, stride, top, temperature, ids.data_ptr(),
+          values.data_ptr(), lse.data_ptr())
+    return ids, values, lse
+
+
+def _list(ids, values, lse, rows, device):
+    """Checks a teacher's lists; returns the library's arguments for them."""
+    if ids.dtype != torch.int32:
+        raise TypeError(f"ids: int32 is needed, not {ids.dtype}")
+    code = _DTYPES.get(values.dtype)
+    if code is None:
+        raise TypeError(f"values: float32, float16 or bfloat16 is needed, not {values.dtype}")
+    if ids.dim() != 2 or ids.shape[0] != rows or ids.shape != values.shape:
+        raise ValueError(f"ids and values: one list per row, {rows} of them, not {tuple(ids.shape)} and {tuple(values.shape)}")
+    top = ids.shape[1]
+    if not 1 <= top <= _b.LDA_TOP_MAX:
+        raise ValueError(f"ids: lists of 1 to {_b.LDA_TOP_MAX} words, not {top}")
+    if top > 1 and (ids.stride(1) != 1 or values.stride(1) != 1):
+        raise ValueError("ids and values: the places of a list must be consecutive in memory")
+    if rows > 1 and ids.stride(0) != values.stride(0):
+        raise ValueError("ids and values: their rows must lie equally far apart")
+    _here(ids, "ids", device)
+    _here(values, "values", device)
+    teacher_lse = None if lse is None else _vector(lse, "lse", torch.float32, rows, device)
+    return ids.data_ptr(), values.data_ptr(), code, top, ids.stride(0), teacher_lse
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, values, lse, temperature):
+        ctx.save_for_backward(logits, ids, values, lse)
+        ctx.temperature = temperature
+        return _loss(logits, ids, values, lse, temperature)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        logits, ids, values, lse = ctx.saved_tensors
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        _grad(logits, ids, values, lse, ctx.temperature, dloss.contiguous(), None, grad)
+        return grad, None, None, None, None
+
+
+def _loss(logits, ids, values, lse, temperature):
+    device = _cuda(logits, "logits")
+    code, rows, V, stride = _rows(logits, "logits")
+    lists = _list(ids, values, lse, rows, device)
+    loss = torch.empty(rows, dtype=torch.float32, device=device)
+    _call(_b.lda_distill_loss, device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, loss.data_ptr())
+    return loss
+
+
+def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
+    device = _cuda(logits, "logits")
+    code, rows, V, stride = _rows(logits, "logits")
+    lists = _list(ids, values, lse, rows, device)
+    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("grad: must have the logits' type and shape")
+    _rows(grad, "grad")
+    _here(grad, "grad", device)
+    w = None if weights is None else _vector(weights, "weights", torch.float32, rows, device)
+    _call(_b.lda_distill_grad, device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
+          None if loss is None else loss.data_ptr(), grad.data_ptr(), grad.stride(0))
+
+
+def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
+    """Loss of every row of a student's logits against a teacher's top logits: temperature^2 KL(teacher || student), float32 [rows].
+
+    ids, values: the teacher's lists, as ``top_logits`` gives them; an id outside the vocabulary is padding.  lse None: the
+    teacher's distribution is the softmax over the list.  With the teacher's log-sum-exp (taken at the same temperature) it
+    is that of its whole row, and all words outside the list make one bucket more.  Differentiable once with respect to
+    ``logits``; a row that gets the gradient 0 passes 0 on, whatever it holds.
+    """
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return _Distill.apply(logits, ids, values, lse, temperature)
+    return _loss(logits, ids, values, lse, temperature)
+
+
+def distill_loss_and_grad(logits, ids, values, lse=None, temperature: float = 1.0, weights=None, grad=None):
+    """``distill_loss`` and the gradient of sum(weights * loss) with respect to the logits, in one pass over them.
+
+    weights: float32 [rows], None for 1 each; a row of weight 0 has gradient 0.  grad: where the gradient goes, None for a
+    new tensor; the logits themselves are allowed and are overwritten then.  Returns (loss, grad).  No autograd graph is made.
+    """
+    logits = logits.detach()
+    if grad is None:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+    _grad(logits, ids, values, lse, temperature, weights, loss, grad)
+    return loss, grad
+
+
+def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, tokens=None, accepted=None):
+    """Which drafted tokens stand against the target's probabilities, and the token that follows them.
+
+    draft_offsets: int64 [n + 1], sequence b has the drafts [offsets[b], offsets[b + 1]) of ``drafts`` (int32); target: one
+    row per draft and one more behind each sequence's last, [drafts + n, V]; draft_probs: the drafter's rows [drafts, V] in
+    the same type, or None where it put its whole mass on its draft; accept_u [drafts] and draw_u [n]: float32 uniforms.
+    Returns (tokens int32 [drafts + n], accepted int32 [n]): at the places of a sequence's target rows its accepted drafts,
+    the token drawn behind them, then -1.  Both may be given; places of no sequence keep what they hold (-1 in new ones).
+    """
+    device = _cuda(target, "target")
+    code, rows, V, stride = _rows(target, "target")
+    if draft_offsets.dim() != 1 or draft_offsets.shape[0] < 1:
+        raise ValueError("draft_offsets: one more than there are sequences is needed")
+    n_seqs, n_drafts = draft_offsets.shape[0] - 1, drafts.shape[0]
+    if rows != n_drafts + n_seqs:
+        raise ValueError(f"target: {n_drafts} drafts of {n_seqs} sequences need {n_drafts + n_seqs} rows, not {rows}")
+    offsets_ptr = _vector(draft_offsets, "draft_offsets", torch.int64, n_seqs + 1, device)
+    drafts_ptr = _vector(drafts, "drafts", torch.int32, n_drafts, device)
+    probs_ptr, probs_stride = None, 0
+    if draft_probs is not None:
+        if draft_probs.dtype != target.dtype or draft_probs.shape != (n_drafts, V):
+            raise ValueError(f"draft_probs: [{n_drafts}, {V}] of {target.dtype} is needed")
+        _, _, _, probs_stride = _rows(draft_probs, "draft_probs")
+        _here(draft_probs, "draft_probs", device)
+        # (without drafts there is nothing to point at; sequences then have one row each, of the target)
+        probs_ptr = draft_probs.data_ptr() if n_drafts else None
+    accept_ptr = _vector(accept_u, "accept_u", torch.float32, n_drafts, device)
+    draw_ptr = _vector(draw_u, "draw_u", torch.float32, n_seqs, device)
+    if tokens is None:
+        tokens = torch.full((rows,), -1, dtype=torch.int32, device=device)
+    if accepted is None:
+        accepted = torch.empty(n_seqs, dtype=torch.int32, device=device)
+    tokens_ptr = _vector(tokens, "tokens", torch.int32, rows, device)
+    accepted_ptr = _vector(accepted, "accepted", torch.int32, n_seqs, device)
+    _call(_b.lda_verify_drafts, device, offsets_ptr, n_seqs, drafts_ptr, n_drafts, target.data_ptr(), stride, probs_ptr,
+          probs_stride, code, V, accept_ptr, draw_ptr, tokens_ptr, accepted_ptr)
+    return tokens, accepted

@@ -1,0 +1,98 @@
+"""What the operators on rows refuse, before anything reaches a GPU (the statuses of the C ABI, the binding's checks)."""
+import pytest
+import torch
+
+from paper_1412_1576_b200 import binding as b
+from paper_1412_1576_b200 import rows
+
+P = 4096      # an address that is never looked at
+
+
+def top(logits=P, dtype=b.LDA_F32, rows=2, V=10, stride=10, top=3, tau=1.0, ids=P, values=P, lse=P):
+    return b.lda_top_logits(logits, dtype, rows, V, stride, top, tau, ids, values, lse)
+
+
+def loss(logits=P, dtype=b.LDA_F32, rows=2, V=10, stride=10, ids=P, values=P, vt=b.LDA_F32, top=3, ls=3, lse=None, tau=1.0, out=P):
+    return b.lda_distill_loss(logits, dtype, rows, V, stride, ids, values, vt, top, ls, lse, tau, out)
+
+
+def grad(logits=P, dtype=b.LDA_F32, rows=2, V=10, stride=10, ids=P, values=P, vt=b.LDA_F32, top=3, ls=3, lse=None, tau=1.0, w=None,
+         out=None, g=P + 4096, gs=10):
+    return b.lda_distill_grad(logits, dtype, rows, V, stride, ids, values, vt, top, ls, lse, tau, w, out, g, gs)
+
+
+def verify(off=P, n=2, drafts=P, nd=3, p=P, ps=10, q=P, qs=10, dtype=b.LDA_F32, V=10, au=P, du=P, tok=P, acc=P):
+    return b.lda_verify_drafts(off, n, drafts, nd, p, ps, q, qs, dtype, V, au, du, tok, acc)
+
+
+ROWS = [dict(dtype=3), dict(dtype=-1), dict(V=0), dict(V=-5), dict(rows=-1), dict(stride=-1), dict(logits=None), dict(logits=P + 2),
+        dict(logits=P + 1, dtype=b.LDA_BF16), dict(tau=0.0), dict(tau=-1.0), dict(tau=float("nan")), dict(tau=float("inf")),
+        dict(tau=1e-7), dict(top=0), dict(top=-1)]
+TOO_LARGE = [dict(V=b.LDA_ROW_MAX_V + 1, stride=1 << 21), dict(rows=1 << 31), dict(stride=(1 << 31) + 1), dict(top=b.LDA_TOP_MAX + 1)]
+
+
+@pytest.mark.parametrize("call", [top, loss, grad])
+@pytest.mark.parametrize("bad", ROWS, ids=str)
+def test_bad_rows_are_refused(call, bad):
+    assert call(**bad) == b.LDA_EINVAL
+
+
+@pytest.mark.parametrize("call", [top, loss, grad])
+@pytest.mark.parametrize("bad", TOO_LARGE, ids=str)
+def test_rows_beyond_the_limits_are_refused(call, bad):
+    if call is grad and "V" in bad:
+        bad = dict(bad, gs=bad["stride"])
+    assert call(**bad) == b.LDA_ERANGE
+
+
+@pytest.mark.parametrize("bad", [dict(ids=None), dict(values=None)], ids=str)
+def test_lists_are_needed(bad):
+    assert top(**bad) == loss(**bad) == grad(**bad) == b.LDA_EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(vt=3), dict(ls=-1), dict(values=P + 2), dict(values=P + 1, vt=b.LDA_F16)], ids=str)
+def test_bad_lists_are_refused(bad):
+    assert loss(**bad) == grad(**bad) == b.LDA_EINVAL
+
+
+def test_outputs_of_the_loss_are_needed():
+    assert loss(out=None) == b.LDA_EINVAL
+    assert grad(g=None) == b.LDA_EINVAL
+    assert grad(gs=9) == b.LDA_EINVAL                          # rows of the gradient would overlap
+    assert grad(g=P, stride=11, gs=10) == b.LDA_EINVAL         # in place: row for row
+    assert grad(ls=(1 << 31) + 1) == b.LDA_ERANGE
+
+
+@pytest.mark.parametrize("bad", [dict(off=None), dict(drafts=None), dict(p=None), dict(au=None), dict(du=None), dict(tok=None),
+                                 dict(acc=None), dict(n=-1), dict(nd=-1), dict(V=0), dict(ps=-1), dict(qs=-1), dict(dtype=9),
+                                 dict(p=P + 1), dict(q=P + 2), dict(n=0)], ids=str)
+def test_bad_verifications_are_refused(bad):
+    assert verify(**bad) == b.LDA_EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(n=1 << 31), dict(nd=1 << 31), dict(V=b.LDA_ROW_MAX_V + 1), dict(qs=(1 << 31) + 1)], ids=str)
+def test_verifications_beyond_the_limits_are_refused(bad):
+    assert verify(**bad) == b.LDA_ERANGE
+
+
+def test_no_rows_is_nothing_to_do():
+    assert top(rows=0, logits=None, ids=None, values=None, lse=None) == b.LDA_OK
+    assert loss(rows=0, logits=None, ids=None, values=None, out=None) == b.LDA_OK
+    assert grad(rows=0, logits=None, ids=None, values=None, g=None) == b.LDA_OK
+    assert verify(n=0, nd=0, off=None, drafts=None, p=None, q=None, au=None, du=None, tok=None, acc=None) == b.LDA_OK
+
+
+def test_tensors_of_the_host_are_refused():
+    x = torch.zeros(2, 10)
+    ids = torch.zeros(2, 3, dtype=torch.int32)
+    values = torch.zeros(2, 3)
+    with pytest.raises(ValueError, match="CUDA"):
+        rows.top_logits(x, 3)
+    with pytest.raises(ValueError, match="CUDA"):
+        rows.distill_loss(x, ids, values)
+    with pytest.raises(ValueError, match="CUDA"):
+        rows.distill_loss(x.clone().requires_grad_(), ids, values)
+    with pytest.raises(ValueError, match="CUDA"):
+        rows.distill_loss_and_grad(x, ids, values)
+    with pytest.raises(ValueError, match="CUDA"):
+        rows.verify_drafts(torch.zeros(2, dtype=torch.int64), ids[0, :0], x[:1], None, x[0, :0], x[0, :1])
