@@ -28,132 +28,276 @@ struct DistillArgs {
     double tau, inv_tau;
 };
 
-constexpr int DISTILL_THREADS = 256;
+constexpr int DISTILL_THREADS = 512;
+constexpr int DISTILL_GROUPS = 4;  // groups a lane has in flight
+constexpr int DISTILL_CTAS = 8;    // of a cluster, at most
 
-// One CTA per row.  Dynamic shared memory: one bit per word of the vocabulary.
-template <typename T, typename TV>
+// What a CTA knows of its part of the row.
+struct DistillPart {
+    ExpSum out, in;  // over the words outside the list and on it, each word once (without a tail: all words, nothing)
+    float max;
+};
+
+// What the gradient needs of the whole row.
+struct DistillRow {
+    float ref, others;     // 2^(x c - ref) times `others` is the gradient of a word outside the list
+    double w, inv, mass;   // weight tau; 1 / sum of exponentials; W
+};
+
+// Bits of a group's elements in a map with a bit for each element.
+template <typename T>
+__device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
+{
+    const uint32_t byte = ((const uint8_t*)bits)[group * PER<T> / 8];
+    return PER<T> == 8 ? byte : (byte >> (group * PER<T> % 8)) & ((1u << PER<T>) - 1);
+}
+
+// One cluster per row; every CTA has the whole list and a part of the row.  The words of the list are marked in a bit map of that
+// part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The CTAs exchange
+// their sums, and each works out the gradient of its part: the same factor times the exponential for all words, from a second read
+// that L2 answers, then the list's words over it.
+template <typename T, typename TV, bool TAIL, bool GRAD>
 __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
 {
-    extern __shared__ uint32_t listed[];
+    constexpr int R = DISTILL_GROUPS, CHUNK = 32 * R * PER<T>, WARPS = DISTILL_THREADS / 32;
+    constexpr bool BITS = TAIL || GRAD;
+    extern __shared__ uint32_t bits[];
     __shared__ int ids[LDA_TOP_MAX];
     __shared__ float p[LDA_TOP_MAX], x[LDA_TOP_MAX];
-    __shared__ double dred[33];
-    __shared__ float fred[32];
+    __shared__ ExpSum ered[WARPS];
+    __shared__ float fred[WARPS];
+    __shared__ DistillPart parts[2][DISTILL_CTAS];
+    __shared__ DistillRow whole;
     __shared__ int s_any, s_twice;
-    const int tid = threadIdx.x, V = a.V;
-    const int64_t r = blockIdx.x;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
+    const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
-    T* grad = a.grad ? (T*)a.grad + r * a.grad_stride : nullptr;
-    const float weight = a.weights && grad ? a.weights[r] : 1.0f;
-    const int words = (V + 31) / 32;
-    for (int i = tid; i < words; i += DISTILL_THREADS) listed[i] = 0;
+    T* grad = GRAD ? (T*)a.grad + r * a.grad_stride : nullptr;
+    const float weight = GRAD && a.weights ? a.weights[r] : 1.0f;
+    const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
+    // this CTA's words, and the word of the map's first bit
+    const int bit0 = chunk_first<T, R>(split.chunk0, split.pre);
+    const int v0 = max(0, bit0), v1 = max(v0, min(V, chunk_first<T, R>(split.chunk1, split.pre)));
     if (tid == 0) s_any = s_twice = 0;
+    if (BITS)
+        for (int i = tid; i < (split.chunk1 - split.chunk0) * (CHUNK / 32); i += DISTILL_THREADS) bits[i] = 0;
     __syncthreads();
+    const TV* values = (const TV*)a.values + r * a.list_stride;
     for (int j = tid; j < a.top; j += DISTILL_THREADS) {
         const int id = a.ids[r * a.list_stride + j];
         const bool ok = id >= 0 && id < V;
         ids[j] = ok ? id : -1;
+        p[j] = row_value(values[j]);
         if (ok) {
             s_any = 1;
-            if (atomicOr(&listed[id >> 5], 1u << (id & 31)) >> (id & 31) & 1) s_twice = 1;
+            if (BITS && id >= v0 && id < v1) {
+                const int bit = id - bit0;
+                if (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
+            }
             x[j] = row_value(row[id]);
         }
     }
     __syncthreads();
-    if (!s_any || (weight == 0.0f && !a.loss)) {
-        if (a.loss && tid == 0) a.loss[r] = 0.0f;
-        if (grad)
-            for (int v = tid; v < V; v += DISTILL_THREADS) grad[v] = row_element<T>(0.0f);
+    if (!s_any || (GRAD && weight == 0.0f && !a.loss)) {  // (the same in every CTA of the cluster)
+        if (a.loss && rank == 0 && tid == 0) a.loss[r] = 0.0f;
+        if (GRAD)
+            for (int v = v0 + tid; v < v1; v += DISTILL_THREADS) grad[v] = row_element<T>(0.0f);
         return;
     }
-    // the teacher's side
-    const TV* values = (const TV*)a.values + r * a.list_stride;
-    double t_ref = 0.0, base;  // log p = (t - t_ref) / tau - base
-    if (a.teacher_lse) base = (double)a.teacher_lse[r];
-    else {
-        float tm = -INFINITY;
-        for (int j = tid; j < a.top; j += DISTILL_THREADS)
-            if (ids[j] >= 0) tm = fmaxf(tm, row_value(values[j]));
-        tm = block_reduce_max(tm, fred);
-        double z = 0;
-        for (int j = tid; j < a.top; j += DISTILL_THREADS)
-            if (ids[j] >= 0) z += (double)expf((float)(((double)row_value(values[j]) - (double)tm) * a.inv_tau));
-        z = block_reduce_sum(z, dred);
-        t_ref = tm == -INFINITY ? 0.0 : (double)tm;
-        base = tm == -INFINITY ? INFINITY : log(z);  // nothing but minus infinity: no mass
-    }
-    double sum_p = 0;
-    for (int j = tid; j < a.top; j += DISTILL_THREADS) {
-        float e = 0.0f;
-        if (ids[j] >= 0) {
-            const float t = row_value(values[j]);
-            e = t == -INFINITY ? 0.0f : expf((float)(((double)t - t_ref) * a.inv_tau - base));
-        }
-        p[j] = e;
-        sum_p += (double)e;
-    }
-    sum_p = block_reduce_sum(sum_p, dred);
-    // the student's side
-    float m = -INFINITY;
-    for (int v = tid; v < V; v += DISTILL_THREADS) m = fmaxf(m, row_value(row[v]));
-    m = block_reduce_max(m, fred);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float in = 0.0f, out = 0.0f;
-    for (int v = tid; v < V; v += DISTILL_THREADS) {
-        const float e = exp2_unit((row_value(row[v]) - ref) * a.scale);
-        if (listed[v >> 5] >> (v & 31) & 1) in += e;
-        else out += e;
-    }
-    in = block_reduce_sum(in, fred);
-    out = block_reduce_sum(out, fred);
-    const double total = (double)in + (double)out;
-    const double log_total = total == 0 ? 0.0 : log(total);  // (a row without mass: log q is minus infinity everywhere)
-    const double p_rest = a.teacher_lse && out != 0.0f ? fmax(0.0, 1.0 - sum_p) + (sum_p != sum_p ? sum_p : 0.0) : 0.0;
-    const double q_rest = total > 0 || total != total ? (double)out / total : 0.0;
-    if (a.loss) {
-        double l = 0;
-        for (int j = tid; j < a.top; j += DISTILL_THREADS)
-            if (p[j] > 0.0f || p[j] != p[j])
-                l += (double)p[j] * ((((double)row_value(values[j]) - t_ref) * a.inv_tau - base) -
-                                     (((double)x[j] - (double)ref) * a.inv_tau - log_total));
-        l = block_reduce_sum(l, dred);
-        if (p_rest != 0.0) l += p_rest * log(p_rest / q_rest);
-        if (tid == 0) a.loss[r] = (float)(l * a.tau * a.tau);
-    }
-    if (!grad) return;
-    const double mass = sum_p + p_rest;
-    const double inv = total == 0 ? 0.0 : 1.0 / total;
-    const double w = (double)weight * a.tau;
-    const float others = weight == 0.0f ? 0.0f : (float)(w * inv * (p_rest != 0.0 ? mass - p_rest / q_rest : mass));
-    __syncthreads();
-    for (int v = tid; v < V; v += DISTILL_THREADS)
-        if (!(listed[v >> 5] >> (v & 31) & 1))
-            grad[v] = row_element<T>(weight == 0.0f ? 0.0f : exp2_unit((row_value(row[v]) - ref) * a.scale) * others);
-    for (int j = tid; j < a.top; j += DISTILL_THREADS) {
-        if (ids[j] < 0) continue;
-        double pj = (double)p[j];
+    cluster_arrive();
+    // which place of the list stands for a word that it holds twice: the first
+    auto leads = [&](int j) {
         bool first = true;
         if (s_twice)
-            for (int o = 0; o < a.top; ++o)
-                if (o != j && ids[o] == ids[j]) {
-                    first = first && o > j;
-                    pj += (double)p[o];
+            for (int o = 0; o < j; ++o) first = first && ids[o] != ids[j];
+        return first;
+    };
+    // the teacher (warp 0): log p = (t - t_ref) / tau - base
+    double t_ref = 0.0, base = 0.0, sum_p = 0.0;
+    ExpSum in = ExpSum::none();
+    if (warp == 0) {
+        if (TAIL) base = (double)a.teacher_lse[r];
+        else {
+            float tm = -INFINITY;
+            for (int j = lane; j < a.top; j += 32)
+                if (ids[j] >= 0) tm = fmaxf(tm, p[j]);
+            tm = warp_reduce_max(tm);
+            double z = 0;
+            for (int j = lane; j < a.top; j += 32)
+                if (ids[j] >= 0) z += (double)expf((float)(((double)p[j] - (double)tm) * a.inv_tau));
+            z = warp_reduce_sum(z);
+            t_ref = tm == -INFINITY ? 0.0 : (double)tm;
+            base = tm == -INFINITY ? INFINITY : log(z);  // nothing but minus infinity: no mass
+        }
+        for (int j = lane; j < a.top; j += 32) {
+            const float t = p[j];
+            const float e = ids[j] < 0 || t == -INFINITY ? 0.0f : expf((float)(((double)t - t_ref) * a.inv_tau - base));
+            p[j] = e;
+            sum_p += (double)e;
+            // the student's words on the list
+            if (TAIL && ids[j] >= v0 && ids[j] < v1 && leads(j)) {
+                in.raise(exp_ref(x[j], a.scale));
+                in.sum += exp2_unit(__fmaf_rn(x[j], a.scale, -in.ref));
+            }
+        }
+        sum_p = warp_reduce_sum(sum_p);
+        if (TAIL) in.warp_reduce();
+    }
+    // the student's words outside the list
+    ExpSum out = ExpSum::none();
+    float m = -INFINITY;
+    // (masked: with minus infinity in the list's places)
+    auto load = [&](int c, uint4 (&raw)[R], float& top) {
+        load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
+        top = groups_max<T, R>(raw);
+        if (TAIL) {
+            const int g = (c - split.chunk0) * 32 * R + lane;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const uint32_t marked = group_bits<T>(bits, g + 32 * k);
+                if (marked) {
+                    union {
+                        uint4 raw;
+                        T e[PER<T>];
+                    } u;
+                    u.raw = raw[k];
+#pragma unroll
+                    for (int i = 0; i < PER<T>; ++i)
+                        if (marked >> i & 1) u.e[i] = row_element<T>(-INFINITY);
+                    raw[k] = u.raw;
                 }
-        const float e = exp2_unit((x[j] - ref) * a.scale);
-        if (first) grad[ids[j]] = row_element<T>(weight == 0.0f ? 0.0f : (float)(w * ((double)e * inv * mass - pj)));
+            }
+        }
+    };
+    for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
+        uint4 raw[R];
+        float top;
+        load(c, raw, top);
+        m = fmaxf(m, top);  // (a NaN goes into the sums)
+        add_groups<T, R>(out, raw, top, a.scale);
+    }
+    out.warp_reduce();
+    m = warp_reduce_max(m);
+    if (lane == 0) ered[warp] = out, fred[warp] = m;
+    __syncthreads();
+    if (warp == 0) {
+        out = lane < WARPS ? ered[lane] : ExpSum::none();
+        out.warp_reduce();
+        m = warp_reduce_max(lane < WARPS ? fred[lane] : -INFINITY);
+    }
+    cluster_wait();
+    if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = DistillPart{out, in, m};
+    cluster.sync();
+    m = parts[0][0].max;
+    for (int k = 1; k < ctas; ++k) m = fmaxf(m, parts[0][k].max);
+    const bool far = exp_far(m, a.scale);
+    if (far) {  // (the same in every CTA of the cluster)
+        float o = 0.0f, l = 0.0f;
+        for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
+            uint4 raw[R];
+            float top;
+            load(c, raw, top);
+            for (int k = 0; k < R; ++k) {
+                float y[PER<T>];
+                unpack<T>(raw[k], y);
+                for (int i = 0; i < PER<T>; ++i) o += exp2_unit((y[i] - m) * a.scale);
+            }
+        }
+        if (TAIL && warp == 0)
+            for (int j = lane; j < a.top; j += 32)
+                if (ids[j] >= v0 && ids[j] < v1 && leads(j)) l += exp2_unit((x[j] - m) * a.scale);
+        o = warp_reduce_sum(o);
+        l = warp_reduce_sum(l);
+        if (lane == 0) fred[warp] = o;
+        __syncthreads();
+        if (warp == 0) o = warp_reduce_sum(lane < WARPS ? fred[lane] : 0.0f);
+        if (tid < ctas) *cluster.map_shared_rank(&parts[1][rank], tid) = DistillPart{{0.0f, o}, {0.0f, l}, m};
+        cluster.sync();
+    }
+    auto exponent = [&](float y, float ref) { return far ? (y - m) * a.scale : __fmaf_rn(y, a.scale, -ref); };
+    if (warp == 0) {
+        out = parts[far][0].out, in = parts[far][0].in;
+        for (int k = 1; k < ctas; ++k) {
+            out.add(parts[far][k].out);
+            in.add(parts[far][k].in);
+        }
+        const float ref = fmaxf(out.ref, in.ref);
+        const double s_out = ldexp((double)out.sum, (int)(out.ref - ref)), total = s_out + ldexp((double)in.sum, (int)(in.ref - ref));
+        const double p_rest = TAIL && s_out != 0 ? fmax(0.0, 1.0 - sum_p) + (sum_p != sum_p ? sum_p : 0.0) : 0.0;
+        const double q_rest = total == 0 ? 0.0 : s_out / total;
+        if (a.loss && rank == 0) {
+            const double log2_total = total == 0 ? 0.0 : (double)log2f((float)total);  // (without mass log q is minus infinity)
+            double l = 0;
+            for (int j = lane; j < a.top; j += 32)
+                if (p[j] > 0.0f || p[j] != p[j]) {
+                    const double y = far ? ((double)x[j] - (double)m) * (double)a.scale : (double)x[j] * (double)a.scale - (double)ref;
+                    l += (double)p[j] * ((((double)row_value(values[j]) - t_ref) * a.inv_tau - base) - (y - log2_total) * LN2);
+                }
+            l = warp_reduce_sum(l);
+            if (p_rest != 0.0) l += p_rest * log(p_rest / q_rest);
+            if (lane == 0) a.loss[r] = (float)(l * a.tau * a.tau);
+        }
+        if (GRAD && lane == 0) {
+            whole.ref = ref;
+            whole.w = (double)weight * a.tau;
+            whole.inv = total == 0 ? 0.0 : 1.0 / total;
+            whole.mass = sum_p + p_rest;
+            whole.others = (float)(whole.w * whole.inv * (p_rest != 0.0 ? whole.mass - p_rest / q_rest : whole.mass));
+        }
+    }
+    if (!GRAD) return;
+    __syncthreads();
+    const float ref = whole.ref, others = whole.others;
+    const bool abreast = (uintptr_t)grad % 16 == (uintptr_t)row % 16;
+    for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
+        const int first = chunk_first<T, R>(c, split.pre);
+        if (weight != 0.0f && abreast && !far && chunk_inside<T, R>(first, V)) {
+            uint4 raw[R];
+            load_chunk<T, R>(row, first, V, row_element<T>(-INFINITY), raw);
+            uint4* to = reinterpret_cast<uint4*>(grad + first) + lane;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                float y[PER<T>];
+                unpack<T>(raw[k], y);
+#pragma unroll
+                for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit(__fmaf_rn(y[i], a.scale, -ref)) * others;
+                __stcs(to + 32 * k, pack<T>(y));
+            }
+        } else {
+#pragma unroll 4
+            for (int i = lane; i < CHUNK; i += 32) {
+                const int v = first + i;
+                if (v >= 0 && v < V)
+                    grad[v] = row_element<T>(weight == 0.0f ? 0.0f : exp2_unit(exponent(row_value(row[v]), ref)) * others);
+            }
+        }
+    }
+    if (weight == 0.0f) return;
+    __syncthreads();  // the list's words over the rest
+    for (int j = tid; j < a.top; j += DISTILL_THREADS) {
+        if (ids[j] < v0 || ids[j] >= v1 || !leads(j)) continue;
+        double pj = (double)p[j];
+        if (s_twice)
+            for (int o = j + 1; o < a.top; ++o)
+                if (ids[o] == ids[j]) pj += (double)p[o];
+        grad[ids[j]] = row_element<T>((float)(whole.w * ((double)exp2_unit(exponent(x[j], ref)) * whole.inv * whole.mass - pj)));
     }
 }
 
 template <typename T, typename TV>
 static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t st)
 {
-    const size_t smem = (size_t)(a.V + 31) / 32 * 4;
-    if (smem > 32 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k_distill<T, TV>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (e != cudaSuccess) return e;
-    }
-    k_distill<T, TV><<<(unsigned)rows, DISTILL_THREADS, smem, st>>>(a);
-    return cudaGetLastError();
+    constexpr int CHUNK = 32 * DISTILL_GROUPS * PER<T>;
+    const int ctas = row_ctas(rows, (int64_t)a.V * sizeof(T), 4, 8192, DISTILL_CTAS);
+    const bool tail = a.teacher_lse, grad = a.grad;
+    // a bit for every word of a CTA's part
+    const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
+    const size_t smem = tail || grad ? (size_t)((chunks + ctas - 1) / ctas) * (CHUNK / 8) : 0;
+    const auto kernel = tail ? (grad ? k_distill<T, TV, true, true> : k_distill<T, TV, true, false>)
+                             : (grad ? k_distill<T, TV, false, true> : k_distill<T, TV, false, false>);
+    return launch_rows(kernel, a, rows, ctas, DISTILL_THREADS, smem, st);
 }
 
 template <typename T>

@@ -1,15 +1,24 @@
 // Shared pieces of the operators on rows of logits or probabilities (toplogits.cu, distill.cu, verify.cu): element types,
 // 2^x, keys that order values, reductions over a CTA.
 #pragma once
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/lda_b200.h"
 
 namespace lda {
+
+namespace cg = cooperative_groups;
+
+// The two halves of a cluster's barrier: shared memory of the others may be written once `wait` has returned (they all run then).
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double LN2 = 0.69314718055994531;
@@ -17,6 +26,10 @@ constexpr double LN2 = 0.69314718055994531;
 __device__ __forceinline__ float row_value(float x) { return x; }
 __device__ __forceinline__ float row_value(__half x) { return __half2float(x); }
 __device__ __forceinline__ float row_value(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+constexpr bool T_is_bf16 = false;
+template <>
+constexpr bool T_is_bf16<__nv_bfloat16> = true;
 template <typename T>
 __device__ __forceinline__ T row_element(float x);
 template <>
@@ -58,6 +71,226 @@ __device__ __forceinline__ float block_reduce_max(float v, float* smem)
     if (lane == 0) smem[warp] = v;
     __syncthreads();
     return warp_reduce_max(lane < nw ? smem[lane] : -INFINITY);
+}
+
+// --- a row in 16-byte groups, split over the CTAs of a cluster -------------------------------------------------------------------
+// Rows start at any element, groups at addresses that are multiples of 16: group g of a row holds its elements
+// g PER - pre .. g PER - pre + PER - 1, where `pre` elements of the first group lie before the row (not read, like those behind its
+// end).  A warp takes 32 R consecutive groups at a time (a chunk; lane l the groups l, 32 + l, ...), and the CTAs of a cluster take
+// runs of consecutive chunks.
+template <typename T>
+constexpr int PER = 16 / (int)sizeof(T);
+
+struct RowSplit {
+    int pre, chunk0, chunk1;  // this CTA's chunks
+    template <typename T, int R>
+    static __device__ __forceinline__ RowSplit of(const T* row, int V, int rank, int ctas)
+    {
+        RowSplit s;
+        s.pre = (int)((uintptr_t)row % 16 / sizeof(T));
+        const int chunks = (int)(((unsigned)(s.pre + V) + 32 * R * PER<T> - 1) / (32 * R * PER<T>));
+        s.chunk0 = (int)((long long)chunks * rank / ctas);
+        s.chunk1 = (int)((long long)chunks * (rank + 1) / ctas);
+        return s;
+    }
+};
+
+// A chunk's first element, and whether all of it lies inside the row.
+template <typename T, int R>
+__device__ __forceinline__ int chunk_first(int chunk, int pre) { return chunk * (32 * R * PER<T>) - pre; }
+template <typename T, int R>
+__device__ __forceinline__ bool chunk_inside(int first, int V) { return first >= 0 && first + 32 * R * PER<T> <= V; }
+
+// A group at the row's edge: element by element, `fill` outside the row.
+template <typename T>
+__device__ __forceinline__ uint4 edge_group(const T* row, int first, int V, T fill)
+{
+    union {
+        uint4 raw;
+        T e[PER<T>];
+    } g;
+#pragma unroll
+    for (int i = 0; i < PER<T>; ++i) g.e[i] = first + i >= 0 && first + i < V ? row[first + i] : fill;
+    return g.raw;
+}
+
+// The lane's groups of a chunk.  (Loads that pass L1 by: what is read twice is read from L2 the second time.)
+template <typename T, int R>
+__device__ __forceinline__ void load_chunk(const T* row, int first, int V, T fill, uint4 (&raw)[R])
+{
+    const int lane = threadIdx.x & 31;
+    if (chunk_inside<T, R>(first, V)) {
+        const uint4* p = reinterpret_cast<const uint4*>(row + first) + lane;
+#pragma unroll
+        for (int r = 0; r < R; ++r) raw[r] = __ldcg(p + 32 * r);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) raw[r] = edge_group(row, first + (32 * r + lane) * PER<T>, V, fill);
+    }
+}
+
+// A group's values.
+template <typename T>
+__device__ __forceinline__ void unpack(uint4 g, float (&x)[PER<T>])
+{
+    if constexpr (sizeof(T) == 4) {
+        x[0] = __uint_as_float(g.x), x[1] = __uint_as_float(g.y), x[2] = __uint_as_float(g.z), x[3] = __uint_as_float(g.w);
+    } else {
+        const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (T_is_bf16<T>) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                x[2 * i] = f.x, x[2 * i + 1] = f.y;
+            }
+        }
+    }
+}
+
+// --- sums of exponentials in one pass ---------------------------------------------------------------------------------------------
+// 2^(x c - R) is added up with R the largest x c met so far, rounded down.  With R whole, moving a sum from one R to another
+// is exact, and x c - R is rounded once (a fused multiply-add).  |R| <= 2^22 keeps R c's rounding out; rows whose maximum lies
+// beyond that (the type's lowest value as a mask, say) are added up again as 2^((x - maximum) c): `far`.
+constexpr float REF_MOST = 4194304.0f;
+__device__ __forceinline__ float exp_ref(float max, float c) { return fminf(fmaxf(floorf(max * c), -REF_MOST), REF_MOST); }
+__device__ __forceinline__ bool exp_far(float max, float c) { return max != -INFINITY && !(fabsf(max * c) < REF_MOST); }
+
+// 2^d for a whole number d <= 0.
+__device__ __forceinline__ float exp2_whole(float d) { return d < -126.0f ? 0.0f : __int_as_float((127 + (int)d) << 23); }
+
+struct ExpSum {
+    float ref, sum;
+    static __device__ __forceinline__ ExpSum none() { return ExpSum{-REF_MOST, 0.0f}; }
+    __device__ __forceinline__ void raise(float to)
+    {
+        if (to > ref) {
+            sum *= exp2_whole(ref - to);
+            ref = to;
+        }
+    }
+    __device__ __forceinline__ void add(ExpSum o)
+    {
+        raise(o.ref);
+        sum += o.sum * exp2_whole(o.ref - ref);
+    }
+    // Of the warp; every lane has it.
+    __device__ __forceinline__ void warp_reduce()
+    {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) add(ExpSum{__shfl_xor_sync(0xffffffffu, ref, o), __shfl_xor_sync(0xffffffffu, sum, o)});
+    }
+};
+
+// The larger of two values, NaN if one of them is.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+// Largest value of N groups (NaN if there is one).
+template <typename T, int N>
+__device__ __forceinline__ float groups_max(const uint4 (&raw)[N])
+{
+    if constexpr (sizeof(T) == 4) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            float x[4];
+            unpack<T>(raw[r], x);
+            m = max_nan(m, max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3])));
+        }
+        return m;
+    } else {
+        // two at a time
+        using T2 = std::conditional_t<T_is_bf16<T>, __nv_bfloat162, __half2>;
+        auto two = [](uint32_t w) { return *reinterpret_cast<T2*>(&w); };
+        T2 m = two(raw[0].x);
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+            m = __hmax2_nan(m, __hmax2_nan(__hmax2_nan(two(raw[r].x), two(raw[r].y)), __hmax2_nan(two(raw[r].z), two(raw[r].w))));
+        return max_nan(row_value(m.x), row_value(m.y));
+    }
+}
+
+// Adds N groups to a sum.  `max`: not below any of their values.
+template <typename T, int N>
+__device__ __forceinline__ void add_groups(ExpSum& s, const uint4 (&raw)[N], float max, float c)
+{
+    s.raise(exp_ref(max, c));
+    float part[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        float x[PER<T>];
+        unpack<T>(raw[r], x);
+#pragma unroll
+        for (int i = 0; i < PER<T>; ++i) x[i] = exp2_unit(__fmaf_rn(x[i], c, -s.ref));
+#pragma unroll
+        for (int w = PER<T> / 2; w > 0; w /= 2)
+#pragma unroll
+            for (int i = 0; i < w; ++i) x[i] += x[i + w];
+        part[r] = x[0];
+    }
+#pragma unroll
+    for (int r = 1; r < N; ++r) part[0] += part[r];
+    s.sum += part[0];
+}
+
+// A group of values, each rounded once.
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&x)[PER<T>])
+{
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (T_is_bf16<T>) {
+                const __nv_bfloat162 two = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&two);
+            } else {
+                const __half2 two = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&two);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// How many CTAs share a row: as many (a power of two, at most `most`) as it takes for `rows` of them to give every
+// multiprocessor `per_sm` CTAs, unless a CTA's share falls below `least` bytes.
+inline int row_ctas(int64_t rows, int64_t row_bytes, int per_sm, int64_t least, int most)
+{
+    int c = 1;
+    while (c < most && rows * c < 148 * per_sm && row_bytes >= 2 * c * least) c *= 2;
+    return c;
+}
+
+// Launches `rows` clusters of `ctas` CTAs.
+template <typename Args>
+inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t rows, int ctas, int threads, size_t smem, cudaStream_t st)
+{
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((unsigned)(rows * ctas));
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)ctas;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    c.attrs = &at;
+    c.numAttrs = 1;
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaLaunchKernelEx(&c, kernel, args);
 }
 
 // Sizes that every one of the operators refuses.

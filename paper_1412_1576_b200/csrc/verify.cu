@@ -22,7 +22,10 @@ struct VerifyArgs {
     int32_t V;
 };
 
-constexpr int VERIFY_THREADS = 256;
+constexpr int VERIFY_THREADS = 512;
+constexpr int VERIFY_GROUPS = 4;  // groups of each row a lane has in flight
+constexpr int VERIFY_CTAS = 8;    // of a cluster, at most
+constexpr int VERIFY_CHUNKS = LDA_ROW_MAX_V / (32 * VERIFY_GROUPS * PER<float>) + 1;
 
 // A probability as a multiple of 2^-42: NaN and what is below zero as 0, what is above one as 1.
 __device__ __forceinline__ unsigned long long prob_mass(float r)
@@ -30,85 +33,164 @@ __device__ __forceinline__ unsigned long long prob_mass(float r)
     return __float2ull_rz(fminf(fmaxf(r, 0.0f), 1.0f) * 4398046511104.0f);
 }
 
+// One cluster per sequence.  Every CTA finds the first draft that is refused by itself (the sequences are short), then each adds
+// up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk, and one
+// warp reads that again to find the word.  Bound by the read of one row of the target and, behind a refusal, one of the drafter.
 template <typename T, bool PROBS>
 __global__ void __launch_bounds__(VERIFY_THREADS) k_verify(VerifyArgs a)
 {
-    __shared__ unsigned long long red[33];
-    __shared__ int s_first, s_token;
-    const int64_t b = blockIdx.x, lo = a.offsets[b], hi = a.offsets[b + 1];
-    if (lo < 0 || hi < lo || hi > a.n_drafts) {
-        if (threadIdx.x == 0) a.accepted[b] = -1;
+    constexpr int R = VERIFY_GROUPS, CHUNK = 32 * R * PER<T>;
+    __shared__ unsigned long long sums[VERIFY_CHUNKS], red[33], parts[2][VERIFY_CTAS], s_want;
+    __shared__ int s_taken, s_chunk;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t b = blockIdx.x / ctas, lo = a.offsets[b], hi = a.offsets[b + 1];
+    if (lo < 0 || hi < lo || hi > a.n_drafts) {  // (the same in every CTA of the cluster)
+        if (rank == 0 && tid == 0) a.accepted[b] = -1;
         return;
     }
-    const int64_t n = hi - lo;
+    const int n = (int)(hi - lo);
     const T* target = (const T*)a.target;
     const T* probs = (const T*)a.probs;
-    int64_t taken = 0;
-    if (threadIdx.x == 0) s_token = -1;
-    for (int64_t base = 0; base < n; base += VERIFY_THREADS) {
-        __syncthreads();
-        if (threadIdx.x == 0) s_first = VERIFY_THREADS;
-        __syncthreads();
-        const int64_t i = lo + base + threadIdx.x;
-        if (i < hi) {
-            const int32_t x = a.drafts[i];
-            bool ok = false;
-            if (x >= 0 && x < a.V) {
-                const double p = row_value(target[(i + b) * a.target_stride + x]);
-                const double q = PROBS ? (double)row_value(probs[i * a.probs_stride + x]) : 1.0;
-                ok = (double)a.accept_u[i] * q < p;
+    cluster_arrive();
+    if (warp == 0) {
+        int taken = n;
+        for (int base = 0; base < n; base += 32) {
+            const int64_t i = lo + base + lane;
+            bool ok = true;
+            if (i < hi) {
+                const int32_t x = a.drafts[i];
+                ok = false;
+                if (x >= 0 && x < a.V) {
+                    const double p = row_value(target[(i + b) * a.target_stride + x]);
+                    const double q = PROBS ? (double)row_value(probs[i * a.probs_stride + x]) : 1.0;
+                    ok = (double)a.accept_u[i] * q < p;
+                }
             }
-            if (!ok) atomicMin(&s_first, (int)threadIdx.x);
+            const uint32_t refusals = __ballot_sync(0xffffffffu, !ok);
+            if (refusals) {
+                taken = base + __ffs((int)refusals) - 1;
+                break;
+            }
         }
-        __syncthreads();
-        if (s_first < VERIFY_THREADS) {
-            taken += s_first;
-            break;
-        }
-        taken += min((int64_t)VERIFY_THREADS, n - base);
+        if (lane == 0) s_taken = taken;
     }
+    __syncthreads();
+    const int taken = s_taken;
     const bool refused = taken < n;
     const T* prow = target + (lo + taken + b) * a.target_stride;
     const T* qrow = PROBS && refused ? probs + (lo + taken) * a.probs_stride : nullptr;
     const int32_t gone = !PROBS && refused ? a.drafts[lo + taken] : -1;
-    const int per = (a.V + VERIFY_THREADS - 1) / VERIFY_THREADS;
-    const int v0 = min(a.V, (int)threadIdx.x * per), v1 = min(a.V, v0 + per);
-    const float u = a.draw_u[b];
-    const unsigned long long U = u > 0.0f ? (u < 1.0f ? __float2ull_rz(u * 4294967296.0f) : 0xFFFFFFFFull) : 0ull;
+    const int V = a.V;
+    const RowSplit split = RowSplit::of<T, R>(prow, V, rank, ctas);
+    const bool abreast = PROBS && (uintptr_t)qrow % 16 == (uintptr_t)prow % 16;
+    cluster_wait();
+    int token = -1;
+    bool here = true;  // whether this CTA writes the token
     for (int plain = 0; plain < 2; ++plain) {
+        const T* q = plain ? nullptr : qrow;
+        const int32_t out = plain ? -1 : gone;
         auto mass = [&](int v) {
-            float r = row_value(prow[v]);
-            if (!plain) r = qrow ? r - row_value(qrow[v]) : v == gone ? 0.0f : r;
-            return prob_mass(r);
+            const float p = row_value(prow[v]);
+            return prob_mass(q ? p - row_value(q[v]) : v == out ? 0.0f : p);
         };
-        unsigned long long sum = 0, total;
-        for (int v = v0; v < v1; ++v) sum += mass(v);
-        const unsigned long long before = block_scan_excl(sum, red, total);
-        if (total == 0) continue;
-        const unsigned long long want = __umul64hi(total, U << 32);
-        if (sum > 0 && before <= want && want < before + sum) {
-            unsigned long long run = before;
-            int v = v0;
-            for (; v < v1; ++v) {
-                run += mass(v);
-                if (run > want) break;
+        for (int c = split.chunk0 + warp; c < split.chunk1; c += VERIFY_THREADS / 32) {
+            const int first = chunk_first<T, R>(c, split.pre);
+            unsigned long long sum = 0;
+            if (q && !abreast || !chunk_inside<T, R>(first, V)) {
+                // rows at different offsets from 16 bytes, and the row's edges: by elements, in any order
+#pragma unroll 8
+                for (int i = lane; i < CHUNK; i += 32) {
+                    const int v = first + i;
+                    if (v >= 0 && v < V) sum += mass(v);
+                }
+            } else {
+                uint4 rp[R], rq[R];
+                load_chunk<T, R>(prow, first, V, row_element<T>(0.0f), rp);
+                if (q) load_chunk<T, R>(q, first, V, row_element<T>(0.0f), rq);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float xp[PER<T>], xq[PER<T>];
+                    unpack<T>(rp[r], xp);
+                    if (q) {
+                        unpack<T>(rq[r], xq);
+#pragma unroll
+                        for (int i = 0; i < PER<T>; ++i) sum += prob_mass(xp[i] - xq[i]);
+                    } else {
+                        const int at = out - (first + (32 * r + lane) * PER<T>);
+#pragma unroll
+                        for (int i = 0; i < PER<T>; ++i) sum += i == at ? 0ull : prob_mass(xp[i]);
+                    }
+                }
             }
-            s_token = v;
+            sum = warp_reduce_sum(sum);
+            if (lane == 0) sums[c - split.chunk0] = sum;
         }
+        __syncthreads();
+        const int chunks = split.chunk1 - split.chunk0;
+        unsigned long long own = 0;
+        for (int c = tid; c < chunks; c += VERIFY_THREADS) own += sums[c];
+        own = block_reduce_sum(own, red);
+        if (tid < ctas) *cluster.map_shared_rank(&parts[plain][rank], tid) = own;
+        cluster.sync();
+        unsigned long long total = 0, before = 0;
+        for (int k = 0; k < ctas; ++k) {
+            if (k < rank) before += parts[plain][k];
+            total += parts[plain][k];
+        }
+        if (total == 0) {
+            here = rank == 0;
+            continue;
+        }
+        const float u = a.draw_u[b];
+        const unsigned long long U = u > 0.0f ? (u < 1.0f ? __float2ull_rz(u * 4294967296.0f) : 0xFFFFFFFFull) : 0ull;
+        const unsigned long long want = __umul64hi(total, U << 32);
+        here = before <= want && want < before + own;
+        if (!here) break;
+        for (int c = 0; c < chunks; c += VERIFY_THREADS) {
+            unsigned long long all;
+            const unsigned long long sum = c + tid < chunks ? sums[c + tid] : 0ull;
+            const unsigned long long start = before + block_scan_excl(sum, red, all);
+            if (start <= want && want < start + sum) {
+                s_chunk = c + tid;
+                s_want = want - start;
+            }
+            before += all;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            // a lane takes consecutive words
+            const int first = chunk_first<T, R>(split.chunk0 + s_chunk, split.pre) + lane * (CHUNK / 32);
+            unsigned long long sum = 0;
+#pragma unroll
+            for (int i = 0; i < CHUNK / 32; ++i)
+                if (first + i >= 0 && first + i < V) sum += mass(first + i);
+            const unsigned long long upto = warp_scan_incl(sum), left = s_want - (upto - sum);
+            if (upto - sum <= s_want && s_want < upto) {
+                unsigned long long run = 0;
+                int v = max(first, 0);
+                for (; v < V; ++v) {
+                    run += mass(v);
+                    if (run > left) break;
+                }
+                s_chunk = v;
+            }
+        }
+        __syncthreads();
+        token = s_chunk;
         break;
     }
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i <= n; i += VERIFY_THREADS)
-        a.tokens[lo + b + i] = i < taken ? a.drafts[lo + i] : i == taken ? s_token : -1;
-    if (threadIdx.x == 0) a.accepted[b] = (int32_t)taken;
+    if (!here) return;
+    for (int i = tid; i <= n; i += VERIFY_THREADS) a.tokens[lo + b + i] = i < taken ? a.drafts[lo + i] : i == taken ? token : -1;
+    if (tid == 0) a.accepted[b] = taken;
 }
 
 template <typename T>
 static cudaError_t run_verify(const VerifyArgs& a, int64_t n_seqs, cudaStream_t st)
 {
-    if (a.probs) k_verify<T, true><<<(unsigned)n_seqs, VERIFY_THREADS, 0, st>>>(a);
-    else k_verify<T, false><<<(unsigned)n_seqs, VERIFY_THREADS, 0, st>>>(a);
-    return cudaGetLastError();
+    const int ctas = row_ctas(n_seqs, (int64_t)a.V * sizeof(T), 4, 8192, VERIFY_CTAS);
+    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, ctas, VERIFY_THREADS, 0, st);
 }
 
 }  // namespace lda
