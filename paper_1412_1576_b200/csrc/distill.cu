@@ -297,7 +297,7 @@ static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t 
     const size_t smem = tail || grad ? (size_t)((chunks + ctas - 1) / ctas) * (CHUNK / 8) : 0;
     const auto kernel = tail ? (grad ? k_distill<T, TV, true, true> : k_distill<T, TV, true, false>)
                              : (grad ? k_distill<T, TV, false, true> : k_distill<T, TV, false, false>);
-    return launch_rows(kernel, a, rows, ctas, DISTILL_THREADS, smem, st);
+    return launch_rows(kernel, a, rows, ctas, DISTILL_THREADS, smem, 7 * 1024, st);
 }
 
 template <typename T>

@@ -271,9 +271,10 @@ inline int row_ctas(int64_t rows, int64_t row_bytes, int per_sm, int64_t least, 
     return c;
 }
 
-// Launches `rows` clusters of `ctas` CTAs.
+// Launches `rows` clusters of `ctas` CTAs; `smem`: dynamic shared memory, `fixed`: what the kernel has besides, about.
 template <typename Args>
-inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t rows, int ctas, int threads, size_t smem, cudaStream_t st)
+inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t rows, int ctas, int threads, size_t smem,
+                               size_t fixed, cudaStream_t st)
 {
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)(rows * ctas));
@@ -286,7 +287,7 @@ inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t r
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     c.attrs = &at;
     c.numAttrs = 1;
-    if (smem > 40 * 1024) {
+    if (smem + fixed > 46 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }

@@ -17,110 +17,325 @@ struct TopArgs {
     float* lse;
 };
 
-constexpr int TOP_THREADS = 256;
+constexpr int TOP_THREADS = 512;
+constexpr int TOP_GROUPS = 4;     // groups a lane has in flight
+constexpr int TOP_CTAS = 8;       // of a cluster, at most
+constexpr int TOP_LIST = 4096;    // words that may be left for the list
+constexpr int TOP_QUEUE = 2048;   // pieces of a CTA's part that are read again
+constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
 
-// One CTA per row: the border value by four passes that count bytes of the keys, then what is above it, then the first words at it.
-template <typename T>
-__global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
+// What a CTA knows of its part of the row.
+struct TopPart {
+    ExpSum sum;
+    float max;
+    uint32_t share, alone;  // borders (half-keys)
+};
+
+struct TopShared {
+    unsigned long long list[TOP_LIST];
+    int queue[TOP_QUEUE];
+    TopPart parts[2][TOP_CTAS];
+    ExpSum ered[TOP_THREADS / 32];
+    float fred[TOP_THREADS / 32];
+    int ired[33];
+    int hist[256];
+    int counts[3];
+    int n, queued, need;
+    uint32_t prefix;
+    float max;
+};
+
+__device__ __forceinline__ unsigned long long top_entry(uint32_t key, int v)
 {
-    __shared__ float fred[32];
-    __shared__ int ired[33];
-    __shared__ int hist[256];
-    __shared__ unsigned long long list[LDA_TOP_MAX];
-    __shared__ uint32_t s_prefix;
-    __shared__ int s_need, s_n;
-    const int tid = threadIdx.x, V = a.V;
-    const T* row = (const T*)a.logits + (int64_t)blockIdx.x * a.stride;
-    float m = -INFINITY;
-    int n_valid = 0;
-    for (int v = tid; v < V; v += TOP_THREADS) {
-        const float x = row_value(row[v]);
-        m = fmaxf(m, x);
-        n_valid += x != -INFINITY;
-    }
-    m = block_reduce_max(m, fred);
-    n_valid = block_reduce_sum(n_valid, ired);
-    float s = 0.0f;
-    for (int v = tid; v < V; v += TOP_THREADS) s += exp2_unit((row_value(row[v]) - m) * a.scale);
-    s = block_reduce_sum(s, fred);
-    const int want = min(a.top, n_valid);
-    // the largest key that at least `want` words reach
-    uint32_t prefix = 0;
-    int need = want;
-    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-        for (int i = tid; i < 256; i += TOP_THREADS) hist[i] = 0;
+    return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)v);
+}
+
+// Descending sort of list[0..n) by the CTA; list[n..) up to the next power of two is overwritten.
+__device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
+{
+    const int tid = threadIdx.x;
+    int size = 32;
+    while (size < n) size *= 2;
+    if (size <= TOP_THREADS) {
+        // an entry per thread: partners up to 16 places away by shuffles, further ones through shared memory
+        unsigned long long x = tid < n ? list[tid] : 0ull;
+        for (int k = 2; k <= size; k *= 2)
+            for (int j = k / 2; j > 0; j /= 2) {
+                unsigned long long y;
+                if (j >= 32) {
+                    __syncthreads();
+                    if (tid < size) list[tid] = x;
+                    __syncthreads();
+                    y = tid < size ? list[tid ^ j] : 0ull;
+                } else {
+                    if (tid >= size) continue;  // (whole warps)
+                    y = __shfl_xor_sync(0xffffffffu, x, j);
+                }
+                // descending runs where bit k of the place is 0
+                const bool keep_large = ((tid & k) == 0) == ((tid & j) == 0);
+                x = (x > y) == keep_large ? x : y;
+            }
         __syncthreads();
-        for (int v = tid; v < V; v += TOP_THREADS) {
-            const uint32_t k = order_key(row_value(row[v]));
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+        if (tid < size) list[tid] = x;
+        __syncthreads();
+        return;
+    }
+    for (int i = n + tid; i < size; i += TOP_THREADS) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int i = tid; i < size / 2; i += TOP_THREADS) {
+                const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                const unsigned long long x = list[lo], y = list[hi];
+                if ((x < y) == ((lo & k) == 0)) list[lo] = y, list[hi] = x;
+            }
+            __syncthreads();
+        }
+}
+
+// For rows where the border leaves too many words (long ties): the border value by four passes that count bytes of the keys, then
+// what is above it, then the first words at it.  One CTA, the whole row; returns how many words the list has.
+template <typename T>
+__device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared& sh)
+{
+    const int tid = threadIdx.x;
+    uint32_t prefix = 0;
+    int need = top;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += TOP_THREADS) sh.hist[i] = 0;
+        __syncthreads();
+        for (int v = tid; v - tid < V; v += TOP_THREADS) {
+            const uint32_t k = v < V ? order_key(row_value(row[v])) : 0u, byte = (k >> shift) & 255;
+            const bool in = v < V && (shift == 24 || (k >> shift >> 8) == (prefix >> shift >> 8));
+            // one addition for all lanes with the first lane's byte
+            const uint32_t lanes = __ballot_sync(0xffffffffu, in);
+            const int first = lanes ? __ffs((int)lanes) - 1 : 0;
+            const uint32_t theirs = __shfl_sync(0xffffffffu, byte, first);
+            const bool like = in && byte == theirs;
+            const uint32_t alike = __ballot_sync(0xffffffffu, like);
+            if (like) {
+                if ((tid & 31) == first) atomicAdd(&sh.hist[byte], __popc(alike));
+            } else if (in)
+                atomicAdd(&sh.hist[byte], 1);
         }
         __syncthreads();
         if (tid == 0) {
             int d = 255, left = need;
-            while (d > 0 && hist[d] < left) left -= hist[d--];
-            s_prefix = prefix | ((uint32_t)d << shift);
-            s_need = left;
+            while (d > 0 && sh.hist[d] < left) left -= sh.hist[d--];
+            sh.prefix = prefix | ((uint32_t)d << shift);
+            sh.need = left;
         }
         __syncthreads();
-        prefix = s_prefix;
-        need = s_need;
+        prefix = sh.prefix;
+        need = sh.need;
         __syncthreads();
     }
-    if (tid == 0) s_n = 0;
+    if (prefix <= KEY_NEG_INF) prefix = KEY_NEG_INF;  // (fewer than `top` words are not masked)
+    if (tid == 0) sh.n = 0;
     __syncthreads();
-    if (want > 0) {
-        for (int v = tid; v < V; v += TOP_THREADS) {
-            const uint32_t k = order_key(row_value(row[v]));
-            if (k > prefix) list[atomicAdd(&s_n, 1)] = ((unsigned long long)k << 32) | (0xFFFFFFFFu - (uint32_t)v);
-        }
+    for (int v = tid; v < V; v += TOP_THREADS) {
+        const uint32_t k = order_key(row_value(row[v]));
+        if (k > prefix) sh.list[atomicAdd(&sh.n, 1)] = top_entry(k, v);
+    }
+    __syncthreads();
+    int have = sh.n;
+    __syncthreads();
+    for (int base = 0; base < V && have < top && prefix > KEY_NEG_INF; base += TOP_THREADS) {
+        const int v = base + tid;
+        const int at = v < V && order_key(row_value(row[v])) == prefix;
+        int total;
+        const int before = block_scan_excl(at, sh.ired, total);
+        if (at && have + before < top) sh.list[have + before] = top_entry(prefix, v);
+        have += total;
         __syncthreads();
-        int have = s_n;
-        for (int base = 0; base < V && have < want; base += TOP_THREADS) {
-            const int v = base + tid;
-            const int at = v < V && order_key(row_value(row[v])) == prefix;
-            int total;
-            const int before = block_scan_excl(at, ired, total);
-            if (at && have + before < want)
-                list[have + before] = ((unsigned long long)prefix << 32) | (0xFFFFFFFFu - (uint32_t)v);
-            have += total;
+    }
+    return min(have, top);
+}
+
+// One cluster per row.  The pass that adds up the exponentials leaves the largest value of every piece (a lane's groups of a chunk;
+// FINE: each group) as the upper half of its key.  A border that at least `top` pieces reach leaves at least `top` words, and few
+// more: the pieces that reach it are read again (from L2), their words at or above it are sorted.
+template <typename T, bool FINE>
+__global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
+{
+    constexpr int R = TOP_GROUPS, WARPS = TOP_THREADS / 32, PIECES = FINE ? R : 1, SIZE = R / PIECES;  // pieces of a lane's groups, groups of a piece
+    extern __shared__ uint32_t pairs[];  // half-keys of the pieces, two to a word
+    uint16_t* keys = (uint16_t*)pairs;
+    __shared__ TopShared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
+    const int64_t r = blockIdx.x / ctas;
+    const T* row = (const T*)a.logits + r * a.stride;
+    const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
+    const int pieces = (split.chunk1 - split.chunk0) * 32 * PIECES;
+    cluster_arrive();
+    if (tid < 3) sh.counts[tid] = 0;
+    if (tid == 0) sh.n = sh.queued = 0;
+    ExpSum sum = ExpSum::none();
+    float m = -INFINITY;
+    uint32_t best = 0;
+    for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
+        uint4 raw[R];
+        load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
+        const int at = (c - split.chunk0) * 32 * PIECES + lane;
+        float top;
+        if (FINE) {
+            top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const uint4 one[1] = {raw[k]};
+                const float x = groups_max<T, 1>(one);
+                keys[at + 32 * k] = (uint16_t)(order_key(x) >> 16);
+                top = max_nan(top, x);
+            }
+        } else {
+            top = groups_max<T, R>(raw);
+            keys[at] = (uint16_t)(order_key(top) >> 16);
+        }
+        best = max(best, order_key(top) >> 16);
+        m = fmaxf(m, top);
+        add_groups<T, R>(sum, raw, top, a.scale);
+    }
+    sum.warp_reduce();
+    m = warp_reduce_max(m);
+    best = __reduce_max_sync(0xffffffffu, best);
+    if (lane == 0) sh.ered[warp] = sum, sh.fred[warp] = m, sh.ired[warp] = (int)best;
+    __syncthreads();
+    best = (uint32_t)__reduce_max_sync(0xffffffffu, lane < WARPS ? sh.ired[lane] : 0);
+    // The largest half-key that at least `want` pieces of this part reach, or one that not many more do: steps of doubling width
+    // down from `hi` (that fewer reach), then halving; minus infinity's successor if there are not that many.
+    int round = 0;
+    auto border_of = [&](int want, uint32_t hi) {
+        uint32_t lo = TOP_LOWEST, step = 64;
+        while (lo + 1 < hi) {
+            const bool down = lo == TOP_LOWEST && hi > lo + step;
+            const uint32_t mid = down ? hi - step : (lo + hi) / 2;
+            step = down ? step * 2 : step;
+            int n = 0;
+            for (int i = tid; i < pieces / 2; i += TOP_THREADS) n += __popc(__vcmpgeu2(pairs[i], mid * 0x10001u));
+            n = __reduce_add_sync(0xffffffffu, n) / 16;
+            if (lane == 0 && n) atomicAdd(&sh.counts[round % 3], n);
+            if (tid == 0) sh.counts[(round + 1) % 3] = 0;
             __syncthreads();
+            n = sh.counts[round++ % 3];
+            if (n >= want) {
+                lo = mid;
+                if (n <= want + want / 4 + 16 / ctas) break;
+            } else
+                hi = mid;
         }
+        return lo;
+    };
+    // `top` pieces of one part are enough, and so are its share of them in every part
+    const uint32_t share = border_of((a.top + ctas - 1) / ctas, best + 1);
+    const uint32_t alone = ctas > 1 ? border_of(a.top, share + 1) : share;
+    if (warp == 0) {
+        sum = lane < WARPS ? sh.ered[lane] : ExpSum::none();
+        sum.warp_reduce();
+        m = warp_reduce_max(lane < WARPS ? sh.fred[lane] : -INFINITY);
     }
-    int size = 1;
-    while (size < want) size *= 2;
-    for (int i = want + tid; i < size; i += TOP_THREADS) list[i] = 0;
+    cluster_wait();
+    if (tid < ctas) *cluster.map_shared_rank(&sh.parts[0][rank], tid) = TopPart{sum, m, share, alone};
+    cluster.sync();
+    uint32_t border = 0, least = 0xFFFFFFFFu;
+    m = -INFINITY;
+    for (int k = 0; k < ctas; ++k) {
+        border = max(border, sh.parts[0][k].alone);
+        least = min(least, sh.parts[0][k].share);
+        m = fmaxf(m, sh.parts[0][k].max);
+    }
+    border = max(border, least);
+    const bool far = exp_far(m, a.scale);
+    if (far) {  // (the same in every CTA of the cluster)
+        float o = 0.0f;
+        for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
+            uint4 raw[R];
+            load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
+            for (int k = 0; k < R; ++k) {
+                float y[PER<T>];
+                unpack<T>(raw[k], y);
+                for (int i = 0; i < PER<T>; ++i) o += exp2_unit((y[i] - m) * a.scale);
+            }
+        }
+        o = warp_reduce_sum(o);
+        if (lane == 0) sh.fred[warp] = o;
+        __syncthreads();
+        if (warp == 0) o = warp_reduce_sum(lane < WARPS ? sh.fred[lane] : 0.0f);
+        if (tid < ctas) *cluster.map_shared_rank(&sh.parts[1][rank], tid) = TopPart{{0.0f, o}, m, 0, 0};
+        cluster.sync();
+    }
+    // the pieces that reach the border, then a group of one to every thread
+    int* n_all = cluster.map_shared_rank(&sh.n, 0);
+    unsigned long long* list = cluster.map_shared_rank(sh.list, 0);
+    for (int i = tid; i < pieces; i += TOP_THREADS)
+        if (keys[i] >= border) {
+            const int at = atomicAdd(&sh.queued, 1);
+            if (at < TOP_QUEUE) sh.queue[at] = i;
+        }
     __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-            for (int i = tid; i < size; i += TOP_THREADS) {
-                const int o = i ^ j;
-                if (o > i) {
-                    const unsigned long long x = list[i], y = list[o];
-                    if ((x < y) == ((i & k) == 0)) list[i] = y, list[o] = x;
+    const int queued = sh.queued;
+    if (queued > TOP_QUEUE) {
+        if (tid == 0) atomicAdd(n_all, TOP_LIST + 1);
+    } else
+        for (int t = tid; t < queued * SIZE; t += TOP_THREADS) {
+            const int i = sh.queue[t / SIZE];  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
+            const int chunk = split.chunk0 + i / (32 * PIECES);
+            const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
+            const int first = chunk_first<T, R>(chunk, split.pre) + group * PER<T>;
+            const uint4 raw = first >= 0 && first + PER<T> <= V ? __ldcg(reinterpret_cast<const uint4*>(row + first))
+                                                                : edge_group(row, first, V, row_element<T>(-INFINITY));
+            float x[PER<T>];
+            unpack<T>(raw, x);
+#pragma unroll
+            for (int e = 0; e < PER<T>; ++e) {
+                const uint32_t k = order_key(x[e]);
+                if ((k >> 16) >= border) {
+                    const int at = atomicAdd(n_all, 1);
+                    if (at < TOP_LIST) list[at] = top_entry(k, first + e);
                 }
             }
-            __syncthreads();
         }
+    cluster.sync();
+    if (rank != 0) return;
+    int n = sh.n;
+    if (n > TOP_LIST) {
+        __syncthreads();
+        n = top_by_bytes<T>(row, V, a.top, sh);
+        __syncthreads();
+    }
+    sort_entries(sh.list, n);
+    const int want = min(n, a.top);
     for (int i = tid; i < a.top; i += TOP_THREADS) {
-        const int64_t at = (int64_t)blockIdx.x * a.top + i;
-        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)list[i]) : -1;
+        const int64_t at = r * a.top + i;
+        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)sh.list[i]) : -1;
         a.ids[at] = v;
         ((T*)a.values)[at] = v >= 0 ? row[v] : row_element<T>(-INFINITY);
     }
     if (a.lse && tid == 0) {
-        const uint32_t first = want > 0 ? (uint32_t)(list[0] >> 32) : 0;
-        a.lse[blockIdx.x] = want == 0 ? -INFINITY
-                            : first == KEY_NAN ? NAN
-                            : m == INFINITY ? INFINITY
-                                            : (float)((double)m * a.inv_tau + (double)logf(s));
+        sum = sh.parts[far][0].sum;
+        for (int k = 1; k < ctas; ++k) sum.add(sh.parts[far][k].sum);
+        const uint32_t first = want > 0 ? (uint32_t)(sh.list[0] >> 32) : 0;
+        // (log2 of the largest exponential: x c, or 0 when far)
+        const double most2 = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
+        a.lse[r] = want == 0 ? -INFINITY
+                   : first == KEY_NAN ? NAN
+                   : m == INFINITY ? INFINITY
+                                   : (float)((double)m * a.inv_tau + ((double)log2f(sum.sum) - most2) * LN2);
     }
 }
 
 template <typename T>
 static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
 {
-    k_top<T><<<(unsigned)rows, TOP_THREADS, 0, st>>>(a);
-    return cudaGetLastError();
+    constexpr int CHUNK = 32 * TOP_GROUPS * PER<T>;
+    int ctas = row_ctas(rows, (int64_t)a.V * sizeof(T), 4, 8192, TOP_CTAS);
+    // every part has to hold several times `top` pieces, or the border stays too low
+    while (ctas > 1 && a.V / PER<T> / ctas < 4 * a.top) ctas /= 2;
+    const bool fine = a.V / PER<T> / TOP_GROUPS / ctas < 4 * a.top;
+    const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
+    const size_t smem = (size_t)((chunks + ctas - 1) / ctas) * 32 * (fine ? TOP_GROUPS : 1) * 2;
+    return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, ctas, TOP_THREADS, smem, sizeof(TopShared), st);
 }
 
 }  // namespace lda

@@ -190,7 +190,7 @@ template <typename T>
 static cudaError_t run_verify(const VerifyArgs& a, int64_t n_seqs, cudaStream_t st)
 {
     const int ctas = row_ctas(n_seqs, (int64_t)a.V * sizeof(T), 4, 8192, VERIFY_CTAS);
-    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, ctas, VERIFY_THREADS, 0, st);
+    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, ctas, VERIFY_THREADS, 0, 17 * 1024, st);
 }
 
 }  // namespace lda
