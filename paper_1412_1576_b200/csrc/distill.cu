@@ -18,6 +18,7 @@ struct DistillArgs {
     int32_t V, top;
     const int32_t* ids;
     const void* values;
+    int values_dtype;
     int64_t list_stride;
     const float* teacher_lse;  // null: softmax over the list
     const float* weights;      // of the rows' losses in the gradient; null: all 1
@@ -28,8 +29,18 @@ struct DistillArgs {
     double tau, inv_tau;
 };
 
-constexpr int DISTILL_THREADS = 512;
-constexpr int DISTILL_GROUPS = 4;  // groups a lane has in flight
+constexpr int DISTILL_THREADS = 512;  // of a CTA, at most
+#ifndef DG
+#define DG 4
+#endif
+#ifndef DB
+#define DB 2
+#endif
+constexpr int DISTILL_GROUPS = DG;  // groups a lane has in flight
+#ifndef DD
+#define DD 3
+#endif
+constexpr int DISTILL_DEPTH = DD;  // chunks on their way
 constexpr int DISTILL_CTAS = 8;    // of a cluster, at most
 
 // What a CTA knows of its part of the row.
@@ -56,22 +67,24 @@ __device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
 // part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The CTAs exchange
 // their sums, and each works out the gradient of its part: the same factor times the exponential for all words, from a second read
 // that L2 answers, then the list's words over it.
-template <typename T, typename TV, bool TAIL, bool GRAD>
-__global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
+template <typename T, bool TAIL, bool GRAD>
+__global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
 {
-    constexpr int R = DISTILL_GROUPS, CHUNK = 32 * R * PER<T>, WARPS = DISTILL_THREADS / 32;
+    constexpr int R = DISTILL_GROUPS, CHUNK = 32 * R * PER<T>;
     constexpr bool BITS = TAIL || GRAD;
-    extern __shared__ uint32_t bits[];
+    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the map of the list's words
+    using Walk = ChunkWalk<T, R, DISTILL_DEPTH>;
+    uint32_t* bits = (uint32_t*)(dynamic + blockDim.x * Walk::BYTES);
     __shared__ int ids[LDA_TOP_MAX];
     __shared__ float p[LDA_TOP_MAX], x[LDA_TOP_MAX];
-    __shared__ ExpSum ered[WARPS];
-    __shared__ float fred[WARPS];
+    __shared__ ExpSum ered[DISTILL_THREADS / 32];
+    __shared__ float fred[DISTILL_THREADS / 32];
     __shared__ DistillPart parts[2][DISTILL_CTAS];
     __shared__ DistillRow whole;
     __shared__ int s_any, s_twice;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, WARPS = threads / 32, V = a.V;
     const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
     T* grad = GRAD ? (T*)a.grad + r * a.grad_stride : nullptr;
@@ -80,30 +93,31 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
     // this CTA's words, and the word of the map's first bit
     const int bit0 = chunk_first<T, R>(split.chunk0, split.pre);
     const int v0 = max(0, bit0), v1 = max(v0, min(V, chunk_first<T, R>(split.chunk1, split.pre)));
+    Walk walk;
+    walk.start(dynamic, row, split, V);
     if (tid == 0) s_any = s_twice = 0;
     if (BITS)
-        for (int i = tid; i < (split.chunk1 - split.chunk0) * (CHUNK / 32); i += DISTILL_THREADS) bits[i] = 0;
+        for (int i = tid; i < (split.chunk1 - split.chunk0) * (CHUNK / 32); i += threads) bits[i] = 0;
     __syncthreads();
-    const TV* values = (const TV*)a.values + r * a.list_stride;
-    for (int j = tid; j < a.top; j += DISTILL_THREADS) {
+    const auto teacher = [&](int j) { return any_value(a.values, a.values_dtype, r * a.list_stride + j); };
+    for (int j = tid; j < a.top; j += threads) {
         const int id = a.ids[r * a.list_stride + j];
         const bool ok = id >= 0 && id < V;
         ids[j] = ok ? id : -1;
-        p[j] = row_value(values[j]);
+        p[j] = teacher(j);
         if (ok) {
             s_any = 1;
             if (BITS && id >= v0 && id < v1) {
                 const int bit = id - bit0;
                 if (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
             }
-            x[j] = row_value(row[id]);
         }
     }
     __syncthreads();
     if (!s_any || (GRAD && weight == 0.0f && !a.loss)) {  // (the same in every CTA of the cluster)
         if (a.loss && rank == 0 && tid == 0) a.loss[r] = 0.0f;
         if (GRAD)
-            for (int v = v0 + tid; v < v1; v += DISTILL_THREADS) grad[v] = row_element<T>(0.0f);
+            for (int v = v0 + tid; v < v1; v += threads) grad[v] = row_element<T>(0.0f);
         return;
     }
     cluster_arrive();
@@ -118,6 +132,8 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
     double t_ref = 0.0, base = 0.0, sum_p = 0.0;
     ExpSum in = ExpSum::none();
     if (warp == 0) {
+        for (int j = lane; j < a.top; j += 32)
+            if (ids[j] >= 0) x[j] = row_value(row[ids[j]]);
         if (TAIL) base = (double)a.teacher_lse[r];
         else {
             float tm = -INFINITY;
@@ -148,36 +164,32 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
     // the student's words outside the list
     ExpSum out = ExpSum::none();
     float m = -INFINITY;
-    // (masked: with minus infinity in the list's places)
-    auto load = [&](int c, uint4 (&raw)[R], float& top) {
-        load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
-        top = groups_max<T, R>(raw);
-        if (TAIL) {
-            const int g = (c - split.chunk0) * 32 * R + lane;
+    // minus infinity in the list's places
+    auto mask = [&](int c, uint4(&raw)[R]) {
+        if (!TAIL) return;
+        const int g = (c - split.chunk0) * 32 * R + lane;
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const uint32_t marked = group_bits<T>(bits, g + 32 * k);
-                if (marked) {
-                    union {
-                        uint4 raw;
-                        T e[PER<T>];
-                    } u;
-                    u.raw = raw[k];
+        for (int k = 0; k < R; ++k) {
+            const uint32_t marked = group_bits<T>(bits, g + 32 * k);
+            if (marked) {
+                union {
+                    uint4 raw;
+                    T e[PER<T>];
+                } u;
+                u.raw = raw[k];
 #pragma unroll
-                    for (int i = 0; i < PER<T>; ++i)
-                        if (marked >> i & 1) u.e[i] = row_element<T>(-INFINITY);
-                    raw[k] = u.raw;
-                }
+                for (int i = 0; i < PER<T>; ++i)
+                    if (marked >> i & 1) u.e[i] = row_element<T>(-INFINITY);
+                raw[k] = u.raw;
             }
         }
     };
-    for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
-        uint4 raw[R];
-        float top;
-        load(c, raw, top);
+    walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, uint4(&raw)[R]) {
+        const float top = groups_max<T, R>(raw);
+        mask(c, raw);
         m = fmaxf(m, top);  // (a NaN goes into the sums)
         add_groups<T, R>(out, raw, top, a.scale);
-    }
+    });
     out.warp_reduce();
     m = warp_reduce_max(m);
     if (lane == 0) ered[warp] = out, fred[warp] = m;
@@ -197,8 +209,8 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
         float o = 0.0f, l = 0.0f;
         for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
             uint4 raw[R];
-            float top;
-            load(c, raw, top);
+            load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
+            mask(c, raw);
             for (int k = 0; k < R; ++k) {
                 float y[PER<T>];
                 unpack<T>(raw[k], y);
@@ -233,7 +245,7 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
             for (int j = lane; j < a.top; j += 32)
                 if (p[j] > 0.0f || p[j] != p[j]) {
                     const double y = far ? ((double)x[j] - (double)m) * (double)a.scale : (double)x[j] * (double)a.scale - (double)ref;
-                    l += (double)p[j] * ((((double)row_value(values[j]) - t_ref) * a.inv_tau - base) - (y - log2_total) * LN2);
+                    l += (double)p[j] * ((((double)teacher(j) - t_ref) * a.inv_tau - base) - (y - log2_total) * LN2);
                 }
             l = warp_reduce_sum(l);
             if (p_rest != 0.0) l += p_rest * log(p_rest / q_rest);
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
     }
     if (weight == 0.0f) return;
     __syncthreads();  // the list's words over the rest
-    for (int j = tid; j < a.top; j += DISTILL_THREADS) {
+    for (int j = tid; j < a.top; j += threads) {
         if (ids[j] < v0 || ids[j] >= v1 || !leads(j)) continue;
         double pj = (double)p[j];
         if (s_twice)
@@ -286,30 +298,28 @@ __global__ void __launch_bounds__(DISTILL_THREADS) k_distill(DistillArgs a)
     }
 }
 
-template <typename T, typename TV>
+template <typename T>
 static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t st)
 {
     constexpr int CHUNK = 32 * DISTILL_GROUPS * PER<T>;
-    const int ctas = row_ctas(rows, (int64_t)a.V * sizeof(T), 4, 8192, DISTILL_CTAS);
+    const int64_t row_bytes = (int64_t)a.V * sizeof(T);
     const bool tail = a.teacher_lse, grad = a.grad;
+    RowShape shape = row_shape(rows, row_bytes, 1024, 64);
+    // what is read twice has to stay in L2 in between: all rows under way together at most 40 MB
+    while (grad && shape.ctas < DISTILL_CTAS && row_bytes * 148 * 1024 / (shape.ctas * shape.threads) > 40ll << 20)
+        shape = shape.threads < 512 ? RowShape{1, shape.threads * 2} : RowShape{shape.ctas * 2, 512};
     // a bit for every word of a CTA's part
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = tail || grad ? (size_t)((chunks + ctas - 1) / ctas) * (CHUNK / 8) : 0;
-    const auto kernel = tail ? (grad ? k_distill<T, TV, true, true> : k_distill<T, TV, true, false>)
-                             : (grad ? k_distill<T, TV, false, true> : k_distill<T, TV, false, false>);
-    return launch_rows(kernel, a, rows, ctas, DISTILL_THREADS, smem, 7 * 1024, st);
+    const size_t smem = shape.threads * ChunkWalk<T, DISTILL_GROUPS, DISTILL_DEPTH>::BYTES +
+                        (tail || grad ? (size_t)((chunks + shape.ctas - 1) / shape.ctas) * (CHUNK / 8) : 0);
+    const auto kernel = tail ? (grad ? k_distill<T, true, true> : k_distill<T, true, false>)
+                             : (grad ? k_distill<T, false, true> : k_distill<T, false, false>);
+    return launch_rows(kernel, a, rows, shape, smem, 7 * 1024, st);
 }
 
-template <typename T>
-static cudaError_t run_distill(const DistillArgs& a, int values_dtype, int64_t rows, cudaStream_t st)
+static int distill(const DistillArgs& a, int dtype, int64_t rows, void* stream)
 {
-    return values_dtype == LDA_F32 ? run_distill<T, float>(a, rows, st)
-           : values_dtype == LDA_F16 ? run_distill<T, __half>(a, rows, st)
-                                     : run_distill<T, __nv_bfloat16>(a, rows, st);
-}
-
-static int distill(const DistillArgs& a, int dtype, int values_dtype, int64_t rows, void* stream)
-{
+    const int values_dtype = a.values_dtype;
     int rc = check_rows(a.logits, dtype, rows, a.V, a.stride);
     if (rc != LDA_OK) return rc;
     if (values_dtype != LDA_F32 && values_dtype != LDA_F16 && values_dtype != LDA_BF16) return LDA_EINVAL;
@@ -318,9 +328,9 @@ static int distill(const DistillArgs& a, int dtype, int values_dtype, int64_t ro
     if (rows == 0) return LDA_OK;
     if (!a.ids || !a.values || (uintptr_t)a.values % (values_dtype == LDA_F32 ? 4 : 2)) return LDA_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = dtype == LDA_F32 ? run_distill<float>(a, values_dtype, rows, st)
-                          : dtype == LDA_F16 ? run_distill<__half>(a, values_dtype, rows, st)
-                                             : run_distill<__nv_bfloat16>(a, values_dtype, rows, st);
+    const cudaError_t e = dtype == LDA_F32 ? run_distill<float>(a, rows, st)
+                          : dtype == LDA_F16 ? run_distill<__half>(a, rows, st)
+                                             : run_distill<__nv_bfloat16>(a, rows, st);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return LDA_ECUDA;
@@ -336,9 +346,9 @@ extern "C" int lda_distill_loss(const void* logits_dev, int dtype, int64_t rows,
 {
     using namespace lda;
     if (rows > 0 && !loss_dev) return LDA_EINVAL;
-    const DistillArgs a{logits_dev, row_stride, V, top, ids_dev, values_dev, list_stride, teacher_lse_dev, nullptr, loss_dev,
+    const DistillArgs a{logits_dev, row_stride, V, top, ids_dev, values_dev, values_dtype, list_stride, teacher_lse_dev, nullptr, loss_dev,
                         nullptr, 0, (float)(1.4426950408889634 / temperature), temperature, 1.0 / temperature};
-    return distill(a, dtype, values_dtype, rows, cuda_stream);
+    return distill(a, dtype, rows, cuda_stream);
 }
 
 extern "C" int lda_distill_grad(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride,
@@ -352,7 +362,7 @@ extern "C" int lda_distill_grad(const void* logits_dev, int dtype, int64_t rows,
     if (rows > 1 && grad_stride < V) return LDA_EINVAL;
     // the gradient may take the logits' place, row for row, and may not overlap them otherwise
     if (grad_dev == logits_dev && rows > 1 && grad_stride != row_stride) return LDA_EINVAL;
-    const DistillArgs a{logits_dev, row_stride, V, top, ids_dev, values_dev, list_stride, teacher_lse_dev, weights_dev, loss_dev,
+    const DistillArgs a{logits_dev, row_stride, V, top, ids_dev, values_dev, values_dtype, list_stride, teacher_lse_dev, weights_dev, loss_dev,
                         grad_dev, grad_stride, (float)(1.4426950408889634 / temperature), temperature, 1.0 / temperature};
-    return distill(a, dtype, values_dtype, rows, cuda_stream);
+    return distill(a, dtype, rows, cuda_stream);
 }

@@ -26,6 +26,12 @@ constexpr double LN2 = 0.69314718055994531;
 __device__ __forceinline__ float row_value(float x) { return x; }
 __device__ __forceinline__ float row_value(__half x) { return __half2float(x); }
 __device__ __forceinline__ float row_value(__nv_bfloat16 x) { return __bfloat162float(x); }
+// Element i of an array whose type (LDA_F32, ...) is an argument.
+__device__ __forceinline__ float any_value(const void* p, int dtype, int64_t i)
+{
+    if (dtype == LDA_F32) return ((const float*)p)[i];
+    return dtype == LDA_F16 ? row_value(((const __half*)p)[i]) : row_value(((const __nv_bfloat16*)p)[i]);
+}
 template <typename T>
 constexpr bool T_is_bf16 = false;
 template <>
@@ -129,6 +135,66 @@ __device__ __forceinline__ void load_chunk(const T* row, int first, int V, T fil
     }
 }
 
+// A warp's walk over its chunks of a part (every warps-th from its own number on).  A lane copies its groups of the next DEPTH chunks
+// into places of its own in shared memory (`ring`: DEPTH R 16 bytes per thread), so that what is on its way costs no registers and
+// nothing has to be waited for but the lane's own copies.
+template <typename T, int R, int DEPTH>
+struct ChunkWalk {
+    static constexpr int BYTES = DEPTH * R * 16;  // per thread
+    uint4* ring;
+    int chunk;  // the next to work on
+    int slot;
+    __device__ __forceinline__ void fetch(const T* row, const RowSplit& split, int V, int c, int into)
+    {
+        if (c < split.chunk1) {
+            const int first = chunk_first<T, R>(c, split.pre);
+            if (chunk_inside<T, R>(first, V)) {
+                const T* from = row + first + (threadIdx.x & 31) * PER<T>;
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + into * R * (int)blockDim.x);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * (uint32_t)blockDim.x * 16),
+                                 "l"(from + 32 * PER<T> * r)
+                                 : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ void start(void* shared, const T* row, const RowSplit& split, int V)
+    {
+        ring = (uint4*)shared + threadIdx.x;
+        chunk = split.chunk0 + (int)(threadIdx.x >> 5);
+        slot = 0;
+        const int warps = (int)(blockDim.x >> 5);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) fetch(row, split, V, chunk + d * warps, d);
+    }
+    // f(chunk, groups) for each; `fill` stands outside the row.
+    template <typename F>
+    __device__ __forceinline__ void each(const T* row, const RowSplit& split, int V, T fill, F f)
+    {
+        const int warps = (int)(blockDim.x >> 5);
+        for (; chunk < split.chunk1; chunk += warps) {
+            const int first = chunk_first<T, R>(chunk, split.pre);
+            asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+            uint4 raw[R];
+            if (chunk_inside<T, R>(first, V)) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) raw[r] = ring[(slot * R + r) * (int)blockDim.x];
+            } else {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    raw[r] = edge_group(row, first + (32 * r + (int)(threadIdx.x & 31)) * PER<T>, V, fill);
+            }
+            f(chunk, raw);
+            // (the place is free: its groups have been worked on)
+            fetch(row, split, V, chunk + DEPTH * warps, slot);
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+};
+
 // A group's values.
 template <typename T>
 __device__ __forceinline__ void unpack(uint4 g, float (&x)[PER<T>])
@@ -217,27 +283,51 @@ __device__ __forceinline__ float groups_max(const uint4 (&raw)[N])
     }
 }
 
+// Two products and sums, or two sums, in one instruction.
+__device__ __forceinline__ float2 fma_two(float2 a, float2 b, float2 c)
+{
+    unsigned long long y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(y)
+        : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+          "l"(*reinterpret_cast<unsigned long long*>(&c)));
+    return *reinterpret_cast<float2*>(&y);
+}
+__device__ __forceinline__ float2 add_two(float2 a, float2 b)
+{
+    unsigned long long y;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(y)
+        : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+    return *reinterpret_cast<float2*>(&y);
+}
+
 // Adds N groups to a sum.  `max`: not below any of their values.
 template <typename T, int N>
 __device__ __forceinline__ void add_groups(ExpSum& s, const uint4 (&raw)[N], float max, float c)
 {
     s.raise(exp_ref(max, c));
-    float part[N];
+    const float2 cc = make_float2(c, c), ref = make_float2(-s.ref, -s.ref);
+    float2 part[N];
 #pragma unroll
     for (int r = 0; r < N; ++r) {
         float x[PER<T>];
         unpack<T>(raw[r], x);
+        float2 e[PER<T> / 2];
 #pragma unroll
-        for (int i = 0; i < PER<T>; ++i) x[i] = exp2_unit(__fmaf_rn(x[i], c, -s.ref));
+        for (int i = 0; i < PER<T> / 2; ++i) {
+            const float2 y = fma_two(make_float2(x[2 * i], x[2 * i + 1]), cc, ref);
+            e[i] = make_float2(exp2_unit(y.x), exp2_unit(y.y));
+        }
 #pragma unroll
-        for (int w = PER<T> / 2; w > 0; w /= 2)
+        for (int w = PER<T> / 4; w > 0; w /= 2)
 #pragma unroll
-            for (int i = 0; i < w; ++i) x[i] += x[i + w];
-        part[r] = x[0];
+            for (int i = 0; i < w; ++i) e[i] = add_two(e[i], e[i + w]);
+        part[r] = e[0];
     }
 #pragma unroll
-    for (int r = 1; r < N; ++r) part[0] += part[r];
-    s.sum += part[0];
+    for (int r = 1; r < N; ++r) part[0] = add_two(part[0], part[r]);
+    s.sum += part[0].x + part[0].y;
 }
 
 // A group of values, each rounded once.
@@ -262,28 +352,31 @@ __device__ __forceinline__ uint4 pack(const float (&x)[PER<T>])
     }
 }
 
-// How many CTAs share a row: as many (a power of two, at most `most`) as it takes for `rows` of them to give every
-// multiprocessor `per_sm` CTAs, unless a CTA's share falls below `least` bytes.
-inline int row_ctas(int64_t rows, int64_t row_bytes, int per_sm, int64_t least, int most)
+// How many threads share a row: a power of two from 128 on, up to clusters of eight CTAs of 512, so that all rows together give
+// every multiprocessor `per_sm` threads, but a thread no less than `least` bytes.
+struct RowShape {
+    int ctas, threads;
+};
+inline RowShape row_shape(int64_t rows, int64_t row_bytes, int64_t per_sm, int64_t least)
 {
-    int c = 1;
-    while (c < most && rows * c < 148 * per_sm && row_bytes >= 2 * c * least) c *= 2;
-    return c;
+    int64_t n = 128;
+    while (n < 8 * 512 && rows * n < 148 * per_sm && row_bytes >= 2 * n * least) n *= 2;
+    return n <= 512 ? RowShape{1, (int)n} : RowShape{(int)(n / 512), 512};
 }
 
-// Launches `rows` clusters of `ctas` CTAs; `smem`: dynamic shared memory, `fixed`: what the kernel has besides, about.
+// Launches a cluster of CTAs for every row; `smem`: dynamic shared memory, `fixed`: what the kernel has besides, about.
 template <typename Args>
-inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t rows, int ctas, int threads, size_t smem,
+inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t rows, RowShape shape, size_t smem,
                                size_t fixed, cudaStream_t st)
 {
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)(rows * ctas));
-    c.blockDim = dim3((unsigned)threads);
+    c.gridDim = dim3((unsigned)(rows * shape.ctas));
+    c.blockDim = dim3((unsigned)shape.threads);
     c.dynamicSmemBytes = smem;
     c.stream = st;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = (unsigned)ctas;
+    at.val.clusterDim.x = (unsigned)shape.ctas;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     c.attrs = &at;
     c.numAttrs = 1;

@@ -17,12 +17,23 @@ struct TopArgs {
     float* lse;
 };
 
-constexpr int TOP_THREADS = 512;
-constexpr int TOP_GROUPS = 4;     // groups a lane has in flight
+constexpr int TOP_THREADS = 512;  // of a CTA, at most
+#ifndef TG
+#define TG 4
+#endif
+#ifndef TB
+#define TB 2
+#endif
+constexpr int TOP_GROUPS = TG;     // groups a lane has in flight
 constexpr int TOP_CTAS = 8;       // of a cluster, at most
-constexpr int TOP_LIST = 4096;    // words that may be left for the list
-constexpr int TOP_QUEUE = 2048;   // pieces of a CTA's part that are read again
+constexpr int TOP_LIST = 2048;    // words that may be left for the list
+constexpr int TOP_QUEUE = 1024;   // pieces of a CTA's part that are read again
 constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
+
+#ifndef TD
+#define TD 3
+#endif
+constexpr int TOP_DEPTH = TD;      // chunks on their way
 
 // What a CTA knows of its part of the row.
 struct TopPart {
@@ -31,9 +42,13 @@ struct TopPart {
     uint32_t share, alone;  // borders (half-keys)
 };
 
-struct TopShared {
+// Behind the pass over the row its shared memory holds these.
+struct TopLists {
     unsigned long long list[TOP_LIST];
     int queue[TOP_QUEUE];
+};
+
+struct TopShared {
     TopPart parts[2][TOP_CTAS];
     ExpSum ered[TOP_THREADS / 32];
     float fred[TOP_THREADS / 32];
@@ -45,6 +60,12 @@ struct TopShared {
     float max;
 };
 
+__host__ __device__ constexpr int top_ring_bytes(int threads)
+{
+    const int ring = threads * TOP_DEPTH * TOP_GROUPS * 16;
+    return ring > (int)sizeof(TopLists) ? ring : (int)sizeof(TopLists);
+}
+
 __device__ __forceinline__ unsigned long long top_entry(uint32_t key, int v)
 {
     return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)v);
@@ -53,10 +74,10 @@ __device__ __forceinline__ unsigned long long top_entry(uint32_t key, int v)
 // Descending sort of list[0..n) by the CTA; list[n..) up to the next power of two is overwritten.
 __device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
 {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, threads = blockDim.x;
     int size = 32;
     while (size < n) size *= 2;
-    if (size <= TOP_THREADS) {
+    if (size <= threads) {
         // an entry per thread: partners up to 16 places away by shuffles, further ones through shared memory
         unsigned long long x = tid < n ? list[tid] : 0ull;
         for (int k = 2; k <= size; k *= 2)
@@ -80,11 +101,11 @@ __device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
         __syncthreads();
         return;
     }
-    for (int i = n + tid; i < size; i += TOP_THREADS) list[i] = 0;
+    for (int i = n + tid; i < size; i += threads) list[i] = 0;
     __syncthreads();
     for (int k = 2; k <= size; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
-            for (int i = tid; i < size / 2; i += TOP_THREADS) {
+            for (int i = tid; i < size / 2; i += threads) {
                 const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
                 const unsigned long long x = list[lo], y = list[hi];
                 if ((x < y) == ((lo & k) == 0)) list[lo] = y, list[hi] = x;
@@ -96,15 +117,15 @@ __device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
 // For rows where the border leaves too many words (long ties): the border value by four passes that count bytes of the keys, then
 // what is above it, then the first words at it.  One CTA, the whole row; returns how many words the list has.
 template <typename T>
-__device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared& sh)
+__device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared& sh, unsigned long long* list)
 {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, threads = blockDim.x;
     uint32_t prefix = 0;
     int need = top;
     for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += TOP_THREADS) sh.hist[i] = 0;
+        for (int i = tid; i < 256; i += threads) sh.hist[i] = 0;
         __syncthreads();
-        for (int v = tid; v - tid < V; v += TOP_THREADS) {
+        for (int v = tid; v - tid < V; v += threads) {
             const uint32_t k = v < V ? order_key(row_value(row[v])) : 0u, byte = (k >> shift) & 255;
             const bool in = v < V && (shift == 24 || (k >> shift >> 8) == (prefix >> shift >> 8));
             // one addition for all lanes with the first lane's byte
@@ -133,19 +154,19 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared
     if (prefix <= KEY_NEG_INF) prefix = KEY_NEG_INF;  // (fewer than `top` words are not masked)
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    for (int v = tid; v < V; v += TOP_THREADS) {
+    for (int v = tid; v < V; v += threads) {
         const uint32_t k = order_key(row_value(row[v]));
-        if (k > prefix) sh.list[atomicAdd(&sh.n, 1)] = top_entry(k, v);
+        if (k > prefix) list[atomicAdd(&sh.n, 1)] = top_entry(k, v);
     }
     __syncthreads();
     int have = sh.n;
     __syncthreads();
-    for (int base = 0; base < V && have < top && prefix > KEY_NEG_INF; base += TOP_THREADS) {
+    for (int base = 0; base < V && have < top && prefix > KEY_NEG_INF; base += threads) {
         const int v = base + tid;
         const int at = v < V && order_key(row_value(row[v])) == prefix;
         int total;
         const int before = block_scan_excl(at, sh.ired, total);
-        if (at && have + before < top) sh.list[have + before] = top_entry(prefix, v);
+        if (at && have + before < top) list[have + before] = top_entry(prefix, v);
         have += total;
         __syncthreads();
     }
@@ -153,31 +174,31 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared
 }
 
 // One cluster per row.  The pass that adds up the exponentials leaves the largest value of every piece (a lane's groups of a chunk;
-// FINE: each group) as the upper half of its key.  A border that at least `top` pieces reach leaves at least `top` words, and few
+// FINE: each group) as the upper half of its key.  A border that at least `top` of them reach leaves at least `top` words, and few
 // more: the pieces that reach it are read again (from L2), their words at or above it are sorted.
 template <typename T, bool FINE>
-__global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
+__global__ void __launch_bounds__(TOP_THREADS, TB) k_top(TopArgs a)
 {
-    constexpr int R = TOP_GROUPS, WARPS = TOP_THREADS / 32, PIECES = FINE ? R : 1, SIZE = R / PIECES;  // pieces of a lane's groups, groups of a piece
-    extern __shared__ uint32_t pairs[];  // half-keys of the pieces, two to a word
-    uint16_t* keys = (uint16_t*)pairs;
+    constexpr int R = TOP_GROUPS, PIECES = FINE ? R : 1, SIZE = R / PIECES;  // pieces of a lane's groups, groups of a piece
+    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring and, later, the lists; the pieces' keys
+    TopLists& lists = *(TopLists*)dynamic;
+    uint16_t* keys = (uint16_t*)(dynamic + top_ring_bytes(blockDim.x));
     __shared__ TopShared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, WARPS = threads / 32, V = a.V;
     const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
     const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
     const int pieces = (split.chunk1 - split.chunk0) * 32 * PIECES;
+    ChunkWalk<T, R, TOP_DEPTH> walk;
+    walk.start(dynamic, row, split, V);
     cluster_arrive();
     if (tid < 3) sh.counts[tid] = 0;
     if (tid == 0) sh.n = sh.queued = 0;
     ExpSum sum = ExpSum::none();
     float m = -INFINITY;
-    uint32_t best = 0;
-    for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
-        uint4 raw[R];
-        load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
+    walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, uint4(&raw)[R]) {
         const int at = (c - split.chunk0) * 32 * PIECES + lane;
         float top;
         if (FINE) {
@@ -193,17 +214,27 @@ __global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
             top = groups_max<T, R>(raw);
             keys[at] = (uint16_t)(order_key(top) >> 16);
         }
-        best = max(best, order_key(top) >> 16);
         m = fmaxf(m, top);
         add_groups<T, R>(sum, raw, top, a.scale);
-    }
+    });
     sum.warp_reduce();
     m = warp_reduce_max(m);
-    best = __reduce_max_sync(0xffffffffu, best);
-    if (lane == 0) sh.ered[warp] = sum, sh.fred[warp] = m, sh.ired[warp] = (int)best;
+    if (lane == 0) sh.ered[warp] = sum, sh.fred[warp] = m;
     __syncthreads();
-    best = (uint32_t)__reduce_max_sync(0xffffffffu, lane < WARPS ? sh.ired[lane] : 0);
-    // The largest half-key that at least `want` pieces of this part reach, or one that not many more do: steps of doubling width
+    // the pieces' keys in eight groups per thread, the largest of each
+    uint32_t tops[8] = {};
+    for (int i = tid; i < pieces; i += 8 * threads)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k * threads < pieces) tops[k] = max(tops[k], (uint32_t)keys[i + k * threads]);
+    uint32_t best = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) best = max(best, tops[k]);
+    best = __reduce_max_sync(0xffffffffu, best);
+    if (lane == 0) sh.ired[warp] = (int)best;
+    __syncthreads();
+    best = __reduce_max_sync(0xffffffffu, lane < WARPS ? (uint32_t)sh.ired[lane] : 0u);
+    // The largest half-key that at least `want` of these groups reach, or one that not many more do: steps of doubling width
     // down from `hi` (that fewer reach), then halving; minus infinity's successor if there are not that many.
     int round = 0;
     auto border_of = [&](int want, uint32_t hi) {
@@ -213,8 +244,9 @@ __global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
             const uint32_t mid = down ? hi - step : (lo + hi) / 2;
             step = down ? step * 2 : step;
             int n = 0;
-            for (int i = tid; i < pieces / 2; i += TOP_THREADS) n += __popc(__vcmpgeu2(pairs[i], mid * 0x10001u));
-            n = __reduce_add_sync(0xffffffffu, n) / 16;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n += tops[k] >= mid;
+            n = __reduce_add_sync(0xffffffffu, n);
             if (lane == 0 && n) atomicAdd(&sh.counts[round % 3], n);
             if (tid == 0) sh.counts[(round + 1) % 3] = 0;
             __syncthreads();
@@ -227,7 +259,7 @@ __global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
         }
         return lo;
     };
-    // `top` pieces of one part are enough, and so are its share of them in every part
+    // `top` groups of one part are enough, and so are its share of them in every part
     const uint32_t share = border_of((a.top + ctas - 1) / ctas, best + 1);
     const uint32_t alone = ctas > 1 ? border_of(a.top, share + 1) : share;
     if (warp == 0) {
@@ -267,19 +299,19 @@ __global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
     }
     // the pieces that reach the border, then a group of one to every thread
     int* n_all = cluster.map_shared_rank(&sh.n, 0);
-    unsigned long long* list = cluster.map_shared_rank(sh.list, 0);
-    for (int i = tid; i < pieces; i += TOP_THREADS)
+    unsigned long long* list = cluster.map_shared_rank(lists.list, 0);
+    for (int i = tid; i < pieces; i += threads)
         if (keys[i] >= border) {
             const int at = atomicAdd(&sh.queued, 1);
-            if (at < TOP_QUEUE) sh.queue[at] = i;
+            if (at < TOP_QUEUE) lists.queue[at] = i;
         }
     __syncthreads();
     const int queued = sh.queued;
     if (queued > TOP_QUEUE) {
         if (tid == 0) atomicAdd(n_all, TOP_LIST + 1);
     } else
-        for (int t = tid; t < queued * SIZE; t += TOP_THREADS) {
-            const int i = sh.queue[t / SIZE];  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
+        for (int t = tid; t < queued * SIZE; t += threads) {
+            const int i = lists.queue[t / SIZE];  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
             const int chunk = split.chunk0 + i / (32 * PIECES);
             const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
             const int first = chunk_first<T, R>(chunk, split.pre) + group * PER<T>;
@@ -301,21 +333,21 @@ __global__ void __launch_bounds__(TOP_THREADS) k_top(TopArgs a)
     int n = sh.n;
     if (n > TOP_LIST) {
         __syncthreads();
-        n = top_by_bytes<T>(row, V, a.top, sh);
+        n = top_by_bytes<T>(row, V, a.top, sh, lists.list);
         __syncthreads();
     }
-    sort_entries(sh.list, n);
+    sort_entries(lists.list, n);
     const int want = min(n, a.top);
-    for (int i = tid; i < a.top; i += TOP_THREADS) {
+    for (int i = tid; i < a.top; i += threads) {
         const int64_t at = r * a.top + i;
-        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)sh.list[i]) : -1;
+        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)lists.list[i]) : -1;
         a.ids[at] = v;
         ((T*)a.values)[at] = v >= 0 ? row[v] : row_element<T>(-INFINITY);
     }
     if (a.lse && tid == 0) {
         sum = sh.parts[far][0].sum;
         for (int k = 1; k < ctas; ++k) sum.add(sh.parts[far][k].sum);
-        const uint32_t first = want > 0 ? (uint32_t)(sh.list[0] >> 32) : 0;
+        const uint32_t first = want > 0 ? (uint32_t)(lists.list[0] >> 32) : 0;
         // (log2 of the largest exponential: x c, or 0 when far)
         const double most2 = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
         a.lse[r] = want == 0 ? -INFINITY
@@ -329,13 +361,12 @@ template <typename T>
 static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
 {
     constexpr int CHUNK = 32 * TOP_GROUPS * PER<T>;
-    int ctas = row_ctas(rows, (int64_t)a.V * sizeof(T), 4, 8192, TOP_CTAS);
-    // every part has to hold several times `top` pieces, or the border stays too low
-    while (ctas > 1 && a.V / PER<T> / ctas < 4 * a.top) ctas /= 2;
-    const bool fine = a.V / PER<T> / TOP_GROUPS / ctas < 4 * a.top;
+    RowShape shape = row_shape(rows, (int64_t)a.V * sizeof(T), 1024, 64);
+    const int per = a.V / PER<T>;
+    const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = (size_t)((chunks + ctas - 1) / ctas) * 32 * (fine ? TOP_GROUPS : 1) * 2;
-    return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, ctas, TOP_THREADS, smem, sizeof(TopShared), st);
+    const size_t smem = top_ring_bytes(shape.threads) + (size_t)((chunks + shape.ctas - 1) / shape.ctas) * 32 * (fine ? TOP_GROUPS : 1) * 2;
+    return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, shape, smem, sizeof(TopShared), st);
 }
 
 }  // namespace lda

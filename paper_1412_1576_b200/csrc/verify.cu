@@ -27,17 +27,26 @@ constexpr int VERIFY_GROUPS = 4;  // groups of each row a lane has in flight
 constexpr int VERIFY_CTAS = 8;    // of a cluster, at most
 constexpr int VERIFY_CHUNKS = LDA_ROW_MAX_V / (32 * VERIFY_GROUPS * PER<float>) + 1;
 
-// A probability as a multiple of 2^-42: NaN and what is below zero as 0, what is above one as 1.
-__device__ __forceinline__ unsigned long long prob_mass(float r)
-{
-    return __float2ull_rz(fminf(fmaxf(r, 0.0f), 1.0f) * 4398046511104.0f);
-}
-
+// Masses: floor(2^42 x) for x in [0, 1], as 19 upper and 23 lower bits.  The bits are pushed to the end of a float by an addition of
+// 2^23 that rounds down; what that leaves over is exact and goes the same way.
+constexpr uint32_t MASS_ONE = 0x4B000000u;  // 2^23
+struct MassSum {
+    uint32_t upper, lower;
+    __device__ __forceinline__ void add(float x)  // x in [0, 1]
+    {
+        const float hi = __fmaf_rz(x, 524288.0f, 8388608.0f);
+        const float rest = __fmaf_rn(x, 524288.0f, 8388608.0f - hi);
+        const float lo = __fmaf_rz(rest, 8388608.0f, 8388608.0f);
+        upper += __float_as_uint(hi) - MASS_ONE;
+        lower += __float_as_uint(lo) - MASS_ONE;
+    }
+    __device__ __forceinline__ unsigned long long value() const { return ((unsigned long long)upper << 23) + lower; }
+};
 // One cluster per sequence.  Every CTA finds the first draft that is refused by itself (the sequences are short), then each adds
 // up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk, and one
 // warp reads that again to find the word.  Bound by the read of one row of the target and, behind a refusal, one of the drafter.
 template <typename T, bool PROBS>
-__global__ void __launch_bounds__(VERIFY_THREADS) k_verify(VerifyArgs a)
+__global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
 {
     constexpr int R = VERIFY_GROUPS, CHUNK = 32 * R * PER<T>;
     __shared__ unsigned long long sums[VERIFY_CHUNKS], red[33], parts[2][VERIFY_CTAS], s_want;
@@ -91,19 +100,19 @@ __global__ void __launch_bounds__(VERIFY_THREADS) k_verify(VerifyArgs a)
     for (int plain = 0; plain < 2; ++plain) {
         const T* q = plain ? nullptr : qrow;
         const int32_t out = plain ? -1 : gone;
-        auto mass = [&](int v) {
+        auto part = [&](int v) {
             const float p = row_value(prow[v]);
-            return prob_mass(q ? p - row_value(q[v]) : v == out ? 0.0f : p);
+            return q ? __saturatef(p - row_value(q[v])) : v == out ? 0.0f : __saturatef(p);
         };
         for (int c = split.chunk0 + warp; c < split.chunk1; c += VERIFY_THREADS / 32) {
             const int first = chunk_first<T, R>(c, split.pre);
-            unsigned long long sum = 0;
+            MassSum sum{0, 0};  // of 32 words at most: below 2^25 and 2^28
             if (q && !abreast || !chunk_inside<T, R>(first, V)) {
                 // rows at different offsets from 16 bytes, and the row's edges: by elements, in any order
 #pragma unroll 8
                 for (int i = lane; i < CHUNK; i += 32) {
                     const int v = first + i;
-                    if (v >= 0 && v < V) sum += mass(v);
+                    if (v >= 0 && v < V) sum.add(part(v));
                 }
             } else {
                 uint4 rp[R], rq[R];
@@ -116,16 +125,18 @@ __global__ void __launch_bounds__(VERIFY_THREADS) k_verify(VerifyArgs a)
                     if (q) {
                         unpack<T>(rq[r], xq);
 #pragma unroll
-                        for (int i = 0; i < PER<T>; ++i) sum += prob_mass(xp[i] - xq[i]);
+                        for (int i = 0; i < PER<T>; ++i) sum.add(__saturatef(xp[i] - xq[i]));
                     } else {
                         const int at = out - (first + (32 * r + lane) * PER<T>);
 #pragma unroll
-                        for (int i = 0; i < PER<T>; ++i) sum += i == at ? 0ull : prob_mass(xp[i]);
+                        for (int i = 0; i < PER<T>; ++i) sum.add(i == at ? 0.0f : __saturatef(xp[i]));
                     }
                 }
             }
-            sum = warp_reduce_sum(sum);
-            if (lane == 0) sums[c - split.chunk0] = sum;
+            // (the lower halves in two parts, so that 32 lanes' sums stay inside 32 bits)
+            const uint32_t upper = __reduce_add_sync(0xffffffffu, sum.upper);
+            const uint32_t low = __reduce_add_sync(0xffffffffu, sum.lower & 0xFFFFu), high = __reduce_add_sync(0xffffffffu, sum.lower >> 16);
+            if (lane == 0) sums[c - split.chunk0] = ((unsigned long long)upper << 23) + ((unsigned long long)high << 16) + low;
         }
         __syncthreads();
         const int chunks = split.chunk1 - split.chunk0;
@@ -160,21 +171,24 @@ __global__ void __launch_bounds__(VERIFY_THREADS) k_verify(VerifyArgs a)
         }
         __syncthreads();
         if (warp == 0) {
-            // a lane takes consecutive words
+            // a lane takes consecutive words (their masses are all read before the first is looked at)
             const int first = chunk_first<T, R>(split.chunk0 + s_chunk, split.pre) + lane * (CHUNK / 32);
-            unsigned long long sum = 0;
+            float x[CHUNK / 32];
+            MassSum all{0, 0};
 #pragma unroll
-            for (int i = 0; i < CHUNK / 32; ++i)
-                if (first + i >= 0 && first + i < V) sum += mass(first + i);
-            const unsigned long long upto = warp_scan_incl(sum), left = s_want - (upto - sum);
+            for (int i = 0; i < CHUNK / 32; ++i) x[i] = first + i >= 0 && first + i < V ? part(first + i) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < CHUNK / 32; ++i) all.add(x[i]);
+            const unsigned long long sum = all.value(), upto = warp_scan_incl(sum), left = s_want - (upto - sum);
             if (upto - sum <= s_want && s_want < upto) {
-                unsigned long long run = 0;
-                int v = max(first, 0);
-                for (; v < V; ++v) {
-                    run += mass(v);
-                    if (run > left) break;
+                MassSum run{0, 0};
+                int passed = 0;
+#pragma unroll
+                for (int i = 0; i < CHUNK / 32; ++i) {
+                    run.add(x[i]);
+                    passed += run.value() <= left;
                 }
-                s_chunk = v;
+                s_chunk = first + passed;
             }
         }
         __syncthreads();
@@ -189,8 +203,9 @@ __global__ void __launch_bounds__(VERIFY_THREADS) k_verify(VerifyArgs a)
 template <typename T>
 static cudaError_t run_verify(const VerifyArgs& a, int64_t n_seqs, cudaStream_t st)
 {
-    const int ctas = row_ctas(n_seqs, (int64_t)a.V * sizeof(T), 4, 8192, VERIFY_CTAS);
-    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, ctas, VERIFY_THREADS, 0, 17 * 1024, st);
+    int ctas = 1;
+    while (ctas < VERIFY_CTAS && n_seqs * ctas < 148 * 4 && (int64_t)a.V * (int)sizeof(T) >= 2 * ctas * 8192) ctas *= 2;
+    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, RowShape{ctas, VERIFY_THREADS}, 0, 17 * 1024, st);
 }
 
 }  // namespace lda
