@@ -120,6 +120,14 @@ __device__ __forceinline__ uint4 edge_group(const T* row, int first, int V, T fi
     return g.raw;
 }
 
+template <typename T>
+__device__ __forceinline__ bool group_inside(int first, int V) { return first >= 0 && first + PER<T> <= V; }
+template <typename T>
+__device__ __forceinline__ uint4 any_group(const T* row, int first, int V, T fill)
+{
+    return group_inside<T>(first, V) ? __ldcg(reinterpret_cast<const uint4*>(row + first)) : edge_group(row, first, V, fill);
+}
+
 // The lane's groups of a chunk.  (Loads that pass L1 by: what is read twice is read from L2 the second time.)
 template <typename T, int R>
 __device__ __forceinline__ void load_chunk(const T* row, int first, int V, T fill, uint4 (&raw)[R])
@@ -131,7 +139,7 @@ __device__ __forceinline__ void load_chunk(const T* row, int first, int V, T fil
         for (int r = 0; r < R; ++r) raw[r] = __ldcg(p + 32 * r);
     } else {
 #pragma unroll
-        for (int r = 0; r < R; ++r) raw[r] = edge_group(row, first + (32 * r + lane) * PER<T>, V, fill);
+        for (int r = 0; r < R; ++r) raw[r] = any_group(row, first + (32 * r + lane) * PER<T>, V, fill);
     }
 }
 
@@ -148,15 +156,16 @@ struct ChunkWalk {
     {
         if (c < split.chunk1) {
             const int first = chunk_first<T, R>(c, split.pre);
-            if (chunk_inside<T, R>(first, V)) {
-                const T* from = row + first + (threadIdx.x & 31) * PER<T>;
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + into * R * (int)blockDim.x);
+            const int mine = first + (int)(threadIdx.x & 31) * PER<T>;
+            const T* from = row + mine;
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + into * R * (int)blockDim.x);
+            const bool inside = chunk_inside<T, R>(first, V);
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r)
+                if (inside || group_inside<T>(mine + 32 * PER<T> * r, V))
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * (uint32_t)blockDim.x * 16),
                                  "l"(from + 32 * PER<T> * r)
                                  : "memory");
-            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
@@ -183,8 +192,10 @@ struct ChunkWalk {
                 for (int r = 0; r < R; ++r) raw[r] = ring[(slot * R + r) * (int)blockDim.x];
             } else {
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-                    raw[r] = edge_group(row, first + (32 * r + (int)(threadIdx.x & 31)) * PER<T>, V, fill);
+                for (int r = 0; r < R; ++r) {
+                    const int v = first + (32 * r + (int)(threadIdx.x & 31)) * PER<T>;
+                    raw[r] = group_inside<T>(v, V) ? ring[(slot * R + r) * (int)blockDim.x] : edge_group(row, v, V, fill);
+                }
             }
             f(chunk, raw);
             // (the place is free: its groups have been worked on)

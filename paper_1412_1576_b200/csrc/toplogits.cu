@@ -315,8 +315,7 @@ __global__ void __launch_bounds__(TOP_THREADS, TB) k_top(TopArgs a)
             const int chunk = split.chunk0 + i / (32 * PIECES);
             const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
             const int first = chunk_first<T, R>(chunk, split.pre) + group * PER<T>;
-            const uint4 raw = first >= 0 && first + PER<T> <= V ? __ldcg(reinterpret_cast<const uint4*>(row + first))
-                                                                : edge_group(row, first, V, row_element<T>(-INFINITY));
+            const uint4 raw = any_group(row, first, V, row_element<T>(-INFINITY));
             float x[PER<T>];
             unpack<T>(raw, x);
 #pragma unroll

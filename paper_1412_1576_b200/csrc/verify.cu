@@ -22,7 +22,7 @@ struct VerifyArgs {
     int32_t V;
 };
 
-constexpr int VERIFY_THREADS = 512;
+constexpr int VERIFY_THREADS = 512;  // of a CTA, at most
 constexpr int VERIFY_GROUPS = 4;  // groups of each row a lane has in flight
 constexpr int VERIFY_CTAS = 8;    // of a cluster, at most
 constexpr int VERIFY_CHUNKS = LDA_ROW_MAX_V / (32 * VERIFY_GROUPS * PER<float>) + 1;
@@ -43,23 +43,24 @@ struct MassSum {
     __device__ __forceinline__ unsigned long long value() const { return ((unsigned long long)upper << 23) + lower; }
 };
 // One cluster per sequence.  Every CTA finds the first draft that is refused by itself (the sequences are short), then each adds
-// up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk, and one
-// warp reads that again to find the word.  Bound by the read of one row of the target and, behind a refusal, one of the drafter.
+// up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk and
+// reads that again to find the word.  Bound by the read of one row of the target and, behind a refusal, one of the drafter.
 template <typename T, bool PROBS>
 __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
 {
     constexpr int R = VERIFY_GROUPS, CHUNK = 32 * R * PER<T>;
     __shared__ unsigned long long sums[VERIFY_CHUNKS], red[33], parts[2][VERIFY_CTAS], s_want;
-    __shared__ int s_taken, s_chunk;
+    __shared__ int s_taken, s_chunk, s_token;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
     const int64_t b = blockIdx.x / ctas, lo = a.offsets[b], hi = a.offsets[b + 1];
     if (lo < 0 || hi < lo || hi > a.n_drafts) {  // (the same in every CTA of the cluster)
         if (rank == 0 && tid == 0) a.accepted[b] = -1;
         return;
     }
     const int n = (int)(hi - lo);
+    const float u = a.draw_u[b];
     const T* target = (const T*)a.target;
     const T* probs = (const T*)a.probs;
     cluster_arrive();
@@ -90,8 +91,9 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
     const bool refused = taken < n;
     const T* prow = target + (lo + taken + b) * a.target_stride;
     const T* qrow = PROBS && refused ? probs + (lo + taken) * a.probs_stride : nullptr;
-    const int32_t gone = !PROBS && refused ? a.drafts[lo + taken] : -1;
     const int V = a.V;
+    int32_t gone = !PROBS && refused ? a.drafts[lo + taken] : -1;  // the word that the draft takes out of p
+    if (gone < 0 || gone >= V) gone = -1;
     const RowSplit split = RowSplit::of<T, R>(prow, V, rank, ctas);
     const bool abreast = PROBS && (uintptr_t)qrow % 16 == (uintptr_t)prow % 16;
     cluster_wait();
@@ -104,12 +106,12 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
             const float p = row_value(prow[v]);
             return q ? __saturatef(p - row_value(q[v])) : v == out ? 0.0f : __saturatef(p);
         };
-        for (int c = split.chunk0 + warp; c < split.chunk1; c += VERIFY_THREADS / 32) {
+        for (int c = split.chunk0 + warp; c < split.chunk1; c += threads / 32) {
             const int first = chunk_first<T, R>(c, split.pre);
             MassSum sum{0, 0};  // of 32 words at most: below 2^25 and 2^28
-            if (q && !abreast || !chunk_inside<T, R>(first, V)) {
-                // rows at different offsets from 16 bytes, and the row's edges: by elements, in any order
-#pragma unroll 8
+            if (q && !abreast) {
+                // rows at different offsets from 16 bytes: by elements, in any order
+#pragma unroll 16
                 for (int i = lane; i < CHUNK; i += 32) {
                     const int v = first + i;
                     if (v >= 0 && v < V) sum.add(part(v));
@@ -141,7 +143,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
         __syncthreads();
         const int chunks = split.chunk1 - split.chunk0;
         unsigned long long own = 0;
-        for (int c = tid; c < chunks; c += VERIFY_THREADS) own += sums[c];
+        for (int c = tid; c < chunks; c += threads) own += sums[c];
         own = block_reduce_sum(own, red);
         if (tid < ctas) *cluster.map_shared_rank(&parts[plain][rank], tid) = own;
         cluster.sync();
@@ -154,12 +156,11 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
             here = rank == 0;
             continue;
         }
-        const float u = a.draw_u[b];
         const unsigned long long U = u > 0.0f ? (u < 1.0f ? __float2ull_rz(u * 4294967296.0f) : 0xFFFFFFFFull) : 0ull;
         const unsigned long long want = __umul64hi(total, U << 32);
         here = before <= want && want < before + own;
         if (!here) break;
-        for (int c = 0; c < chunks; c += VERIFY_THREADS) {
+        for (int c = 0; c < chunks; c += threads) {
             unsigned long long all;
             const unsigned long long sum = c + tid < chunks ? sums[c + tid] : 0ull;
             const unsigned long long start = before + block_scan_excl(sum, red, all);
@@ -170,42 +171,33 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
             before += all;
         }
         __syncthreads();
-        if (warp == 0) {
-            // a lane takes consecutive words (their masses are all read before the first is looked at)
-            const int first = chunk_first<T, R>(split.chunk0 + s_chunk, split.pre) + lane * (CHUNK / 32);
-            float x[CHUNK / 32];
-            MassSum all{0, 0};
-#pragma unroll
-            for (int i = 0; i < CHUNK / 32; ++i) x[i] = first + i >= 0 && first + i < V ? part(first + i) : 0.0f;
-#pragma unroll
-            for (int i = 0; i < CHUNK / 32; ++i) all.add(x[i]);
-            const unsigned long long sum = all.value(), upto = warp_scan_incl(sum), left = s_want - (upto - sum);
-            if (upto - sum <= s_want && s_want < upto) {
-                MassSum run{0, 0};
-                int passed = 0;
-#pragma unroll
-                for (int i = 0; i < CHUNK / 32; ++i) {
-                    run.add(x[i]);
-                    passed += run.value() <= left;
-                }
-                s_chunk = first + passed;
-            }
+        // a thread takes consecutive words
+        const int first = chunk_first<T, R>(split.chunk0 + s_chunk, split.pre);
+        const unsigned long long looked_for = s_want;
+        unsigned long long start = 0;
+        for (int i = tid; i - tid < CHUNK; i += threads) {
+            const int v = first + i;
+            MassSum one{0, 0};
+            if (i < CHUNK && v >= 0 && v < V) one.add(part(v));
+            unsigned long long all;
+            const unsigned long long upto = start + block_scan_excl(one.value(), red, all);
+            if (upto <= looked_for && looked_for < upto + one.value()) s_token = v;
+            start += all;
         }
         __syncthreads();
-        token = s_chunk;
+        token = s_token;
         break;
     }
     if (!here) return;
-    for (int i = tid; i <= n; i += VERIFY_THREADS) a.tokens[lo + b + i] = i < taken ? a.drafts[lo + i] : i == taken ? token : -1;
+    for (int i = tid; i <= n; i += threads) a.tokens[lo + b + i] = i < taken ? a.drafts[lo + i] : i == taken ? token : -1;
     if (tid == 0) a.accepted[b] = taken;
 }
 
 template <typename T>
 static cudaError_t run_verify(const VerifyArgs& a, int64_t n_seqs, cudaStream_t st)
 {
-    int ctas = 1;
-    while (ctas < VERIFY_CTAS && n_seqs * ctas < 148 * 4 && (int64_t)a.V * (int)sizeof(T) >= 2 * ctas * 8192) ctas *= 2;
-    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, RowShape{ctas, VERIFY_THREADS}, 0, 17 * 1024, st);
+    const RowShape shape = row_shape(n_seqs, (int64_t)a.V * sizeof(T), 1024, 64);
+    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, shape, 0, 17 * 1024, st);
 }
 
 }  // namespace lda

@@ -18,21 +18,24 @@ _DTYPES = {torch.float32: _b.LDA_F32, torch.float16: _b.LDA_F16, torch.bfloat16:
 def _rows(x, name):
     """Checks a matrix whose rows are consecutive in memory; returns (dtype code, rows, V, row stride)."""
     code = _DTYPES.get(x.dtype)
-    if code is None:
-        raise TypeError(f"{name}: float32, float16 or bfloat16 is needed, not {x.dtype}")
-    if x.dim() != 2 or x.shape[1] < 1:
-        raise ValueError(f"{name}: a matrix with at least one column is needed, not {tuple(x.shape)}")
-    if x.shape[1] > 1 and x.stride(1) != 1:
+    shape = x.shape
+    if code is None or len(shape) != 2 or shape[1] < 1:
+        if code is None:
+            raise TypeError(f"{name}: float32, float16 or bfloat16 is needed, not {x.dtype}")
+        raise ValueError(f"{name}: a matrix with at least one column is needed, not {tuple(shape)}")
+    between, step = x.stride()
+    if step != 1 and shape[1] > 1:
         raise ValueError(f"{name}: the words of a row must be consecutive in memory")
-    return code, x.shape[0], x.shape[1], x.stride(0)
+    return code, shape[0], shape[1], between if shape[0] > 1 else shape[1]
 
 
 def _vector(x, name, dtype, n, device):
-    if x.dtype != dtype:
+    """Checks a contiguous vector; returns its address."""
+    if x.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {x.dtype}")
-    if x.dim() != 1 or x.shape[0] != n:
+    if x.shape != (n,):
         raise ValueError(f"{name}: {n} values are needed, not {tuple(x.shape)}")
-    if n > 1 and x.stride(0) != 1:
+    if not x.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
     _here(x, name, device)
     return x.data_ptr()
@@ -49,16 +52,19 @@ def _cuda(x, name):
     return x.device
 
 
-def _call(fn, device, *args):
+def _call(name, device, *args):
     """One library call on the device's current stream."""
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
+    fn = getattr(_b.load_library(), name)
+    index = device.index
+    # (the stream's address as torch's own generated code asks for it: a fifth of current_stream()'s time)
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch.cuda.current_device() == index:
         rc = fn(*args, stream)
     else:
         with torch.cuda.device(device):
             rc = fn(*args, stream)
     if rc:
-        raise _b.LdaError(rc, fn.__name__)
+        raise _b.LdaError(rc, name)
 
 
 def top_logits(logits, top: int, temperature: float = 1.0):
@@ -74,7 +80,7 @@ def top_logits(logits, top: int, temperature: float = 1.0):
     ids = torch.empty((rows, top), dtype=torch.int32, device=device)
     values = torch.empty((rows, top), dtype=logits.dtype, device=device)
     lse = torch.empty(rows, dtype=torch.float32, device=device)
-    _call(_b.lda_top_logits, device, logits.data_ptr(), code, rows, V, stride, top, temperature, ids.data_ptr(),
+    _call("lda_top_logits", device, logits.data_ptr(), code, rows, V, stride, top, temperature, ids.data_ptr(),
           values.data_ptr(), lse.data_ptr())
     return ids, values, lse
 
@@ -91,14 +97,15 @@ def _list(ids, values, lse, rows, device):
     top = ids.shape[1]
     if not 1 <= top <= _b.LDA_TOP_MAX:
         raise ValueError(f"ids: lists of 1 to {_b.LDA_TOP_MAX} words, not {top}")
-    if top > 1 and (ids.stride(1) != 1 or values.stride(1) != 1):
+    (between, step), (values_between, values_step) = ids.stride(), values.stride()
+    if top > 1 and (step != 1 or values_step != 1):
         raise ValueError("ids and values: the places of a list must be consecutive in memory")
-    if rows > 1 and ids.stride(0) != values.stride(0):
+    if rows > 1 and between != values_between:
         raise ValueError("ids and values: their rows must lie equally far apart")
     _here(ids, "ids", device)
     _here(values, "values", device)
     teacher_lse = None if lse is None else _vector(lse, "lse", torch.float32, rows, device)
-    return ids.data_ptr(), values.data_ptr(), code, top, ids.stride(0), teacher_lse
+    return ids.data_ptr(), values.data_ptr(), code, top, between if rows > 1 else top, teacher_lse
 
 
 class _Distill(torch.autograd.Function):
@@ -122,7 +129,7 @@ def _loss(logits, ids, values, lse, temperature):
     code, rows, V, stride = _rows(logits, "logits")
     lists = _list(ids, values, lse, rows, device)
     loss = torch.empty(rows, dtype=torch.float32, device=device)
-    _call(_b.lda_distill_loss, device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, loss.data_ptr())
+    _call("lda_distill_loss", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, loss.data_ptr())
     return loss
 
 
@@ -132,11 +139,11 @@ def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
     lists = _list(ids, values, lse, rows, device)
     if grad.dtype != logits.dtype or grad.shape != logits.shape:
         raise ValueError("grad: must have the logits' type and shape")
-    _rows(grad, "grad")
+    grad_stride = _rows(grad, "grad")[3]
     _here(grad, "grad", device)
     w = None if weights is None else _vector(weights, "weights", torch.float32, rows, device)
-    _call(_b.lda_distill_grad, device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
-          None if loss is None else loss.data_ptr(), grad.data_ptr(), grad.stride(0))
+    _call("lda_distill_grad", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
+          None if loss is None else loss.data_ptr(), grad.data_ptr(), grad_stride)
 
 
 def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
@@ -158,7 +165,8 @@ def distill_loss_and_grad(logits, ids, values, lse=None, temperature: float = 1.
     weights: float32 [rows], None for 1 each; a row of weight 0 has gradient 0.  grad: where the gradient goes, None for a
     new tensor; the logits themselves are allowed and are overwritten then.  Returns (loss, grad).  No autograd graph is made.
     """
-    logits = logits.detach()
+    if logits.requires_grad:
+        logits = logits.detach()
     if grad is None:
         grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
@@ -200,6 +208,6 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
         accepted = torch.empty(n_seqs, dtype=torch.int32, device=device)
     tokens_ptr = _vector(tokens, "tokens", torch.int32, rows, device)
     accepted_ptr = _vector(accepted, "accepted", torch.int32, n_seqs, device)
-    _call(_b.lda_verify_drafts, device, offsets_ptr, n_seqs, drafts_ptr, n_drafts, target.data_ptr(), stride, probs_ptr,
+    _call("lda_verify_drafts", device, offsets_ptr, n_seqs, drafts_ptr, n_drafts, target.data_ptr(), stride, probs_ptr,
           probs_stride, code, V, accept_ptr, draw_ptr, tokens_ptr, accepted_ptr)
     return tokens, accepted
