@@ -7,6 +7,8 @@
 //   dloss / dx_v = tau (W q_v - sum of the p_j at v)   for a word of the list, W = sum p_j + P
 //                = tau q_v (W - P / Q)                 for any other
 // Q is summed over the unlisted words themselves: 1 - sum q_j would lose what matters where the list holds nearly all mass.
+#include <algorithm>
+
 #include "lda_device.cuh"
 #include "rows.cuh"
 
@@ -29,19 +31,17 @@ struct DistillArgs {
     double tau, inv_tau;
 };
 
-constexpr int DISTILL_THREADS = 512;  // of a CTA, at most
 #ifndef DG
 #define DG 4
 #endif
 #ifndef DB
 #define DB 2
 #endif
-constexpr int DISTILL_GROUPS = DG;  // groups a lane has in flight
 #ifndef DD
 #define DD 3
 #endif
-constexpr int DISTILL_DEPTH = DD;  // chunks on their way
-constexpr int DISTILL_CTAS = 8;    // of a cluster, at most
+constexpr int DISTILL_GROUPS = DG;  // groups of a lane in a chunk
+constexpr int DISTILL_DEPTH = DD;   // chunks on their way
 
 // What a CTA knows of its part of the row.
 struct DistillPart {
@@ -49,10 +49,10 @@ struct DistillPart {
     float max;
 };
 
-// What the gradient needs of the whole row.
+// What the gradient needs of the whole row: 2^(x c - ref) times `others` for a word outside the list; weight tau W / sum of
+// exponentials and weight tau for those of the list.
 struct DistillRow {
-    float ref, others;     // 2^(x c - ref) times `others` is the gradient of a word outside the list
-    double w, inv, mass;   // weight tau; 1 / sum of exponentials; W
+    float ref, others, listed, w, list_ref;
 };
 
 // Bits of a group's elements in a map with a bit for each element.
@@ -65,21 +65,21 @@ __device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
 
 // One cluster per row; every CTA has the whole list and a part of the row.  The words of the list are marked in a bit map of that
 // part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The CTAs exchange
-// their sums, and each works out the gradient of its part: the same factor times the exponential for all words, from a second read
-// that L2 answers, then the list's words over it.
-template <typename T, bool TAIL, bool GRAD>
-__global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
+// their sums, and each works out the gradient of its part: the same factor times the exponential for all words, then the list's
+// words over it.  KEEP: the ring holds all of the CTA's part from the first pass on; else it is read again, from L2.
+template <typename T, bool TAIL, bool GRAD, bool KEEP>
+__global__ void __launch_bounds__(ROW_THREADS, DB) k_distill(DistillArgs a)
 {
     constexpr int R = DISTILL_GROUPS, CHUNK = 32 * R * PER<T>;
     constexpr bool BITS = TAIL || GRAD;
-    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the map of the list's words
     using Walk = ChunkWalk<T, R, DISTILL_DEPTH>;
-    uint32_t* bits = (uint32_t*)(dynamic + blockDim.x * Walk::BYTES);
-    __shared__ int ids[LDA_TOP_MAX];
-    __shared__ float p[LDA_TOP_MAX], x[LDA_TOP_MAX];
-    __shared__ ExpSum ered[DISTILL_THREADS / 32];
-    __shared__ float fred[DISTILL_THREADS / 32];
-    __shared__ DistillPart parts[2][DISTILL_CTAS];
+    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the list, the map of its words
+    int* ids = (int*)(dynamic + blockDim.x * Walk::BYTES);
+    float *p = (float*)(ids + a.top), *log_p = p + a.top, *x = log_p + a.top;
+    uint32_t* bits = (uint32_t*)(x + a.top);
+    __shared__ ExpSum ered[ROW_THREADS / 32];
+    __shared__ float fred[ROW_THREADS / 32];
+    __shared__ DistillPart parts[2][ROW_CTAS];
     __shared__ DistillRow whole;
     __shared__ int s_any, s_twice;
     cg::cluster_group cluster = cg::this_cluster();
@@ -88,7 +88,9 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
     const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
     T* grad = GRAD ? (T*)a.grad + r * a.grad_stride : nullptr;
+    const T none = row_element<T>(-INFINITY);
     const float weight = GRAD && a.weights ? a.weights[r] : 1.0f;
+    const float teacher_lse = TAIL ? a.teacher_lse[r] : 0.0f;
     const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
     // this CTA's words, and the word of the map's first bit
     const int bit0 = chunk_first<T, R>(split.chunk0, split.pre);
@@ -97,30 +99,40 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
     walk.start(dynamic, row, split, V);
     if (tid == 0) s_any = s_twice = 0;
     if (BITS)
-        for (int i = tid; i < (split.chunk1 - split.chunk0) * (CHUNK / 32); i += threads) bits[i] = 0;
+        for (int i = tid; i < (split.chunk1 - split.chunk0) * (CHUNK / 128); i += threads) ((uint4*)bits)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    const auto teacher = [&](int j) { return any_value(a.values, a.values_dtype, r * a.list_stride + j); };
     for (int j = tid; j < a.top; j += threads) {
-        const int id = a.ids[r * a.list_stride + j];
+        const int64_t at = r * a.list_stride + j;
+        const int id = a.ids[at];
         const bool ok = id >= 0 && id < V;
+        p[j] = any_value(a.values, a.values_dtype, at);
         ids[j] = ok ? id : -1;
-        p[j] = teacher(j);
         if (ok) {
             s_any = 1;
             if (BITS && id >= v0 && id < v1) {
                 const int bit = id - bit0;
                 if (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
             }
+            x[j] = row_value(row[id]);
         }
     }
     __syncthreads();
     if (!s_any || (GRAD && weight == 0.0f && !a.loss)) {  // (the same in every CTA of the cluster)
         if (a.loss && rank == 0 && tid == 0) a.loss[r] = 0.0f;
-        if (GRAD)
-            for (int v = v0 + tid; v < v1; v += threads) grad[v] = row_element<T>(0.0f);
+        walk.drop();
+        if (GRAD) {
+            const bool aligned = (uintptr_t)grad % 16 == (uintptr_t)row % 16;
+            for (int v = v0 + tid * PER<T>; v < v1 + PER<T>; v += threads * PER<T>) {
+                const int first = (v + split.pre) / PER<T> * PER<T> - split.pre;  // the group that v is in
+                if (aligned && first >= v0 && first + PER<T> <= v1)
+                    *reinterpret_cast<uint4*>(grad + first) = make_uint4(0, 0, 0, 0);
+                else
+                    for (int i = max(first, v0); i < min(first + PER<T>, v1); ++i) grad[i] = row_element<T>(0.0f);
+            }
+        }
         return;
     }
-    cluster_arrive();
+    if (ctas > 1) cluster_arrive();
     // which place of the list stands for a word that it holds twice: the first
     auto leads = [&](int j) {
         bool first = true;
@@ -128,38 +140,41 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
             for (int o = 0; o < j; ++o) first = first && ids[o] != ids[j];
         return first;
     };
-    // the teacher (warp 0): log p = (t - t_ref) / tau - base
-    double t_ref = 0.0, base = 0.0, sum_p = 0.0;
+    // the teacher's probabilities and the student's words on the list (warp 0)
+    float sum_p = 0.0f;
     ExpSum in = ExpSum::none();
     if (warp == 0) {
-        for (int j = lane; j < a.top; j += 32)
-            if (ids[j] >= 0) x[j] = row_value(row[ids[j]]);
-        if (TAIL) base = (double)a.teacher_lse[r];
-        else {
-            float tm = -INFINITY;
+        float max_t = -INFINITY, z = 0.0f;
+        if (!TAIL) {
             for (int j = lane; j < a.top; j += 32)
-                if (ids[j] >= 0) tm = fmaxf(tm, p[j]);
-            tm = warp_reduce_max(tm);
-            double z = 0;
-            for (int j = lane; j < a.top; j += 32)
-                if (ids[j] >= 0) z += (double)expf((float)(((double)p[j] - (double)tm) * a.inv_tau));
-            z = warp_reduce_sum(z);
-            t_ref = tm == -INFINITY ? 0.0 : (double)tm;
-            base = tm == -INFINITY ? INFINITY : log(z);  // nothing but minus infinity: no mass
+                if (ids[j] >= 0) max_t = fmaxf(max_t, p[j]);
+            max_t = warp_reduce_max(max_t);
         }
         for (int j = lane; j < a.top; j += 32) {
             const float t = p[j];
-            const float e = ids[j] < 0 || t == -INFINITY ? 0.0f : expf((float)(((double)t - t_ref) * a.inv_tau - base));
+            float l = (float)(TAIL ? (double)t * a.inv_tau - (double)teacher_lse : ((double)t - (double)max_t) * a.inv_tau);
+            if (ids[j] < 0 || t == -INFINITY) l = -INFINITY;
+            const float e = l == -INFINITY ? 0.0f : expf(l);
+            log_p[j] = l;
             p[j] = e;
-            sum_p += (double)e;
-            // the student's words on the list
+            z += e;
             if (TAIL && ids[j] >= v0 && ids[j] < v1 && leads(j)) {
                 in.raise(exp_ref(x[j], a.scale));
                 in.sum += exp2_unit(__fmaf_rn(x[j], a.scale, -in.ref));
             }
         }
-        sum_p = warp_reduce_sum(sum_p);
-        if (TAIL) in.warp_reduce();
+        z = warp_reduce_sum(z);
+        if (TAIL) {
+            sum_p = z;
+            in.warp_reduce();
+        } else if (z > 0.0f || z != z) {  // (a list of nothing but minus infinity has no mass)
+            const float log_z = logf(z);
+            for (int j = lane; j < a.top; j += 32) {
+                p[j] = p[j] / z;
+                log_p[j] -= log_z;
+            }
+            sum_p = z == z ? 1.0f : z;
+        }
     }
     // the student's words outside the list
     ExpSum out = ExpSum::none();
@@ -179,17 +194,18 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
                 u.raw = raw[k];
 #pragma unroll
                 for (int i = 0; i < PER<T>; ++i)
-                    if (marked >> i & 1) u.e[i] = row_element<T>(-INFINITY);
+                    if (marked >> i & 1) u.e[i] = none;
                 raw[k] = u.raw;
             }
         }
     };
-    walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, uint4(&raw)[R]) {
+    walk.each(row, split, V, none, [&](int c, uint4(&raw)[R]) {
         const float top = groups_max<T, R>(raw);
         mask(c, raw);
         m = fmaxf(m, top);  // (a NaN goes into the sums)
         add_groups<T, R>(out, raw, top, a.scale);
     });
+    if (GRAD && !KEEP) walk.start(dynamic, row, split, V);  // the second read is under way while the sums are put together
     out.warp_reduce();
     m = warp_reduce_max(m);
     if (lane == 0) ered[warp] = out, fred[warp] = m;
@@ -199,9 +215,9 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
         out.warp_reduce();
         m = warp_reduce_max(lane < WARPS ? fred[lane] : -INFINITY);
     }
-    cluster_wait();
+    if (ctas > 1) cluster_wait();
     if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = DistillPart{out, in, m};
-    cluster.sync();
+    row_sync(cluster, ctas);
     m = parts[0][0].max;
     for (int k = 1; k < ctas; ++k) m = fmaxf(m, parts[0][k].max);
     const bool far = exp_far(m, a.scale);
@@ -209,7 +225,7 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
         float o = 0.0f, l = 0.0f;
         for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
             uint4 raw[R];
-            load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
+            load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, none, raw);
             mask(c, raw);
             for (int k = 0; k < R; ++k) {
                 float y[PER<T>];
@@ -226,7 +242,7 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
         __syncthreads();
         if (warp == 0) o = warp_reduce_sum(lane < WARPS ? fred[lane] : 0.0f);
         if (tid < ctas) *cluster.map_shared_rank(&parts[1][rank], tid) = DistillPart{{0.0f, o}, {0.0f, l}, m};
-        cluster.sync();
+        row_sync(cluster, ctas);
     }
     auto exponent = [&](float y, float ref) { return far ? (y - m) * a.scale : __fmaf_rn(y, a.scale, -ref); };
     if (warp == 0) {
@@ -235,66 +251,89 @@ __global__ void __launch_bounds__(DISTILL_THREADS, DB) k_distill(DistillArgs a)
             out.add(parts[far][k].out);
             in.add(parts[far][k].in);
         }
-        const float ref = fmaxf(out.ref, in.ref);
-        const double s_out = ldexp((double)out.sum, (int)(out.ref - ref)), total = s_out + ldexp((double)in.sum, (int)(in.ref - ref));
-        const double p_rest = TAIL && s_out != 0 ? fmax(0.0, 1.0 - sum_p) + (sum_p != sum_p ? sum_p : 0.0) : 0.0;
-        const double q_rest = total == 0 ? 0.0 : s_out / total;
+        const float ref = fmaxf(out.ref, in.ref), gap = out.ref - ref;
+        const float s_out = out.sum * exp2_whole(gap), total = s_out + in.sum * exp2_whole(in.ref - ref);
+        const bool rest = TAIL && out.sum != 0.0f;
+        const float p_rest = rest ? (sum_p != sum_p ? sum_p : fmaxf(0.0f, 1.0f - sum_p)) : 0.0f;
+        const float log2_total = total == 0.0f ? 0.0f : log2f(total);  // (without mass log q is minus infinity)
         if (a.loss && rank == 0) {
-            const double log2_total = total == 0 ? 0.0 : (double)log2f((float)total);  // (without mass log q is minus infinity)
+            // (in 64 bits: a listed word at the type's lowest value has a finite log q)
             double l = 0;
             for (int j = lane; j < a.top; j += 32)
                 if (p[j] > 0.0f || p[j] != p[j]) {
                     const double y = far ? ((double)x[j] - (double)m) * (double)a.scale : (double)x[j] * (double)a.scale - (double)ref;
-                    l += (double)p[j] * ((((double)teacher(j) - t_ref) * a.inv_tau - base) - (y - log2_total) * LN2);
+                    l += (double)p[j] * ((double)log_p[j] - (y - (double)log2_total) * LN2);
                 }
             l = warp_reduce_sum(l);
-            if (p_rest != 0.0) l += p_rest * log(p_rest / q_rest);
+            if (p_rest != 0.0f) l += (double)(p_rest * (logf(p_rest) - (gap + log2f(out.sum) - log2_total) * (float)LN2));
             if (lane == 0) a.loss[r] = (float)(l * a.tau * a.tau);
         }
         if (GRAD && lane == 0) {
-            whole.ref = ref;
-            whole.w = (double)weight * a.tau;
-            whole.inv = total == 0 ? 0.0 : 1.0 / total;
-            whole.mass = sum_p + p_rest;
-            whole.others = (float)(whole.w * whole.inv * (p_rest != 0.0 ? whole.mass - p_rest / q_rest : whole.mass));
+            const float w = (float)((double)weight * a.tau), mass = sum_p + p_rest;
+            const float q = total == 0.0f ? 0.0f : mass / total;
+            whole.list_ref = whole.ref = ref;
+            whole.w = w;
+            whole.listed = q;
+            whole.others = w * (p_rest != 0.0f ? q - p_rest / s_out : q);
+            if (gap < -100.0f) {
+                // less than 2^-80 of the student's mass is outside the list: it counts for the bucket alone, on a scale of its own
+                whole.ref = out.ref;
+                whole.others = p_rest != 0.0f ? -w * p_rest / out.sum : 0.0f;
+            }
         }
     }
     if (!GRAD) return;
     __syncthreads();
     const float ref = whole.ref, others = whole.others;
     const bool abreast = (uintptr_t)grad % 16 == (uintptr_t)row % 16;
-    for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
+    const auto put = [&](int c, uint4(&raw)[R]) {
         const int first = chunk_first<T, R>(c, split.pre);
-        if (weight != 0.0f && abreast && !far && chunk_inside<T, R>(first, V)) {
-            uint4 raw[R];
-            load_chunk<T, R>(row, first, V, row_element<T>(-INFINITY), raw);
-            uint4* to = reinterpret_cast<uint4*>(grad + first) + lane;
+        const bool inside = chunk_inside<T, R>(first, V);
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                float y[PER<T>];
-                unpack<T>(raw[k], y);
+        for (int k = 0; k < R; ++k) {
+            float y[PER<T>];
+            unpack<T>(raw[k], y);
+            if (!far) {
 #pragma unroll
                 for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit(__fmaf_rn(y[i], a.scale, -ref)) * others;
-                __stcs(to + 32 * k, pack<T>(y));
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit((y[i] - m) * a.scale) * others;
             }
-        } else {
-#pragma unroll 4
-            for (int i = lane; i < CHUNK; i += 32) {
-                const int v = first + i;
-                if (v >= 0 && v < V)
-                    grad[v] = row_element<T>(weight == 0.0f ? 0.0f : exp2_unit(exponent(row_value(row[v]), ref)) * others);
-            }
+            raw[k] = weight == 0.0f ? make_uint4(0, 0, 0, 0) : pack<T>(y);
         }
-    }
+        if (abreast && inside) {
+            uint4* to = reinterpret_cast<uint4*>(grad + first) + lane;
+#pragma unroll
+            for (int k = 0; k < R; ++k) __stcs(to + 32 * k, raw[k]);
+        } else {
+            // the row's edges, and rows that lie otherwise to 16 bytes than the logits': through the ring, by elements
+#pragma unroll
+            for (int k = 0; k < R; ++k) *walk.place(k) = raw[k];
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const T* from = (const T*)(walk.place(k) - lane);
+#pragma unroll
+                for (int i = lane; i < 32 * PER<T>; i += 32) {
+                    const int v = first + 32 * PER<T> * k + i;
+                    if (v >= 0 && v < V) grad[v] = from[i];
+                }
+            }
+            __syncwarp();
+        }
+    };
+    if (KEEP) walk.again(row, split, V, none, put);
+    else walk.each(row, split, V, none, put);
     if (weight == 0.0f) return;
     __syncthreads();  // the list's words over the rest
     for (int j = tid; j < a.top; j += threads) {
         if (ids[j] < v0 || ids[j] >= v1 || !leads(j)) continue;
-        double pj = (double)p[j];
+        float pj = p[j];
         if (s_twice)
             for (int o = j + 1; o < a.top; ++o)
-                if (ids[o] == ids[j]) pj += (double)p[o];
-        grad[ids[j]] = row_element<T>((float)(whole.w * ((double)exp2_unit(exponent(x[j], ref)) * whole.inv * whole.mass - pj)));
+                if (ids[o] == ids[j]) pj += p[o];
+        grad[ids[j]] = row_element<T>(whole.w * (exp2_unit(exponent(x[j], whole.list_ref)) * whole.listed - pj));
     }
 }
 
@@ -304,17 +343,28 @@ static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t 
     constexpr int CHUNK = 32 * DISTILL_GROUPS * PER<T>;
     const int64_t row_bytes = (int64_t)a.V * sizeof(T);
     const bool tail = a.teacher_lse, grad = a.grad;
+    using Walk = ChunkWalk<T, DISTILL_GROUPS, DISTILL_DEPTH>;
     RowShape shape = row_shape(rows, row_bytes, 1024, 64);
-    // what is read twice has to stay in L2 in between: all rows under way together at most 40 MB
-    while (grad && shape.ctas < DISTILL_CTAS && row_bytes * 148 * 1024 / (shape.ctas * shape.threads) > 40ll << 20)
-        shape = shape.threads < 512 ? RowShape{1, shape.threads * 2} : RowShape{shape.ctas * 2, 512};
+    bool keep = false;
+    if (grad) {
+        // as many threads as it takes to hold the row; else what is read twice has to stay in L2 in between: all rows under way
+        // together at most 40 MB
+        RowShape large = shape;
+        while (!Walk::holds(large, a.V) && large.ctas * large.threads < ROW_CTAS * ROW_THREADS) {
+            if (large.threads < 256 || large.ctas == ROW_CTAS) large.threads *= 2;
+            else large.ctas *= 2;
+        }
+        keep = Walk::holds(large, a.V);
+        shape = keep ? large : row_shape(std::min<int64_t>(rows, std::max<int64_t>(1, (40ll << 20) / row_bytes)), row_bytes, 1024, 64);
+    }
     // a bit for every word of a CTA's part
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = shape.threads * ChunkWalk<T, DISTILL_GROUPS, DISTILL_DEPTH>::BYTES +
+    const size_t smem = shape.threads * Walk::BYTES + 16 * a.top +
                         (tail || grad ? (size_t)((chunks + shape.ctas - 1) / shape.ctas) * (CHUNK / 8) : 0);
-    const auto kernel = tail ? (grad ? k_distill<T, true, true> : k_distill<T, true, false>)
-                             : (grad ? k_distill<T, false, true> : k_distill<T, false, false>);
-    return launch_rows(kernel, a, rows, shape, smem, 7 * 1024, st);
+    const auto kernel = !grad ? (tail ? k_distill<T, true, false, false> : k_distill<T, false, false, false>)
+                        : keep ? (tail ? k_distill<T, true, true, true> : k_distill<T, false, true, true>)
+                               : (tail ? k_distill<T, true, true, false> : k_distill<T, false, true, false>);
+    return launch_rows(kernel, a, rows, shape, smem, 2 * 1024, st);
 }
 
 static int distill(const DistillArgs& a, int dtype, int64_t rows, void* stream)

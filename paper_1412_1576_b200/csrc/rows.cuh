@@ -143,6 +143,23 @@ __device__ __forceinline__ void load_chunk(const T* row, int first, int V, T fil
     }
 }
 
+// How the rows share the GPU's threads: a row has a CTA, or a cluster of 2, 4 or 8 of them, so that all rows together come to about
+// `per_sm` threads per multiprocessor, but a row has at least 128 threads and a thread at least `least` bytes.
+struct RowShape {
+    int ctas, threads;  // threads of a CTA: 128, 256 or 512
+};
+constexpr int ROW_THREADS = 512, ROW_CTAS = 8;  // at most
+inline RowShape row_shape(int64_t rows, int64_t row_bytes, int64_t per_sm, int64_t least)
+{
+    int64_t n = 148 * per_sm / rows;
+    if (n > row_bytes / least) n = row_bytes / least;
+    int ctas = 1;
+    while (ctas < ROW_CTAS && n > 320 * ctas) ctas *= 2;
+    int threads = 128;  // (powers of two: whole CTAs fill a multiprocessor's registers)
+    while (threads < ROW_THREADS && 2 * threads * ctas <= n) threads *= 2;
+    return RowShape{ctas, threads};
+}
+
 // A warp's walk over its chunks of a part (every warps-th from its own number on).  A lane copies its groups of the next DEPTH chunks
 // into places of its own in shared memory (`ring`: DEPTH R 16 bytes per thread), so that what is on its way costs no registers and
 // nothing has to be waited for but the lane's own copies.
@@ -178,25 +195,51 @@ struct ChunkWalk {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) fetch(row, split, V, chunk + d * warps, d);
     }
+    // Gives up what is on its way.
+    __device__ __forceinline__ void drop() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+    // Group r of the chunk that f is called for, in the ring (the warp's groups of one r are consecutive).
+    __device__ __forceinline__ uint4* place(int r) const { return ring + (slot * R + r) * (int)blockDim.x; }
+    // Whether the ring holds all that a warp walks over, so that `again` finds it there.
+    static bool holds(const RowShape& shape, int V)
+    {
+        const int chunks = (V + PER<T> - 1 + 32 * R * PER<T> - 1) / (32 * R * PER<T>);
+        return (chunks + shape.ctas - 1) / shape.ctas <= DEPTH * (shape.threads / 32);
+    }
+    // A second walk over what the ring holds.
+    template <typename F>
+    __device__ __forceinline__ void again(const T* row, const RowSplit& split, int V, T fill, F f)
+    {
+        slot = 0;
+        for (chunk = split.chunk0 + (int)(threadIdx.x >> 5); chunk < split.chunk1; chunk += (int)(blockDim.x >> 5)) {
+            uint4 raw[R];
+            take(row, split, V, fill, raw);
+            f(chunk, raw);
+            ++slot;
+        }
+    }
+    __device__ __forceinline__ void take(const T* row, const RowSplit& split, int V, T fill, uint4 (&raw)[R])
+    {
+        const int first = chunk_first<T, R>(chunk, split.pre);
+        if (chunk_inside<T, R>(first, V)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) raw[r] = *place(r);
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int v = first + (32 * r + (int)(threadIdx.x & 31)) * PER<T>;
+                raw[r] = group_inside<T>(v, V) ? *place(r) : edge_group(row, v, V, fill);
+            }
+        }
+    }
     // f(chunk, groups) for each; `fill` stands outside the row.
     template <typename F>
     __device__ __forceinline__ void each(const T* row, const RowSplit& split, int V, T fill, F f)
     {
         const int warps = (int)(blockDim.x >> 5);
         for (; chunk < split.chunk1; chunk += warps) {
-            const int first = chunk_first<T, R>(chunk, split.pre);
             asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
             uint4 raw[R];
-            if (chunk_inside<T, R>(first, V)) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) raw[r] = ring[(slot * R + r) * (int)blockDim.x];
-            } else {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int v = first + (32 * r + (int)(threadIdx.x & 31)) * PER<T>;
-                    raw[r] = group_inside<T>(v, V) ? ring[(slot * R + r) * (int)blockDim.x] : edge_group(row, v, V, fill);
-                }
-            }
+            take(row, split, V, fill, raw);
             f(chunk, raw);
             // (the place is free: its groups have been worked on)
             fetch(row, split, V, chunk + DEPTH * warps, slot);
@@ -363,16 +406,11 @@ __device__ __forceinline__ uint4 pack(const float (&x)[PER<T>])
     }
 }
 
-// How many threads share a row: a power of two from 128 on, up to clusters of eight CTAs of 512, so that all rows together give
-// every multiprocessor `per_sm` threads, but a thread no less than `least` bytes.
-struct RowShape {
-    int ctas, threads;
-};
-inline RowShape row_shape(int64_t rows, int64_t row_bytes, int64_t per_sm, int64_t least)
+// Barrier of all threads that share a row.
+__device__ __forceinline__ void row_sync(cg::cluster_group& cluster, int ctas)
 {
-    int64_t n = 128;
-    while (n < 8 * 512 && rows * n < 148 * per_sm && row_bytes >= 2 * n * least) n *= 2;
-    return n <= 512 ? RowShape{1, (int)n} : RowShape{(int)(n / 512), 512};
+    if (ctas > 1) cluster.sync();
+    else __syncthreads();
 }
 
 // Launches a cluster of CTAs for every row; `smem`: dynamic shared memory, `fixed`: what the kernel has besides, about.

@@ -17,7 +17,6 @@ struct TopArgs {
     float* lse;
 };
 
-constexpr int TOP_THREADS = 512;  // of a CTA, at most
 #ifndef TG
 #define TG 4
 #endif
@@ -25,13 +24,14 @@ constexpr int TOP_THREADS = 512;  // of a CTA, at most
 #define TB 2
 #endif
 constexpr int TOP_GROUPS = TG;     // groups a lane has in flight
-constexpr int TOP_CTAS = 8;       // of a cluster, at most
-constexpr int TOP_LIST = 2048;    // words that may be left for the list
-constexpr int TOP_QUEUE = 1024;   // pieces of a CTA's part that are read again
+constexpr int TOP_LIST = 2048;      // words that may be left for the longest lists
+constexpr int TOP_VALUES = 1024;  // groups of pieces whose largest keys give the border, at most
+// Words and pieces that may be left for lists of `top`: about four times what is expected.
+__host__ __device__ constexpr int top_room(int top) { return top <= 64 ? 512 : top <= 256 ? 1024 : TOP_LIST; }
 constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
 
 #ifndef TD
-#define TD 3
+#define TD 2
 #endif
 constexpr int TOP_DEPTH = TD;      // chunks on their way
 
@@ -44,26 +44,26 @@ struct TopPart {
 
 // Behind the pass over the row its shared memory holds these.
 struct TopLists {
-    unsigned long long list[TOP_LIST];
-    int queue[TOP_QUEUE];
+    unsigned long long* list;  // the words that are left
+    uint16_t* tops;            // (before that, in the same place) the groups' largest keys
+    int* queue;                // the pieces that are read again
 };
 
 struct TopShared {
-    TopPart parts[2][TOP_CTAS];
-    ExpSum ered[TOP_THREADS / 32];
-    float fred[TOP_THREADS / 32];
+    TopPart parts[2][ROW_CTAS];
+    ExpSum ered[ROW_THREADS / 32];
+    float fred[ROW_THREADS / 32];
     int ired[33];
     int hist[256];
-    int counts[3];
     int n, queued, need;
     uint32_t prefix;
     float max;
 };
 
-__host__ __device__ constexpr int top_ring_bytes(int threads)
+__host__ __device__ constexpr int top_ring_bytes(int threads, int room)
 {
-    const int ring = threads * TOP_DEPTH * TOP_GROUPS * 16;
-    return ring > (int)sizeof(TopLists) ? ring : (int)sizeof(TopLists);
+    const int ring = threads * TOP_DEPTH * TOP_GROUPS * 16, lists = room * 12;
+    return ring > lists ? ring : lists;
 }
 
 __device__ __forceinline__ unsigned long long top_entry(uint32_t key, int v)
@@ -177,12 +177,13 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared
 // FINE: each group) as the upper half of its key.  A border that at least `top` of them reach leaves at least `top` words, and few
 // more: the pieces that reach it are read again (from L2), their words at or above it are sorted.
 template <typename T, bool FINE>
-__global__ void __launch_bounds__(TOP_THREADS, TB) k_top(TopArgs a)
+__global__ void __launch_bounds__(ROW_THREADS, TB) k_top(TopArgs a)
 {
     constexpr int R = TOP_GROUPS, PIECES = FINE ? R : 1, SIZE = R / PIECES;  // pieces of a lane's groups, groups of a piece
     extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring and, later, the lists; the pieces' keys
-    TopLists& lists = *(TopLists*)dynamic;
-    uint16_t* keys = (uint16_t*)(dynamic + top_ring_bytes(blockDim.x));
+    const int room = top_room(a.top);
+    const TopLists lists{(unsigned long long*)dynamic, (uint16_t*)dynamic, (int*)(dynamic + 8 * room)};
+    uint16_t* keys = (uint16_t*)(dynamic + top_ring_bytes(blockDim.x, room));
     __shared__ TopShared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -193,8 +194,7 @@ __global__ void __launch_bounds__(TOP_THREADS, TB) k_top(TopArgs a)
     const int pieces = (split.chunk1 - split.chunk0) * 32 * PIECES;
     ChunkWalk<T, R, TOP_DEPTH> walk;
     walk.start(dynamic, row, split, V);
-    cluster_arrive();
-    if (tid < 3) sh.counts[tid] = 0;
+    if (ctas > 1) cluster_arrive();
     if (tid == 0) sh.n = sh.queued = 0;
     ExpSum sum = ExpSum::none();
     float m = -INFINITY;
@@ -221,55 +221,58 @@ __global__ void __launch_bounds__(TOP_THREADS, TB) k_top(TopArgs a)
     m = warp_reduce_max(m);
     if (lane == 0) sh.ered[warp] = sum, sh.fred[warp] = m;
     __syncthreads();
-    // the pieces' keys in eight groups per thread, the largest of each
-    uint32_t tops[8] = {};
-    for (int i = tid; i < pieces; i += 8 * threads)
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (i + k * threads < pieces) tops[k] = max(tops[k], (uint32_t)keys[i + k * threads]);
-    uint32_t best = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) best = max(best, tops[k]);
-    best = __reduce_max_sync(0xffffffffu, best);
-    if (lane == 0) sh.ired[warp] = (int)best;
+    // the pieces' keys in `values` groups, the largest of each; every fourth at most will reach the border
+    int values = 256;
+    while (values < 4 * a.top && values < TOP_VALUES) values *= 2;
+    for (int g = tid; g < values; g += threads) {
+        uint32_t top = 0;
+        for (int i = g; i < pieces; i += values) top = max(top, (uint32_t)keys[i]);
+        lists.tops[g] = (uint16_t)top;
+    }
     __syncthreads();
-    best = __reduce_max_sync(0xffffffffu, lane < WARPS ? (uint32_t)sh.ired[lane] : 0u);
-    // The largest half-key that at least `want` of these groups reach, or one that not many more do: steps of doubling width
-    // down from `hi` (that fewer reach), then halving; minus infinity's successor if there are not that many.
-    int round = 0;
-    auto border_of = [&](int want, uint32_t hi) {
-        uint32_t lo = TOP_LOWEST, step = 64;
-        while (lo + 1 < hi) {
-            const bool down = lo == TOP_LOWEST && hi > lo + step;
-            const uint32_t mid = down ? hi - step : (lo + hi) / 2;
-            step = down ? step * 2 : step;
-            int n = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) n += tops[k] >= mid;
-            n = __reduce_add_sync(0xffffffffu, n);
-            if (lane == 0 && n) atomicAdd(&sh.counts[round % 3], n);
-            if (tid == 0) sh.counts[(round + 1) % 3] = 0;
-            __syncthreads();
-            n = sh.counts[round++ % 3];
-            if (n >= want) {
-                lo = mid;
-                if (n <= want + want / 4 + 16 / ctas) break;
-            } else
-                hi = mid;
-        }
-        return lo;
-    };
-    // `top` groups of one part are enough, and so are its share of them in every part
-    const uint32_t share = border_of((a.top + ctas - 1) / ctas, best + 1);
-    const uint32_t alone = ctas > 1 ? border_of(a.top, share + 1) : share;
+    uint32_t share = 0, alone = 0;
     if (warp == 0) {
         sum = lane < WARPS ? sh.ered[lane] : ExpSum::none();
         sum.warp_reduce();
         m = warp_reduce_max(lane < WARPS ? sh.fred[lane] : -INFINITY);
+        const int per = values / 32;
+        uint32_t tops[TOP_VALUES / 32], best = 0;
+#pragma unroll
+        for (int k = 0; k < TOP_VALUES / 32; ++k) {
+            tops[k] = k < per ? lists.tops[k * 32 + lane] : 0u;
+            best = max(best, tops[k]);
+        }
+        best = __reduce_max_sync(0xffffffffu, best);
+        // The largest half-key that at least `want` of the groups reach, or one that not many more do: steps of doubling width down
+        // from `hi` (that fewer reach), then halving; minus infinity's successor if there are not that many.
+        auto border_of = [&](int want, uint32_t hi) {
+            uint32_t lo = TOP_LOWEST, step = 64;
+            while (lo + 1 < hi) {
+                const bool down = lo == TOP_LOWEST && hi > lo + step;
+                const uint32_t mid = down ? hi - step : (lo + hi) / 2;
+                step = down ? step * 2 : step;
+                int n = 0;
+#pragma unroll
+                for (int k = 0; k < TOP_VALUES / 32; k += 8)
+                    if (k < per)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) n += tops[k + e] >= mid;
+                n = __reduce_add_sync(0xffffffffu, n);
+                if (n >= want) {
+                    lo = mid;
+                    if (n <= want + want / 4 + 16 / ctas) break;
+                } else
+                    hi = mid;
+            }
+            return lo;
+        };
+        // `top` groups of one part are enough, and so are its share of them in every part
+        share = border_of((a.top + ctas - 1) / ctas, best + 1);
+        alone = ctas > 1 ? border_of(a.top, share + 1) : share;
     }
-    cluster_wait();
+    if (ctas > 1) cluster_wait();
     if (tid < ctas) *cluster.map_shared_rank(&sh.parts[0][rank], tid) = TopPart{sum, m, share, alone};
-    cluster.sync();
+    row_sync(cluster, ctas);
     uint32_t border = 0, least = 0xFFFFFFFFu;
     m = -INFINITY;
     for (int k = 0; k < ctas; ++k) {
@@ -295,42 +298,61 @@ __global__ void __launch_bounds__(TOP_THREADS, TB) k_top(TopArgs a)
         __syncthreads();
         if (warp == 0) o = warp_reduce_sum(lane < WARPS ? sh.fred[lane] : 0.0f);
         if (tid < ctas) *cluster.map_shared_rank(&sh.parts[1][rank], tid) = TopPart{{0.0f, o}, m, 0, 0};
-        cluster.sync();
+        row_sync(cluster, ctas);
     }
     // the pieces that reach the border, then a group of one to every thread
     int* n_all = cluster.map_shared_rank(&sh.n, 0);
     unsigned long long* list = cluster.map_shared_rank(lists.list, 0);
-    for (int i = tid; i < pieces; i += threads)
-        if (keys[i] >= border) {
-            const int at = atomicAdd(&sh.queued, 1);
-            if (at < TOP_QUEUE) lists.queue[at] = i;
-        }
+    for (int i = 8 * tid; i < pieces; i += 8 * threads) {
+        const uint4 eight = *reinterpret_cast<const uint4*>(keys + i);
+        const uint32_t two[4] = {eight.x, eight.y, eight.z, eight.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (((two[e / 2] >> (e % 2 * 16)) & 0xFFFFu) >= border) {
+                const int at = atomicAdd(&sh.queued, 1);
+                if (at < room) lists.queue[at] = i + e;
+            }
+    }
     __syncthreads();
     const int queued = sh.queued;
-    if (queued > TOP_QUEUE) {
-        if (tid == 0) atomicAdd(n_all, TOP_LIST + 1);
+    if (queued > room) {
+        if (tid == 0) atomicAdd(n_all, room + 1);
     } else
-        for (int t = tid; t < queued * SIZE; t += threads) {
-            const int i = lists.queue[t / SIZE];  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
-            const int chunk = split.chunk0 + i / (32 * PIECES);
-            const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
-            const int first = chunk_first<T, R>(chunk, split.pre) + group * PER<T>;
-            const uint4 raw = any_group(row, first, V, row_element<T>(-INFINITY));
-            float x[PER<T>];
-            unpack<T>(raw, x);
+        for (int base = 0; base < queued * SIZE; base += 2 * threads) {
+            // (two groups at a time: the second is on its way while the first is looked at)
+            uint4 raw[2];
+            int first[2];
 #pragma unroll
-            for (int e = 0; e < PER<T>; ++e) {
-                const uint32_t k = order_key(x[e]);
-                if ((k >> 16) >= border) {
-                    const int at = atomicAdd(n_all, 1);
-                    if (at < TOP_LIST) list[at] = top_entry(k, first + e);
+            for (int h = 0; h < 2; ++h) {
+                const int t = base + h * threads + tid;
+                const bool any = t < queued * SIZE;
+                const int i = any ? lists.queue[t / SIZE] : 0;  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
+                const int chunk = split.chunk0 + i / (32 * PIECES);
+                const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
+                first[h] = any ? chunk_first<T, R>(chunk, split.pre) + group * PER<T> : V;
+                raw[h] = any_group(row, first[h], V, row_element<T>(-INFINITY));
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x[PER<T>];
+                unpack<T>(raw[h], x);
+#pragma unroll
+                for (int e = 0; e < PER<T>; ++e) {
+                    const uint32_t k = order_key(x[e]);
+                    const bool hit = (k >> 16) >= border;
+                    const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+                    if (hits == 0) continue;
+                    int at = 0;
+                    if (lane == 0) at = ctas == 1 ? atomicAdd(&sh.n, __popc(hits)) : atomicAdd(n_all, __popc(hits));
+                    at = __shfl_sync(0xffffffffu, at, 0) + __popc(hits & ((1u << lane) - 1));
+                    if (hit && at < room) list[at] = top_entry(k, first[h] + e);
                 }
             }
         }
-    cluster.sync();
+    row_sync(cluster, ctas);
     if (rank != 0) return;
     int n = sh.n;
-    if (n > TOP_LIST) {
+    if (n > room) {
         __syncthreads();
         n = top_by_bytes<T>(row, V, a.top, sh, lists.list);
         __syncthreads();
@@ -364,7 +386,7 @@ static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
     const int per = a.V / PER<T>;
     const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = top_ring_bytes(shape.threads) + (size_t)((chunks + shape.ctas - 1) / shape.ctas) * 32 * (fine ? TOP_GROUPS : 1) * 2;
+    const size_t smem = top_ring_bytes(shape.threads, top_room(a.top)) + (size_t)((chunks + shape.ctas - 1) / shape.ctas) * 32 * (fine ? TOP_GROUPS : 1) * 2;
     return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, shape, smem, sizeof(TopShared), st);
 }
 

@@ -22,9 +22,7 @@ struct VerifyArgs {
     int32_t V;
 };
 
-constexpr int VERIFY_THREADS = 512;  // of a CTA, at most
 constexpr int VERIFY_GROUPS = 4;  // groups of each row a lane has in flight
-constexpr int VERIFY_CTAS = 8;    // of a cluster, at most
 constexpr int VERIFY_CHUNKS = LDA_ROW_MAX_V / (32 * VERIFY_GROUPS * PER<float>) + 1;
 
 // Masses: floor(2^42 x) for x in [0, 1], as 19 upper and 23 lower bits.  The bits are pushed to the end of a float by an addition of
@@ -46,10 +44,10 @@ struct MassSum {
 // up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk and
 // reads that again to find the word.  Bound by the read of one row of the target and, behind a refusal, one of the drafter.
 template <typename T, bool PROBS>
-__global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
+__global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
 {
     constexpr int R = VERIFY_GROUPS, CHUNK = 32 * R * PER<T>;
-    __shared__ unsigned long long sums[VERIFY_CHUNKS], red[33], parts[2][VERIFY_CTAS], s_want;
+    __shared__ unsigned long long sums[VERIFY_CHUNKS], red[33], parts[2][ROW_CTAS], s_want;
     __shared__ int s_taken, s_chunk, s_token;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -63,7 +61,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
     const float u = a.draw_u[b];
     const T* target = (const T*)a.target;
     const T* probs = (const T*)a.probs;
-    cluster_arrive();
+    if (ctas > 1) cluster_arrive();
     if (warp == 0) {
         int taken = n;
         for (int base = 0; base < n; base += 32) {
@@ -96,7 +94,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
     if (gone < 0 || gone >= V) gone = -1;
     const RowSplit split = RowSplit::of<T, R>(prow, V, rank, ctas);
     const bool abreast = PROBS && (uintptr_t)qrow % 16 == (uintptr_t)prow % 16;
-    cluster_wait();
+    if (ctas > 1) cluster_wait();
     int token = -1;
     bool here = true;  // whether this CTA writes the token
     for (int plain = 0; plain < 2; ++plain) {
@@ -146,7 +144,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS, 2) k_verify(VerifyArgs a)
         for (int c = tid; c < chunks; c += threads) own += sums[c];
         own = block_reduce_sum(own, red);
         if (tid < ctas) *cluster.map_shared_rank(&parts[plain][rank], tid) = own;
-        cluster.sync();
+        row_sync(cluster, ctas);
         unsigned long long total = 0, before = 0;
         for (int k = 0; k < ctas; ++k) {
             if (k < rank) before += parts[plain][k];
