@@ -31,17 +31,8 @@ struct DistillArgs {
     double tau, inv_tau;
 };
 
-#ifndef DG
-#define DG 4
-#endif
-#ifndef DB
-#define DB 2
-#endif
-#ifndef DD
-#define DD 3
-#endif
-constexpr int DISTILL_GROUPS = DG;  // groups of a lane in a chunk
-constexpr int DISTILL_DEPTH = DD;   // chunks on their way
+constexpr int DISTILL_GROUPS = 4;  // groups of a lane in a chunk
+__host__ __device__ constexpr int distill_depth(bool grad) { return grad ? 2 : 3; }  // chunks on their way
 
 // What a CTA knows of its part of the row.
 struct DistillPart {
@@ -49,13 +40,90 @@ struct DistillPart {
     float max;
 };
 
-// What the gradient needs of the whole row: 2^(x c - ref) times `others` for a word outside the list; weight tau W / sum of
-// exponentials and weight tau for those of the list.
-struct DistillRow {
-    float ref, others, listed, w, list_ref;
+// The list in shared memory, and a map with a bit for each word of the CTA's part.
+struct DistillList {
+    int* ids;                // -1: padding
+    float *p, *log_p, *x;    // the teacher's probabilities (at first: its logits), the student's logits
+    uint32_t* bits;
+    static __host__ __device__ constexpr int bytes(int top, int bits_bytes) { return (16 * top + bits_bytes + 15) / 16 * 16; }
+    __device__ __forceinline__ DistillList(void* at, int top)
+        : ids((int*)at), p((float*)at + top), log_p((float*)at + 2 * top), x((float*)at + 3 * top), bits((uint32_t*)at + 4 * top)
+    {
+    }
+    // Whether place j stands for its word, which the list may hold twice: the first does.
+    __device__ __forceinline__ bool leads(int j, bool twice) const
+    {
+        bool first = true;
+        if (twice)
+            for (int o = 0; o < j; ++o) first = first && ids[o] != ids[j];
+        return first;
+    }
 };
 
-// Bits of a group's elements in a map with a bit for each element.
+// A CTA's part of a row: its words v0..v1-1; the map's first bit is word bit0.
+template <typename T>
+struct DistillSpan {
+    RowSplit split;
+    int bit0, v0, v1;
+    __device__ __forceinline__ DistillSpan(const T* row, int V, int rank, int ctas)
+    {
+        split = RowSplit::of<T, DISTILL_GROUPS>(row, V, rank, ctas);
+        bit0 = chunk_first<T, DISTILL_GROUPS>(split.chunk0, split.pre);
+        v0 = max(0, bit0);
+        v1 = max(v0, min(V, chunk_first<T, DISTILL_GROUPS>(split.chunk1, split.pre)));
+    }
+};
+
+// Bytes of the map for parts of `chunks` chunks.
+template <typename T>
+__host__ __device__ constexpr int distill_bits(int chunks) { return chunks * (32 * DISTILL_GROUPS * PER<T> / 8); }
+
+// What the list says, worked out by one warp from ids, p (the logits) and x.
+struct DistillSums {
+    float sum_p;
+    ExpSum in;
+};
+template <bool TAIL>
+__device__ __forceinline__ DistillSums distill_list(const DistillArgs& a, const DistillList& list, float teacher_lse, int v0, int v1,
+                                                    bool twice)
+{
+    const int lane = threadIdx.x & 31;
+    DistillSums s{0.0f, ExpSum::none()};
+    float max_t = -INFINITY, z = 0.0f;
+    if (!TAIL) {
+        for (int j = lane; j < a.top; j += 32)
+            if (list.ids[j] >= 0) max_t = fmaxf(max_t, list.p[j]);
+        max_t = warp_reduce_max(max_t);
+    }
+    for (int j = lane; j < a.top; j += 32) {
+        const int id = list.ids[j];
+        const float t = list.p[j];
+        float l = (float)(TAIL ? (double)t * a.inv_tau - (double)teacher_lse : ((double)t - (double)max_t) * a.inv_tau);
+        if (id < 0 || t == -INFINITY) l = -INFINITY;
+        const float e = l == -INFINITY ? 0.0f : expf(l);
+        list.log_p[j] = l;
+        list.p[j] = e;
+        z += e;
+        if (TAIL && id >= v0 && id < v1 && list.leads(j, twice)) {
+            const float x = list.x[j];
+            s.in.raise(exp_ref(x, a.scale));
+            s.in.sum += exp2_unit(__fmaf_rn(x, a.scale, -s.in.ref));
+        }
+    }
+    s.sum_p = z = warp_reduce_sum(z);
+    if (TAIL) s.in.warp_reduce();
+    else if (z > 0.0f || z != z) {  // (a list of nothing but minus infinity has no mass)
+        const float log_z = logf(z);
+        for (int j = lane; j < a.top; j += 32) {
+            list.p[j] = list.p[j] / z;
+            list.log_p[j] -= log_z;
+        }
+        s.sum_p = z == z ? 1.0f : z;
+    }
+    return s;
+}
+
+// Bits of a group's elements in the map.
 template <typename T>
 __device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
 {
@@ -63,278 +131,286 @@ __device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
     return PER<T> == 8 ? byte : (byte >> (group * PER<T> % 8)) & ((1u << PER<T>) - 1);
 }
 
-// One cluster per row; every CTA has the whole list and a part of the row.  The words of the list are marked in a bit map of that
-// part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The CTAs exchange
-// their sums, and each works out the gradient of its part: the same factor times the exponential for all words, then the list's
-// words over it.  KEEP: the ring holds all of the CTA's part from the first pass on; else it is read again, from L2.
-template <typename T, bool TAIL, bool GRAD, bool KEEP>
-__global__ void __launch_bounds__(ROW_THREADS, DB) k_distill(DistillArgs a)
+// Minus infinity in the list's places of a lane's groups; `group`: the first one's number in the part.
+template <typename T>
+__device__ __forceinline__ void distill_mask(uint4 (&raw)[DISTILL_GROUPS], const uint32_t* bits, int group)
 {
-    constexpr int R = DISTILL_GROUPS, CHUNK = 32 * R * PER<T>;
+#pragma unroll
+    for (int k = 0; k < DISTILL_GROUPS; ++k) {
+        const uint32_t marked = group_bits<T>(bits, group + 32 * k);
+        if (marked) {
+            union {
+                uint4 raw;
+                T e[PER<T>];
+            } u;
+            u.raw = raw[k];
+#pragma unroll
+            for (int i = 0; i < PER<T>; ++i)
+                if (marked >> i & 1) u.e[i] = row_element<T>(-INFINITY);
+            raw[k] = u.raw;
+        }
+    }
+}
+
+// Sum of 2^((x - m) c) over a warp's chunks of the part, the list's words left out (TAIL).
+template <typename T, bool TAIL>
+__device__ __noinline__ float distill_far_sum(const T* row, const RowSplit& split, int V, float m, float c, const uint32_t* bits, int warps)
+{
+    constexpr int R = DISTILL_GROUPS;
+    const int lane = threadIdx.x & 31;
+    float o = 0.0f;
+    for (int chunk = split.chunk0 + (int)(threadIdx.x >> 5); chunk < split.chunk1; chunk += warps) {
+        uint4 raw[R];
+        load_chunk<T, R>(row, chunk_first<T, R>(chunk, split.pre), V, row_element<T>(-INFINITY), raw);
+        if (TAIL) distill_mask<T>(raw, bits, (chunk - split.chunk0) * 32 * R + lane);
+        for (int k = 0; k < R; ++k) {
+            float y[PER<T>];
+            unpack<T>(raw[k], y);
+            for (int i = 0; i < PER<T>; ++i) o += exp2_unit((y[i] - m) * c);
+        }
+    }
+    return warp_reduce_sum(o);
+}
+
+// The row's sums from its parts: exponentials 2^(x c - ref), or 2^((x - max) c) where `far`.
+struct DistillRow {
+    ExpSum out;
+    float max, ref, total, sum_p, p_rest;
+    bool far;
+    template <bool TAIL>
+    static __device__ __forceinline__ DistillRow of(const DistillPart* parts, int ctas, float max, bool far, float sum_p)
+    {
+        DistillRow w;
+        w.max = max;
+        w.far = far;
+        w.sum_p = sum_p;
+        w.out = parts[0].out;
+        ExpSum in = parts[0].in;
+        for (int k = 1; k < ctas; ++k) {
+            w.out.add(parts[k].out);
+            in.add(parts[k].in);
+        }
+        w.ref = fmaxf(w.out.ref, in.ref);
+        w.total = w.out.sum * exp2_whole(w.out.ref - w.ref) + in.sum * exp2_whole(in.ref - w.ref);
+        w.p_rest = TAIL && w.out.sum != 0.0f ? (sum_p != sum_p ? sum_p : fmaxf(0.0f, 1.0f - sum_p)) : 0.0f;
+        return w;
+    }
+    __device__ __forceinline__ float exponent(float x, float c, float r) const { return far ? (x - max) * c : __fmaf_rn(x, c, -r); }
+    // The row's loss, by one warp.
+    __device__ __forceinline__ float loss(const DistillArgs& a, const DistillList& list) const
+    {
+        const float log2_total = total == 0.0f ? 0.0f : log2f(total);  // (without mass log q is minus infinity)
+        double l = 0;  // (64 bits: a listed word at the type's lowest value has a finite log q)
+        for (int j = threadIdx.x & 31; j < a.top; j += 32) {
+            const float p = list.p[j];
+            if (p > 0.0f || p != p) {
+                const double x = (double)list.x[j], y = far ? (x - (double)max) * (double)a.scale : x * (double)a.scale - (double)ref;
+                l += (double)p * ((double)list.log_p[j] - (y - (double)log2_total) * LN2);
+            }
+        }
+        l = warp_reduce_sum(l);
+        if (p_rest != 0.0f) l += (double)(p_rest * (logf(p_rest) - (out.ref - ref + log2f(out.sum) - log2_total) * (float)LN2));
+        return (float)(l * a.tau * a.tau);
+    }
+};
+
+// The gradient: 2^(x c - ref) times `others` for a word outside the list; w (2^(x c - list_ref) listed - p) for one of the list.
+struct DistillFactors {
+    float ref, others, listed, w, list_ref;
+    __device__ __forceinline__ DistillFactors(const DistillRow& row, float weight, double tau)
+    {
+        w = (float)((double)weight * tau);
+        list_ref = ref = row.ref;
+        listed = row.total == 0.0f ? 0.0f : (row.sum_p + row.p_rest) / row.total;
+        const float gap = row.out.ref - row.ref;
+        others = w * (row.p_rest != 0.0f ? listed - row.p_rest / (row.out.sum * exp2_whole(gap)) : listed);
+        if (gap < -100.0f) {
+            // less than 2^-80 of the student's mass is outside the list: it counts for the bucket alone, on a scale of its own
+            ref = row.out.ref;
+            others = row.p_rest != 0.0f ? -w * row.p_rest / row.out.sum : 0.0f;
+        }
+        if (weight == 0.0f) others = 0.0f;
+    }
+};
+
+// The gradient of a lane's groups of a chunk as if no word were listed; `stage`: the lane's places of the walk's ring.
+template <typename T, typename Walk>
+__device__ __forceinline__ void distill_put(T* grad, int first, int V, uint4 (&raw)[DISTILL_GROUPS], const DistillFactors& f,
+                                            const DistillRow& w, float c, bool zero, bool abreast, const Walk& walk, int slot)
+{
+    constexpr int R = DISTILL_GROUPS;
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        float y[PER<T>];
+        unpack<T>(raw[k], y);
+        if (!w.far) {
+#pragma unroll
+            for (int i = 0; i < PER<T>; i += 2) {
+                const float2 e = fma_two(make_float2(y[i], y[i + 1]), make_float2(c, c), make_float2(-f.ref, -f.ref));
+                const float2 g = mul_two(make_float2(exp2_unit(e.x), exp2_unit(e.y)), make_float2(f.others, f.others));
+                y[i] = g.x, y[i + 1] = g.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit((y[i] - w.max) * c) * f.others;
+        }
+        raw[k] = zero ? make_uint4(0, 0, 0, 0) : pack<T>(y);
+    }
+    if (abreast && chunk_inside<T, R>(first, V)) {
+        uint4* to = reinterpret_cast<uint4*>(grad + first) + lane;
+#pragma unroll
+        for (int k = 0; k < R; ++k) __stcs(to + 32 * k, raw[k]);
+    } else {
+        // the row's edges, and rows that lie otherwise to 16 bytes than the logits': through the ring, by elements
+#pragma unroll
+        for (int k = 0; k < R; ++k) *walk.place(slot, k) = raw[k];
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const T* from = (const T*)(walk.place(slot, k) - lane);
+#pragma unroll
+            for (int i = lane; i < 32 * PER<T>; i += 32) {
+                const int v = first + 32 * PER<T> * k + i;
+                if (v >= 0 && v < V) grad[v] = from[i];
+            }
+        }
+        __syncwarp();
+    }
+}
+
+// The list's words over that, by threads tid, tid + threads, ...
+template <typename T>
+__device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, const DistillList& list, int v0, int v1, bool twice,
+                                                 const DistillFactors& f, const DistillRow& w, int tid, int threads)
+{
+    for (int j = tid; j < a.top; j += threads) {
+        const int id = list.ids[j];
+        if (id < v0 || id >= v1 || !list.leads(j, twice)) continue;
+        float p = list.p[j];
+        if (twice)
+            for (int o = j + 1; o < a.top; ++o)
+                if (list.ids[o] == id) p += list.p[o];
+        grad[id] = row_element<T>(f.w * (exp2_unit(w.exponent(list.x[j], a.scale, f.list_ref)) * f.listed - p));
+    }
+}
+
+// Rows of any length, one cluster per row; every CTA has the whole list and a part of the row.  The words of the list are marked in
+// a bit map of that part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The
+// CTAs exchange their sums; each works out the gradient of its part from a second read, which L2 answers.
+template <typename T, bool TAIL, bool GRAD>
+__global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
+{
+    constexpr int R = DISTILL_GROUPS;
     constexpr bool BITS = TAIL || GRAD;
-    using Walk = ChunkWalk<T, R, DISTILL_DEPTH>;
-    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the list, the map of its words
-    int* ids = (int*)(dynamic + blockDim.x * Walk::BYTES);
-    float *p = (float*)(ids + a.top), *log_p = p + a.top, *x = log_p + a.top;
-    uint32_t* bits = (uint32_t*)(x + a.top);
+    using Walk = ChunkWalk<T, R, distill_depth(GRAD)>;
+    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the list
+    const DistillList list(dynamic + blockDim.x * Walk::BYTES, a.top);
     __shared__ ExpSum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ DistillPart parts[2][ROW_CTAS];
-    __shared__ DistillRow whole;
+    __shared__ float s_sum_p;
     __shared__ int s_any, s_twice;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, WARPS = threads / 32, V = a.V;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads / 32, V = a.V;
     const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
     T* grad = GRAD ? (T*)a.grad + r * a.grad_stride : nullptr;
     const T none = row_element<T>(-INFINITY);
     const float weight = GRAD && a.weights ? a.weights[r] : 1.0f;
     const float teacher_lse = TAIL ? a.teacher_lse[r] : 0.0f;
-    const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
-    // this CTA's words, and the word of the map's first bit
-    const int bit0 = chunk_first<T, R>(split.chunk0, split.pre);
-    const int v0 = max(0, bit0), v1 = max(v0, min(V, chunk_first<T, R>(split.chunk1, split.pre)));
+    const DistillSpan<T> span(row, V, rank, ctas);
+    const RowSplit& split = span.split;
+    const int v0 = span.v0, v1 = span.v1;
     Walk walk;
-    walk.start(dynamic, row, split, V);
+    walk.start(dynamic, threads, row, split, V, GRAD);
     if (tid == 0) s_any = s_twice = 0;
     if (BITS)
-        for (int i = tid; i < (split.chunk1 - split.chunk0) * (CHUNK / 128); i += threads) ((uint4*)bits)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = tid; i < distill_bits<T>(split.chunk1 - split.chunk0) / 16; i += threads)
+            ((uint4*)list.bits)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     for (int j = tid; j < a.top; j += threads) {
         const int64_t at = r * a.list_stride + j;
         const int id = a.ids[at];
         const bool ok = id >= 0 && id < V;
-        p[j] = any_value(a.values, a.values_dtype, at);
-        ids[j] = ok ? id : -1;
+        list.p[j] = any_value(a.values, a.values_dtype, at);
+        list.ids[j] = ok ? id : -1;
         if (ok) {
             s_any = 1;
             if (BITS && id >= v0 && id < v1) {
-                const int bit = id - bit0;
-                if (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
+                const int bit = id - span.bit0;
+                if (atomicOr(&list.bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
             }
-            x[j] = row_value(row[id]);
+            list.x[j] = row_value(row[id]);
         }
     }
     __syncthreads();
+    const bool twice = s_twice;
     if (!s_any || (GRAD && weight == 0.0f && !a.loss)) {  // (the same in every CTA of the cluster)
         if (a.loss && rank == 0 && tid == 0) a.loss[r] = 0.0f;
-        walk.drop();
-        if (GRAD) {
-            const bool aligned = (uintptr_t)grad % 16 == (uintptr_t)row % 16;
-            for (int v = v0 + tid * PER<T>; v < v1 + PER<T>; v += threads * PER<T>) {
-                const int first = (v + split.pre) / PER<T> * PER<T> - split.pre;  // the group that v is in
-                if (aligned && first >= v0 && first + PER<T> <= v1)
-                    *reinterpret_cast<uint4*>(grad + first) = make_uint4(0, 0, 0, 0);
-                else
-                    for (int i = max(first, v0); i < min(first + PER<T>, v1); ++i) grad[i] = row_element<T>(0.0f);
-            }
-        }
+        Walk::template wait<0>();
+        if (GRAD)
+            for (int v = v0 + tid; v < v1; v += threads) grad[v] = row_element<T>(0.0f);
         return;
     }
     if (ctas > 1) cluster_arrive();
-    // which place of the list stands for a word that it holds twice: the first
-    auto leads = [&](int j) {
-        bool first = true;
-        if (s_twice)
-            for (int o = 0; o < j; ++o) first = first && ids[o] != ids[j];
-        return first;
-    };
-    // the teacher's probabilities and the student's words on the list (warp 0)
-    float sum_p = 0.0f;
-    ExpSum in = ExpSum::none();
+    DistillSums sums{0.0f, ExpSum::none()};
     if (warp == 0) {
-        float max_t = -INFINITY, z = 0.0f;
-        if (!TAIL) {
-            for (int j = lane; j < a.top; j += 32)
-                if (ids[j] >= 0) max_t = fmaxf(max_t, p[j]);
-            max_t = warp_reduce_max(max_t);
-        }
-        for (int j = lane; j < a.top; j += 32) {
-            const float t = p[j];
-            float l = (float)(TAIL ? (double)t * a.inv_tau - (double)teacher_lse : ((double)t - (double)max_t) * a.inv_tau);
-            if (ids[j] < 0 || t == -INFINITY) l = -INFINITY;
-            const float e = l == -INFINITY ? 0.0f : expf(l);
-            log_p[j] = l;
-            p[j] = e;
-            z += e;
-            if (TAIL && ids[j] >= v0 && ids[j] < v1 && leads(j)) {
-                in.raise(exp_ref(x[j], a.scale));
-                in.sum += exp2_unit(__fmaf_rn(x[j], a.scale, -in.ref));
-            }
-        }
-        z = warp_reduce_sum(z);
-        if (TAIL) {
-            sum_p = z;
-            in.warp_reduce();
-        } else if (z > 0.0f || z != z) {  // (a list of nothing but minus infinity has no mass)
-            const float log_z = logf(z);
-            for (int j = lane; j < a.top; j += 32) {
-                p[j] = p[j] / z;
-                log_p[j] -= log_z;
-            }
-            sum_p = z == z ? 1.0f : z;
-        }
+        sums = distill_list<TAIL>(a, list, teacher_lse, v0, v1, twice);
+        s_sum_p = sums.sum_p;
     }
-    // the student's words outside the list
     ExpSum out = ExpSum::none();
     float m = -INFINITY;
-    // minus infinity in the list's places
-    auto mask = [&](int c, uint4(&raw)[R]) {
-        if (!TAIL) return;
-        const int g = (c - split.chunk0) * 32 * R + lane;
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const uint32_t marked = group_bits<T>(bits, g + 32 * k);
-            if (marked) {
-                union {
-                    uint4 raw;
-                    T e[PER<T>];
-                } u;
-                u.raw = raw[k];
-#pragma unroll
-                for (int i = 0; i < PER<T>; ++i)
-                    if (marked >> i & 1) u.e[i] = none;
-                raw[k] = u.raw;
-            }
-        }
-    };
-    walk.each(row, split, V, none, [&](int c, uint4(&raw)[R]) {
+    walk.each(row, split, V, none, [&](int chunk, int, uint4(&raw)[R]) {
         const float top = groups_max<T, R>(raw);
-        mask(c, raw);
+        if (TAIL) distill_mask<T>(raw, list.bits, (chunk - split.chunk0) * 32 * R + lane);
         m = fmaxf(m, top);  // (a NaN goes into the sums)
         add_groups<T, R>(out, raw, top, a.scale);
     });
-    if (GRAD && !KEEP) walk.start(dynamic, row, split, V);  // the second read is under way while the sums are put together
+    if (GRAD) walk.start(dynamic, threads, row, split, V, false);  // the second read is under way while the sums are put together
     out.warp_reduce();
     m = warp_reduce_max(m);
     if (lane == 0) ered[warp] = out, fred[warp] = m;
     __syncthreads();
     if (warp == 0) {
-        out = lane < WARPS ? ered[lane] : ExpSum::none();
+        out = lane < warps ? ered[lane] : ExpSum::none();
         out.warp_reduce();
-        m = warp_reduce_max(lane < WARPS ? fred[lane] : -INFINITY);
+        m = warp_reduce_max(lane < warps ? fred[lane] : -INFINITY);
     }
     if (ctas > 1) cluster_wait();
-    if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = DistillPart{out, in, m};
+    if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = DistillPart{out, sums.in, m};
     row_sync(cluster, ctas);
     m = parts[0][0].max;
     for (int k = 1; k < ctas; ++k) m = fmaxf(m, parts[0][k].max);
     const bool far = exp_far(m, a.scale);
     if (far) {  // (the same in every CTA of the cluster)
-        float o = 0.0f, l = 0.0f;
-        for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
-            uint4 raw[R];
-            load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, none, raw);
-            mask(c, raw);
-            for (int k = 0; k < R; ++k) {
-                float y[PER<T>];
-                unpack<T>(raw[k], y);
-                for (int i = 0; i < PER<T>; ++i) o += exp2_unit((y[i] - m) * a.scale);
-            }
-        }
+        float o = distill_far_sum<T, TAIL>(row, split, V, m, a.scale, list.bits, warps), l = 0.0f;
         if (TAIL && warp == 0)
             for (int j = lane; j < a.top; j += 32)
-                if (ids[j] >= v0 && ids[j] < v1 && leads(j)) l += exp2_unit((x[j] - m) * a.scale);
-        o = warp_reduce_sum(o);
+                if (list.ids[j] >= v0 && list.ids[j] < v1 && list.leads(j, twice)) l += exp2_unit((list.x[j] - m) * a.scale);
         l = warp_reduce_sum(l);
         if (lane == 0) fred[warp] = o;
         __syncthreads();
-        if (warp == 0) o = warp_reduce_sum(lane < WARPS ? fred[lane] : 0.0f);
+        if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
         if (tid < ctas) *cluster.map_shared_rank(&parts[1][rank], tid) = DistillPart{{0.0f, o}, {0.0f, l}, m};
         row_sync(cluster, ctas);
     }
-    auto exponent = [&](float y, float ref) { return far ? (y - m) * a.scale : __fmaf_rn(y, a.scale, -ref); };
-    if (warp == 0) {
-        out = parts[far][0].out, in = parts[far][0].in;
-        for (int k = 1; k < ctas; ++k) {
-            out.add(parts[far][k].out);
-            in.add(parts[far][k].in);
-        }
-        const float ref = fmaxf(out.ref, in.ref), gap = out.ref - ref;
-        const float s_out = out.sum * exp2_whole(gap), total = s_out + in.sum * exp2_whole(in.ref - ref);
-        const bool rest = TAIL && out.sum != 0.0f;
-        const float p_rest = rest ? (sum_p != sum_p ? sum_p : fmaxf(0.0f, 1.0f - sum_p)) : 0.0f;
-        const float log2_total = total == 0.0f ? 0.0f : log2f(total);  // (without mass log q is minus infinity)
-        if (a.loss && rank == 0) {
-            // (in 64 bits: a listed word at the type's lowest value has a finite log q)
-            double l = 0;
-            for (int j = lane; j < a.top; j += 32)
-                if (p[j] > 0.0f || p[j] != p[j]) {
-                    const double y = far ? ((double)x[j] - (double)m) * (double)a.scale : (double)x[j] * (double)a.scale - (double)ref;
-                    l += (double)p[j] * ((double)log_p[j] - (y - (double)log2_total) * LN2);
-                }
-            l = warp_reduce_sum(l);
-            if (p_rest != 0.0f) l += (double)(p_rest * (logf(p_rest) - (gap + log2f(out.sum) - log2_total) * (float)LN2));
-            if (lane == 0) a.loss[r] = (float)(l * a.tau * a.tau);
-        }
-        if (GRAD && lane == 0) {
-            const float w = (float)((double)weight * a.tau), mass = sum_p + p_rest;
-            const float q = total == 0.0f ? 0.0f : mass / total;
-            whole.list_ref = whole.ref = ref;
-            whole.w = w;
-            whole.listed = q;
-            whole.others = w * (p_rest != 0.0f ? q - p_rest / s_out : q);
-            if (gap < -100.0f) {
-                // less than 2^-80 of the student's mass is outside the list: it counts for the bucket alone, on a scale of its own
-                whole.ref = out.ref;
-                whole.others = p_rest != 0.0f ? -w * p_rest / out.sum : 0.0f;
-            }
-        }
+    if (!GRAD && (warp != 0 || rank != 0)) return;
+    const DistillRow whole = DistillRow::of<TAIL>(parts[far], ctas, m, far, s_sum_p);
+    if (a.loss && rank == 0 && warp == 0) {
+        const float l = whole.loss(a, list);
+        if (lane == 0) a.loss[r] = l;
     }
     if (!GRAD) return;
-    __syncthreads();
-    const float ref = whole.ref, others = whole.others;
+    const DistillFactors f(whole, weight, a.tau);
     const bool abreast = (uintptr_t)grad % 16 == (uintptr_t)row % 16;
-    const auto put = [&](int c, uint4(&raw)[R]) {
-        const int first = chunk_first<T, R>(c, split.pre);
-        const bool inside = chunk_inside<T, R>(first, V);
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            float y[PER<T>];
-            unpack<T>(raw[k], y);
-            if (!far) {
-#pragma unroll
-                for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit(__fmaf_rn(y[i], a.scale, -ref)) * others;
-            } else {
-#pragma unroll
-                for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit((y[i] - m) * a.scale) * others;
-            }
-            raw[k] = weight == 0.0f ? make_uint4(0, 0, 0, 0) : pack<T>(y);
-        }
-        if (abreast && inside) {
-            uint4* to = reinterpret_cast<uint4*>(grad + first) + lane;
-#pragma unroll
-            for (int k = 0; k < R; ++k) __stcs(to + 32 * k, raw[k]);
-        } else {
-            // the row's edges, and rows that lie otherwise to 16 bytes than the logits': through the ring, by elements
-#pragma unroll
-            for (int k = 0; k < R; ++k) *walk.place(k) = raw[k];
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const T* from = (const T*)(walk.place(k) - lane);
-#pragma unroll
-                for (int i = lane; i < 32 * PER<T>; i += 32) {
-                    const int v = first + 32 * PER<T> * k + i;
-                    if (v >= 0 && v < V) grad[v] = from[i];
-                }
-            }
-            __syncwarp();
-        }
-    };
-    if (KEEP) walk.again(row, split, V, none, put);
-    else walk.each(row, split, V, none, put);
+    walk.each(row, split, V, none, [&](int chunk, int slot, uint4(&raw)[R]) {
+        distill_put<T>(grad, chunk_first<T, R>(chunk, split.pre), V, raw, f, whole, a.scale, weight == 0.0f, abreast, walk, slot);
+    });
     if (weight == 0.0f) return;
-    __syncthreads();  // the list's words over the rest
-    for (int j = tid; j < a.top; j += threads) {
-        if (ids[j] < v0 || ids[j] >= v1 || !leads(j)) continue;
-        float pj = p[j];
-        if (s_twice)
-            for (int o = j + 1; o < a.top; ++o)
-                if (ids[o] == ids[j]) pj += p[o];
-        grad[ids[j]] = row_element<T>(whole.w * (exp2_unit(exponent(x[j], whole.list_ref)) * whole.listed - pj));
-    }
+    __syncthreads();
+    distill_put_list<T>(grad, a, list, v0, v1, twice, f, whole, tid, threads);
 }
 
 template <typename T>
@@ -343,27 +419,15 @@ static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t 
     constexpr int CHUNK = 32 * DISTILL_GROUPS * PER<T>;
     const int64_t row_bytes = (int64_t)a.V * sizeof(T);
     const bool tail = a.teacher_lse, grad = a.grad;
-    using Walk = ChunkWalk<T, DISTILL_GROUPS, DISTILL_DEPTH>;
-    RowShape shape = row_shape(rows, row_bytes, 1024, 64);
-    bool keep = false;
-    if (grad) {
-        // as many threads as it takes to hold the row; else what is read twice has to stay in L2 in between: all rows under way
-        // together at most 40 MB
-        RowShape large = shape;
-        while (!Walk::holds(large, a.V) && large.ctas * large.threads < ROW_CTAS * ROW_THREADS) {
-            if (large.threads < 256 || large.ctas == ROW_CTAS) large.threads *= 2;
-            else large.ctas *= 2;
-        }
-        keep = Walk::holds(large, a.V);
-        shape = keep ? large : row_shape(std::min<int64_t>(rows, std::max<int64_t>(1, (40ll << 20) / row_bytes)), row_bytes, 1024, 64);
-    }
+    // what is read twice has to stay in L2 in between: rows of about 60 MB under way together
+    const int64_t most = grad ? std::min<int64_t>(rows, std::max<int64_t>(1, (60ll << 20) / row_bytes)) : rows;
+    const RowShape shape = row_shape(most, row_bytes, 1024, 64);
     // a bit for every word of a CTA's part
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = shape.threads * Walk::BYTES + 16 * a.top +
-                        (tail || grad ? (size_t)((chunks + shape.ctas - 1) / shape.ctas) * (CHUNK / 8) : 0);
-    const auto kernel = !grad ? (tail ? k_distill<T, true, false, false> : k_distill<T, false, false, false>)
-                        : keep ? (tail ? k_distill<T, true, true, true> : k_distill<T, false, true, true>)
-                               : (tail ? k_distill<T, true, true, false> : k_distill<T, false, true, false>);
+    const size_t smem = shape.threads * distill_depth(grad) * DISTILL_GROUPS * 16 +
+                        DistillList::bytes(a.top, tail || grad ? distill_bits<T>((chunks + shape.ctas - 1) / shape.ctas) : 0);
+    const auto kernel = tail ? (grad ? k_distill<T, true, true> : k_distill<T, true, false>)
+                             : (grad ? k_distill<T, false, true> : k_distill<T, false, false>);
     return launch_rows(kernel, a, rows, shape, smem, 2 * 1024, st);
 }
 

@@ -95,8 +95,9 @@ struct RowSplit {
         RowSplit s;
         s.pre = (int)((uintptr_t)row % 16 / sizeof(T));
         const int chunks = (int)(((unsigned)(s.pre + V) + 32 * R * PER<T> - 1) / (32 * R * PER<T>));
-        s.chunk0 = (int)((long long)chunks * rank / ctas);
-        s.chunk1 = (int)((long long)chunks * (rank + 1) / ctas);
+        const int shift = __ffs(ctas) - 1;  // (a power of two)
+        s.chunk0 = chunks * rank >> shift;
+        s.chunk1 = chunks * (rank + 1) >> shift;
         return s;
     }
 };
@@ -143,21 +144,20 @@ __device__ __forceinline__ void load_chunk(const T* row, int first, int V, T fil
     }
 }
 
-// How the rows share the GPU's threads: a row has a CTA, or a cluster of 2, 4 or 8 of them, so that all rows together come to about
-// `per_sm` threads per multiprocessor, but a row has at least 128 threads and a thread at least `least` bytes.
+// How the rows share the GPU's threads: a row has a CTA, or a cluster of 2, 4 or 8 of them, so that all rows together come to not
+// quite `per_sm` threads per multiprocessor, but a row has at least 128 threads and a thread at least `least` bytes.
 struct RowShape {
     int ctas, threads;  // threads of a CTA: 128, 256 or 512
 };
 constexpr int ROW_THREADS = 512, ROW_CTAS = 8;  // at most
 inline RowShape row_shape(int64_t rows, int64_t row_bytes, int64_t per_sm, int64_t least)
 {
-    int64_t n = 148 * per_sm / rows;
-    if (n > row_bytes / least) n = row_bytes / least;
-    int ctas = 1;
-    while (ctas < ROW_CTAS && n > 320 * ctas) ctas *= 2;
-    int threads = 128;  // (powers of two: whole CTAs fill a multiprocessor's registers)
-    while (threads < ROW_THREADS && 2 * threads * ctas <= n) threads *= 2;
-    return RowShape{ctas, threads};
+    int64_t most = 148 * per_sm / rows;
+    if (most > row_bytes / least) most = row_bytes / least;
+    int n = 128;
+    while (n < ROW_CTAS * ROW_THREADS && 2 * n <= most) n *= 2;
+    const int threads = n < 256 ? 128 : n <= 256 * ROW_CTAS ? 256 : ROW_THREADS;
+    return RowShape{n / threads, threads};
 }
 
 // A warp's walk over its chunks of a part (every warps-th from its own number on).  A lane copies its groups of the next DEPTH chunks
@@ -167,85 +167,79 @@ template <typename T, int R, int DEPTH>
 struct ChunkWalk {
     static constexpr int BYTES = DEPTH * R * 16;  // per thread
     uint4* ring;
-    int chunk;  // the next to work on
-    int slot;
-    __device__ __forceinline__ void fetch(const T* row, const RowSplit& split, int V, int c, int into)
+    int threads, warps;  // that walk together
+    unsigned long long policy;  // of L2
+    // Chunk c (if the part has it) into the ring's slot; one group of copies, empty or not.
+    __device__ __forceinline__ void fetch(const T* row, const RowSplit& split, int V, int c, int slot)
     {
         if (c < split.chunk1) {
             const int first = chunk_first<T, R>(c, split.pre);
             const int mine = first + (int)(threadIdx.x & 31) * PER<T>;
             const T* from = row + mine;
-            const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + into * R * (int)blockDim.x);
+            const uint32_t to = (uint32_t)__cvta_generic_to_shared(place(slot, 0));
             const bool inside = chunk_inside<T, R>(first, V);
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 if (inside || group_inside<T>(mine + 32 * PER<T> * r, V))
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * (uint32_t)blockDim.x * 16),
-                                 "l"(from + 32 * PER<T> * r)
+                    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to + r * (uint32_t)threads * 16),
+                                 "l"(from + 32 * PER<T> * r), "l"(policy)
                                  : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ void start(void* shared, const T* row, const RowSplit& split, int V)
+    template <int LEFT>
+    static __device__ __forceinline__ void wait()
+    {
+        asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+    }
+    // Group r of a slot's chunk (the warp's groups of one r are consecutive).
+    __device__ __forceinline__ uint4* place(int slot, int r) const { return ring + (slot * R + r) * threads; }
+    // again: what is read will be read once more, from L2.
+    __device__ __forceinline__ void start(void* shared, int threads_, const T* row, const RowSplit& split, int V, bool again)
     {
         ring = (uint4*)shared + threadIdx.x;
-        chunk = split.chunk0 + (int)(threadIdx.x >> 5);
-        slot = 0;
-        const int warps = (int)(blockDim.x >> 5);
+        threads = threads_;
+        warps = threads / 32;
+        from(row, split, V, again);
+    }
+    // (the same place, another row)
+    __device__ __forceinline__ void from(const T* row, const RowSplit& split, int V, bool again)
+    {
+        if (again) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+        else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) fetch(row, split, V, chunk + d * warps, d);
+        for (int d = 0; d < DEPTH; ++d) fetch(row, split, V, split.chunk0 + (int)(threadIdx.x >> 5) + d * warps, d);
     }
-    // Gives up what is on its way.
-    __device__ __forceinline__ void drop() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-    // Group r of the chunk that f is called for, in the ring (the warp's groups of one r are consecutive).
-    __device__ __forceinline__ uint4* place(int r) const { return ring + (slot * R + r) * (int)blockDim.x; }
-    // Whether the ring holds all that a warp walks over, so that `again` finds it there.
-    static bool holds(const RowShape& shape, int V)
-    {
-        const int chunks = (V + PER<T> - 1 + 32 * R * PER<T> - 1) / (32 * R * PER<T>);
-        return (chunks + shape.ctas - 1) / shape.ctas <= DEPTH * (shape.threads / 32);
-    }
-    // A second walk over what the ring holds.
-    template <typename F>
-    __device__ __forceinline__ void again(const T* row, const RowSplit& split, int V, T fill, F f)
-    {
-        slot = 0;
-        for (chunk = split.chunk0 + (int)(threadIdx.x >> 5); chunk < split.chunk1; chunk += (int)(blockDim.x >> 5)) {
-            uint4 raw[R];
-            take(row, split, V, fill, raw);
-            f(chunk, raw);
-            ++slot;
-        }
-    }
-    __device__ __forceinline__ void take(const T* row, const RowSplit& split, int V, T fill, uint4 (&raw)[R])
+    // What a slot holds of a chunk; `fill` stands outside the row.
+    __device__ __forceinline__ void take(const T* row, const RowSplit& split, int V, T fill, int chunk, int slot, uint4 (&raw)[R])
     {
         const int first = chunk_first<T, R>(chunk, split.pre);
         if (chunk_inside<T, R>(first, V)) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) raw[r] = *place(r);
+            for (int r = 0; r < R; ++r) raw[r] = *place(slot, r);
         } else {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int v = first + (32 * r + (int)(threadIdx.x & 31)) * PER<T>;
-                raw[r] = group_inside<T>(v, V) ? *place(r) : edge_group(row, v, V, fill);
+                raw[r] = group_inside<T>(v, V) ? *place(slot, r) : edge_group(row, v, V, fill);
             }
         }
     }
-    // f(chunk, groups) for each; `fill` stands outside the row.
+    // f(chunk, slot, groups) for each chunk of a part of any length.
     template <typename F>
     __device__ __forceinline__ void each(const T* row, const RowSplit& split, int V, T fill, F f)
     {
-        const int warps = (int)(blockDim.x >> 5);
-        for (; chunk < split.chunk1; chunk += warps) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+        int slot = 0;
+        for (int chunk = split.chunk0 + (int)(threadIdx.x >> 5); chunk < split.chunk1; chunk += warps) {
+            wait<DEPTH - 1>();
             uint4 raw[R];
-            take(row, split, V, fill, raw);
-            f(chunk, raw);
+            take(row, split, V, fill, chunk, slot, raw);
+            f(chunk, slot, raw);
             // (the place is free: its groups have been worked on)
             fetch(row, split, V, chunk + DEPTH * warps, slot);
             slot = slot + 1 == DEPTH ? 0 : slot + 1;
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        wait<0>();
     }
 };
 
@@ -337,7 +331,7 @@ __device__ __forceinline__ float groups_max(const uint4 (&raw)[N])
     }
 }
 
-// Two products and sums, or two sums, in one instruction.
+// Two products and sums, products or sums in one instruction.
 __device__ __forceinline__ float2 fma_two(float2 a, float2 b, float2 c)
 {
     unsigned long long y;
@@ -345,6 +339,14 @@ __device__ __forceinline__ float2 fma_two(float2 a, float2 b, float2 c)
         : "=l"(y)
         : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
           "l"(*reinterpret_cast<unsigned long long*>(&c)));
+    return *reinterpret_cast<float2*>(&y);
+}
+__device__ __forceinline__ float2 mul_two(float2 a, float2 b)
+{
+    unsigned long long y;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(y)
+        : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
     return *reinterpret_cast<float2*>(&y);
 }
 __device__ __forceinline__ float2 add_two(float2 a, float2 b)
@@ -405,6 +407,10 @@ __device__ __forceinline__ uint4 pack(const float (&x)[PER<T>])
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
+
+// Barrier `id` of the CTA for `threads` of its threads (whole warps): waiting, and arriving without a wait.
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // Barrier of all threads that share a row.
 __device__ __forceinline__ void row_sync(cg::cluster_group& cluster, int ctas)

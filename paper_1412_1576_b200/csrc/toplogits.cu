@@ -1,6 +1,8 @@
 // The largest logits of every row, with their words, and the row's log-sum-exp.
 //
 // A row's words are ordered by value (NaN first), equal values by the lower word; what is minus infinity is not listed.
+#include <algorithm>
+
 #include "lda_device.cuh"
 #include "rows.cuh"
 
@@ -17,62 +19,39 @@ struct TopArgs {
     float* lse;
 };
 
-#ifndef TG
-#define TG 4
-#endif
-#ifndef TB
-#define TB 2
-#endif
-constexpr int TOP_GROUPS = TG;     // groups a lane has in flight
-constexpr int TOP_LIST = 2048;      // words that may be left for the longest lists
-constexpr int TOP_VALUES = 1024;  // groups of pieces whose largest keys give the border, at most
-// Words and pieces that may be left for lists of `top`: about four times what is expected.
-__host__ __device__ constexpr int top_room(int top) { return top <= 64 ? 512 : top <= 256 ? 1024 : TOP_LIST; }
-constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
-
+constexpr int TOP_GROUPS = 4;     // groups of a lane in a chunk
 #ifndef TD
 #define TD 2
 #endif
 constexpr int TOP_DEPTH = TD;      // chunks on their way
+constexpr int TOP_VALUES = 1024;  // groups of pieces whose largest keys give the border, at most
+constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
+// Words and pieces that may be left for lists of `top`: about four times what is expected.
+__host__ __device__ constexpr int top_room(int top) { return top <= 64 ? 512 : top <= 256 ? 1024 : 2048; }
 
-// What a CTA knows of its part of the row.
-struct TopPart {
-    ExpSum sum;
-    float max;
-    uint32_t share, alone;  // borders (half-keys)
-};
-
-// Behind the pass over the row its shared memory holds these.
+// What takes the ring's place behind the pass.
 struct TopLists {
     unsigned long long* list;  // the words that are left
-    uint16_t* tops;            // (before that, in the same place) the groups' largest keys
     int* queue;                // the pieces that are read again
+    __device__ __forceinline__ TopLists(void* at, int room)
+        : list((unsigned long long*)at), queue((int*)at + 2 * room)
+    {
+    }
+    static __host__ __device__ constexpr int bytes(int room) { return 12 * room; }
 };
-
-struct TopShared {
-    TopPart parts[2][ROW_CTAS];
-    ExpSum ered[ROW_THREADS / 32];
-    float fred[ROW_THREADS / 32];
-    int ired[33];
-    int hist[256];
+struct TopCounts {
     int n, queued, need;
     uint32_t prefix;
-    float max;
+    int hist[256];
 };
-
-__host__ __device__ constexpr int top_ring_bytes(int threads, int room)
-{
-    const int ring = threads * TOP_DEPTH * TOP_GROUPS * 16, lists = room * 12;
-    return ring > lists ? ring : lists;
-}
 
 __device__ __forceinline__ unsigned long long top_entry(uint32_t key, int v)
 {
     return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)v);
 }
 
-// Descending sort of list[0..n) by the CTA; list[n..) up to the next power of two is overwritten.
-__device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
+// Descending sort of list[0..n); list[n..) up to the next power of two is overwritten.
+__device__ __forceinline__ void top_sort(unsigned long long* list, int n)
 {
     const int tid = threadIdx.x, threads = blockDim.x;
     int size = 32;
@@ -105,6 +84,7 @@ __device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
     __syncthreads();
     for (int k = 2; k <= size; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
+#pragma unroll 2
             for (int i = tid; i < size / 2; i += threads) {
                 const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
                 const unsigned long long x = list[lo], y = list[hi];
@@ -115,14 +95,15 @@ __device__ __forceinline__ void sort_entries(unsigned long long* list, int n)
 }
 
 // For rows where the border leaves too many words (long ties): the border value by four passes that count bytes of the keys, then
-// what is above it, then the first words at it.  One CTA, the whole row; returns how many words the list has.
+// what is above it, then the first words at it.  Returns how many words the list has.
 template <typename T>
-__device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared& sh, unsigned long long* list)
+__device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopCounts& sh, unsigned long long* list)
 {
-    const int tid = threadIdx.x, threads = blockDim.x;
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31;
     uint32_t prefix = 0;
     int need = top;
     for (int shift = 24; shift >= 0; shift -= 8) {
+        __syncthreads();
         for (int i = tid; i < 256; i += threads) sh.hist[i] = 0;
         __syncthreads();
         for (int v = tid; v - tid < V; v += threads) {
@@ -135,7 +116,7 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared
             const bool like = in && byte == theirs;
             const uint32_t alike = __ballot_sync(0xffffffffu, like);
             if (like) {
-                if ((tid & 31) == first) atomicAdd(&sh.hist[byte], __popc(alike));
+                if (lane == first) atomicAdd(&sh.hist[byte], __popc(alike));
             } else if (in)
                 atomicAdd(&sh.hist[byte], 1);
         }
@@ -149,9 +130,8 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared
         __syncthreads();
         prefix = sh.prefix;
         need = sh.need;
-        __syncthreads();
     }
-    if (prefix <= KEY_NEG_INF) prefix = KEY_NEG_INF;  // (fewer than `top` words are not masked)
+    prefix = max(prefix, KEY_NEG_INF);  // (where fewer than `top` words are not masked)
     if (tid == 0) sh.n = 0;
     __syncthreads();
     for (int v = tid; v < V; v += threads) {
@@ -159,235 +139,323 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopShared
         if (k > prefix) list[atomicAdd(&sh.n, 1)] = top_entry(k, v);
     }
     __syncthreads();
-    int have = sh.n;
-    __syncthreads();
-    for (int base = 0; base < V && have < top && prefix > KEY_NEG_INF; base += threads) {
-        const int v = base + tid;
-        const int at = v < V && order_key(row_value(row[v])) == prefix;
-        int total;
-        const int before = block_scan_excl(at, sh.ired, total);
-        if (at && have + before < top) list[have + before] = top_entry(prefix, v);
-        have += total;
-        __syncthreads();
+    // the words at the border in their order: one warp
+    if (tid < 32 && prefix > KEY_NEG_INF) {
+        int have = sh.n;
+        for (int base = 0; base < V && have < top; base += 32) {
+            const int v = base + lane;
+            const bool at = v < V && order_key(row_value(row[v])) == prefix;
+            const uint32_t all = __ballot_sync(0xffffffffu, at);
+            const int place = have + __popc(all & ((1u << lane) - 1));
+            if (at && place < top) list[place] = top_entry(prefix, v);
+            have += __popc(all);
+        }
+        if (lane == 0) sh.n = min(have, top);
     }
-    return min(have, top);
+    __syncthreads();
+    return sh.n;
 }
 
-// One cluster per row.  The pass that adds up the exponentials leaves the largest value of every piece (a lane's groups of a chunk;
-// FINE: each group) as the upper half of its key.  A border that at least `top` of them reach leaves at least `top` words, and few
-// more: the pieces that reach it are read again (from L2), their words at or above it are sorted.
+// What the pass over a row does with a chunk: its values into the sum, the largest of every piece (a lane's groups of the chunk; FINE:
+// each group) as the upper half of its key, and of every group of pieces (`tops`).
 template <typename T, bool FINE>
-__global__ void __launch_bounds__(ROW_THREADS, TB) k_top(TopArgs a)
+__device__ __forceinline__ void top_chunk(const uint4 (&raw)[TOP_GROUPS], uint16_t* keys, uint16_t* tops, float c, float& m, ExpSum& sum)
+{
+    float top;
+    if (FINE) {
+        top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < TOP_GROUPS; ++k) {
+            const uint4 one[1] = {raw[k]};
+            const float x = groups_max<T, 1>(one);
+            keys[32 * k] = (uint16_t)(order_key(x) >> 16);
+            top = max_nan(top, x);
+        }
+    }
+    if (!FINE) top = groups_max<T, TOP_GROUPS>(raw);
+    const uint16_t key = (uint16_t)(order_key(top) >> 16);
+    if (!FINE) keys[0] = key;
+    *tops = max(*tops, key);
+    m = fmaxf(m, top);
+    add_groups<T, TOP_GROUPS>(sum, raw, top, c);
+}
+
+// Groups of pieces: a power of two of them per thread, so that a fourth at most will reach the border where that is possible.
+__host__ __device__ constexpr int top_groups(int threads, int top)
+{
+    int n = threads < 256 ? 256 : threads;
+    while (n < 4 * top && n < TOP_VALUES) n *= 2;
+    return n;
+}
+
+// By one warp: the largest half-key that at least `share` of the groups reach, or one that not many more do, and the same for `top` of
+// them: steps of doubling width down from the largest key, then halving; minus infinity's successor if there are not that many.
+struct TopBorders {
+    uint32_t share, alone;
+};
+__device__ __forceinline__ TopBorders top_borders(const uint16_t* tops, int values, int share, int top)
+{
+    const int lane = threadIdx.x & 31, per = values / 32;
+    uint32_t mine[TOP_VALUES / 32], best = 0;
+#pragma unroll
+    for (int k = 0; k < TOP_VALUES / 32; k += 8)
+        if (k < per)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                mine[k + e] = tops[(k + e) * 32 + lane];
+                best = max(best, mine[k + e]);
+            }
+    best = __reduce_max_sync(0xffffffffu, best);
+    const auto border = [&](int want, uint32_t hi) {
+        uint32_t lo = TOP_LOWEST, step = 64;
+        while (lo + 1 < hi) {
+            const bool down = lo == TOP_LOWEST && hi > lo + step;
+            const uint32_t mid = down ? hi - step : (lo + hi) / 2;
+            step = down ? step * 2 : step;
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < TOP_VALUES / 32; k += 8)
+                if (k < per)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) n += mine[k + e] >= mid;
+            n = __reduce_add_sync(0xffffffffu, n);
+            if (n >= want) {
+                lo = mid;
+                if (n <= want + want / 4 + (share == top ? 16 : 2)) break;
+            } else
+                hi = mid;
+        }
+        return lo;
+    };
+    TopBorders b;
+    b.share = border(share, best + 1);
+    b.alone = share == top ? b.share : border(top, b.share + 1);
+    return b;
+}
+
+// The words that reach the border, into `list` (n counts them, beyond its room too): the pieces that do are read again, a group of
+// one to every thread.
+template <typename T, bool FINE>
+__device__ __forceinline__ void top_collect(const T* row, const RowSplit& split, int V, const uint16_t* keys,
+                                            int pieces, uint32_t border, int room, int* queue, int* queued, unsigned long long* list, int* n)
 {
     constexpr int R = TOP_GROUPS, PIECES = FINE ? R : 1, SIZE = R / PIECES;  // pieces of a lane's groups, groups of a piece
-    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring and, later, the lists; the pieces' keys
-    const int room = top_room(a.top);
-    const TopLists lists{(unsigned long long*)dynamic, (uint16_t*)dynamic, (int*)(dynamic + 8 * room)};
-    uint16_t* keys = (uint16_t*)(dynamic + top_ring_bytes(blockDim.x, room));
-    __shared__ TopShared sh;
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31;
+    for (int base = 0; base < pieces; base += 32 * threads) {
+        // 32 pieces of each thread: eight at a time in four places
+        uint32_t hits = 0;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int i = base + 8 * (h * threads + tid);
+            if (i >= pieces) break;
+            const uint4 eight = *reinterpret_cast<const uint4*>(keys + i);
+            const uint32_t two[4] = {eight.x, eight.y, eight.z, eight.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                hits |= (uint32_t)((two[e] & 0xFFFFu) >= border) << (8 * h + 2 * e);
+                hits |= (uint32_t)((two[e] >> 16) >= border) << (8 * h + 2 * e + 1);
+            }
+        }
+        if (!__any_sync(0xffffffffu, hits)) continue;
+        const int upto = warp_scan_incl(__popc(hits));
+        int at = 0;
+        if (lane == 31) at = atomicAdd(queued, upto);
+        at = __shfl_sync(0xffffffffu, at, 31) + upto - __popc(hits);
+        for (; hits; hits &= hits - 1, ++at) {
+            const int bit = __ffs((int)hits) - 1;
+            if (at < room) queue[at] = base + 8 * (bit / 8 * threads + tid) + bit % 8;
+        }
+    }
+    __syncthreads();
+    const int tasks = *queued * SIZE;
+    if (*queued > room) {
+        if (tid == 0) atomicAdd(n, room + 1);
+        return;
+    }
+    constexpr int AHEAD = 4;  // groups of a thread that are on their way together
+    for (int base = 0; base < tasks; base += AHEAD * threads) {
+        uint4 raw[AHEAD];
+        int first[AHEAD];
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) {
+            const int t = base + h * threads + tid;
+            const int i = t < tasks ? queue[t / SIZE] : 0;  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
+            const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
+            first[h] = t < tasks ? chunk_first<T, R>(split.chunk0 + i / (32 * PIECES), split.pre) + group * PER<T> : V;
+            raw[h] = t < tasks ? any_group(row, first[h], V, row_element<T>(-INFINITY)) : uint4{};
+        }
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) {
+            if (base + h * threads >= tasks) break;
+            float x[PER<T>];
+            unpack<T>(raw[h], x);
+            uint32_t hits = 0;
+#pragma unroll
+            for (int e = 0; e < PER<T>; ++e) hits |= (uint32_t)((order_key(x[e]) >> 16) >= border) << e;
+            if (first[h] >= V) hits = 0;
+            if (!__any_sync(0xffffffffu, hits)) continue;
+            // (one addition for the warp)
+            const int upto = warp_scan_incl(__popc(hits));
+            int at = 0;
+            if (lane == 31) at = atomicAdd(n, upto);
+            at = __shfl_sync(0xffffffffu, at, 31) + upto - __popc(hits);
+#pragma unroll
+            for (int e = 0; e < PER<T>; ++e)
+                if (hits >> e & 1) {
+                    if (at < room) list[at] = top_entry(order_key(x[e]), first[h] + e);
+                    ++at;
+                }
+        }
+    }
+}
+
+// The row's outputs from its n candidates (room + 1 or more: they did not fit).
+template <typename T>
+__device__ __forceinline__ void top_finish(const TopArgs& a, int64_t r, const T* row, int room, int n,
+                                           unsigned long long* list, TopCounts& sh, ExpSum sum, float m, bool far)
+{
+    if (n > room) n = top_by_bytes<T>(row, a.V, a.top, sh, list);
+    top_sort(list, n);
+    const int tid = threadIdx.x, threads = blockDim.x, want = min(n, a.top);
+    for (int i = tid; i < a.top; i += threads) {
+        const int64_t at = r * a.top + i;
+        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)list[i]) : -1;
+        a.ids[at] = v;
+        ((T*)a.values)[at] = v >= 0 ? row[v] : row_element<T>(-INFINITY);
+    }
+    if (a.lse && tid == 0) {
+        const uint32_t first = want > 0 ? (uint32_t)(list[0] >> 32) : 0;
+        // (log2 of the largest exponential: x c - R, or 0 when far)
+        const double largest = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
+        a.lse[r] = want == 0 ? -INFINITY
+                   : first == KEY_NAN ? NAN
+                   : m == INFINITY ? INFINITY
+                                   : (float)((double)m * a.inv_tau + ((double)log2f(sum.sum) - largest) * LN2);
+    }
+}
+
+// Sum of 2^((x - m) c) over a warp's chunks.
+template <typename T>
+__device__ __noinline__ float top_far_sum(const T* row, const RowSplit& split, int V, float m, float c, int warp, int warps)
+{
+    constexpr int R = TOP_GROUPS;
+    float o = 0.0f;
+    for (int chunk = split.chunk0 + warp; chunk < split.chunk1; chunk += warps) {
+        uint4 raw[R];
+        load_chunk<T, R>(row, chunk_first<T, R>(chunk, split.pre), V, row_element<T>(-INFINITY), raw);
+        for (int k = 0; k < R; ++k) {
+            float y[PER<T>];
+            unpack<T>(raw[k], y);
+            for (int i = 0; i < PER<T>; ++i) o += exp2_unit((y[i] - m) * c);
+        }
+    }
+    return warp_reduce_sum(o);
+}
+
+// What a CTA knows of its part of the row.
+struct TopPart {
+    ExpSum sum;
+    float max;
+    TopBorders borders;
+};
+
+__host__ __device__ constexpr int top_ring_bytes(int threads) { return threads * TOP_DEPTH * TOP_GROUPS * 16; }
+
+// One cluster per row.  The pass leaves the pieces' largest keys.  A border that at least `top` groups of pieces reach
+// leaves at least `top` words, and few more; the pieces that reach it are read again (from L2), their words are sorted.
+template <typename T, bool FINE>
+__global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
+{
+    constexpr int R = TOP_GROUPS, PIECES = FINE ? R : 1;
+    extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring and, later, the lists; the groups' and the pieces' largest keys
+    __shared__ TopPart parts[2][ROW_CTAS];
+    __shared__ ExpSum ered[ROW_THREADS / 32];
+    __shared__ float fred[ROW_THREADS / 32];
+    __shared__ TopCounts sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, WARPS = threads / 32, V = a.V;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads / 32, V = a.V;
+    const int room = top_room(a.top);
+    const TopLists lists(dynamic, room);
+    uint16_t* tops = (uint16_t*)(dynamic + max(top_ring_bytes(threads), TopLists::bytes(room)));
+    const int groups = top_groups(threads, a.top), share = groups / threads - 1;
+    uint16_t* keys = tops + groups;
     const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
     const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
     const int pieces = (split.chunk1 - split.chunk0) * 32 * PIECES;
     ChunkWalk<T, R, TOP_DEPTH> walk;
-    walk.start(dynamic, row, split, V);
+    walk.start(dynamic, threads, row, split, V, true);
     if (ctas > 1) cluster_arrive();
     if (tid == 0) sh.n = sh.queued = 0;
+    for (int g = tid; g < groups; g += threads) tops[g] = 0;  // (a thread's own)
+    int turn = 0;
     ExpSum sum = ExpSum::none();
     float m = -INFINITY;
-    walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, uint4(&raw)[R]) {
-        const int at = (c - split.chunk0) * 32 * PIECES + lane;
-        float top;
-        if (FINE) {
-            top = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const uint4 one[1] = {raw[k]};
-                const float x = groups_max<T, 1>(one);
-                keys[at + 32 * k] = (uint16_t)(order_key(x) >> 16);
-                top = max_nan(top, x);
-            }
-        } else {
-            top = groups_max<T, R>(raw);
-            keys[at] = (uint16_t)(order_key(top) >> 16);
-        }
-        m = fmaxf(m, top);
-        add_groups<T, R>(sum, raw, top, a.scale);
+    walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, int, uint4(&raw)[R]) {
+        top_chunk<T, FINE>(raw, keys + (c - split.chunk0) * 32 * PIECES + lane, tops + (turn++ & share) * threads + tid, a.scale, m, sum);
     });
     sum.warp_reduce();
     m = warp_reduce_max(m);
-    if (lane == 0) sh.ered[warp] = sum, sh.fred[warp] = m;
+    if (lane == 0) ered[warp] = sum, fred[warp] = m;
     __syncthreads();
-    // the pieces' keys in `values` groups, the largest of each; every fourth at most will reach the border
-    int values = 256;
-    while (values < 4 * a.top && values < TOP_VALUES) values *= 2;
-    for (int g = tid; g < values; g += threads) {
-        uint32_t top = 0;
-        for (int i = g; i < pieces; i += values) top = max(top, (uint32_t)keys[i]);
-        lists.tops[g] = (uint16_t)top;
-    }
-    __syncthreads();
-    uint32_t share = 0, alone = 0;
+    TopBorders borders{0, 0};
     if (warp == 0) {
-        sum = lane < WARPS ? sh.ered[lane] : ExpSum::none();
+        sum = lane < warps ? ered[lane] : ExpSum::none();
         sum.warp_reduce();
-        m = warp_reduce_max(lane < WARPS ? sh.fred[lane] : -INFINITY);
-        const int per = values / 32;
-        uint32_t tops[TOP_VALUES / 32], best = 0;
-#pragma unroll
-        for (int k = 0; k < TOP_VALUES / 32; ++k) {
-            tops[k] = k < per ? lists.tops[k * 32 + lane] : 0u;
-            best = max(best, tops[k]);
-        }
-        best = __reduce_max_sync(0xffffffffu, best);
-        // The largest half-key that at least `want` of the groups reach, or one that not many more do: steps of doubling width down
-        // from `hi` (that fewer reach), then halving; minus infinity's successor if there are not that many.
-        auto border_of = [&](int want, uint32_t hi) {
-            uint32_t lo = TOP_LOWEST, step = 64;
-            while (lo + 1 < hi) {
-                const bool down = lo == TOP_LOWEST && hi > lo + step;
-                const uint32_t mid = down ? hi - step : (lo + hi) / 2;
-                step = down ? step * 2 : step;
-                int n = 0;
-#pragma unroll
-                for (int k = 0; k < TOP_VALUES / 32; k += 8)
-                    if (k < per)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) n += tops[k + e] >= mid;
-                n = __reduce_add_sync(0xffffffffu, n);
-                if (n >= want) {
-                    lo = mid;
-                    if (n <= want + want / 4 + 16 / ctas) break;
-                } else
-                    hi = mid;
-            }
-            return lo;
-        };
+        m = warp_reduce_max(lane < warps ? fred[lane] : -INFINITY);
         // `top` groups of one part are enough, and so are its share of them in every part
-        share = border_of((a.top + ctas - 1) / ctas, best + 1);
-        alone = ctas > 1 ? border_of(a.top, share + 1) : share;
+        borders = top_borders(tops, groups, (a.top + ctas - 1) / ctas, a.top);
     }
     if (ctas > 1) cluster_wait();
-    if (tid < ctas) *cluster.map_shared_rank(&sh.parts[0][rank], tid) = TopPart{sum, m, share, alone};
+    if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = TopPart{sum, m, borders};
     row_sync(cluster, ctas);
     uint32_t border = 0, least = 0xFFFFFFFFu;
     m = -INFINITY;
     for (int k = 0; k < ctas; ++k) {
-        border = max(border, sh.parts[0][k].alone);
-        least = min(least, sh.parts[0][k].share);
-        m = fmaxf(m, sh.parts[0][k].max);
+        border = max(border, parts[0][k].borders.alone);
+        least = min(least, parts[0][k].borders.share);
+        m = fmaxf(m, parts[0][k].max);
     }
     border = max(border, least);
     const bool far = exp_far(m, a.scale);
     if (far) {  // (the same in every CTA of the cluster)
-        float o = 0.0f;
-        for (int c = split.chunk0 + warp; c < split.chunk1; c += WARPS) {
-            uint4 raw[R];
-            load_chunk<T, R>(row, chunk_first<T, R>(c, split.pre), V, row_element<T>(-INFINITY), raw);
-            for (int k = 0; k < R; ++k) {
-                float y[PER<T>];
-                unpack<T>(raw[k], y);
-                for (int i = 0; i < PER<T>; ++i) o += exp2_unit((y[i] - m) * a.scale);
-            }
-        }
-        o = warp_reduce_sum(o);
-        if (lane == 0) sh.fred[warp] = o;
+        float o = top_far_sum<T>(row, split, V, m, a.scale, warp, warps);
+        if (lane == 0) fred[warp] = o;
         __syncthreads();
-        if (warp == 0) o = warp_reduce_sum(lane < WARPS ? sh.fred[lane] : 0.0f);
-        if (tid < ctas) *cluster.map_shared_rank(&sh.parts[1][rank], tid) = TopPart{{0.0f, o}, m, 0, 0};
+        if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
+        if (tid < ctas) *cluster.map_shared_rank(&parts[1][rank], tid) = TopPart{{0.0f, o}, m, {0, 0}};
         row_sync(cluster, ctas);
     }
-    // the pieces that reach the border, then a group of one to every thread
-    int* n_all = cluster.map_shared_rank(&sh.n, 0);
-    unsigned long long* list = cluster.map_shared_rank(lists.list, 0);
-    for (int i = 8 * tid; i < pieces; i += 8 * threads) {
-        const uint4 eight = *reinterpret_cast<const uint4*>(keys + i);
-        const uint32_t two[4] = {eight.x, eight.y, eight.z, eight.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (((two[e / 2] >> (e % 2 * 16)) & 0xFFFFu) >= border) {
-                const int at = atomicAdd(&sh.queued, 1);
-                if (at < room) lists.queue[at] = i + e;
-            }
-    }
-    __syncthreads();
-    const int queued = sh.queued;
-    if (queued > room) {
-        if (tid == 0) atomicAdd(n_all, room + 1);
-    } else
-        for (int base = 0; base < queued * SIZE; base += 2 * threads) {
-            // (two groups at a time: the second is on its way while the first is looked at)
-            uint4 raw[2];
-            int first[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int t = base + h * threads + tid;
-                const bool any = t < queued * SIZE;
-                const int i = any ? lists.queue[t / SIZE] : 0;  // piece i: chunk i / (32 PIECES), its groups 32 k + (i mod 32)
-                const int chunk = split.chunk0 + i / (32 * PIECES);
-                const int group = FINE ? i % (32 * PIECES) : 32 * (t % SIZE) + i % 32;
-                first[h] = any ? chunk_first<T, R>(chunk, split.pre) + group * PER<T> : V;
-                raw[h] = any_group(row, first[h], V, row_element<T>(-INFINITY));
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float x[PER<T>];
-                unpack<T>(raw[h], x);
-#pragma unroll
-                for (int e = 0; e < PER<T>; ++e) {
-                    const uint32_t k = order_key(x[e]);
-                    const bool hit = (k >> 16) >= border;
-                    const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-                    if (hits == 0) continue;
-                    int at = 0;
-                    if (lane == 0) at = ctas == 1 ? atomicAdd(&sh.n, __popc(hits)) : atomicAdd(n_all, __popc(hits));
-                    at = __shfl_sync(0xffffffffu, at, 0) + __popc(hits & ((1u << lane) - 1));
-                    if (hit && at < room) list[at] = top_entry(k, first[h] + e);
-                }
-            }
-        }
+    top_collect<T, FINE>(row, split, V, keys, pieces, border, room, lists.queue, &sh.queued,
+                         cluster.map_shared_rank(lists.list, 0), cluster.map_shared_rank(&sh.n, 0));
     row_sync(cluster, ctas);
     if (rank != 0) return;
-    int n = sh.n;
-    if (n > room) {
-        __syncthreads();
-        n = top_by_bytes<T>(row, V, a.top, sh, lists.list);
-        __syncthreads();
-    }
-    sort_entries(lists.list, n);
-    const int want = min(n, a.top);
-    for (int i = tid; i < a.top; i += threads) {
-        const int64_t at = r * a.top + i;
-        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)lists.list[i]) : -1;
-        a.ids[at] = v;
-        ((T*)a.values)[at] = v >= 0 ? row[v] : row_element<T>(-INFINITY);
-    }
-    if (a.lse && tid == 0) {
-        sum = sh.parts[far][0].sum;
-        for (int k = 1; k < ctas; ++k) sum.add(sh.parts[far][k].sum);
-        const uint32_t first = want > 0 ? (uint32_t)(lists.list[0] >> 32) : 0;
-        // (log2 of the largest exponential: x c, or 0 when far)
-        const double most2 = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
-        a.lse[r] = want == 0 ? -INFINITY
-                   : first == KEY_NAN ? NAN
-                   : m == INFINITY ? INFINITY
-                                   : (float)((double)m * a.inv_tau + ((double)log2f(sum.sum) - most2) * LN2);
-    }
+    sum = parts[far][0].sum;
+    for (int k = 1; k < ctas; ++k) sum.add(parts[far][k].sum);
+    top_finish<T>(a, r, row, room, sh.n, lists.list, sh, sum, m, far);
 }
 
 template <typename T>
 static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
 {
     constexpr int CHUNK = 32 * TOP_GROUPS * PER<T>;
-    RowShape shape = row_shape(rows, (int64_t)a.V * sizeof(T), 1024, 64);
-    const int per = a.V / PER<T>;
-    const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
+    const int64_t row_bytes = (int64_t)a.V * sizeof(T);
+    const int per = a.V / PER<T>, room = top_room(a.top);
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = top_ring_bytes(shape.threads, top_room(a.top)) + (size_t)((chunks + shape.ctas - 1) / shape.ctas) * 32 * (fine ? TOP_GROUPS : 1) * 2;
-    return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, shape, smem, sizeof(TopShared), st);
+    const auto pieces = [&](int ctas, bool fine) { return (chunks + ctas - 1) / ctas * 32 * (fine ? TOP_GROUPS : 1); };
+#ifdef FORCE_T
+    const RowShape shape = rows > 700 ? RowShape{1, FORCE_T} : row_shape(rows, row_bytes, 1024, 64);
+#else
+    const RowShape shape = row_shape(rows, row_bytes, 1024, 64);
+#endif
+#ifdef FINE_K
+    const bool fine = a.top > FINE_K || per / TOP_GROUPS / shape.ctas < 4 * a.top;
+#else
+    const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
+#endif
+    const size_t smem = std::max(top_ring_bytes(shape.threads), TopLists::bytes(room)) + 2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
+    return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, shape, smem, sizeof(TopCounts) + 1024, st);
 }
 
 }  // namespace lda
