@@ -78,17 +78,11 @@ struct DistillSpan {
 template <typename T>
 __host__ __device__ constexpr int distill_bits(int chunks) { return chunks * (32 * DISTILL_GROUPS * PER<T> / 8); }
 
-// What the list says, worked out by one warp from ids, p (the logits) and x.
-struct DistillSums {
-    float sum_p;
-    ExpSum in;
-};
+// The teacher's probabilities (by one warp): p and log_p from the logits in p; returns the sum of p.
 template <bool TAIL>
-__device__ __forceinline__ DistillSums distill_list(const DistillArgs& a, const DistillList& list, float teacher_lse, int v0, int v1,
-                                                    bool twice)
+__device__ __forceinline__ float distill_teacher(const DistillArgs& a, const DistillList& list, float teacher_lse)
 {
     const int lane = threadIdx.x & 31;
-    DistillSums s{0.0f, ExpSum::none()};
     float max_t = -INFINITY, z = 0.0f;
     if (!TAIL) {
         for (int j = lane; j < a.top; j += 32)
@@ -96,31 +90,36 @@ __device__ __forceinline__ DistillSums distill_list(const DistillArgs& a, const 
         max_t = warp_reduce_max(max_t);
     }
     for (int j = lane; j < a.top; j += 32) {
-        const int id = list.ids[j];
         const float t = list.p[j];
         float l = (float)(TAIL ? (double)t * a.inv_tau - (double)teacher_lse : ((double)t - (double)max_t) * a.inv_tau);
-        if (id < 0 || t == -INFINITY) l = -INFINITY;
+        if (list.ids[j] < 0 || t == -INFINITY) l = -INFINITY;
         const float e = l == -INFINITY ? 0.0f : expf(l);
         list.log_p[j] = l;
         list.p[j] = e;
         z += e;
-        if (TAIL && id >= v0 && id < v1 && list.leads(j, twice)) {
-            const float x = list.x[j];
-            s.in.raise(exp_ref(x, a.scale));
-            s.in.sum += exp2_unit(__fmaf_rn(x, a.scale, -s.in.ref));
-        }
     }
-    s.sum_p = z = warp_reduce_sum(z);
-    if (TAIL) s.in.warp_reduce();
-    else if (z > 0.0f || z != z) {  // (a list of nothing but minus infinity has no mass)
-        const float log_z = logf(z);
-        for (int j = lane; j < a.top; j += 32) {
-            list.p[j] = list.p[j] / z;
-            list.log_p[j] -= log_z;
-        }
-        s.sum_p = z == z ? 1.0f : z;
+    z = warp_reduce_sum(z);
+    if (TAIL || !(z > 0.0f || z != z)) return z;  // (a list of nothing but minus infinity has no mass)
+    const float log_z = logf(z);
+    for (int j = lane; j < a.top; j += 32) {
+        list.p[j] = list.p[j] / z;
+        list.log_p[j] -= log_z;
     }
-    return s;
+    return z == z ? 1.0f : z;
+}
+
+// Sum of the exponentials of the list's words in v0..v1-1, each once (by one warp).
+__device__ __forceinline__ ExpSum distill_listed(const DistillArgs& a, const DistillList& list, int v0, int v1, bool twice)
+{
+    ExpSum in = ExpSum::none();
+    for (int j = threadIdx.x & 31; j < a.top; j += 32) {
+        if (list.ids[j] < v0 || list.ids[j] >= v1 || !list.leads(j, twice)) continue;
+        const float x = list.x[j];
+        in.raise(exp_ref(x, a.scale));
+        in.sum += exp2_unit(__fmaf_rn(x, a.scale, -in.ref));
+    }
+    in.warp_reduce();
+    return in;
 }
 
 // Bits of a group's elements in the map.
@@ -324,13 +323,19 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     const RowSplit& split = span.split;
     const int v0 = span.v0, v1 = span.v1;
     Walk walk;
-    walk.start(dynamic, threads, row, split, V, GRAD);
+    walk.start(dynamic, threads, row, split, V);
     if (tid == 0) s_any = s_twice = 0;
     if (BITS)
         for (int i = tid; i < distill_bits<T>(split.chunk1 - split.chunk0) / 16; i += threads)
             ((uint4*)list.bits)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    for (int j = tid; j < a.top; j += threads) {
+    // (the student's logits of the list stay in registers until behind the pass: nothing waits for them)
+    constexpr int OWN = LDA_TOP_MAX / 128;
+    float own[OWN] = {};
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int j = tid + i * threads;
+        if (j >= a.top) break;
         const int64_t at = r * a.list_stride + j;
         const int id = a.ids[at];
         const bool ok = id >= 0 && id < V;
@@ -342,7 +347,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
                 const int bit = id - span.bit0;
                 if (atomicOr(&list.bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
             }
-            list.x[j] = row_value(row[id]);
+            own[i] = row_value(row[id]);
         }
     }
     __syncthreads();
@@ -355,11 +360,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         return;
     }
     if (ctas > 1) cluster_arrive();
-    DistillSums sums{0.0f, ExpSum::none()};
-    if (warp == 0) {
-        sums = distill_list<TAIL>(a, list, teacher_lse, v0, v1, twice);
-        s_sum_p = sums.sum_p;
-    }
+    if (warp == 0) s_sum_p = distill_teacher<TAIL>(a, list, teacher_lse);
     ExpSum out = ExpSum::none();
     float m = -INFINITY;
     walk.each(row, split, V, none, [&](int chunk, int, uint4(&raw)[R]) {
@@ -368,18 +369,25 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         m = fmaxf(m, top);  // (a NaN goes into the sums)
         add_groups<T, R>(out, raw, top, a.scale);
     });
-    if (GRAD) walk.start(dynamic, threads, row, split, V, false);  // the second read is under way while the sums are put together
+    if (GRAD) walk.start(dynamic, threads, row, split, V);  // the second read is under way while the sums are put together
     out.warp_reduce();
     m = warp_reduce_max(m);
     if (lane == 0) ered[warp] = out, fred[warp] = m;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int j = tid + i * threads;
+        if (j < a.top) list.x[j] = own[i];
+    }
     __syncthreads();
+    ExpSum in = ExpSum::none();
     if (warp == 0) {
+        if (TAIL) in = distill_listed(a, list, v0, v1, twice);
         out = lane < warps ? ered[lane] : ExpSum::none();
         out.warp_reduce();
         m = warp_reduce_max(lane < warps ? fred[lane] : -INFINITY);
     }
     if (ctas > 1) cluster_wait();
-    if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = DistillPart{out, sums.in, m};
+    if (tid < ctas) *row_peer(cluster, &parts[0][rank], tid, ctas) = DistillPart{out, in, m};
     row_sync(cluster, ctas);
     m = parts[0][0].max;
     for (int k = 1; k < ctas; ++k) m = fmaxf(m, parts[0][k].max);
@@ -393,7 +401,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         if (lane == 0) fred[warp] = o;
         __syncthreads();
         if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
-        if (tid < ctas) *cluster.map_shared_rank(&parts[1][rank], tid) = DistillPart{{0.0f, o}, {0.0f, l}, m};
+        if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = DistillPart{{0.0f, o}, {0.0f, l}, m};
         row_sync(cluster, ctas);
     }
     if (!GRAD && (warp != 0 || rank != 0)) return;

@@ -168,7 +168,6 @@ struct ChunkWalk {
     static constexpr int BYTES = DEPTH * R * 16;  // per thread
     uint4* ring;
     int threads, warps;  // that walk together
-    unsigned long long policy;  // of L2
     // Chunk c (if the part has it) into the ring's slot; one group of copies, empty or not.
     __device__ __forceinline__ void fetch(const T* row, const RowSplit& split, int V, int c, int slot)
     {
@@ -181,8 +180,8 @@ struct ChunkWalk {
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 if (inside || group_inside<T>(mine + 32 * PER<T> * r, V))
-                    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to + r * (uint32_t)threads * 16),
-                                 "l"(from + 32 * PER<T> * r), "l"(policy)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * (uint32_t)threads * 16),
+                                 "l"(from + 32 * PER<T> * r)
                                  : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -194,19 +193,11 @@ struct ChunkWalk {
     }
     // Group r of a slot's chunk (the warp's groups of one r are consecutive).
     __device__ __forceinline__ uint4* place(int slot, int r) const { return ring + (slot * R + r) * threads; }
-    // again: what is read will be read once more, from L2.
-    __device__ __forceinline__ void start(void* shared, int threads_, const T* row, const RowSplit& split, int V, bool again)
+    __device__ __forceinline__ void start(void* shared, int threads_, const T* row, const RowSplit& split, int V)
     {
         ring = (uint4*)shared + threadIdx.x;
         threads = threads_;
         warps = threads / 32;
-        from(row, split, V, again);
-    }
-    // (the same place, another row)
-    __device__ __forceinline__ void from(const T* row, const RowSplit& split, int V, bool again)
-    {
-        if (again) asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
-        else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) fetch(row, split, V, split.chunk0 + (int)(threadIdx.x >> 5) + d * warps, d);
     }
@@ -293,7 +284,7 @@ struct ExpSum {
     // Of the warp; every lane has it.
     __device__ __forceinline__ void warp_reduce()
     {
-#pragma unroll
+#pragma unroll 1  // (small code: what runs once is fetched once, and small calls are bound by that)
         for (int o = 16; o > 0; o >>= 1) add(ExpSum{__shfl_xor_sync(0xffffffffu, ref, o), __shfl_xor_sync(0xffffffffu, sum, o)});
     }
 };
@@ -411,6 +402,13 @@ __device__ __forceinline__ uint4 pack(const float (&x)[PER<T>])
 // Barrier `id` of the CTA for `threads` of its threads (whole warps): waiting, and arriving without a wait.
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// `p`, a variable in shared memory, in the CTA `rank` of the cluster.
+template <typename P>
+__device__ __forceinline__ P* row_peer(cg::cluster_group& cluster, P* p, int rank, int ctas)
+{
+    return ctas > 1 ? cluster.map_shared_rank(p, rank) : p;
+}
 
 // Barrier of all threads that share a row.
 __device__ __forceinline__ void row_sync(cg::cluster_group& cluster, int ctas)

@@ -50,48 +50,56 @@ __device__ __forceinline__ unsigned long long top_entry(uint32_t key, int v)
     return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)v);
 }
 
-// Descending sort of list[0..n); list[n..) up to the next power of two is overwritten.
-__device__ __forceinline__ void top_sort(unsigned long long* list, int n)
+__device__ __forceinline__ void top_order(unsigned long long& x, unsigned long long& y, bool descending)
 {
-    const int tid = threadIdx.x, threads = blockDim.x;
-    int size = 32;
-    while (size < n) size *= 2;
-    if (size <= threads) {
-        // an entry per thread: partners up to 16 places away by shuffles, further ones through shared memory
-        unsigned long long x = tid < n ? list[tid] : 0ull;
-        for (int k = 2; k <= size; k *= 2)
-            for (int j = k / 2; j > 0; j /= 2) {
-                unsigned long long y;
-                if (j >= 32) {
-                    __syncthreads();
-                    if (tid < size) list[tid] = x;
-                    __syncthreads();
-                    y = tid < size ? list[tid ^ j] : 0ull;
-                } else {
-                    if (tid >= size) continue;  // (whole warps)
-                    y = __shfl_xor_sync(0xffffffffu, x, j);
+    const bool swap = (x < y) == descending;
+    const unsigned long long t = x;
+    x = swap ? y : x;
+    y = swap ? t : y;
+}
+
+// Sorts list[128 w .. 128 w + 127] for every w, descending, by a warp each, four places to a lane; places from n on become 0.
+constexpr int TOP_RUN = 128;
+__device__ __forceinline__ void top_sort_runs(unsigned long long* list, int n)
+{
+    const int lane = threadIdx.x & 31;
+    for (int run = threadIdx.x >> 5; run * TOP_RUN < n; run += blockDim.x >> 5) {
+        const int place = 4 * lane, at = run * TOP_RUN + place;
+        unsigned long long x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = at + e < n ? list[at + e] : 0ull;
+        top_order(x[0], x[1], true);
+        top_order(x[2], x[3], false);
+#pragma unroll 1
+        for (int k = 4; k <= TOP_RUN; k *= 2) {
+            const bool down = (place & k) == 0;  // descending runs where bit k of the place is 0
+#pragma unroll 1
+            for (int j = k / 2; j >= 4; j /= 2) {
+                const bool keep_large = down == ((place & j) == 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const unsigned long long y = __shfl_xor_sync(0xffffffffu, x[e], j / 4);
+                    x[e] = (x[e] > y) == keep_large ? x[e] : y;
                 }
-                // descending runs where bit k of the place is 0
-                const bool keep_large = ((tid & k) == 0) == ((tid & j) == 0);
-                x = (x > y) == keep_large ? x : y;
             }
-        __syncthreads();
-        if (tid < size) list[tid] = x;
-        __syncthreads();
-        return;
-    }
-    for (int i = n + tid; i < size; i += threads) list[i] = 0;
-    __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-#pragma unroll 2
-            for (int i = tid; i < size / 2; i += threads) {
-                const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-                const unsigned long long x = list[lo], y = list[hi];
-                if ((x < y) == ((lo & k) == 0)) list[lo] = y, list[hi] = x;
-            }
-            __syncthreads();
+            top_order(x[0], x[2], down);
+            top_order(x[1], x[3], down);
+            top_order(x[0], x[1], down);
+            top_order(x[2], x[3], down);
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) list[at + e] = x[e];
+    }
+}
+
+// How many entries of a sorted run are above x.
+__device__ __forceinline__ int top_above(const unsigned long long* run, unsigned long long x)
+{
+    int n = 0;
+#pragma unroll
+    for (int step = TOP_RUN / 2; step > 0; step /= 2)
+        if (run[n + step - 1] > x) n += step;
+    return n + (run[n] > x);
 }
 
 // For rows where the border leaves too many words (long ties): the border value by four passes that count bytes of the keys, then
@@ -188,49 +196,51 @@ __host__ __device__ constexpr int top_groups(int threads, int top)
     return n;
 }
 
-// By one warp: the largest half-key that at least `share` of the groups reach, or one that not many more do, and the same for `top` of
-// them: steps of doubling width down from the largest key, then halving; minus infinity's successor if there are not that many.
-struct TopBorders {
-    uint32_t share, alone;
-};
-__device__ __forceinline__ TopBorders top_borders(const uint16_t* tops, int values, int share, int top)
+// The largest half-key that at least `want` of the groups reach, or one that not many more do; minus infinity's successor if there are
+// not that many.  Every warp tries another one at a time: at first below `hi` (that fewer reach) by 64, 256, 1024, ..., then at equal
+// distances between what is too low and what is too high.
+__device__ __forceinline__ uint32_t top_border(const uint16_t* tops, int groups, int want, int spare, uint32_t hi, int (*counts)[ROW_THREADS / 32])
 {
-    const int lane = threadIdx.x & 31, per = values / 32;
-    uint32_t mine[TOP_VALUES / 32], best = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    uint32_t lo = TOP_LOWEST;
+    bool wide = true;
+    for (int round = 0; lo + 1 < hi; round ^= 1) {
+        const auto at = [&](int w) {
+            if (!wide) return lo + (hi - lo) * (w + 1) / (warps + 1);
+            const uint32_t below = 64u << (2 * min(w, 8));
+            return hi > lo + below ? hi - below : lo;
+        };
+        const uint32_t mid = at(warp);
+        int n = 0;
+#pragma unroll 1
+        for (int i = lane; i < groups / 8; i += 32) {
+            const uint4 eight = reinterpret_cast<const uint4*>(tops)[i];
+            const uint32_t two[4] = {eight.x, eight.y, eight.z, eight.w};
 #pragma unroll
-    for (int k = 0; k < TOP_VALUES / 32; k += 8)
-        if (k < per)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                mine[k + e] = tops[(k + e) * 32 + lane];
-                best = max(best, mine[k + e]);
-            }
-    best = __reduce_max_sync(0xffffffffu, best);
-    const auto border = [&](int want, uint32_t hi) {
-        uint32_t lo = TOP_LOWEST, step = 64;
-        while (lo + 1 < hi) {
-            const bool down = lo == TOP_LOWEST && hi > lo + step;
-            const uint32_t mid = down ? hi - step : (lo + hi) / 2;
-            step = down ? step * 2 : step;
-            int n = 0;
-#pragma unroll
-            for (int k = 0; k < TOP_VALUES / 32; k += 8)
-                if (k < per)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) n += mine[k + e] >= mid;
-            n = __reduce_add_sync(0xffffffffu, n);
-            if (n >= want) {
-                lo = mid;
-                if (n <= want + want / 4 + (share == top ? 16 : 2)) break;
-            } else
-                hi = mid;
+            for (int e = 0; e < 4; ++e) n += ((two[e] & 0xFFFFu) >= mid) + ((two[e] >> 16) >= mid);
         }
-        return lo;
-    };
-    TopBorders b;
-    b.share = border(share, best + 1);
-    b.alone = share == top ? b.share : border(top, b.share + 1);
-    return b;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if (lane == 0) counts[round][warp] = n;
+        __syncthreads();
+        uint32_t low = lo, high = hi;
+        int reach = 0;
+#pragma unroll 1
+        for (int w = 0; w < warps; ++w) {
+            const uint32_t k = at(w);
+            const int c = counts[round][w];
+            if (k <= lo) continue;
+            if (c >= want) {
+                if (k > low) low = k, reach = c;
+            } else
+                high = min(high, k);
+        }
+        if (low == lo && high == hi) wide = false;  // (can only be after a wide try)
+        lo = low;
+        hi = high;
+        wide = wide && lo == TOP_LOWEST;
+        if (reach && reach <= want + spare) break;
+    }
+    return lo;
 }
 
 // The words that reach the border, into `list` (n counts them, beyond its room too): the pieces that do are read again, a group of
@@ -315,16 +325,29 @@ __device__ __forceinline__ void top_finish(const TopArgs& a, int64_t r, const T*
                                            unsigned long long* list, TopCounts& sh, ExpSum sum, float m, bool far)
 {
     if (n > room) n = top_by_bytes<T>(row, a.V, a.top, sh, list);
-    top_sort(list, n);
+    top_sort_runs(list, n);
+    __syncthreads();
+    // an entry's place: its place in its run, and how many are above it in the others
     const int tid = threadIdx.x, threads = blockDim.x, want = min(n, a.top);
-    for (int i = tid; i < a.top; i += threads) {
-        const int64_t at = r * a.top + i;
-        const int v = i < want ? (int)(0xFFFFFFFFu - (uint32_t)list[i]) : -1;
-        a.ids[at] = v;
-        ((T*)a.values)[at] = v >= 0 ? row[v] : row_element<T>(-INFINITY);
+    for (int i = tid; i < n; i += threads) {
+        const unsigned long long x = list[i];
+        int place = i % TOP_RUN;
+        for (int at = 0; at < n; at += TOP_RUN)
+            if (at / TOP_RUN != i / TOP_RUN) place += top_above(list + at, x);
+        if (place >= want) continue;
+        const int v = (int)(0xFFFFFFFFu - (uint32_t)x);
+        a.ids[r * a.top + place] = v;
+        ((T*)a.values)[r * a.top + place] = row[v];
+        if (place == 0) sh.prefix = (uint32_t)(x >> 32);
     }
-    if (a.lse && tid == 0) {
-        const uint32_t first = want > 0 ? (uint32_t)(list[0] >> 32) : 0;
+    for (int i = want + tid; i < a.top; i += threads) {
+        a.ids[r * a.top + i] = -1;
+        ((T*)a.values)[r * a.top + i] = row_element<T>(-INFINITY);
+    }
+    if (!a.lse) return;
+    __syncthreads();
+    if (tid == 0) {
+        const uint32_t first = sh.prefix;
         // (log2 of the largest exponential: x c - R, or 0 when far)
         const double largest = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
         a.lse[r] = want == 0 ? -INFINITY
@@ -356,7 +379,7 @@ __device__ __noinline__ float top_far_sum(const T* row, const RowSplit& split, i
 struct TopPart {
     ExpSum sum;
     float max;
-    TopBorders borders;
+    uint32_t share, alone;  // borders
 };
 
 __host__ __device__ constexpr int top_ring_bytes(int threads) { return threads * TOP_DEPTH * TOP_GROUPS * 16; }
@@ -371,6 +394,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     __shared__ TopPart parts[2][ROW_CTAS];
     __shared__ ExpSum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
+    __shared__ int counts[2][ROW_THREADS / 32];
     __shared__ TopCounts sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -378,14 +402,14 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     const int room = top_room(a.top);
     const TopLists lists(dynamic, room);
     uint16_t* tops = (uint16_t*)(dynamic + max(top_ring_bytes(threads), TopLists::bytes(room)));
-    const int groups = top_groups(threads, a.top), share = groups / threads - 1;
+    const int groups = top_groups(threads, a.top), turns = groups / threads - 1;
     uint16_t* keys = tops + groups;
     const int64_t r = blockIdx.x / ctas;
     const T* row = (const T*)a.logits + r * a.stride;
     const RowSplit split = RowSplit::of<T, R>(row, V, rank, ctas);
     const int pieces = (split.chunk1 - split.chunk0) * 32 * PIECES;
     ChunkWalk<T, R, TOP_DEPTH> walk;
-    walk.start(dynamic, threads, row, split, V, true);
+    walk.start(dynamic, threads, row, split, V);
     if (ctas > 1) cluster_arrive();
     if (tid == 0) sh.n = sh.queued = 0;
     for (int g = tid; g < groups; g += threads) tops[g] = 0;  // (a thread's own)
@@ -393,28 +417,38 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     ExpSum sum = ExpSum::none();
     float m = -INFINITY;
     walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, int, uint4(&raw)[R]) {
-        top_chunk<T, FINE>(raw, keys + (c - split.chunk0) * 32 * PIECES + lane, tops + (turn++ & share) * threads + tid, a.scale, m, sum);
+        top_chunk<T, FINE>(raw, keys + (c - split.chunk0) * 32 * PIECES + lane, tops + (turn++ & turns) * threads + tid, a.scale, m, sum);
     });
     sum.warp_reduce();
     m = warp_reduce_max(m);
-    if (lane == 0) ered[warp] = sum, fred[warp] = m;
+    uint32_t best = 0;
+    for (int g = tid; g < groups; g += threads) best = max(best, (uint32_t)tops[g]);  // (its own)
+    best = __reduce_max_sync(0xffffffffu, best);
+    if (lane == 0) ered[warp] = sum, fred[warp] = m, counts[1][warp] = (int)best;
     __syncthreads();
-    TopBorders borders{0, 0};
+    best = __reduce_max_sync(0xffffffffu, lane < warps ? (uint32_t)counts[1][lane] : 0u);
+    // `top` groups of one part are enough, and so are its share of them in every part
+    const int part = (a.top + ctas - 1) / ctas;
+    uint32_t alone = 0, share = 0;
+#pragma unroll 1
+    for (int i = 0; i < (ctas > 1 ? 2 : 1); ++i) {
+        alone = top_border(tops, groups, i ? a.top : part, (i ? a.top : part) / 4 + 16 / ctas, (i ? share : best) + 1, counts);
+        if (i == 0) share = alone;
+        __syncthreads();
+    }
     if (warp == 0) {
         sum = lane < warps ? ered[lane] : ExpSum::none();
         sum.warp_reduce();
         m = warp_reduce_max(lane < warps ? fred[lane] : -INFINITY);
-        // `top` groups of one part are enough, and so are its share of them in every part
-        borders = top_borders(tops, groups, (a.top + ctas - 1) / ctas, a.top);
     }
     if (ctas > 1) cluster_wait();
-    if (tid < ctas) *cluster.map_shared_rank(&parts[0][rank], tid) = TopPart{sum, m, borders};
+    if (tid < ctas) *row_peer(cluster, &parts[0][rank], tid, ctas) = TopPart{sum, m, share, alone};
     row_sync(cluster, ctas);
     uint32_t border = 0, least = 0xFFFFFFFFu;
     m = -INFINITY;
     for (int k = 0; k < ctas; ++k) {
-        border = max(border, parts[0][k].borders.alone);
-        least = min(least, parts[0][k].borders.share);
+        border = max(border, parts[0][k].alone);
+        least = min(least, parts[0][k].share);
         m = fmaxf(m, parts[0][k].max);
     }
     border = max(border, least);
@@ -424,11 +458,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
         if (lane == 0) fred[warp] = o;
         __syncthreads();
         if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
-        if (tid < ctas) *cluster.map_shared_rank(&parts[1][rank], tid) = TopPart{{0.0f, o}, m, {0, 0}};
+        if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = TopPart{{0.0f, o}, m, 0, 0};
         row_sync(cluster, ctas);
     }
     top_collect<T, FINE>(row, split, V, keys, pieces, border, room, lists.queue, &sh.queued,
-                         cluster.map_shared_rank(lists.list, 0), cluster.map_shared_rank(&sh.n, 0));
+                         row_peer(cluster, lists.list, 0, ctas), row_peer(cluster, &sh.n, 0, ctas));
     row_sync(cluster, ctas);
     if (rank != 0) return;
     sum = parts[far][0].sum;

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
         unsigned long long own = 0;
         for (int c = tid; c < chunks; c += threads) own += sums[c];
         own = block_reduce_sum(own, red);
-        if (tid < ctas) *cluster.map_shared_rank(&parts[plain][rank], tid) = own;
+        if (tid < ctas) *row_peer(cluster, &parts[plain][rank], tid, ctas) = own;
         row_sync(cluster, ctas);
         unsigned long long total = 0, before = 0;
         for (int k = 0; k < ctas; ++k) {
@@ -169,18 +169,27 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
             before += all;
         }
         __syncthreads();
-        // a thread takes consecutive words
-        const int first = chunk_first<T, R>(split.chunk0 + s_chunk, split.pre);
+        // a thread takes consecutive words, all read before the first is looked at
+        const int each = CHUNK / threads;  // 8 at most
+        const int first = chunk_first<T, R>(split.chunk0 + s_chunk, split.pre) + tid * each;
         const unsigned long long looked_for = s_want;
-        unsigned long long start = 0;
-        for (int i = tid; i - tid < CHUNK; i += threads) {
-            const int v = first + i;
-            MassSum one{0, 0};
-            if (i < CHUNK && v >= 0 && v < V) one.add(part(v));
-            unsigned long long all;
-            const unsigned long long upto = start + block_scan_excl(one.value(), red, all);
-            if (upto <= looked_for && looked_for < upto + one.value()) s_token = v;
-            start += all;
+        float x[8];
+        MassSum mine{0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < each && first + i >= 0 && first + i < V ? part(first + i) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine.add(x[i]);
+        unsigned long long all, upto = block_scan_excl(mine.value(), red, all);
+        if (upto <= looked_for && looked_for < upto + mine.value()) {
+            int passed = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                MassSum one{0, 0};
+                one.add(x[i]);
+                upto += one.value();
+                passed += upto <= looked_for;
+            }
+            s_token = first + passed;
         }
         __syncthreads();
         token = s_token;

@@ -77,9 +77,9 @@ def top_logits(logits, top: int, temperature: float = 1.0):
     code, rows, V, stride = _rows(logits, "logits")
     if not 1 <= top <= _b.LDA_TOP_MAX:
         raise ValueError(f"top: 1 to {_b.LDA_TOP_MAX}, not {top}")
-    ids = torch.empty((rows, top), dtype=torch.int32, device=device)
-    values = torch.empty((rows, top), dtype=logits.dtype, device=device)
-    lse = torch.empty(rows, dtype=torch.float32, device=device)
+    values = logits.new_empty((rows, top))
+    ids = logits.new_empty((rows, top), dtype=torch.int32)
+    lse = logits.new_empty(rows, dtype=torch.float32)
     _call("lda_top_logits", device, logits.data_ptr(), code, rows, V, stride, top, temperature, ids.data_ptr(),
           values.data_ptr(), lse.data_ptr())
     return ids, values, lse
@@ -128,7 +128,7 @@ def _loss(logits, ids, values, lse, temperature):
     device = _cuda(logits, "logits")
     code, rows, V, stride = _rows(logits, "logits")
     lists = _list(ids, values, lse, rows, device)
-    loss = torch.empty(rows, dtype=torch.float32, device=device)
+    loss = logits.new_empty(rows, dtype=torch.float32)
     _call("lda_distill_loss", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, loss.data_ptr())
     return loss
 
@@ -168,8 +168,8 @@ def distill_loss_and_grad(logits, ids, values, lse=None, temperature: float = 1.
     if logits.requires_grad:
         logits = logits.detach()
     if grad is None:
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+        grad = logits.new_empty(logits.shape)
+    loss = logits.new_empty(logits.shape[:1], dtype=torch.float32)
     _grad(logits, ids, values, lse, temperature, weights, loss, grad)
     return loss, grad
 
