@@ -32,7 +32,7 @@ struct DistillArgs {
 };
 
 constexpr int DISTILL_GROUPS = 4;  // groups of a lane in a chunk
-__host__ __device__ constexpr int distill_depth(bool grad) { return grad ? 2 : 3; }  // chunks on their way
+__host__ __device__ constexpr int distill_depth(bool grad) { return grad ? 3 : 4; }  // chunks on their way
 
 // What a CTA knows of its part of the row.
 struct DistillPart {
@@ -322,6 +322,19 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     const DistillSpan<T> span(row, V, rank, ctas);
     const RowSplit& split = span.split;
     const int v0 = span.v0, v1 = span.v1;
+    // The list's reads go ahead of the row's, which would hold them up for as long as it takes to fill the rings of all CTAs.  (The
+    // student's logits of the list stay in registers until behind the pass: nothing waits for them.)
+    constexpr int OWN = LDA_TOP_MAX / 128;  // places of the list per thread
+    int id[OWN];
+    float t[OWN];
+    T own[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int j = tid + i * threads;
+        const int64_t at = r * a.list_stride + j;
+        id[i] = j < a.top ? a.ids[at] : -1;
+        t[i] = j < a.top ? any_value(a.values, a.values_dtype, at) : 0.0f;
+    }
     Walk walk;
     walk.start(dynamic, threads, row, split, V);
     if (tid == 0) s_any = s_twice = 0;
@@ -329,25 +342,21 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         for (int i = tid; i < distill_bits<T>(split.chunk1 - split.chunk0) / 16; i += threads)
             ((uint4*)list.bits)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    // (the student's logits of the list stay in registers until behind the pass: nothing waits for them)
-    constexpr int OWN = LDA_TOP_MAX / 128;
-    float own[OWN] = {};
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
         const int j = tid + i * threads;
         if (j >= a.top) break;
-        const int64_t at = r * a.list_stride + j;
-        const int id = a.ids[at];
-        const bool ok = id >= 0 && id < V;
-        list.p[j] = any_value(a.values, a.values_dtype, at);
-        list.ids[j] = ok ? id : -1;
+        const bool ok = id[i] >= 0 && id[i] < V;
+        if (!ok) id[i] = -1;
+        list.p[j] = t[i];
+        list.ids[j] = id[i];
         if (ok) {
             s_any = 1;
-            if (BITS && id >= v0 && id < v1) {
-                const int bit = id - span.bit0;
+            if (BITS && id[i] >= v0 && id[i] < v1) {
+                const int bit = id[i] - span.bit0;
                 if (atomicOr(&list.bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1) s_twice = 1;
             }
-            own[i] = row_value(row[id]);
+            own[i] = row[id[i]];
         }
     }
     __syncthreads();
@@ -376,7 +385,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
         const int j = tid + i * threads;
-        if (j < a.top) list.x[j] = own[i];
+        if (j < a.top) list.x[j] = id[i] >= 0 ? row_value(own[i]) : 0.0f;
     }
     __syncthreads();
     ExpSum in = ExpSum::none();
@@ -434,9 +443,12 @@ static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t 
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
     const size_t smem = shape.threads * distill_depth(grad) * DISTILL_GROUPS * 16 +
                         DistillList::bytes(a.top, tail || grad ? distill_bits<T>((chunks + shape.ctas - 1) / shape.ctas) : 0);
-    const auto kernel = tail ? (grad ? k_distill<T, true, true> : k_distill<T, true, false>)
-                             : (grad ? k_distill<T, false, true> : k_distill<T, false, false>);
-    return launch_rows(kernel, a, rows, shape, smem, 2 * 1024, st);
+    constexpr size_t fixed = 2 * 1024;
+    if (tail)
+        return grad ? launch_rows<k_distill<T, true, true>>(a, rows, shape, smem, fixed, st)
+                    : launch_rows<k_distill<T, true, false>>(a, rows, shape, smem, fixed, st);
+    return grad ? launch_rows<k_distill<T, false, true>>(a, rows, shape, smem, fixed, st)
+                : launch_rows<k_distill<T, false, false>>(a, rows, shape, smem, fixed, st);
 }
 
 static int distill(const DistillArgs& a, int dtype, int64_t rows, void* stream)

@@ -8,6 +8,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "../../include/lda_b200.h"
@@ -417,10 +418,10 @@ __device__ __forceinline__ void row_sync(cg::cluster_group& cluster, int ctas)
     else __syncthreads();
 }
 
-// Launches a cluster of CTAs for every row; `smem`: dynamic shared memory, `fixed`: what the kernel has besides, about.
-template <typename Args>
-inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t rows, RowShape shape, size_t smem,
-                               size_t fixed, cudaStream_t st)
+// Launches a cluster of CTAs for every row; `smem`: dynamic shared memory, `fixed`: what the kernel has besides, about.  The
+// allowance for more than 48 KB is asked for once per kernel and device, as large as it can be (a call costs a microsecond).
+template <auto Kernel, typename Args>
+inline cudaError_t launch_rows(const Args& args, int64_t rows, RowShape shape, size_t smem, size_t fixed, cudaStream_t st)
 {
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)(rows * shape.ctas));
@@ -432,12 +433,22 @@ inline cudaError_t launch_rows(void (*kernel)(Args), const Args& args, int64_t r
     at.val.clusterDim.x = (unsigned)shape.ctas;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     c.attrs = &at;
-    c.numAttrs = 1;
+    c.numAttrs = shape.ctas > 1 ? 1 : 0;
     if (smem + fixed > 46 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        static std::atomic<bool> allowed[64];
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
+        if (dev >= 64 || !allowed[dev].load(std::memory_order_acquire)) {
+            cudaFuncAttributes f;
+            e = cudaFuncGetAttributes(&f, Kernel);
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)f.sharedSizeBytes);
+            if (e != cudaSuccess) return e;
+            if (dev < 64) allowed[dev].store(true, std::memory_order_release);
+        }
     }
-    return cudaLaunchKernelEx(&c, kernel, args);
+    return cudaLaunchKernelEx(&c, Kernel, args);
 }
 
 // Sizes that every one of the operators refuses.

@@ -20,10 +20,7 @@ struct TopArgs {
 };
 
 constexpr int TOP_GROUPS = 4;     // groups of a lane in a chunk
-#ifndef TD
-#define TD 2
-#endif
-constexpr int TOP_DEPTH = TD;      // chunks on their way
+constexpr int TOP_DEPTH = 2;      // chunks on their way
 constexpr int TOP_VALUES = 1024;  // groups of pieces whose largest keys give the border, at most
 constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
 // Words and pieces that may be left for lists of `top`: about four times what is expected.
@@ -202,11 +199,13 @@ __host__ __device__ constexpr int top_groups(int threads, int top)
 __device__ __forceinline__ uint32_t top_border(const uint16_t* tops, int groups, int want, int spare, uint32_t hi, int (*counts)[ROW_THREADS / 32])
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const float share = 1.0f / (float)(warps + 1);
     uint32_t lo = TOP_LOWEST;
     bool wide = true;
     for (int round = 0; lo + 1 < hi; round ^= 1) {
         const auto at = [&](int w) {
-            if (!wide) return lo + (hi - lo) * (w + 1) / (warps + 1);
+            // (rounded down: above lo for the last of them, below hi for all)
+            if (!wide) return lo + (uint32_t)((float)(hi - lo) * (float)(w + 1) * share);
             const uint32_t below = 64u << (2 * min(w, 8));
             return hi > lo + below ? hi - below : lo;
         };
@@ -222,23 +221,18 @@ __device__ __forceinline__ uint32_t top_border(const uint16_t* tops, int groups,
         n = __reduce_add_sync(0xffffffffu, n);
         if (lane == 0) counts[round][warp] = n;
         __syncthreads();
-        uint32_t low = lo, high = hi;
-        int reach = 0;
-#pragma unroll 1
-        for (int w = 0; w < warps; ++w) {
-            const uint32_t k = at(w);
-            const int c = counts[round][w];
-            if (k <= lo) continue;
-            if (c >= want) {
-                if (k > low) low = k, reach = c;
-            } else
-                high = min(high, k);
+        // lane w looks at warp w's: the highest that enough reach (with their number), the lowest that too few do
+        const uint32_t k = at(lane);
+        const bool tried = lane < warps && k > lo;
+        const int c = tried ? counts[round][lane] : 0;
+        const uint32_t reached = __reduce_max_sync(0xffffffffu, tried && c >= want ? k << 11 | (uint32_t)c : 0u);
+        const uint32_t missed = __reduce_min_sync(0xffffffffu, tried && c < want ? k : hi);
+        if (wide && (reached || missed == hi)) wide = false;
+        hi = missed;
+        if (reached) {
+            lo = reached >> 11;
+            if ((int)(reached & 2047) <= want + spare) break;
         }
-        if (low == lo && high == hi) wide = false;  // (can only be after a wide try)
-        lo = low;
-        hi = high;
-        wide = wide && lo == TOP_LOWEST;
-        if (reach && reach <= want + spare) break;
     }
     return lo;
 }
@@ -478,18 +472,11 @@ static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
     const int per = a.V / PER<T>, room = top_room(a.top);
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
     const auto pieces = [&](int ctas, bool fine) { return (chunks + ctas - 1) / ctas * 32 * (fine ? TOP_GROUPS : 1); };
-#ifdef FORCE_T
-    const RowShape shape = rows > 700 ? RowShape{1, FORCE_T} : row_shape(rows, row_bytes, 1024, 64);
-#else
     const RowShape shape = row_shape(rows, row_bytes, 1024, 64);
-#endif
-#ifdef FINE_K
-    const bool fine = a.top > FINE_K || per / TOP_GROUPS / shape.ctas < 4 * a.top;
-#else
     const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
-#endif
     const size_t smem = std::max(top_ring_bytes(shape.threads), TopLists::bytes(room)) + 2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
-    return launch_rows(fine ? k_top<T, true> : k_top<T, false>, a, rows, shape, smem, sizeof(TopCounts) + 1024, st);
+    return fine ? launch_rows<k_top<T, true>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st)
+                : launch_rows<k_top<T, false>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st);
 }
 
 }  // namespace lda

@@ -204,7 +204,8 @@ template <typename T>
 static cudaError_t run_verify(const VerifyArgs& a, int64_t n_seqs, cudaStream_t st)
 {
     const RowShape shape = row_shape(n_seqs, (int64_t)a.V * sizeof(T), 1024, 64);
-    return launch_rows(a.probs ? k_verify<T, true> : k_verify<T, false>, a, n_seqs, shape, 0, 17 * 1024, st);
+    return a.probs ? launch_rows<k_verify<T, true>>(a, n_seqs, shape, 0, 17 * 1024, st)
+                   : launch_rows<k_verify<T, false>>(a, n_seqs, shape, 0, 17 * 1024, st);
 }
 
 }  // namespace lda

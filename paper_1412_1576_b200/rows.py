@@ -31,14 +31,14 @@ def _rows(x, name):
 
 def _vector(x, name, dtype, n, device):
     """Checks a contiguous vector; returns its address."""
+    if x.dtype is dtype and x.shape == (n,) and x.device == device and x.is_contiguous():
+        return x.data_ptr()
     if x.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {x.dtype}")
     if x.shape != (n,):
         raise ValueError(f"{name}: {n} values are needed, not {tuple(x.shape)}")
-    if not x.is_contiguous():
-        raise ValueError(f"{name}: must be contiguous")
     _here(x, name, device)
-    return x.data_ptr()
+    raise ValueError(f"{name}: must be contiguous")
 
 
 def _here(x, name, device):
@@ -87,25 +87,28 @@ def top_logits(logits, top: int, temperature: float = 1.0):
 
 def _list(ids, values, lse, rows, device):
     """Checks a teacher's lists; returns the library's arguments for them."""
-    if ids.dtype != torch.int32:
-        raise TypeError(f"ids: int32 is needed, not {ids.dtype}")
     code = _DTYPES.get(values.dtype)
+    shape = ids.shape
+    if ids.dtype is not torch.int32:
+        raise TypeError(f"ids: int32 is needed, not {ids.dtype}")
     if code is None:
         raise TypeError(f"values: float32, float16 or bfloat16 is needed, not {values.dtype}")
-    if ids.dim() != 2 or ids.shape[0] != rows or ids.shape != values.shape:
-        raise ValueError(f"ids and values: one list per row, {rows} of them, not {tuple(ids.shape)} and {tuple(values.shape)}")
-    top = ids.shape[1]
+    if len(shape) != 2 or shape[0] != rows or shape != values.shape:
+        raise ValueError(f"ids and values: one list per row, {rows} of them, not {tuple(shape)} and {tuple(values.shape)}")
+    top = shape[1]
     if not 1 <= top <= _b.LDA_TOP_MAX:
         raise ValueError(f"ids: lists of 1 to {_b.LDA_TOP_MAX} words, not {top}")
-    (between, step), (values_between, values_step) = ids.stride(), values.stride()
-    if top > 1 and (step != 1 or values_step != 1):
-        raise ValueError("ids and values: the places of a list must be consecutive in memory")
-    if rows > 1 and between != values_between:
-        raise ValueError("ids and values: their rows must lie equally far apart")
-    _here(ids, "ids", device)
-    _here(values, "values", device)
+    between = ids.stride()
+    if between != values.stride() or between[1] != 1:
+        if top > 1 and (between[1] != 1 or values.stride(1) != 1):
+            raise ValueError("ids and values: the places of a list must be consecutive in memory")
+        if rows > 1 and between[0] != values.stride(0):
+            raise ValueError("ids and values: their rows must lie equally far apart")
+    if ids.device != device or values.device != device:
+        _here(ids, "ids", device)
+        _here(values, "values", device)
     teacher_lse = None if lse is None else _vector(lse, "lse", torch.float32, rows, device)
-    return ids.data_ptr(), values.data_ptr(), code, top, between if rows > 1 else top, teacher_lse
+    return ids.data_ptr(), values.data_ptr(), code, top, between[0] if rows > 1 else top, teacher_lse
 
 
 class _Distill(torch.autograd.Function):

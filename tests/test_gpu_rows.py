@@ -96,6 +96,23 @@ def test_top_logits_of_few_and_of_many_rows(n_rows):
     check_top(make(n_rows, 3_001, BF16, n_rows), 16, tau=0.7)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_many_rows_of_the_longest_vocabulary(dtype):
+    """Enough rows for one CTA each: its share of the row is the largest there is."""
+    V, n = 1 << 20, 1300
+    one = make(1, V, dtype, 77)
+    x = one.expand(n, V)
+    ids, values, lse = rows.top_logits(x, 512)
+    want = top_reference(one.cpu(), 512, 1.0)
+    assert torch.equal(ids.cpu(), want[0].expand(n, 512)) and torch.equal(values.cpu(), want[1].expand(n, 512))
+    assert bool((lse == lse[0]).all()) and abs(float(lse[0]) - float(want[2])) <= float(lse_error(one.cpu().double(), 1.0)) + 2.0**-20
+    ids, values, teacher = lists_of(make(1, V, dtype, 78).cpu(), 512, 1.0, True, dtype)
+    loss = rows.distill_loss(x, ids.expand(n, 512), values.expand(n, 512), teacher.repeat(n))
+    want, tol, _, _ = distill_reference(one.cpu(), ids.cpu(), values.cpu(), teacher.cpu(), 1.0, torch.ones(1))
+    assert bool((loss == loss[0]).all())
+    same(loss[:1], want, tol, F32)
+
+
 def special_rows(dtype):
     """Rows where a selection can go wrong, V = 20 000."""
     V = 20_000
