@@ -672,6 +672,8 @@ def test_tensors_that_do_not_fit_are_refused():
         rows.distill_loss_and_grad(x, ids, values, lse, grad=torch.empty_like(x, dtype=BF16))
     with pytest.raises(ValueError):
         rows.distill_loss_and_grad(x, ids, values, lse, weights=torch.ones(2, device="cuda"))
+    with pytest.raises(ValueError):
+        rows.distill_loss_and_grad(x, ids, values, lse, grad=torch.empty_like(x).requires_grad_())
     with pytest.raises(b.LdaError):
         rows.distill_loss_and_grad(x, ids, values, lse, grad=torch.empty(50, device="cuda").expand(3, 50))
     offsets, drafts, p, q, au, du = drafts_of([2, 1], 50, F32, 1)
