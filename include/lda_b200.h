@@ -296,7 +296,8 @@ int lda_dense_table_noalloc(const int32_t* n_k_dev, int32_t K, int32_t V, double
  *   V        1 .. LDA_ROW_MAX_V words per row, consecutive in memory
  *   stride   elements from one row to the next, 0 .. 2^31 (0: the same row again); rows that are written need >= V
  *
- * LDA_EINVAL: NULL where a pointer is needed, unknown dtype, negative size, a misaligned row, a temperature outside [1e-6, 1e6];
+ * LDA_EINVAL: NULL where a pointer is needed, unknown dtype, negative size, a pointer that is not a multiple of its elements' size,
+ * a temperature outside [1e-6, 1e6];
  * LDA_ERANGE: sizes beyond the limits; LDA_ECUDA: the launch failed.  The contents of DEVICE memory are not looked at by the
  * call; the kernels read and write nothing outside the rows and lists that the arguments describe, whatever ids and offsets hold. */
 #define LDA_F32 0

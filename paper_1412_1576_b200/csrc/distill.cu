@@ -80,10 +80,11 @@ __host__ __device__ constexpr int distill_bits(int chunks) { return chunks * (32
 
 // The teacher's probabilities (by one warp): p and log_p from the logits in p; returns the sum of p.
 template <bool TAIL>
-__device__ __forceinline__ float distill_teacher(const DistillArgs& a, const DistillList& list, float teacher_lse)
+__device__ __forceinline__ double distill_teacher(const DistillArgs& a, const DistillList& list, float teacher_lse)
 {
     const int lane = threadIdx.x & 31;
-    float max_t = -INFINITY, z = 0.0f;
+    float max_t = -INFINITY;
+    double z = 0;
     if (!TAIL) {
         for (int j = lane; j < a.top; j += 32)
             if (list.ids[j] >= 0) max_t = fmaxf(max_t, list.p[j]);
@@ -96,16 +97,16 @@ __device__ __forceinline__ float distill_teacher(const DistillArgs& a, const Dis
         const float e = l == -INFINITY ? 0.0f : expf(l);
         list.log_p[j] = l;
         list.p[j] = e;
-        z += e;
+        z += (double)e;
     }
     z = warp_reduce_sum(z);
-    if (TAIL || !(z > 0.0f || z != z)) return z;  // (a list of nothing but minus infinity has no mass)
-    const float log_z = logf(z);
+    if (TAIL || !(z > 0 || z != z)) return z;  // (a list of nothing but minus infinity has no mass)
+    const float log_z = logf((float)z), all = (float)z;
     for (int j = lane; j < a.top; j += 32) {
-        list.p[j] = list.p[j] / z;
+        list.p[j] = list.p[j] / all;
         list.log_p[j] -= log_z;
     }
-    return z == z ? 1.0f : z;
+    return z == z ? 1.0 : z;
 }
 
 // Sum of the exponentials of the list's words in v0..v1-1, each once (by one warp).
@@ -130,14 +131,16 @@ __device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
     return PER<T> == 8 ? byte : (byte >> (group * PER<T> % 8)) & ((1u << PER<T>) - 1);
 }
 
-// Minus infinity in the list's places of a lane's groups; `group`: the first one's number in the part.
+// Minus infinity in the list's places of a lane's groups; `group`: the first one's number in the part.  Returns whether there are any.
 template <typename T>
-__device__ __forceinline__ void distill_mask(uint4 (&raw)[DISTILL_GROUPS], const uint32_t* bits, int group)
+__device__ __forceinline__ bool distill_mask(uint4 (&raw)[DISTILL_GROUPS], const uint32_t* bits, int group)
 {
+    bool any = false;
 #pragma unroll
     for (int k = 0; k < DISTILL_GROUPS; ++k) {
         const uint32_t marked = group_bits<T>(bits, group + 32 * k);
         if (marked) {
+            any = true;
             union {
                 uint4 raw;
                 T e[PER<T>];
@@ -149,6 +152,7 @@ __device__ __forceinline__ void distill_mask(uint4 (&raw)[DISTILL_GROUPS], const
             raw[k] = u.raw;
         }
     }
+    return any;
 }
 
 // Sum of 2^((x - m) c) over a warp's chunks of the part, the list's words left out (TAIL).
@@ -173,42 +177,45 @@ __device__ __noinline__ float distill_far_sum(const T* row, const RowSplit& spli
 
 // The row's sums from its parts: exponentials 2^(x c - ref), or 2^((x - max) c) where `far`.
 struct DistillRow {
-    ExpSum out;
-    float max, ref, total, sum_p, p_rest;
+    ExpSum out, in;
+    float max, ref;
+    float sum_p, p_rest;
     bool far;
     template <bool TAIL>
-    static __device__ __forceinline__ DistillRow of(const DistillPart* parts, int ctas, float max, bool far, float sum_p)
+    static __device__ __forceinline__ DistillRow of(const DistillPart* parts, int ctas, float max, bool far, float sum_p, float p_rest)
     {
         DistillRow w;
         w.max = max;
         w.far = far;
         w.sum_p = sum_p;
         w.out = parts[0].out;
-        ExpSum in = parts[0].in;
+        w.in = parts[0].in;
         for (int k = 1; k < ctas; ++k) {
             w.out.add(parts[k].out);
-            in.add(parts[k].in);
+            w.in.add(parts[k].in);
         }
-        w.ref = fmaxf(w.out.ref, in.ref);
-        w.total = w.out.sum * exp2_whole(w.out.ref - w.ref) + in.sum * exp2_whole(in.ref - w.ref);
-        w.p_rest = TAIL && w.out.sum != 0.0f ? (sum_p != sum_p ? sum_p : fmaxf(0.0f, 1.0f - sum_p)) : 0.0f;
+        w.ref = fmaxf(w.out.ref, w.in.ref);
+        w.p_rest = TAIL && w.out.sum != 0.0f ? p_rest : 0.0f;
         return w;
     }
     __device__ __forceinline__ float exponent(float x, float c, float r) const { return far ? (x - max) * c : __fmaf_rn(x, c, -r); }
-    // The row's loss, by one warp.
-    __device__ __forceinline__ float loss(const DistillArgs& a, const DistillList& list) const
+    // The row's loss, by one warp, in 64 bits: it is a small difference of large logarithms where the student is near the teacher
+    // (in single precision 1e-4 of a loss of 0.03, at 2 units of the last place of a logarithm of 17), and a listed word at the
+    // type's lowest value has a finite log q.
+    __device__ __forceinline__ float loss(const DistillArgs& a, const DistillList& list, double p_rest_exact) const
     {
-        const float log2_total = total == 0.0f ? 0.0f : log2f(total);  // (without mass log q is minus infinity)
-        double l = 0;  // (64 bits: a listed word at the type's lowest value has a finite log q)
+        const double s_out = ldexp((double)out.sum, (int)(out.ref - ref)), total = s_out + ldexp((double)in.sum, (int)(in.ref - ref));
+        const double log_total = total == 0 ? 0.0 : log(total);  // (without mass log q is minus infinity)
+        double l = 0;
         for (int j = threadIdx.x & 31; j < a.top; j += 32) {
             const float p = list.p[j];
             if (p > 0.0f || p != p) {
                 const double x = (double)list.x[j], y = far ? (x - (double)max) * (double)a.scale : x * (double)a.scale - (double)ref;
-                l += (double)p * ((double)list.log_p[j] - (y - (double)log2_total) * LN2);
+                l += (double)p * ((double)list.log_p[j] - (y * LN2 - log_total));
             }
         }
         l = warp_reduce_sum(l);
-        if (p_rest != 0.0f) l += (double)(p_rest * (logf(p_rest) - (out.ref - ref + log2f(out.sum) - log2_total) * (float)LN2));
+        if (p_rest != 0.0f) l += p_rest_exact * log(p_rest_exact * (total / s_out));
         return (float)(l * a.tau * a.tau);
     }
 };
@@ -220,13 +227,15 @@ struct DistillFactors {
     {
         w = (float)((double)weight * tau);
         list_ref = ref = row.ref;
-        listed = row.total == 0.0f ? 0.0f : (row.sum_p + row.p_rest) / row.total;
-        const float gap = row.out.ref - row.ref;
-        others = w * (row.p_rest != 0.0f ? listed - row.p_rest / (row.out.sum * exp2_whole(gap)) : listed);
+        const float gap = row.out.ref - row.ref, s_out = row.out.sum * exp2_whole(gap);
+        const float s_in = row.in.sum * exp2_whole(row.in.ref - row.ref), total = s_out + s_in, p_rest = row.p_rest;
+        listed = total == 0.0f ? 0.0f : (row.sum_p + p_rest) / total;
+        // W / total - P / s_out, without the part that is in both
+        others = w * (p_rest != 0.0f ? (row.sum_p * s_out - p_rest * s_in) / s_out / total : listed);
         if (gap < -100.0f) {
             // less than 2^-80 of the student's mass is outside the list: it counts for the bucket alone, on a scale of its own
             ref = row.out.ref;
-            others = row.p_rest != 0.0f ? -w * row.p_rest / row.out.sum : 0.0f;
+            others = p_rest != 0.0f ? -w * p_rest / row.out.sum : 0.0f;
         }
         if (weight == 0.0f) others = 0.0f;
     }
@@ -308,7 +317,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     __shared__ ExpSum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ DistillPart parts[2][ROW_CTAS];
-    __shared__ float s_sum_p;
+    __shared__ double s_rest;
+    __shared__ float s_sum_p, s_p_rest;
     __shared__ int s_any, s_twice;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -369,13 +379,16 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         return;
     }
     if (ctas > 1) cluster_arrive();
-    if (warp == 0) s_sum_p = distill_teacher<TAIL>(a, list, teacher_lse);
+    if (warp == 0) {
+        const double sum_p = distill_teacher<TAIL>(a, list, teacher_lse), rest = sum_p != sum_p ? sum_p : fmax(0.0, 1.0 - sum_p);
+        if (lane == 0) s_rest = rest, s_sum_p = (float)sum_p, s_p_rest = (float)rest;
+    }
     ExpSum out = ExpSum::none();
     float m = -INFINITY;
     walk.each(row, split, V, none, [&](int chunk, int, uint4(&raw)[R]) {
-        const float top = groups_max<T, R>(raw);
-        if (TAIL) distill_mask<T>(raw, list.bits, (chunk - split.chunk0) * 32 * R + lane);
+        float top = groups_max<T, R>(raw);
         m = fmaxf(m, top);  // (a NaN goes into the sums)
+        if (TAIL && distill_mask<T>(raw, list.bits, (chunk - split.chunk0) * 32 * R + lane)) top = groups_max<T, R>(raw);
         add_groups<T, R>(out, raw, top, a.scale);
     });
     if (GRAD) walk.start(dynamic, threads, row, split, V);  // the second read is under way while the sums are put together
@@ -414,9 +427,9 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         row_sync(cluster, ctas);
     }
     if (!GRAD && (warp != 0 || rank != 0)) return;
-    const DistillRow whole = DistillRow::of<TAIL>(parts[far], ctas, m, far, s_sum_p);
+    const DistillRow whole = DistillRow::of<TAIL>(parts[far], ctas, m, far, s_sum_p, s_p_rest);
     if (a.loss && rank == 0 && warp == 0) {
-        const float l = whole.loss(a, list);
+        const float l = whole.loss(a, list, s_rest);
         if (lane == 0) a.loss[r] = l;
     }
     if (!GRAD) return;
@@ -460,7 +473,8 @@ static int distill(const DistillArgs& a, int dtype, int64_t rows, void* stream)
     if (a.top < 1 || a.list_stride < 0 || !temperature_ok(a.tau)) return LDA_EINVAL;
     if (a.top > LDA_TOP_MAX || a.list_stride > (1ll << 31)) return LDA_ERANGE;
     if (rows == 0) return LDA_OK;
-    if (!a.ids || !a.values || (uintptr_t)a.values % (values_dtype == LDA_F32 ? 4 : 2)) return LDA_EINVAL;
+    if (!a.ids || !a.values || !aligned(a.ids, 4) || !aligned(a.values, values_dtype == LDA_F32 ? 4 : 2)) return LDA_EINVAL;
+    if (!aligned(a.teacher_lse, 4) || !aligned(a.weights, 4) || !aligned(a.loss, 4)) return LDA_EINVAL;
     cudaStream_t st = (cudaStream_t)stream;
     const cudaError_t e = dtype == LDA_F32 ? run_distill<float>(a, rows, st)
                           : dtype == LDA_F16 ? run_distill<__half>(a, rows, st)

@@ -1,5 +1,5 @@
 // Shared pieces of the operators on rows of logits or probabilities (toplogits.cu, distill.cu, verify.cu): element types,
-// 2^x, keys that order values, reductions over a CTA.
+// 2^x, keys that order values, a row split over CTAs and walked over, sums of exponentials, launches.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -21,7 +21,6 @@ namespace cg = cooperative_groups;
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr double LN2 = 0.69314718055994531;
 
 __device__ __forceinline__ float row_value(float x) { return x; }
@@ -67,17 +66,6 @@ __device__ __forceinline__ float warp_reduce_max(float v)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
-}
-
-// Block-wide maximum; `smem` holds at least 32 floats; result returned to every thread.
-__device__ __forceinline__ float block_reduce_max(float v, float* smem)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
-    v = warp_reduce_max(v);
-    __syncthreads();
-    if (lane == 0) smem[warp] = v;
-    __syncthreads();
-    return warp_reduce_max(lane < nw ? smem[lane] : -INFINITY);
 }
 
 // --- a row in 16-byte groups, split over the CTAs of a cluster -------------------------------------------------------------------
@@ -400,10 +388,6 @@ __device__ __forceinline__ uint4 pack(const float (&x)[PER<T>])
     }
 }
 
-// Barrier `id` of the CTA for `threads` of its threads (whole warps): waiting, and arriving without a wait.
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
 // `p`, a variable in shared memory, in the CTA `rank` of the cluster.
 template <typename P>
 __device__ __forceinline__ P* row_peer(cg::cluster_group& cluster, P* p, int rank, int ctas)
@@ -462,6 +446,9 @@ inline int check_rows(const void* p, int dtype, int64_t rows, int32_t V, int64_t
     if (rows > 0 && (!p || (uintptr_t)p % (dtype == LDA_F32 ? 4 : 2))) return LDA_EINVAL;
     return LDA_OK;
 }
+
+// Whether an address is a multiple of n (NULL is).
+inline bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 // Temperatures at which 1 / tau and log2(e) / tau are ordinary single-precision values.
 inline bool temperature_ok(double tau) { return tau >= 1e-6 && tau <= 1e6; }

@@ -20,7 +20,7 @@ struct TopArgs {
 };
 
 constexpr int TOP_GROUPS = 4;     // groups of a lane in a chunk
-constexpr int TOP_DEPTH = 2;      // chunks on their way
+constexpr int TOP_DEPTH = 2;      // chunks on their way (three: the same time)
 constexpr int TOP_VALUES = 1024;  // groups of pieces whose largest keys give the border, at most
 constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
 // Words and pieces that may be left for lists of `top`: about four times what is expected.
@@ -491,7 +491,8 @@ static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
     const auto pieces = [&](int ctas, bool fine) { return (chunks + ctas - 1) / ctas * 32 * (fine ? TOP_GROUPS : 1); };
     const RowShape shape = row_shape(rows, row_bytes, 1024, 64);
     const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
-    const size_t smem = std::max(top_ring_bytes(shape.threads), TopLists::bytes(room)) + 2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
+    const size_t smem = std::max(top_ring_bytes(shape.threads), TopLists::bytes(room)) +
+                        2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
     return fine ? launch_rows<k_top<T, true>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st)
                 : launch_rows<k_top<T, false>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st);
 }
@@ -508,6 +509,7 @@ extern "C" int lda_top_logits(const void* logits_dev, int dtype, int64_t rows, i
     if (top > LDA_TOP_MAX) return LDA_ERANGE;
     if (rows == 0) return LDA_OK;
     if (!ids_dev || !values_dev) return LDA_EINVAL;
+    if (!aligned(ids_dev, 4) || !aligned(values_dev, dtype == LDA_F32 ? 4 : 2) || !aligned(lse_dev, 4)) return LDA_EINVAL;
     TopArgs a{logits_dev, row_stride, V, top, (float)(1.4426950408889634 / temperature), 1.0 / temperature, ids_dev, values_dev,
               lse_dev};
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -224,6 +224,9 @@ extern "C" int lda_verify_drafts(const int64_t* draft_offsets_dev, int64_t n_seq
     if (n_seqs == 0) return n_drafts == 0 ? LDA_OK : LDA_EINVAL;
     if (!draft_offsets_dev || !draw_u_dev || !tokens_dev || !accepted_dev) return LDA_EINVAL;
     if (n_drafts > 0 && (!drafts_dev || !accept_u_dev)) return LDA_EINVAL;
+    if (!aligned(draft_offsets_dev, 8) || !aligned(drafts_dev, 4) || !aligned(accept_u_dev, 4) || !aligned(draw_u_dev, 4) ||
+        !aligned(tokens_dev, 4) || !aligned(accepted_dev, 4))
+        return LDA_EINVAL;
     VerifyArgs a{draft_offsets_dev, drafts_dev, target_dev, draft_probs_dev, accept_u_dev, draw_u_dev, tokens_dev,
                  accepted_dev, n_drafts, target_stride, probs_stride, V};
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -72,7 +72,8 @@ def top_logits(logits, top: int, temperature: float = 1.0):
     """The `top` largest logits of every row: (ids int32 [rows, top], values [rows, top], lse float32 [rows]).
 
     Values descend, equal ones by the lower word.  Words at minus infinity are masked: never listed, and places that no word
-    is left for have id -1 and value minus infinity.  ``lse`` is log sum exp(x / temperature) of the whole row.
+    is left for have id -1 and value minus infinity.  ``lse`` is log sum exp(x / temperature) of the whole row.  None of the
+    three is followed by autograd.
     """
     device = _cuda(logits, "logits")
     code, rows, V, stride = _rows(logits, "logits")
@@ -158,7 +159,9 @@ def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
     ids, values: the teacher's lists, as ``top_logits`` gives them; an id outside the vocabulary is padding.  lse None: the
     teacher's distribution is the softmax over the list.  With the teacher's log-sum-exp (taken at the same temperature) it
     is that of its whole row, and all words outside the list make one bucket more.  Differentiable once, with respect to
-    ``logits`` alone; a row that gets the gradient 0 passes 0 on, whatever it holds.
+    ``logits`` alone (the teacher is a constant); a row that gets the gradient 0 passes 0 on, whatever it holds.  A backward pass that is
+    captured into a CUDA graph needs, as always with torch, that no eager graph of the same leaves is alive;
+    ``distill_loss_and_grad`` does not.
     """
     if torch.is_grad_enabled() and logits.requires_grad:
         return _Distill.apply(logits, ids, values, lse, temperature)

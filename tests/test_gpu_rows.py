@@ -5,6 +5,9 @@ x - m and its product are rounded (2^-24 each, relative to a number of at most |
 2^-22 off at most, or zero where it is less than 2^-126 (a row's maximum gives 1, so a share q loses no more than that).  A sum of positive terms whose longest chain of additions has `DEPTH` steps adds DEPTH 2^-24, relative.
 """
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -339,6 +342,36 @@ def test_distill_masked_and_infinite_places(dtype, tail):
     assert bool((grad[[2, 6, 7]] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("above", [60.0, 100.0, 300.0])
+def test_distill_student_with_next_to_no_mass_outside_the_list(dtype, above):
+    """The words outside the list have e^-above of the student's mass, less than a single-precision number holds: their gradient
+    is -tau P share, share their softmax among themselves.  Errors: those of the sums and of one exponential, P's is 2^-22."""
+    V, top, tau = 5_000, 40, 1.0
+    x = make(3, V, dtype, 61)
+    ids, values, lse = lists_of(make(3, V, dtype, 62).cpu(), top, tau, True, dtype)
+    lse = lse + 0.5                                     # the teacher has more mass outside
+    x.scatter_add_(1, ids.long(), torch.full((3, top), above, dtype=dtype, device="cuda"))
+    loss, grad = rows.distill_loss_and_grad(x, ids, values, lse, temperature=tau)
+    d = x.cpu().double()
+    outside = torch.ones(3, V, dtype=torch.bool).scatter_(1, ids.cpu().long(), False)
+    rest = d.masked_fill(~outside, -INF)
+    p = torch.exp(values.cpu().double() / tau - lse.cpu().double()[:, None])
+    p_rest = 1 - p.sum(1)
+    log_p = values.cpu().double() / tau - lse.cpu().double()[:, None]
+    log_q = torch.gather(torch.log_softmax(d / tau, 1), 1, ids.cpu().long())
+    log_q_rest = torch.logsumexp(rest / tau, 1) - torch.logsumexp(d / tau, 1)
+    want = tau**2 * ((p * (log_p - log_q)).sum(1) + p_rest * (torch.log(p_rest) - log_q_rest))
+    assert bool(((loss.cpu().double() - want).abs() <= 2e-5 * tau**2 + 2.0**-22 * (want.abs() + above)).all())
+    share = torch.softmax(rest / tau, 1)
+    far = torch.nan_to_num((rest.max(1, keepdim=True).values - rest) / tau, posinf=0.0)
+    want = -tau * p_rest[:, None] * share + tau * torch.softmax(d / tau, 1).masked_fill(~outside, 0.0)
+    got = grad.cpu().double().masked_fill(~outside, 0.0)
+    error = DEPTH * 2.0**-23 + 2.0**-20 + 3 * 2.0**-24 * far * 1.4427 + 2.0**-22 / p_rest[:, None]
+    bound = want.abs() * (error + HALF_STEP[dtype]) + tau * 2.0**-24 * share + SMALLEST[dtype] + 2.0**-126
+    assert bool(((got - want).abs() <= bound).all()), float(((got - want).abs() / bound).max())
+
+
 def test_distill_teacher_without_mass_on_its_list():
     x = make(2, 400, F32, 1)
     ids, values, lse = lists_of(make(2, 400, F32, 2).cpu(), 10, 1.0, True, F32)
@@ -622,6 +655,66 @@ def test_two_captured_graphs_replayed_in_turn():
     for k in (0, 1):
         again = all_results(*ins[k])
         assert all(torch.equal(a, c) for a, c in zip(outs[k], again))
+
+
+@pytest.mark.parametrize("through", ["autograd", "loss_and_grad"])
+def test_a_captured_training_step(through):
+    """Loss, gradient and a step of plain descent in one graph.  Without autograd an eager graph of the same tensor may live on (a
+    captured backward pass of torch's breaks its capture then, whatever the operator)."""
+    x, ids, values, lse, w, _ = inputs(9, V=5_003, dtype=F32)
+    student = x.clone().requires_grad_()
+    eager = rows.distill_loss(student, ids, values, lse) if through == "loss_and_grad" else None
+
+    def step():
+        if through == "autograd":
+            loss = rows.distill_loss(student, ids, values, lse)
+            grad, = torch.autograd.grad((loss * w).sum(), student)
+            loss = loss.detach()
+        else:
+            loss, grad = rows.distill_loss_and_grad(student, ids, values, lse, weights=w)
+        with torch.no_grad():
+            student.sub_(grad, alpha=3.0)
+        return loss, grad
+    want = x.clone()
+    for _ in range(5):
+        loss, grad = rows.distill_loss_and_grad(want, ids, values, lse, weights=w)
+        want.sub_(grad, alpha=3.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(4):
+        graph.replay()
+    assert torch.equal(student.detach(), want) and torch.equal(out[0], loss) and torch.equal(out[1], grad)
+    assert eager is None or eager.requires_grad
+
+
+FIRST_IN_A_CAPTURE = """
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import torch
+import test_gpu_rows as T
+ins = T.inputs(3)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = T.all_results(*ins)
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(out, T.all_results(*ins)))
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_in_a_capture():
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", FIRST_IN_A_CAPTURE.format(root=os.path.dirname(here), tests=here)], capture_output=True,
+                       text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
 
 
 def test_elements_beyond_32_bits():

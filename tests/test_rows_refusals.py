@@ -75,6 +75,15 @@ def test_verifications_beyond_the_limits_are_refused(bad):
     assert verify(**bad) == b.LDA_ERANGE
 
 
+def test_misaligned_pointers_are_refused():
+    assert top(ids=P + 2) == top(values=P + 2) == top(lse=P + 1) == b.LDA_EINVAL
+    assert top(dtype=b.LDA_BF16, values=P + 1) == b.LDA_EINVAL
+    for call in (loss, grad):
+        assert call(ids=P + 1) == call(lse=P + 2) == call(out=P + 3) == b.LDA_EINVAL
+    assert grad(w=P + 2) == grad(g=P + 2) == b.LDA_EINVAL
+    assert verify(off=P + 4) == verify(drafts=P + 2) == verify(au=P + 1) == verify(du=P + 2) == verify(tok=P + 2) == verify(acc=P + 3) == b.LDA_EINVAL
+
+
 def test_no_rows_is_nothing_to_do():
     assert top(rows=0, logits=None, ids=None, values=None, lse=None) == b.LDA_OK
     assert loss(rows=0, logits=None, ids=None, values=None, out=None) == b.LDA_OK
