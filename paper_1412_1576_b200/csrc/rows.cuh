@@ -266,7 +266,12 @@ __device__ __forceinline__ void unpack(uint4 g, float (&x)[PER<T>])
 // is exact, and x c - R is rounded once (a fused multiply-add).  |R| <= 2^22 keeps R c's rounding out; rows whose maximum lies
 // beyond that (the type's lowest value as a mask, say) are added up again as 2^((x - maximum) c): `far`.
 constexpr float REF_MOST = 4194304.0f;
-__device__ __forceinline__ float exp_ref(float max, float c) { return fminf(fmaxf(floorf(max * c), -REF_MOST), REF_MOST); }
+__device__ __forceinline__ float exp_ref(float max, float c)
+{
+    // (rounded down by adding 1.5 2^23, whose neighbours are 1 away: floorf is the multifunction unit's, which is the busiest)
+    const float x = fminf(fmaxf(max * c, -REF_MOST), REF_MOST);
+    return __fadd_rd(x, 12582912.0f) - 12582912.0f;
+}
 __device__ __forceinline__ bool exp_far(float max, float c) { return max != -INFINITY && !(fabsf(max * c) < REF_MOST); }
 
 // 2^d for a whole number d <= 0.
