@@ -299,7 +299,9 @@ int lda_dense_table_noalloc(const int32_t* n_k_dev, int32_t K, int32_t V, double
  * LDA_EINVAL: NULL where a pointer is needed, unknown dtype, negative size, a pointer that is not a multiple of its elements' size,
  * a temperature outside [1e-6, 1e6];
  * LDA_ERANGE: sizes beyond the limits; LDA_ECUDA: the launch failed.  The contents of DEVICE memory are not looked at by the
- * call; the kernels read and write nothing outside the rows and lists that the arguments describe, whatever ids and offsets hold. */
+ * call; the kernels read and write nothing outside the rows and lists that the arguments describe, whatever ids and offsets hold.
+ * The same call gives the same bits; with another number of rows, sums of exponentials (lse, loss, gradient) may differ in the
+ * last places, since a row is shared out over other numbers of threads.  Lists and tokens never do. */
 #define LDA_F32 0
 #define LDA_F16 1
 #define LDA_BF16 2
@@ -320,7 +322,8 @@ int lda_top_logits(const void* logits_dev, int dtype, int64_t rows, int32_t V, i
  *   (teacher_lse[rows]: the teacher's log sum exp(x / tau) over its whole row, as lda_top_logits gives it)
  *   loss = tau^2 ( sum_j p_j (log p_j - log q_{ids_j}) + P (log P - log Q) )
  * Where the student has no mass outside the list the last term is left out.  A word that the list holds twice counts with both
- * entries.  A row whose list holds nothing but padding has loss 0 and gradient 0. */
+ * entries.  A row whose list holds nothing but padding has loss 0 and gradient 0; otherwise a NaN in a row or in its list makes
+ * the row's loss and gradient NaN. */
 int lda_distill_loss(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride,
                      const int32_t* ids_dev, const void* values_dev, int values_dtype, int32_t top, int64_t list_stride,
                      const float* teacher_lse_dev, double temperature, float* loss_dev, void* cuda_stream);

@@ -153,6 +153,24 @@ def test_top_logits_where_a_selection_can_go_wrong(dtype, top):
     check_top(special_rows(dtype), top)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+def test_top_logits_where_a_selection_can_go_wrong_in_many_rows(dtype):
+    """The same rows among so many that each has one CTA."""
+    x = special_rows(dtype)
+    few = rows.top_logits(x, 100)
+    check_top(x, 100)
+    many = rows.top_logits(x.repeat(64, 1), 100)
+    for a, c in zip(few[:2], many[:2]):
+        c = c.view(64, *a.shape)
+        a, c = torch.nan_to_num(a.float(), nan=1.0, posinf=2.0, neginf=3.0), torch.nan_to_num(c.float(), nan=1.0, posinf=2.0, neginf=3.0)
+        assert bool((c == a).all())
+    bound = 2 * (lse_error(x.cpu().double(), 1.0) + 2.0**-23 + HALF_STEP[F32] * few[2].cpu().double().abs())
+    off = (many[2].view(64, -1) - few[2]).abs().cpu().double()
+    plain = torch.isfinite(few[2]).cpu()
+    assert bool((off <= bound)[:, plain].all())
+    assert torch.equal(torch.nan_to_num(many[2].view(64, -1)[:, ~plain], nan=5.0), torch.nan_to_num(few[2][~plain], nan=5.0).expand(64, -1))
+
+
 def test_top_logits_of_one_row_again_and_again():
     x = make(1, 5_003, BF16, 1).expand(6, 5_003)       # row stride 0
     check_top(x, 9)
@@ -313,9 +331,11 @@ def test_distill_a_word_listed_twice():
     check_distill(x, ids, values, None)
 
 
+@pytest.mark.parametrize("n_rows", [10, 1300])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
 @pytest.mark.parametrize("tail", [False, True], ids=["list", "tail"])
-def test_distill_masked_and_infinite_places(dtype, tail):
+def test_distill_masked_and_infinite_places(dtype, tail, n_rows):
+    """A few rows are shared out over clusters, many have one CTA each."""
     V, low = 6_000, torch.finfo(dtype).min
     x = make(10, V, dtype, 11)
     teacher = make(10, V, dtype, 12)
@@ -333,6 +353,16 @@ def test_distill_masked_and_infinite_places(dtype, tail):
     values = values.clone()
     values[7, 3] = NAN
     w = torch.full((10,), 2.0, device="cuda")
+    if n_rows > 10:
+        again = lambda t: t.repeat(n_rows // 10, *[1] * (t.dim() - 1))      # noqa: E731
+        want_loss, loss_tol, want_grad, grad_tol = distill_reference(x.cpu(), ids.cpu(), values.cpu(), None if lse is None else lse.cpu(), 1.0, w.cpu())
+        loss, grad = rows.distill_loss_and_grad(again(x), again(ids), again(values), None if lse is None else again(lse), weights=again(w))
+        alone = rows.distill_loss(again(x), again(ids), again(values), None if lse is None else again(lse))
+        for k in (0, n_rows // 20, n_rows // 10 - 1):
+            same(loss[10 * k: 10 * k + 10], want_loss, loss_tol, F32)
+            same(alone[10 * k: 10 * k + 10], want_loss, loss_tol, F32)
+            same(grad[10 * k: 10 * k + 10], want_grad, grad_tol, dtype)
+        return
     loss, grad = check_distill(x, ids, values, lse, weights=w)
     assert math.isinf(float(loss[2])) and bool(torch.isfinite(grad[2]).all())
     assert bool(torch.isnan(grad[6]).all()) and bool(torch.isnan(loss[6])) and bool(torch.isnan(loss[7]))
