@@ -161,26 +161,29 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopCounts
     return sh.n;
 }
 
-// What the pass over a row does with a chunk: its values into the sum, the largest of every piece (a lane's groups of the chunk; FINE:
-// each group) as the upper half of its key, and of every group of pieces (`tops`).
+// What the pass over a row does with a thread's chunk number `turn`: its values into the sum, the largest of every piece (a lane's groups
+// of the chunk; FINE: each group) as the upper half of its key, and of every group of pieces (`tops`: this thread's of the first
+// groups; it has turns + 1 of them, `threads` places apart).
 template <typename T, bool FINE>
-__device__ __forceinline__ void top_chunk(const uint4 (&raw)[TOP_GROUPS], uint16_t* keys, uint16_t* tops, float c, float& m, ExpSum& sum)
+__device__ __forceinline__ void top_chunk(const uint4 (&raw)[TOP_GROUPS], uint16_t* keys, uint16_t* tops, int turn, int turns, int threads,
+                                          float c, float& m, ExpSum& sum)
 {
-    float top;
-    if (FINE) {
-        top = -INFINITY;
+    constexpr int PIECES = FINE ? TOP_GROUPS : 1;
+    float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < TOP_GROUPS; ++k) {
+    for (int k = 0; k < PIECES; ++k) {
+        float x;
+        if constexpr (FINE) {
             const uint4 one[1] = {raw[k]};
-            const float x = groups_max<T, 1>(one);
-            keys[32 * k] = (uint16_t)(order_key(x) >> 16);
-            top = max_nan(top, x);
-        }
+            x = groups_max<T, 1>(one);
+        } else
+            x = groups_max<T, TOP_GROUPS>(raw);
+        const uint16_t key = (uint16_t)(order_key(x) >> 16);
+        keys[32 * k] = key;
+        uint16_t* group = tops + (turn * PIECES + k & turns) * threads;
+        *group = max(*group, key);
+        top = FINE ? max_nan(top, x) : x;
     }
-    if (!FINE) top = groups_max<T, TOP_GROUPS>(raw);
-    const uint16_t key = (uint16_t)(order_key(top) >> 16);
-    if (!FINE) keys[0] = key;
-    *tops = max(*tops, key);
     m = fmaxf(m, top);
     add_groups<T, TOP_GROUPS>(sum, raw, top, c);
 }
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     ExpSum sum = ExpSum::none();
     float m = -INFINITY;
     walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, int, uint4(&raw)[R]) {
-        top_chunk<T, FINE>(raw, keys + (c - split.chunk0) * 32 * PIECES + lane, tops + (turn++ & turns) * threads + tid, a.scale, m, sum);
+        top_chunk<T, FINE>(raw, keys + (c - split.chunk0) * 32 * PIECES + lane, tops + tid, turn++, turns, threads, a.scale, m, sum);
     });
     sum.warp_reduce();
     m = warp_reduce_max(m);

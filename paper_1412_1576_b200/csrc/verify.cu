@@ -41,6 +41,28 @@ struct MassSum {
     __device__ __forceinline__ unsigned long long value() const { return ((unsigned long long)upper << 23) + lower; }
 };
 
+// The PER values of a row from element `first` on, whose address is `off` bytes behind a multiple of 16 (off > 0, the same for all
+// groups of a chunk walk): the two aligned pieces that hold them, pushed together.  Zeros outside the row.
+template <typename T>
+__device__ __forceinline__ uint4 shifted_group(const T* row, int first, int V, int off)
+{
+    const int back = off / (int)sizeof(T);  // elements of the first piece that are not wanted
+    if (first - back < 0 || first - back + 2 * PER<T> > V) return edge_group(row, first, V, row_element<T>(0.0f));
+    const uint4* p = reinterpret_cast<const uint4*>(row + first - back);
+    const uint4 a = p[0], b = p[1];  // (b is the next lane's a: from L1)
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (off & 8)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    if (off & 4)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    if (sizeof(T) == 2 && (off & 2))
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // One cluster per sequence.  Every CTA finds the first draft that is refused by itself (the sequences are short), then each adds
 // up the masses of its part of the row, a sum per chunk; the CTA in whose part the drawn mass falls looks for the chunk and
 // reads that again to find the word.
@@ -99,7 +121,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
     int32_t gone = !PROBS && refused ? a.drafts[lo + taken] : -1;  // the word that the draft takes out of p
     if (gone < 0 || gone >= V) gone = -1;
     const RowSplit split = RowSplit::of<T, R>(prow, V, rank, ctas);
-    const bool abreast = PROBS && (uintptr_t)qrow % 16 == (uintptr_t)prow % 16;
+    // how far the drafter's groups are behind multiples of 16 bytes, where the target's are at one
+    const int off = PROBS && qrow ? (int)(((uintptr_t)qrow - (uintptr_t)prow) & 15) : 0;
     if (ctas > 1) cluster_wait();
     int token = -1;
     bool here = true;  // whether this CTA writes the token
@@ -113,30 +136,26 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
         for (int c = split.chunk0 + warp; c < split.chunk1; c += threads / 32) {
             const int first = chunk_first<T, R>(c, split.pre);
             MassSum sum{0, 0};  // of 32 words at most: below 2^25 and 2^28
-            if (q && !abreast) {
-                // rows at different offsets from 16 bytes: by elements, in any order
-#pragma unroll 16
-                for (int i = lane; i < CHUNK; i += 32) {
-                    const int v = first + i;
-                    if (v >= 0 && v < V) sum.add(part(v));
-                }
-            } else {
-                uint4 rp[R], rq[R];
-                load_chunk<T, R>(prow, first, V, row_element<T>(0.0f), rp);
-                if (q) load_chunk<T, R>(q, first, V, row_element<T>(0.0f), rq);
+            uint4 rp[R], rq[R];
+            load_chunk<T, R>(prow, first, V, row_element<T>(0.0f), rp);
+            if (q) {
+                if (off == 0) load_chunk<T, R>(q, first, V, row_element<T>(0.0f), rq);
+                else
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    float xp[PER<T>], xq[PER<T>];
-                    unpack<T>(rp[r], xp);
-                    if (q) {
-                        unpack<T>(rq[r], xq);
+                    for (int r = 0; r < R; ++r) rq[r] = shifted_group(q, first + (32 * r + lane) * PER<T>, V, off);
+            }
 #pragma unroll
-                        for (int i = 0; i < PER<T>; ++i) sum.add(__saturatef(xp[i] - xq[i]));
-                    } else {
-                        const int at = out - (first + (32 * r + lane) * PER<T>);
+            for (int r = 0; r < R; ++r) {
+                float xp[PER<T>], xq[PER<T>];
+                unpack<T>(rp[r], xp);
+                if (q) {
+                    unpack<T>(rq[r], xq);
 #pragma unroll
-                        for (int i = 0; i < PER<T>; ++i) sum.add(i == at ? 0.0f : __saturatef(xp[i]));
-                    }
+                    for (int i = 0; i < PER<T>; ++i) sum.add(__saturatef(xp[i] - xq[i]));
+                } else {
+                    const int at = out - (first + (32 * r + lane) * PER<T>);
+#pragma unroll
+                    for (int i = 0; i < PER<T>; ++i) sum.add(i == at ? 0.0f : __saturatef(xp[i]));
                 }
             }
             // (the lower halves in two parts, so that 32 lanes' sums stay inside 32 bits)
