@@ -29,6 +29,7 @@ struct DistillArgs {
     int64_t grad_stride;
     float scale;               // log2(e) / tau
     double tau, inv_tau;
+    int ring;                  // bytes of the walk's ring
 };
 
 constexpr int DISTILL_GROUPS = 4;  // groups of a lane in a chunk
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     constexpr bool BITS = TAIL || GRAD;
     using Walk = ChunkWalk<T, R, distill_depth(GRAD)>;
     extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the list
-    const DistillList list(dynamic + blockDim.x * Walk::BYTES, a.top);
+    const DistillList list(dynamic + a.ring, a.top);
     __shared__ ExpSum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ DistillPart parts[2][ROW_CTAS];
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
 }
 
 template <typename T>
-static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t st)
+static cudaError_t run_distill(DistillArgs a, int64_t rows, cudaStream_t st)
 {
     constexpr int CHUNK = 32 * DISTILL_GROUPS * PER<T>;
     const int64_t row_bytes = (int64_t)a.V * sizeof(T);
@@ -459,10 +460,12 @@ static cudaError_t run_distill(const DistillArgs& a, int64_t rows, cudaStream_t 
     // what is read twice has to stay in L2 in between: rows of about 60 MB under way together (40 MB, more CTAs to a row: 302 us for
     // the 258 above; 90 MB: 280)
     const int64_t most = grad ? std::min<int64_t>(rows, std::max<int64_t>(1, (60ll << 20) / row_bytes)) : rows;
-    const RowShape shape = row_shape(most, row_bytes, 1024, 64);
+    const RowShape shape = row_shape(most, row_bytes, 1024, 128);
     // a bit for every word of a CTA's part
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    const size_t smem = shape.threads * distill_depth(grad) * DISTILL_GROUPS * 16 +
+    a.ring = grad ? ChunkWalk<T, DISTILL_GROUPS, distill_depth(true)>::bytes(shape, a.V)
+                  : ChunkWalk<T, DISTILL_GROUPS, distill_depth(false)>::bytes(shape, a.V);
+    const size_t smem = a.ring +
                         DistillList::bytes(a.top, tail || grad ? distill_bits<T>((chunks + shape.ctas - 1) / shape.ctas) : 0);
     constexpr size_t fixed = 2 * 1024;
     if (tail)
@@ -503,7 +506,7 @@ extern "C" int lda_distill_loss(const void* logits_dev, int dtype, int64_t rows,
     using namespace lda;
     if (rows > 0 && !loss_dev) return LDA_EINVAL;
     const DistillArgs a{logits_dev, row_stride, V, top, ids_dev, values_dev, values_dtype, list_stride, teacher_lse_dev, nullptr, loss_dev,
-                        nullptr, 0, (float)(1.4426950408889634 / temperature), temperature, 1.0 / temperature};
+                        nullptr, 0, (float)(1.4426950408889634 / temperature), temperature, 1.0 / temperature, 0};
     return distill(a, dtype, rows, cuda_stream);
 }
 
@@ -519,6 +522,6 @@ extern "C" int lda_distill_grad(const void* logits_dev, int dtype, int64_t rows,
     // the gradient may take the logits' place, row for row, and may not overlap them otherwise
     if (grad_dev == logits_dev && rows > 1 && grad_stride != row_stride) return LDA_EINVAL;
     const DistillArgs a{logits_dev, row_stride, V, top, ids_dev, values_dev, values_dtype, list_stride, teacher_lse_dev, weights_dev, loss_dev,
-                        grad_dev, grad_stride, (float)(1.4426950408889634 / temperature), temperature, 1.0 / temperature};
+                        grad_dev, grad_stride, (float)(1.4426950408889634 / temperature), temperature, 1.0 / temperature, 0};
     return distill(a, dtype, rows, cuda_stream);
 }

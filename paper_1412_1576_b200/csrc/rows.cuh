@@ -150,11 +150,18 @@ inline RowShape row_shape(int64_t rows, int64_t row_bytes, int64_t per_sm, int64
 }
 
 // A warp's walk over its chunks of a part (every warps-th from its own number on).  A lane copies its groups of the next DEPTH chunks
-// into places of its own in shared memory (`ring`: DEPTH R 16 bytes per thread), so that what is on its way costs no registers and
+// into places of its own in shared memory (`ring`: R 16 bytes per thread for each of them), so that what is on its way costs no registers and
 // nothing has to be waited for but the lane's own copies.
 template <typename T, int R, int DEPTH>
 struct ChunkWalk {
-    static constexpr int BYTES = DEPTH * R * 16;  // per thread
+    // Bytes of the ring: for no more chunks than a warp has to walk over.
+    static int bytes(const RowShape& shape, int V)
+    {
+        const int chunks = (V + PER<T> - 1 + 32 * R * PER<T> - 1) / (32 * R * PER<T>), warps = shape.ctas * shape.threads / 32;
+        const int slots = (chunks + shape.ctas - 1) / shape.ctas * shape.ctas;  // (CTAs' parts differ by a chunk)
+        const int each = (slots + warps - 1) / warps;
+        return shape.threads * R * 16 * (each < DEPTH ? each : DEPTH);
+    }
     uint4* ring;
     int threads, warps;  // that walk together
     // Chunk c (if the part has it) into the ring's slot; one group of copies, empty or not.

@@ -17,6 +17,7 @@ struct TopArgs {
     int32_t* ids;
     void* values;
     float* lse;
+    int ring;  // bytes of the walk's ring, or of the lists that take its place
 };
 
 constexpr int TOP_GROUPS = 4;     // groups of a lane in a chunk (two: 242 us for 229)
@@ -384,8 +385,6 @@ struct TopPart {
     uint32_t share, alone;  // borders
 };
 
-__host__ __device__ constexpr int top_ring_bytes(int threads) { return threads * TOP_DEPTH * TOP_GROUPS * 16; }
-
 // One cluster per row.  The pass leaves the pieces' largest keys.  A border that at least `top` groups of pieces reach
 // leaves at least `top` words, and few more (95 for 64 of 131 072); the pieces that reach it are read again (from L2), their words
 // sorted, in runs of 128 by a warp each, and merged by rank.
@@ -409,7 +408,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads / 32, V = a.V;
     const int room = top_room(a.top);
     const TopLists lists(dynamic, room);
-    uint16_t* tops = (uint16_t*)(dynamic + max(top_ring_bytes(threads), TopLists::bytes(room)));
+    uint16_t* tops = (uint16_t*)(dynamic + a.ring);
     const int groups = top_groups(threads, a.top), turns = groups / threads - 1;
     uint16_t* keys = tops + groups;
     const int64_t r = blockIdx.x / ctas;
@@ -491,17 +490,21 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
 }
 
 template <typename T>
-static cudaError_t run_top(const TopArgs& a, int64_t rows, cudaStream_t st)
+static cudaError_t run_top(TopArgs a, int64_t rows, cudaStream_t st)
 {
     constexpr int CHUNK = 32 * TOP_GROUPS * PER<T>;
     const int64_t row_bytes = (int64_t)a.V * sizeof(T);
     const int per = a.V / PER<T>, room = top_room(a.top);
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
     const auto pieces = [&](int ctas, bool fine) { return (chunks + ctas - 1) / ctas * 32 * (fine ? TOP_GROUPS : 1); };
-    const RowShape shape = row_shape(rows, row_bytes, 1024, 64);
+    // 128 bytes a thread at least: one row of 131 072 words of bf16 11.2 us for the 12.6 of 64 bytes, 16 rows 13.4 for 16.2.  Short
+    // rows that do not fill the GPU have 256 threads all the same, for the sorting (64 rows of 8 000 words of fp32, the 256 largest:
+    // 11.3 us for 14.4 with 128 threads; of 4 000 words: 10.8 for 13.3)
+    RowShape shape = row_shape(rows, row_bytes, 1024, 128);
+    if (shape.threads == 128 && row_bytes >= 16000 && rows <= 148 * 4) shape.threads = 256;
     const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
-    const size_t smem = std::max(top_ring_bytes(shape.threads), TopLists::bytes(room)) +
-                        2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
+    a.ring = std::max(ChunkWalk<T, TOP_GROUPS, TOP_DEPTH>::bytes(shape, a.V), TopLists::bytes(room));
+    const size_t smem = a.ring + 2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
     return fine ? launch_rows<k_top<T, true>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st)
                 : launch_rows<k_top<T, false>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st);
 }
@@ -520,7 +523,7 @@ extern "C" int lda_top_logits(const void* logits_dev, int dtype, int64_t rows, i
     if (!ids_dev || !values_dev) return LDA_EINVAL;
     if (!aligned(ids_dev, 4) || !aligned(values_dev, dtype == LDA_F32 ? 4 : 2) || !aligned(lse_dev, 4)) return LDA_EINVAL;
     TopArgs a{logits_dev, row_stride, V, top, (float)(1.4426950408889634 / temperature), 1.0 / temperature, ids_dev, values_dev,
-              lse_dev};
+              lse_dev, 0};
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const cudaError_t e = dtype == LDA_F32 ? run_top<float>(a, rows, st)
                           : dtype == LDA_F16 ? run_top<__half>(a, rows, st)

@@ -70,7 +70,8 @@ __device__ __forceinline__ uint4 shifted_group(const T* row, int first, int V, i
 // 141 000 words of bf16 (108 MB) take 29 us, of which the pass is 16 us at 6.6 TB/s; before it stand three reads that need each other
 // (offsets, drafts, probabilities: 3 us), behind it the cluster's exchange and the search (6 us).  All sequences are on the GPU at
 // once (row_shape: 256 threads in two CTAs each here); with twice the threads, in two turns, 34 us.  Eight groups of each row in
-// flight 36 us, two 31.
+// flight 36 us, two 31.  Where a drafter's row starts at another offset from 16 bytes than the target's, its groups are put
+// together from two aligned pieces: 42 us (word by word: 104).
 template <typename T, bool PROBS>
 __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
 {
@@ -228,7 +229,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_verify(VerifyArgs a)
 template <typename T>
 static cudaError_t run_verify(const VerifyArgs& a, int64_t n_seqs, cudaStream_t st)
 {
-    const RowShape shape = row_shape(n_seqs, (int64_t)a.V * sizeof(T), 1024, 64);
+    // 128 bytes a thread where the sequences fill the GPU (256 of 32 000 words of bf16: 10.9 us for the 12.7 of 32 bytes); few
+    // short rows are done sooner by more CTAs (one of 32 000 words: 7.4 us for 9.2), of 256 threads at most (16 of 131 072 words by
+    // eight CTAs of 256: 8.1 us for the 9.2 of eight of 512)
+    const int64_t row_bytes = (int64_t)a.V * sizeof(T);
+    RowShape shape = row_shape(n_seqs, row_bytes, 1024, 128);
+    const RowShape wide = row_shape(n_seqs, row_bytes, 256, 32);
+    if (wide.threads <= 256 && wide.ctas * wide.threads > shape.ctas * shape.threads) shape = wide;
     return a.probs ? launch_rows<k_verify<T, true>>(a, n_seqs, shape, 0, 17 * 1024, st)
                    : launch_rows<k_verify<T, false>>(a, n_seqs, shape, 0, 17 * 1024, st);
 }
