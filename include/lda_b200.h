@@ -295,6 +295,7 @@ int lda_dense_table_noalloc(const int32_t* n_k_dev, int32_t K, int32_t V, double
  *   rows     0 .. 2^31-1; 0 is legal and does nothing
  *   V        1 .. LDA_ROW_MAX_V words per row, consecutive in memory
  *   stride   elements from one row to the next, 0 .. 2^31 (0: the same row again); rows that are written need >= V
+ *   outputs  overlap neither the inputs nor each other, but for a gradient in its logits' place
  *
  * LDA_EINVAL: NULL where a pointer is needed, unknown dtype, negative size, a pointer that is not a multiple of its elements' size,
  * a temperature outside [1e-6, 1e6];

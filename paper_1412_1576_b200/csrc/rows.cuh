@@ -470,7 +470,7 @@ inline int check_rows(const void* p, int dtype, int64_t rows, int32_t V, int64_t
     if (dtype != LDA_F32 && dtype != LDA_F16 && dtype != LDA_BF16) return LDA_EINVAL;
     if (rows < 0 || V <= 0 || stride < 0) return LDA_EINVAL;
     if (rows > 0x7fffffffll || V > LDA_ROW_MAX_V) return LDA_ERANGE;
-    // an element's offset in bytes stays inside 63 bits
+    // an element's number stays inside 63 bits
     if (stride > (1ll << 31)) return LDA_ERANGE;
     if (rows > 0 && (!p || (uintptr_t)p % (dtype == LDA_F32 ? 4 : 2))) return LDA_EINVAL;
     return LDA_OK;

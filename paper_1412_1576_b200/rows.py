@@ -142,7 +142,8 @@ def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
     device = _cuda(logits, "logits")
     code, rows, V, stride = _rows(logits, "logits")
     lists = _list(ids, values, lse, rows, device)
-    if grad is None:
+    given = grad is not None
+    if not given:
         grad, grad_stride = torch.empty_like(logits, memory_format=torch.contiguous_format), V
     else:
         if grad.dtype != logits.dtype or grad.shape != logits.shape:
@@ -154,6 +155,8 @@ def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
     w = None if weights is None else _vector(weights, "weights", torch.float32, rows, device)
     _call("lda_distill_grad", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
           None if loss is None else loss.data_ptr(), grad.data_ptr(), grad_stride)
+    if given:
+        torch.autograd.graph.increment_version(grad)  # (a graph that has saved what was there finds out)
     return grad
 
 
@@ -191,13 +194,14 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
     row per draft and one more behind each sequence's last, [drafts + n, V]; draft_probs: the drafter's rows [drafts, V] in
     the same type, or None where it put its whole mass on its draft; accept_u [drafts] and draw_u [n]: float32 uniforms.
     Returns (tokens int32 [drafts + n], accepted int32 [n]): at the places of a sequence's target rows its accepted drafts,
-    the token drawn behind them, then -1.  Both may be given; places of no sequence keep what they hold (-1 in new ones).
+    the token drawn behind them, then -1.  Both may be given, apart from the inputs' memory; places of no sequence keep what they
+    hold (-1 in new ones).
     """
     device = _cuda(target, "target")
     code, rows, V, stride = _rows(target, "target")
     if draft_offsets.dim() != 1 or draft_offsets.shape[0] < 1:
         raise ValueError("draft_offsets: one more than there are sequences is needed")
-    n_seqs, n_drafts = draft_offsets.shape[0] - 1, drafts.shape[0]
+    n_seqs, n_drafts = draft_offsets.shape[0] - 1, drafts.numel()
     if rows != n_drafts + n_seqs:
         raise ValueError(f"target: {n_drafts} drafts of {n_seqs} sequences need {n_drafts + n_seqs} rows, not {rows}")
     offsets_ptr = _vector(draft_offsets, "draft_offsets", torch.int64, n_seqs + 1, device)

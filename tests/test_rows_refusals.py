@@ -105,3 +105,27 @@ def test_tensors_of_the_host_are_refused():
         rows.distill_loss_and_grad(x, ids, values)
     with pytest.raises(ValueError, match="CUDA"):
         rows.verify_drafts(torch.zeros(2, dtype=torch.int64), ids[0, :0], x[:1], None, x[0, :0], x[0, :1])
+
+
+def test_a_gradient_over_saved_logits_is_noticed(monkeypatch):
+    # (no GPU: the library's calls are left out, the tensors' bookkeeping is torch's)
+    monkeypatch.setattr(rows, "_cuda", lambda x, name: x.device)
+    monkeypatch.setattr(rows, "_call", lambda name, device, *args: None)
+    x = torch.zeros(2, 10, requires_grad=True)
+    ids, values = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3)
+    kept = rows.distill_loss(x, ids, values)
+    rows.distill_loss_and_grad(x, ids, values)
+    kept.sum().backward()
+    lost = rows.distill_loss(x, ids, values)
+    rows.distill_loss_and_grad(x, ids, values, grad=x.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        lost.sum().backward()
+
+
+@pytest.mark.parametrize("shape", [(), (2, 2)], ids=str)
+def test_drafts_that_are_no_vector_are_refused(monkeypatch, shape):
+    monkeypatch.setattr(rows, "_cuda", lambda x, name: x.device)
+    drafts = torch.zeros(shape, dtype=torch.int32)
+    n = drafts.numel()
+    with pytest.raises(ValueError, match="drafts"):
+        rows.verify_drafts(torch.tensor([0, n]), drafts, torch.zeros(n + 1, 10), None, torch.zeros(n), torch.zeros(1))
