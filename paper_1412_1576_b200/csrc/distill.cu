@@ -29,11 +29,11 @@ struct DistillArgs {
     int64_t grad_stride;
     float scale;               // log2(e) / tau
     double tau, inv_tau;
-    int ring;                  // bytes of the walk's ring
+    int ring;                  // bytes of the walk's ring (loss alone)
 };
 
 constexpr int DISTILL_GROUPS = 4;  // groups of a lane in a chunk
-// Chunks on their way.  With a gradient two: 274 us for the 258 below (more rows at a time, which L2 holds less well); the loss alone
+// Chunks on their way.  With a gradient two: 274 us for 258 (more rows at a time, which L2 holds less well); the loss alone
 // with three: 150 us for 147.
 __host__ __device__ constexpr int distill_depth(bool grad) { return grad ? 3 : 4; }
 
@@ -309,7 +309,7 @@ __device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, 
 // One cluster per row; every CTA has the whole list and a part of the row.  The words of the list are marked in a bit map of that
 // part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The CTAs exchange
 // their sums; each works out the gradient of its part from a second read, which L2 answers, and puts the list's words over it.
-// 2048 rows of 141 000 words of bf16, lists of 64, loss and gradient: 258 us, 4.5 TB/s of the logits' one read and the gradient's
+// 2048 rows of 141 000 words of bf16, lists of 64, loss and gradient: 254 us, 4.5 TB/s of the logits' one read and the gradient's
 // write (DRAM sees 10 % more).  Both exponentials per word keep the multifunction units 54 % busy, the issue slots are 54 % full; a
 // CTA (half a row) spends 14 of 24 us on the two passes, the rest on the list, the exchange and the sums, three CTAs at a time.
 // The loss alone, 4096 rows of 100 000 of fp16, lists of 128: 148 us, 5.5 TB/s.
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     constexpr bool BITS = TAIL || GRAD;
     using Walk = ChunkWalk<T, R, distill_depth(GRAD)>;
     extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring, the list
-    const DistillList list(dynamic + a.ring, a.top);
+    const DistillList list(dynamic + (GRAD ? (int)blockDim.x * Walk::BYTES : a.ring), a.top);
     __shared__ ExpSum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ DistillPart parts[2][ROW_CTAS];
@@ -458,12 +458,14 @@ static cudaError_t run_distill(DistillArgs a, int64_t rows, cudaStream_t st)
     const int64_t row_bytes = (int64_t)a.V * sizeof(T);
     const bool tail = a.teacher_lse, grad = a.grad;
     // what is read twice has to stay in L2 in between: rows of about 60 MB under way together (40 MB, more CTAs to a row: 302 us for
-    // the 258 above; 90 MB: 280)
+    // the 258 of then; 90 MB: 280)
     const int64_t most = grad ? std::min<int64_t>(rows, std::max<int64_t>(1, (60ll << 20) / row_bytes)) : rows;
     const RowShape shape = row_shape(most, row_bytes, 1024, 128);
     // a bit for every word of a CTA's part
     const int chunks = (a.V + PER<T> - 1 + CHUNK - 1) / CHUNK;
-    a.ring = grad ? ChunkWalk<T, DISTILL_GROUPS, distill_depth(true)>::bytes(shape, a.V)
+    // the loss alone has a ring no larger than it needs (64 rows of 131 072 words of bf16: 11.5 us for 16.3); with a gradient the list's
+    // places come out cheaper from a ring of one size (the 254 above: for 260)
+    a.ring = grad ? shape.threads * ChunkWalk<T, DISTILL_GROUPS, distill_depth(true)>::BYTES
                   : ChunkWalk<T, DISTILL_GROUPS, distill_depth(false)>::bytes(shape, a.V);
     const size_t smem = a.ring +
                         DistillList::bytes(a.top, tail || grad ? distill_bits<T>((chunks + shape.ctas - 1) / shape.ctas) : 0);

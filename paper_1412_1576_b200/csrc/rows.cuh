@@ -154,7 +154,8 @@ inline RowShape row_shape(int64_t rows, int64_t row_bytes, int64_t per_sm, int64
 // nothing has to be waited for but the lane's own copies.
 template <typename T, int R, int DEPTH>
 struct ChunkWalk {
-    // Bytes of the ring: for no more chunks than a warp has to walk over.
+    static constexpr int BYTES = DEPTH * R * 16;  // of the ring, per thread
+    // Bytes of a ring for no more chunks than a warp has to walk over.
     static int bytes(const RowShape& shape, int V)
     {
         const int chunks = (V + PER<T> - 1 + 32 * R * PER<T> - 1) / (32 * R * PER<T>), warps = shape.ctas * shape.threads / 32;

@@ -246,6 +246,46 @@ __device__ __forceinline__ uint32_t top_border(const uint16_t* tops, int groups,
     return lo;
 }
 
+// Element e of a group of 16-bit values.
+template <typename T>
+__device__ __forceinline__ float pair_value(uint4 g, int e)
+{
+    const uint32_t word = e & 4 ? (e & 2 ? g.w : g.z) : (e & 2 ? g.y : g.x), half = e & 1 ? word >> 16 : word & 0xFFFFu;
+    if constexpr (T_is_bf16<T>) return __uint_as_float(half << 16);
+    return __half2float(__ushort_as_half((unsigned short)half));
+}
+
+// Bits of the elements of a group whose half-keys reach the border.  `least`: the border as a value, rounded up (16-bit types, two
+// at a time: not below it, or NaN, which is above everything).
+template <typename T>
+__device__ __forceinline__ uint32_t top_hits(uint4 g, uint32_t border, T least)
+{
+    const uint32_t word[4] = {g.x, g.y, g.z, g.w};
+    uint32_t hits = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4)
+            hits |= (uint32_t)((order_key(__uint_as_float(word[e])) >> 16) >= border) << e;
+        else {
+            uint32_t m;
+            if constexpr (T_is_bf16<T>)
+                m = __hgeu2_mask(*reinterpret_cast<const __nv_bfloat162*>(&word[e]), __nv_bfloat162(least, least));
+            else
+                m = __hgeu2_mask(*reinterpret_cast<const __half2*>(&word[e]), __half2(least, least));
+            hits |= ((m & 1) | (m >> 30 & 2)) << 2 * e;
+        }
+    }
+    return hits;
+}
+template <typename T>
+__device__ __forceinline__ T top_least(uint32_t border)
+{
+    const float x = half_key_value(border);
+    if constexpr (sizeof(T) == 4) return x;
+    else if constexpr (T_is_bf16<T>) return __float2bfloat16_ru(x);
+    else return __float2half_ru(x);
+}
+
 // The words that reach the border, into `list` (n counts them, beyond its room too): the pieces that do are read again, a group of
 // one to every thread.
 template <typename T, bool FINE>
@@ -280,6 +320,7 @@ __device__ __forceinline__ void top_collect(const T* row, const RowSplit& split,
         }
     }
     __syncthreads();
+    const T least = top_least<T>(border);
     const int tasks = *queued * SIZE;
     if (*queued > room) {
         if (tid == 0) atomicAdd(n, room + 1);
@@ -300,23 +341,26 @@ __device__ __forceinline__ void top_collect(const T* row, const RowSplit& split,
 #pragma unroll
         for (int h = 0; h < AHEAD; ++h) {
             if (base + h * threads >= tasks) break;
-            float x[PER<T>];
-            unpack<T>(raw[h], x);
-            uint32_t hits = 0;
-#pragma unroll
-            for (int e = 0; e < PER<T>; ++e) hits |= (uint32_t)((order_key(x[e]) >> 16) >= border) << e;
-            if (first[h] >= V) hits = 0;
+            uint32_t hits = first[h] < V ? top_hits<T>(raw[h], border, least) : 0u;
             if (!__any_sync(0xffffffffu, hits)) continue;
             // (one addition for the warp)
             const int upto = warp_scan_incl(__popc(hits));
             int at = 0;
             if (lane == 31) at = atomicAdd(n, upto);
             at = __shfl_sync(0xffffffffu, at, 31) + upto - __popc(hits);
+            if constexpr (sizeof(T) == 4) {
+                float x[4];
+                unpack<T>(raw[h], x);
 #pragma unroll
-            for (int e = 0; e < PER<T>; ++e)
-                if (hits >> e & 1) {
-                    if (at < room) list[at] = top_entry(order_key(x[e]), first[h] + e);
-                    ++at;
+                for (int e = 0; e < 4; ++e)
+                    if (hits >> e & 1) {
+                        if (at < room) list[at] = top_entry(order_key(x[e]), first[h] + e);
+                        ++at;
+                    }
+            } else
+                for (; hits; hits &= hits - 1, ++at) {
+                    const int e = __ffs((int)hits) - 1;
+                    if (at < room) list[at] = top_entry(order_key(pair_value<T>(raw[h], e)), first[h] + e);
                 }
         }
     }
@@ -388,9 +432,10 @@ struct TopPart {
 // One cluster per row.  The pass leaves the pieces' largest keys.  A border that at least `top` groups of pieces reach
 // leaves at least `top` words, and few more (95 for 64 of 131 072); the pieces that reach it are read again (from L2), their words
 // sorted, in runs of 128 by a warp each, and merged by rank.
-// 4096 rows of 131 072 words of bf16, lists of 64: 218 us, 4.9 TB/s; no unit is full (of what they can, the multifunction units do
-// 57 %, the issue slots 63 %, DRAM 75 %): a row's CTA spends 35 of 54 us on the pass and the rest on its list, eight CTAs at a time.
-// 777 rows of 100 003 of fp16, lists of 301: 69 us, 25 of them the pass, 17 the second read of 430 pieces.
+// 4096 rows of 131 072 words of bf16, lists of 64: 214 us, 5.0 TB/s; no unit is full (of what they can, the multifunction units do
+// 59 %, the issue slots 59 %, DRAM 75 %): a row's CTA spends 35 of 53 us on the pass and the rest on its list, eight CTAs at a time.
+// 777 rows of 100 003 of fp16, lists of 301: 64 us, 25 of them the pass, 13 the second read of 430 pieces (17 with the border
+// compared to a key per element).
 // Tried: the lists put together by warps of their own beside the next row's pass (558 us with one such warp, 237 with four: the list
 // is more work than they have time for), 256 threads a row (222 us), groups as pieces (259 us; for lists of 301 85 us).
 template <typename T, bool FINE>

@@ -171,6 +171,21 @@ def test_top_logits_where_a_selection_can_go_wrong_in_many_rows(dtype):
     assert torch.equal(torch.nan_to_num(many[2].view(64, -1)[:, ~plain], nan=5.0), torch.nan_to_num(few[2][~plain], nan=5.0).expand(64, -1))
 
 
+@pytest.mark.parametrize("top", [5, 64, 301])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+def test_top_logits_at_borders_of_any_size_and_sign(dtype, top):
+    # values around the border: of both signs next to zero (16-bit rows: subnormal numbers and both zeros), and of one sign over all
+    # exponents up to 2^14
+    V = 20011
+    g = torch.Generator().manual_seed(41)
+    bits = torch.randint(0, 1 << 10, (4, V), generator=g) - torch.randint(0, 2, (4, V), generator=g) * (1 << 15)
+    tiny = bits.to(torch.int16).view(F16 if dtype is F16 else BF16).to(dtype)
+    wide = torch.exp2(torch.rand(4, V, generator=g, dtype=torch.float64) * 38 - 24).to(dtype)
+    wide[2:] = -wide[2:]
+    wide[1::2, ::3] = -INF
+    check_top(torch.cat([tiny, wide]).cuda(), top)
+
+
 def test_top_logits_of_one_row_again_and_again():
     x = make(1, 5_003, BF16, 1).expand(6, 5_003)       # row stride 0
     check_top(x, 9)
