@@ -218,7 +218,8 @@ struct DistillRow {
             }
         }
         l = warp_reduce_sum(l);
-        if (p_rest != 0.0f) l += p_rest_exact * log(p_rest_exact * (total / s_out));
+        // (log Q in logarithms: Q itself may be less than any number of 64 bits)
+        if (p_rest != 0.0f) l += p_rest_exact * (log(p_rest_exact / (double)out.sum) + log_total - ((double)out.ref - (double)ref) * LN2);
         return (float)(l * a.tau * a.tau);
     }
 };

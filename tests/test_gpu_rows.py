@@ -469,6 +469,82 @@ def test_distill_through_autograd(dtype):
         g.sum().backward()
 
 
+# --- a list far above or far below the words outside it -----------------------------------------------------------------------
+
+def check_apart(x, ids, values, lse, tau):
+    """Loss and gradient where the list and the words outside it lie any distance apart: all in logarithms, in 64 bits.
+
+    Errors.  log q: the exponents' factor c is rounded (2^-24 of |log q|, and as much of the distance between the two sums, which
+    counts by their share: 2^-24 of at most 1), both sums are `s` off, each by its own largest word.  p: ep as above, its logarithm
+    2^-24 |log p|; P is as far off as the sum of the p.  Gradient: one exponential more, relative to the largest on its side, or 0 below 2^-126."""
+    n, V = x.shape
+    d, at = x.cpu().double(), ids.cpu().long()
+    outside = torch.ones(n, V, dtype=torch.bool).scatter_(1, at, False)
+    listed, rest = torch.gather(d, 1, at) / tau, d.masked_fill(~outside, -INF) / tau
+    log_in, log_out = torch.logsumexp(listed, 1, keepdim=True), torch.logsumexp(rest, 1, keepdim=True)
+    log_z = torch.logaddexp(log_in, log_out)
+    a = values.cpu().double() / tau - lse.cpu().double()[:, None]
+    p = torch.exp(a)
+    p_rest = 1 - p.sum(1, keepdim=True)
+    assert float(p_rest.min()) > 0.1
+    log_q, log_q_rest = listed - log_z, log_out - log_z
+    ratio, rest_ratio = a - log_q, torch.log(p_rest) - log_q_rest
+    want_loss = tau**2 * ((p * ratio).sum(1) + (p_rest * rest_ratio)[:, 0])
+    s = torch.maximum(lse_error(listed * tau, tau), lse_error(rest * tau, tau))[:, None] + 2.0**-24
+    ep = 2.0**-22 + 2.0**-24 * a.abs().max(1, keepdim=True).values
+    off_p = ep * p.sum(1, keepdim=True)
+    loss_tol = (p * (2.0**-24 * (log_q.abs() + a.abs()) + s + ep * ratio.abs())).sum(1, keepdim=True) \
+        + p_rest * (2.0**-24 * log_q_rest.abs() + 2 * s) + off_p * (rest_ratio.abs() + 1)
+    loss_tol = tau**2 * loss_tol[:, 0]
+    mass = p.sum(1, keepdim=True) + p_rest
+    apart = torch.clamp((log_z - log_out) * 1.4427 * 2.0**-24, max=1.0)      # of e^(log_out - log_z)
+
+    def one(y):      # a word's exponential, by its distance from the largest on its side
+        return 2.0**-22 + 3 * 2.0**-24 * torch.nan_to_num((y.max(1, keepdim=True).values - y) * 1.4427, posinf=0.0) + 8 * 2.0**-24
+    q, share = torch.exp(rest - log_z), torch.exp(rest - log_out)
+    want = mass * q - p_rest * share
+    tol = (mass * q + p_rest * share) * (one(rest) + 2 * s) + mass * q * apart + share * off_p + 2.0**-126 * mass
+    q_list = torch.exp(log_q)
+    tol_list = mass * q_list * (one(listed) + 2 * s + torch.clamp((log_z - log_in) * 1.4427 * 2.0**-24, max=1.0)) \
+        + q_list * off_p + p * ep + 2.0**-126 * mass
+    want.scatter_(1, at, mass * q_list - p)
+    tol.scatter_(1, at, tol_list)
+    many = 1500 // n      # a CTA each
+    for times in (1, many):
+        again = [t.repeat(times, *[1] * (t.dim() - 1)) for t in (x, ids, values, lse)]
+        alone = rows.distill_loss(*again, temperature=tau)
+        loss, grad = rows.distill_loss_and_grad(*again, temperature=tau)
+        for part in (slice(0, n), slice((times - 1) * n, times * n)):
+            same(alone[part], want_loss, loss_tol, F32)
+            same(loss[part], want_loss, loss_tol, F32)
+            same(grad[part], tau * want, tau * tol, x.dtype)
+
+
+def apart(V, dtype, seed, tau, spread=3.0):
+    """Three rows of ordinary logits, in units of tau, and a teacher's lists of 40 with four tenths of its mass outside."""
+    x = (make(3, V, F32, seed, spread=spread) * tau).to(dtype)
+    ids, values, lse = lists_of((make(3, V, F32, seed + 1) * tau).to(dtype).cpu(), 40, tau, True, dtype)
+    p = torch.exp(values.double() / tau - lse.double()[:, None]).sum(1)
+    return x, ids, values, (lse.double() + torch.log(p / 0.6)).float()
+
+
+@pytest.mark.parametrize("V", [5_000, 40_000])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("tau,above", [(1.0, 600.0), (1.0, 800.0), (1.0, 1000.0), (1.0, 20_000.0), (0.01, 7.5), (0.01, 12.0), (30.0, 30_000.0)])
+def test_distill_list_far_above_the_words_outside(tau, above, dtype, V):
+    x, ids, values, lse = apart(V, dtype, 71, tau)
+    x.scatter_add_(1, ids.long(), torch.full((3, 40), above, dtype=dtype, device="cuda"))
+    check_apart(x, ids, values, lse, tau)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("low", [-1e4, -6e4])
+def test_distill_words_outside_the_list_at_a_low_value(low, dtype):
+    x, ids, values, lse = apart(6_000, dtype, 73, 1.0)
+    x = torch.full_like(x, low).scatter_(1, ids.long(), torch.gather(x, 1, ids.long()))
+    check_apart(x, ids, values, lse, 1.0)
+
+
 # --- verification of drafts --------------------------------------------------------------------------------------------------
 
 def verify_reference(offsets, drafts, target, probs, au, du):
