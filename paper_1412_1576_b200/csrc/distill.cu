@@ -225,22 +225,20 @@ struct DistillRow {
 };
 
 // The gradient: 2^(x c - ref) times `others` for a word outside the list; w (2^(x c - list_ref) listed - p) for one of the list.
+// The words outside are on a scale of their own: the bucket's part, -w P times their share of it, is as large where they have next to
+// nothing of the student's mass.
 struct DistillFactors {
     float ref, others, listed, w, list_ref;
     __device__ __forceinline__ DistillFactors(const DistillRow& row, float weight, double tau)
     {
         w = (float)((double)weight * tau);
-        list_ref = ref = row.ref;
-        const float gap = row.out.ref - row.ref, s_out = row.out.sum * exp2_whole(gap);
+        ref = row.out.ref;
+        list_ref = row.ref;
+        const float to_row = exp2_whole(ref - row.ref), s_out = row.out.sum * to_row;
         const float s_in = row.in.sum * exp2_whole(row.in.ref - row.ref), total = s_out + s_in, p_rest = row.p_rest;
         listed = total == 0.0f ? 0.0f : (row.sum_p + p_rest) / total;
-        // W / total - P / s_out, without the part that is in both
-        others = w * (p_rest != 0.0f ? (row.sum_p * s_out - p_rest * s_in) / s_out / total : listed);
-        if (gap < -100.0f) {
-            // less than 2^-80 of the student's mass is outside the list: it counts for the bucket alone, on a scale of its own
-            ref = row.out.ref;
-            others = p_rest != 0.0f ? -w * p_rest / row.out.sum : 0.0f;
-        }
+        // W to_row / total - P / out.sum, without the part that is in both
+        others = w * (p_rest != 0.0f ? (row.sum_p * s_out - p_rest * s_in) / (total * row.out.sum) : listed * to_row);
         if (weight == 0.0f) others = 0.0f;
     }
 };

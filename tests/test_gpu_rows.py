@@ -545,6 +545,15 @@ def test_distill_words_outside_the_list_at_a_low_value(low, dtype):
     check_apart(x, ids, values, lse, 1.0)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("above", [20.0, 41.0, 55.0, 64.0, 67.0, 68.5, 69.5, 75.0, 86.0])
+def test_distill_gradient_of_words_far_below_the_list(above, dtype):
+    """Words outside the list lie up to 50 below the largest of them, which itself lies `above` below the list."""
+    x, ids, values, lse = apart(5_000, dtype, 75, 1.0, spread=6.0)
+    x.scatter_(1, ids.long(), x.max(1, keepdim=True).values.expand(3, 40) + above)
+    check_apart(x, ids, values, lse, 1.0)
+
+
 # --- verification of drafts --------------------------------------------------------------------------------------------------
 
 def verify_reference(offsets, drafts, target, probs, au, du):
