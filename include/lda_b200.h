@@ -322,7 +322,8 @@ int lda_top_logits(const void* logits_dev, int dtype, int64_t rows, int32_t V, i
  *   p_j = exp(values_j / tau - teacher_lse) and P = max(0, 1 - sum p_j) for all words outside the list, whose q add up to Q
  *   (teacher_lse[rows]: the teacher's log sum exp(x / tau) over its whole row, as lda_top_logits gives it)
  *   loss = tau^2 ( sum_j p_j (log p_j - log q_{ids_j}) + P (log P - log Q) )
- * Where the student has no mass outside the list the last term is left out.  A word that the list holds twice counts with both
+ * Where the student has no mass outside the list (all its words are at minus infinity) the last term is left out.  Words at a large
+ * finite value, the type's lowest among them, are words: their log q is what it is.  A word that the list holds twice counts with both
  * entries.  A row whose list holds nothing but padding has loss 0 and gradient 0; otherwise a NaN in a row or in its list makes
  * the row's loss and gradient NaN. */
 int lda_distill_loss(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride,

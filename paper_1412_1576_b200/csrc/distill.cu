@@ -37,10 +37,25 @@ constexpr int DISTILL_GROUPS = 4;  // groups of a lane in a chunk
 // with three: 150 us for 147.
 __host__ __device__ constexpr int distill_depth(bool grad) { return grad ? 3 : 4; }
 
-// What a CTA knows of its part of the row.
+// What a CTA knows of its part of the row: exponentials of the words outside the list and of those on it, each word once (without a
+// tail: of all words, and none), and the largest value of the former.
 struct DistillPart {
-    ExpSum out, in;  // over the words outside the list and on it, each word once (without a tail: all words, nothing)
-    float max;
+    ExpSum out;
+    float in, max;
+};
+
+// What the exponentials of one side, outside or on the list, are relative to: 2^(x c - ref), or 2^((x - max) c) where `far`.  Each side
+// has its own, by its largest value: neither loses what it has to the other's distance, or to the row's from zero.
+struct DistillScale {
+    float ref, max;
+    bool far;
+    static __device__ __forceinline__ DistillScale of(float max, float c) { return DistillScale{exp_ref(max, c), max, exp_far(max, c)}; }
+    __device__ __forceinline__ float exponent(float x, float c) const { return far ? (x - max) * c : __fmaf_rn(x, c, -ref); }
+    // Where its exponents start; minus infinity for a side without mass.
+    __device__ __forceinline__ double origin(float sum, float c) const
+    {
+        return sum == 0.0f ? -INFINITY : far ? (double)max * (double)c : (double)ref;
+    }
 };
 
 // The list in shared memory, and a map with a bit for each word of the CTA's part.
@@ -112,18 +127,22 @@ __device__ __forceinline__ double distill_teacher(const DistillArgs& a, const Di
     return z == z ? 1.0 : z;
 }
 
-// Sum of the exponentials of the list's words in v0..v1-1, each once (by one warp).
-__device__ __forceinline__ ExpSum distill_listed(const DistillArgs& a, const DistillList& list, int v0, int v1, bool twice)
+// Largest of the student's logits of the list (by one warp).
+__device__ __forceinline__ float distill_list_max(const DistillArgs& a, const DistillList& list)
 {
-    ExpSum in = ExpSum::none();
-    for (int j = threadIdx.x & 31; j < a.top; j += 32) {
-        if (list.ids[j] < v0 || list.ids[j] >= v1 || !list.leads(j, twice)) continue;
-        const float x = list.x[j];
-        in.raise(exp_ref(x, a.scale));
-        in.sum += exp2_unit(__fmaf_rn(x, a.scale, -in.ref));
-    }
-    in.warp_reduce();
-    return in;
+    float m = -INFINITY;
+    for (int j = threadIdx.x & 31; j < a.top; j += 32)
+        if (list.ids[j] >= 0) m = fmaxf(m, list.x[j]);
+    return key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
+}
+
+// Sum of the exponentials of the list's words in v0..v1-1, each once (by one warp).
+__device__ __forceinline__ float distill_listed(const DistillArgs& a, const DistillList& list, int v0, int v1, bool twice, const DistillScale& scale)
+{
+    float in = 0.0f;
+    for (int j = threadIdx.x & 31; j < a.top; j += 32)
+        if (list.ids[j] >= v0 && list.ids[j] < v1 && list.leads(j, twice)) in += exp2_unit(scale.exponent(list.x[j], a.scale));
+    return warp_reduce_sum(in);
 }
 
 // Bits of a group's elements in the map.
@@ -134,16 +153,14 @@ __device__ __forceinline__ uint32_t group_bits(const uint32_t* bits, int group)
     return PER<T> == 8 ? byte : (byte >> (group * PER<T> % 8)) & ((1u << PER<T>) - 1);
 }
 
-// Minus infinity in the list's places of a lane's groups; `group`: the first one's number in the part.  Returns whether there are any.
+// Minus infinity in the list's places of a lane's groups; `group`: the first one's number in the part.
 template <typename T>
-__device__ __forceinline__ bool distill_mask(uint4 (&raw)[DISTILL_GROUPS], const uint32_t* bits, int group)
+__device__ __forceinline__ void distill_mask(uint4 (&raw)[DISTILL_GROUPS], const uint32_t* bits, int group)
 {
-    bool any = false;
 #pragma unroll
     for (int k = 0; k < DISTILL_GROUPS; ++k) {
         const uint32_t marked = group_bits<T>(bits, group + 32 * k);
         if (marked) {
-            any = true;
             union {
                 uint4 raw;
                 T e[PER<T>];
@@ -155,7 +172,6 @@ __device__ __forceinline__ bool distill_mask(uint4 (&raw)[DISTILL_GROUPS], const
             raw[k] = u.raw;
         }
     }
-    return any;
 }
 
 // Sum of 2^((x - m) c) over a warp's chunks of the part, the list's words left out (TAIL).
@@ -178,75 +194,77 @@ __device__ __noinline__ float distill_far_sum(const T* row, const RowSplit& spli
     return warp_reduce_sum(o);
 }
 
-// The row's sums from its parts: exponentials 2^(x c - ref), or 2^((x - max) c) where `far`.
+// The row's sums from its parts.
 struct DistillRow {
-    ExpSum out, in;
-    float max, ref;
+    DistillScale out_scale, in_scale;  // (without a tail the list's words are among the others: on their scale)
+    float out, in;
     float sum_p, p_rest;
-    bool far;
     template <bool TAIL>
-    static __device__ __forceinline__ DistillRow of(const DistillPart* parts, int ctas, float max, bool far, float sum_p, float p_rest)
+    static __device__ __forceinline__ DistillRow of(const DistillPart (*parts)[ROW_CTAS], int ctas, DistillScale out_scale, float in_max, float c,
+                                                    float sum_p, float p_rest)
     {
         DistillRow w;
-        w.max = max;
-        w.far = far;
-        w.sum_p = sum_p;
-        w.out = parts[0].out;
-        w.in = parts[0].in;
+        ExpSum out = parts[out_scale.far][0].out;
+        w.in = parts[0][0].in;
         for (int k = 1; k < ctas; ++k) {
-            w.out.add(parts[k].out);
-            w.in.add(parts[k].in);
+            out.add(parts[out_scale.far][k].out);
+            w.in += parts[0][k].in;
         }
-        w.ref = fmaxf(w.out.ref, w.in.ref);
-        w.p_rest = TAIL && w.out.sum != 0.0f ? p_rest : 0.0f;
+        w.out = out.sum;
+        w.out_scale = out_scale;
+        w.out_scale.ref = out.ref;
+        w.in_scale = TAIL ? DistillScale::of(in_max, c) : w.out_scale;
+        w.sum_p = sum_p;
+        w.p_rest = TAIL && w.out != 0.0f ? p_rest : 0.0f;
         return w;
     }
-    __device__ __forceinline__ float exponent(float x, float c, float r) const { return far ? (x - max) * c : __fmaf_rn(x, c, -r); }
     // The row's loss, by one warp, in 64 bits: it is a small difference of large logarithms where the student is near the teacher
     // (in single precision 1e-4 of a loss of 0.03, at 2 units of the last place of a logarithm of 17), and a listed word at the
     // type's lowest value has a finite log q.
     __device__ __forceinline__ float loss(const DistillArgs& a, const DistillList& list, double p_rest_exact) const
     {
-        const double s_out = ldexp((double)out.sum, (int)(out.ref - ref)), total = s_out + ldexp((double)in.sum, (int)(in.ref - ref));
+        const double c = a.scale, from_out = out_scale.origin(out, a.scale), from_in = in_scale.origin(in, a.scale);
+        const double from = fmax(fmax(from_out, from_in), -1e300), apart = from_out - from_in;
+        const double total = apart < 0 ? (double)in + (double)out * exp2(apart) : apart < INFINITY ? (double)out + (double)in * exp2(-apart) : (double)out;
         const double log_total = total == 0 ? 0.0 : log(total);  // (without mass log q is minus infinity)
         double l = 0;
         for (int j = threadIdx.x & 31; j < a.top; j += 32) {
             const float p = list.p[j];
-            if (p > 0.0f || p != p) {
-                const double x = (double)list.x[j], y = far ? (x - (double)max) * (double)a.scale : x * (double)a.scale - (double)ref;
-                l += (double)p * ((double)list.log_p[j] - (y * LN2 - log_total));
-            }
+            if (p > 0.0f || p != p) l += (double)p * ((double)list.log_p[j] - (((double)list.x[j] * c - from) * LN2 - log_total));
         }
         l = warp_reduce_sum(l);
         // (log Q in logarithms: Q itself may be less than any number of 64 bits)
-        if (p_rest != 0.0f) l += p_rest_exact * (log(p_rest_exact / (double)out.sum) + log_total - ((double)out.ref - (double)ref) * LN2);
+        if (p_rest != 0.0f) l += p_rest_exact * (log(p_rest_exact / (double)out) + log_total - (from_out - from) * LN2);
         return (float)(l * a.tau * a.tau);
     }
 };
 
-// The gradient: 2^(x c - ref) times `others` for a word outside the list; w (2^(x c - list_ref) listed - p) for one of the list.
-// The words outside are on a scale of their own: the bucket's part, -w P times their share of it, is as large where they have next to
-// nothing of the student's mass.
+// The gradient: e times `others` for a word outside the list, w (e listed - p) for one of the list, e by its side's scale.  So the
+// bucket's part, -w P times their share of it, is as large where the words outside have next to nothing of the student's mass.
 struct DistillFactors {
-    float ref, others, listed, w, list_ref;
-    __device__ __forceinline__ DistillFactors(const DistillRow& row, float weight, double tau)
+    float others, listed, w;
+    template <bool TAIL>
+    static __device__ __forceinline__ DistillFactors of(const DistillRow& row, float weight, double tau, float c)
     {
-        w = (float)((double)weight * tau);
-        ref = row.out.ref;
-        list_ref = row.ref;
-        const float to_row = exp2_whole(ref - row.ref), s_out = row.out.sum * to_row;
-        const float s_in = row.in.sum * exp2_whole(row.in.ref - row.ref), total = s_out + s_in, p_rest = row.p_rest;
-        listed = total == 0.0f ? 0.0f : (row.sum_p + p_rest) / total;
-        // W to_row / total - P / out.sum, without the part that is in both
-        others = w * (p_rest != 0.0f ? (row.sum_p * s_out - p_rest * s_in) / (total * row.out.sum) : listed * to_row);
-        if (weight == 0.0f) others = 0.0f;
+        DistillFactors f;
+        f.w = (float)((double)weight * tau);
+        // each side's scale to the larger one (without a tail there is one)
+        const float apart = TAIL ? (float)(row.out_scale.origin(row.out, c) - row.in_scale.origin(row.in, c)) : INFINITY;
+        const float out_to = apart < 0 ? exp2f(apart) : 1.0f, in_to = apart > 0 ? exp2f(-apart) : 1.0f;
+        const float s_out = row.out * out_to, s_in = row.in * in_to, total = s_out + s_in, p_rest = row.p_rest;
+        const float each = total == 0.0f ? 0.0f : (row.sum_p + p_rest) / total;
+        f.listed = each * (TAIL ? in_to : out_to);
+        // W out_to / total - P / out, without the part that is in both
+        f.others = f.w * (p_rest != 0.0f ? (row.sum_p * s_out - p_rest * s_in) / (total * row.out) : each * out_to);
+        if (weight == 0.0f) f.others = 0.0f;
+        return f;
     }
 };
 
 // The gradient of a lane's groups of a chunk as if no word were listed; `stage`: the lane's places of the walk's ring.
 template <typename T, typename Walk>
 __device__ __forceinline__ void distill_put(T* grad, int first, int V, uint4 (&raw)[DISTILL_GROUPS], const DistillFactors& f,
-                                            const DistillRow& w, float c, bool zero, bool abreast, const Walk& walk, int slot)
+                                            const DistillScale& scale, float c, bool zero, bool abreast, const Walk& walk, int slot)
 {
     constexpr int R = DISTILL_GROUPS;
     const int lane = threadIdx.x & 31;
@@ -254,16 +272,16 @@ __device__ __forceinline__ void distill_put(T* grad, int first, int V, uint4 (&r
     for (int k = 0; k < R; ++k) {
         float y[PER<T>];
         unpack<T>(raw[k], y);
-        if (!w.far) {
+        if (!scale.far) {
 #pragma unroll
             for (int i = 0; i < PER<T>; i += 2) {
-                const float2 e = fma_two(make_float2(y[i], y[i + 1]), make_float2(c, c), make_float2(-f.ref, -f.ref));
+                const float2 e = fma_two(make_float2(y[i], y[i + 1]), make_float2(c, c), make_float2(-scale.ref, -scale.ref));
                 const float2 g = mul_two(make_float2(exp2_unit(e.x), exp2_unit(e.y)), make_float2(f.others, f.others));
                 y[i] = g.x, y[i + 1] = g.y;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit((y[i] - w.max) * c) * f.others;
+            for (int i = 0; i < PER<T>; ++i) y[i] = exp2_unit((y[i] - scale.max) * c) * f.others;
         }
         raw[k] = zero ? make_uint4(0, 0, 0, 0) : pack<T>(y);
     }
@@ -292,7 +310,7 @@ __device__ __forceinline__ void distill_put(T* grad, int first, int V, uint4 (&r
 // The list's words over that, by threads tid, tid + threads, ...
 template <typename T>
 __device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, const DistillList& list, int v0, int v1, bool twice,
-                                                 const DistillFactors& f, const DistillRow& w, int tid, int threads)
+                                                 const DistillFactors& f, const DistillScale& scale, int tid, int threads)
 {
     for (int j = tid; j < a.top; j += threads) {
         const int id = list.ids[j];
@@ -301,7 +319,7 @@ __device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, 
         if (twice)
             for (int o = j + 1; o < a.top; ++o)
                 if (list.ids[o] == id) p += list.p[o];
-        grad[id] = row_element<T>(f.w * (exp2_unit(w.exponent(list.x[j], a.scale, f.list_ref)) * f.listed - p));
+        grad[id] = row_element<T>(f.w * (exp2_unit(scale.exponent(list.x[j], a.scale)) * f.listed - p));
     }
 }
 
@@ -326,7 +344,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ DistillPart parts[2][ROW_CTAS];
     __shared__ double s_rest;
-    __shared__ float s_sum_p, s_p_rest;
+    __shared__ float s_sum_p, s_p_rest, s_list_max;
     __shared__ int s_any, s_twice;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -394,9 +412,9 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     ExpSum out = ExpSum::none();
     float m = -INFINITY;
     walk.each(row, split, V, none, [&](int chunk, int, uint4(&raw)[R]) {
-        float top = groups_max<T, R>(raw);
+        if (TAIL) distill_mask<T>(raw, list.bits, (chunk - split.chunk0) * 32 * R + lane);
+        const float top = groups_max<T, R>(raw);
         m = fmaxf(m, top);  // (a NaN goes into the sums)
-        if (TAIL && distill_mask<T>(raw, list.bits, (chunk - split.chunk0) * 32 * R + lane)) top = groups_max<T, R>(raw);
         add_groups<T, R>(out, raw, top, a.scale);
     });
     out.warp_reduce();
@@ -408,9 +426,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         if (j < a.top) list.x[j] = id[i] >= 0 ? row_value(own[i]) : 0.0f;
     }
     __syncthreads();
-    ExpSum in = ExpSum::none();
+    float in = 0.0f;
     if (warp == 0) {
-        if (TAIL) in = distill_listed(a, list, v0, v1, twice);
+        if (TAIL) {
+            const float most = distill_list_max(a, list);
+            in = distill_listed(a, list, v0, v1, twice, DistillScale::of(most, a.scale));
+            if (lane == 0) s_list_max = most;
+        }
         out = lane < warps ? ered[lane] : ExpSum::none();
         out.warp_reduce();
         m = warp_reduce_max(lane < warps ? fred[lane] : -INFINITY);
@@ -422,32 +444,28 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     for (int k = 1; k < ctas; ++k) m = fmaxf(m, parts[0][k].max);
     const bool far = exp_far(m, a.scale);
     if (far) {  // (the same in every CTA of the cluster)
-        float o = distill_far_sum<T, TAIL>(row, split, V, m, a.scale, list.bits, warps), l = 0.0f;
-        if (TAIL && warp == 0)
-            for (int j = lane; j < a.top; j += 32)
-                if (list.ids[j] >= v0 && list.ids[j] < v1 && list.leads(j, twice)) l += exp2_unit((list.x[j] - m) * a.scale);
-        l = warp_reduce_sum(l);
+        float o = distill_far_sum<T, TAIL>(row, split, V, m, a.scale, list.bits, warps);
         if (lane == 0) fred[warp] = o;
         __syncthreads();
         if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
-        if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = DistillPart{{0.0f, o}, {0.0f, l}, m};
+        if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = DistillPart{{0.0f, o}, 0.0f, m};
         row_sync(cluster, ctas);
     }
     if (!GRAD && (warp != 0 || rank != 0)) return;
-    const DistillRow whole = DistillRow::of<TAIL>(parts[far], ctas, m, far, s_sum_p, s_p_rest);
+    const DistillRow whole = DistillRow::of<TAIL>(parts, ctas, DistillScale{0.0f, m, far}, s_list_max, a.scale, s_sum_p, s_p_rest);
     if (a.loss && rank == 0 && warp == 0) {
         const float l = whole.loss(a, list, s_rest);
         if (lane == 0) a.loss[r] = l;
     }
     if (!GRAD) return;
-    const DistillFactors f(whole, weight, a.tau);
+    const DistillFactors f = DistillFactors::of<TAIL>(whole, weight, a.tau, a.scale);
     const bool abreast = (uintptr_t)grad % 16 == (uintptr_t)row % 16;
     walk.back(row, split, V, none, [&](int chunk, int slot, uint4(&raw)[R]) {
-        distill_put<T>(grad, chunk_first<T, R>(chunk, split.pre), V, raw, f, whole, a.scale, weight == 0.0f, abreast, walk, slot);
+        distill_put<T>(grad, chunk_first<T, R>(chunk, split.pre), V, raw, f, whole.out_scale, a.scale, weight == 0.0f, abreast, walk, slot);
     });
     if (weight == 0.0f) return;
     __syncthreads();
-    distill_put_list<T>(grad, a, list, v0, v1, twice, f, whole, tid, threads);
+    distill_put_list<T>(grad, a, list, v0, v1, twice, f, whole.in_scale, tid, threads);
 }
 
 template <typename T>

@@ -60,6 +60,7 @@ __device__ __forceinline__ uint32_t order_key(float x)
     const uint32_t b = __float_as_uint(x + 0.0f);
     return x != x ? KEY_NAN : b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
+__device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key); }
 
 __device__ __forceinline__ float warp_reduce_max(float v)
 {

@@ -198,11 +198,7 @@ __host__ __device__ constexpr int top_groups(int threads, int top)
 }
 
 // The value of a half-key.
-__device__ __forceinline__ float half_key_value(uint32_t k)
-{
-    const uint32_t key = k << 16;
-    return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key);
-}
+__device__ __forceinline__ float half_key_value(uint32_t k) { return key_value(k << 16); }
 
 // A half-key that at least `want` of the groups reach, and not more than `spare` others if there is one; lo: one that at least `want`
 // reach, hi: above all that do.  Every warp tries another one at a time, at equal distances between what is too low and what is too

@@ -165,7 +165,8 @@ def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
 
     ids, values: the teacher's lists, as ``top_logits`` gives them; an id outside the vocabulary is padding.  lse None: the
     teacher's distribution is the softmax over the list.  With the teacher's log-sum-exp (taken at the same temperature) it
-    is that of its whole row, and all words outside the list make one bucket more.  Differentiable once, with respect to
+    is that of its whole row, and all words outside the list make one bucket more, unless the student has them all masked, with
+    minus infinity (a large negative number is a logit like any other).  Differentiable once, with respect to
     ``logits`` alone (the teacher is a constant); a row that gets the gradient 0 passes 0 on, whatever it holds.  A backward pass that is
     captured into a CUDA graph needs, as always with torch, that no eager graph of the same leaves is alive;
     ``distill_loss_and_grad`` does not.

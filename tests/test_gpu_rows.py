@@ -501,10 +501,11 @@ def check_apart(x, ids, values, lse, tau):
 
     def one(y):      # a word's exponential, by its distance from the largest on its side
         return 2.0**-22 + 3 * 2.0**-24 * torch.nan_to_num((y.max(1, keepdim=True).values - y) * 1.4427, posinf=0.0) + 8 * 2.0**-24
-    q, share = torch.exp(rest - log_z), torch.exp(rest - log_out)
+    share = torch.softmax(rest, 1)      # (by differences of the logits: at the lowest values a logarithm has no places for their number)
+    q = share * torch.exp(log_out - log_z)
     want = mass * q - p_rest * share
     tol = (mass * q + p_rest * share) * (one(rest) + 2 * s) + mass * q * apart + share * off_p + 2.0**-126 * mass
-    q_list = torch.exp(log_q)
+    q_list = torch.softmax(listed, 1) * torch.exp(log_in - log_z)
     tol_list = mass * q_list * (one(listed) + 2 * s + torch.clamp((log_z - log_in) * 1.4427 * 2.0**-24, max=1.0)) \
         + q_list * off_p + p * ep + 2.0**-126 * mass
     want.scatter_(1, at, mass * q_list - p)
@@ -552,6 +553,45 @@ def test_distill_gradient_of_words_far_below_the_list(above, dtype):
     x, ids, values, lse = apart(5_000, dtype, 75, 1.0, spread=6.0)
     x.scatter_(1, ids.long(), x.max(1, keepdim=True).values.expand(3, 40) + above)
     check_apart(x, ids, values, lse, 1.0)
+
+
+@pytest.mark.parametrize("above", [0.0, 100.0, 150.0, 2000.0, -40.0, -150.0, -2000.0])
+@pytest.mark.parametrize("base", [0.0, 3000.0, -3000.0, 2.0**15])
+def test_distill_does_not_depend_on_a_constant_added_to_the_row(base, above):
+    """At this temperature rows that lie 3000 from zero have exponents beyond 2^22 (2^15: beyond 2^25).  All sums are exact."""
+    tau, V = 1e-3, 40_000
+    x, ids, values, lse = apart(V, F32, 77, tau)
+    x = torch.round(x * 2.0**8) / 2.0**8               # (with the base, at most 24 bits)
+    x.scatter_add_(1, ids.long(), torch.full((3, 40), round(above * tau * 2**8) / 2**8, device="cuda"))
+    check_apart(x + base, ids, values, lse, tau)
+
+
+@pytest.mark.parametrize("V", [5_000, 40_000])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("side", ["outside", "list"])
+def test_distill_one_side_at_the_lowest_value(side, dtype, V):
+    """Words at the type's lowest value are words: only minus infinity has no mass."""
+    tau = 0.5                                           # (tau^2 times the lowest value is still a number)
+    x, ids, values, lse = apart(V, dtype, 79, tau)
+    at, low = ids.long(), torch.finfo(dtype).min
+    if side == "outside":
+        x = torch.full_like(x, low).scatter_(1, at, torch.gather(x, 1, at))
+    else:
+        x.scatter_(1, at, low)
+    check_apart(x, ids, values, lse, tau)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+def test_distill_rows_far_from_zero_in_steps_of_their_type(dtype):
+    tau = 1e-3
+    x, ids, values, lse = apart(5_000, dtype, 81, 1.0)
+    values, lse = values * tau, lse * 1.0
+    values = (values.float()).to(F32)
+    p = torch.exp(values.double() / tau - lse.double()[:, None]).sum(1)
+    lse = (lse.double() + torch.log(p / 0.6)).float()
+    steps = torch.randint(0, 4, (3, 5_000), generator=torch.Generator().manual_seed(5)).cuda()
+    x = (2944 + 16 * steps).to(dtype)                  # 23 000 powers of two from one to the next
+    check_apart(x, ids, values, lse, tau)
 
 
 # --- verification of drafts --------------------------------------------------------------------------------------------------
