@@ -61,11 +61,11 @@ struct DistillScale {
 // The list in shared memory, and a map with a bit for each word of the CTA's part.
 struct DistillList {
     int* ids;                // -1: padding
-    float *p, *log_p, *x;    // the teacher's probabilities (at first: its logits), the student's logits
+    float *p, *t, *x;        // the teacher's exponentials (with a tail: probabilities) and logits, the student's logits
     uint32_t* bits;
     static __host__ __device__ constexpr int bytes(int top, int bits_bytes) { return (16 * top + bits_bytes + 15) / 16 * 16; }
     __device__ __forceinline__ DistillList(void* at, int top)
-        : ids((int*)at), p((float*)at + top), log_p((float*)at + 2 * top), x((float*)at + 3 * top), bits((uint32_t*)at + 4 * top)
+        : ids((int*)at), p((float*)at + top), t((float*)at + 2 * top), x((float*)at + 3 * top), bits((uint32_t*)at + 4 * top)
     {
     }
     // Whether place j stands for its word, which the list may hold twice: the first does.
@@ -96,35 +96,36 @@ struct DistillSpan {
 template <typename T>
 __host__ __device__ constexpr int distill_bits(int chunks) { return chunks * (32 * DISTILL_GROUPS * PER<T> / 8); }
 
-// The teacher's probabilities (by one warp): p and log_p from the logits in p; returns the sum of p.
-template <bool TAIL>
-__device__ __forceinline__ double distill_teacher(const DistillArgs& a, const DistillList& list, float teacher_lse)
+// Logarithm of a teacher's exponential e^(t / tau - shift), and the exponential in 64 bits from what expf makes of it in 32, at most two
+// units of the last place off: the rounding of its argument, much larger for small probabilities, is taken out.
+struct DistillTeacher {
+    double inv_tau, shift;  // shift: the teacher's log-sum-exp, or the largest of the list
+    __device__ __forceinline__ double log_of(float t) const { return (double)t * inv_tau - shift; }
+    static __device__ __forceinline__ double exact(float e, double log_e) { return (double)e * (1.0 + (log_e - (double)(float)log_e)); }
+};
+
+// The teacher's exponentials (by one warp); returns their sum.
+__device__ __forceinline__ double distill_teacher(const DistillArgs& a, const DistillList& list, const DistillTeacher& teacher)
 {
-    const int lane = threadIdx.x & 31;
-    float max_t = -INFINITY;
     double z = 0;
-    if (!TAIL) {
-        for (int j = lane; j < a.top; j += 32)
-            if (list.ids[j] >= 0) max_t = fmaxf(max_t, list.p[j]);
-        max_t = warp_reduce_max(max_t);
-    }
-    for (int j = lane; j < a.top; j += 32) {
-        const float t = list.p[j];
-        float l = (float)(TAIL ? (double)t * a.inv_tau - (double)teacher_lse : ((double)t - (double)max_t) * a.inv_tau);
-        if (list.ids[j] < 0 || t == -INFINITY) l = -INFINITY;
-        const float e = l == -INFINITY ? 0.0f : expf(l);
-        list.log_p[j] = l;
+    for (int j = threadIdx.x & 31; j < a.top; j += 32) {
+        const float t = list.t[j];
+        const double l = teacher.log_of(t);
+        const bool none = list.ids[j] < 0 || t == -INFINITY;
+        const float e = none ? 0.0f : expf((float)l);
         list.p[j] = e;
-        z += (double)e;
+        if (!none) z += DistillTeacher::exact(e, l);
     }
-    z = warp_reduce_sum(z);
-    if (TAIL || !(z > 0 || z != z)) return z;  // (a list of nothing but minus infinity has no mass)
-    const float log_z = logf((float)z), all = (float)z;
-    for (int j = lane; j < a.top; j += 32) {
-        list.p[j] = list.p[j] / all;
-        list.log_p[j] -= log_z;
-    }
-    return z == z ? 1.0 : z;
+    return warp_reduce_sum(z);
+}
+
+// Largest of the teacher's logits of the list (by one warp).
+__device__ __forceinline__ float distill_teacher_max(const DistillArgs& a, const DistillList& list)
+{
+    float m = -INFINITY;
+    for (int j = threadIdx.x & 31; j < a.top; j += 32)
+        if (list.ids[j] >= 0) m = fmaxf(m, list.t[j]);
+    return warp_reduce_max(m);
 }
 
 // Largest of the student's logits of the list (by one warp).
@@ -198,7 +199,7 @@ __device__ __noinline__ float distill_far_sum(const T* row, const RowSplit& spli
 struct DistillRow {
     DistillScale out_scale, in_scale;  // (without a tail the list's words are among the others: on their scale)
     float out, in;
-    float sum_p, p_rest;
+    float sum_p, p_rest;  // the teacher's probabilities: on the list, outside
     template <bool TAIL>
     static __device__ __forceinline__ DistillRow of(const DistillPart (*parts)[ROW_CTAS], int ctas, DistillScale out_scale, float in_max, float c,
                                                     float sum_p, float p_rest)
@@ -220,8 +221,9 @@ struct DistillRow {
     }
     // The row's loss, by one warp, in 64 bits: it is a small difference of large logarithms where the student is near the teacher
     // (in single precision 1e-4 of a loss of 0.03, at 2 units of the last place of a logarithm of 17), and a listed word at the
-    // type's lowest value has a finite log q.
-    __device__ __forceinline__ float loss(const DistillArgs& a, const DistillList& list, double p_rest_exact) const
+    // type's lowest value has a finite log q.  z: the sum of the teacher's exponentials.
+    template <bool TAIL>
+    __device__ __forceinline__ float loss(const DistillArgs& a, const DistillList& list, const DistillTeacher& teacher, double z) const
     {
         const double c = a.scale, from_out = out_scale.origin(out, a.scale), from_in = in_scale.origin(in, a.scale);
         const double from = fmax(fmax(from_out, from_in), -1e300), apart = from_out - from_in;
@@ -229,12 +231,15 @@ struct DistillRow {
         const double log_total = total == 0 ? 0.0 : log(total);  // (without mass log q is minus infinity)
         double l = 0;
         for (int j = threadIdx.x & 31; j < a.top; j += 32) {
-            const float p = list.p[j];
-            if (p > 0.0f || p != p) l += (double)p * ((double)list.log_p[j] - (((double)list.x[j] * c - from) * LN2 - log_total));
+            const float e = list.p[j];
+            if (!(e > 0.0f || e != e)) continue;
+            const double log_p = teacher.log_of(list.t[j]);
+            l += DistillTeacher::exact(e, log_p) * (log_p - (((double)list.x[j] * c - from) * LN2 - log_total));
         }
         l = warp_reduce_sum(l);
+        if (!TAIL) l = z == 0 ? 0.0 : l / z - log(z);
         // (log Q in logarithms: Q itself may be less than any number of 64 bits)
-        if (p_rest != 0.0f) l += p_rest_exact * (log(p_rest_exact / (double)out) + log_total - (from_out - from) * LN2);
+        else if (p_rest != 0.0f) l += (1 - z) * (log((1 - z) / (double)out) + log_total - (from_out - from) * LN2);
         return (float)(l * a.tau * a.tau);
     }
 };
@@ -307,10 +312,10 @@ __device__ __forceinline__ void distill_put(T* grad, int first, int V, uint4 (&r
     }
 }
 
-// The list's words over that, by threads tid, tid + threads, ...
+// The list's words over that, by threads tid, tid + threads, ...; all: what the teacher's exponentials are divided by.
 template <typename T>
 __device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, const DistillList& list, int v0, int v1, bool twice,
-                                                 const DistillFactors& f, const DistillScale& scale, int tid, int threads)
+                                                 const DistillFactors& f, const DistillScale& scale, float all, int tid, int threads)
 {
     for (int j = tid; j < a.top; j += threads) {
         const int id = list.ids[j];
@@ -319,7 +324,7 @@ __device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, 
         if (twice)
             for (int o = j + 1; o < a.top; ++o)
                 if (list.ids[o] == id) p += list.p[o];
-        grad[id] = row_element<T>(f.w * (exp2_unit(scale.exponent(list.x[j], a.scale)) * f.listed - p));
+        grad[id] = row_element<T>(f.w * (exp2_unit(scale.exponent(list.x[j], a.scale)) * f.listed - p / all));
     }
 }
 
@@ -343,8 +348,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     __shared__ ExpSum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ DistillPart parts[2][ROW_CTAS];
-    __shared__ double s_rest;
-    __shared__ float s_sum_p, s_p_rest, s_list_max;
+    __shared__ double s_z;
+    __shared__ float s_max_t, s_list_max;
     __shared__ int s_any, s_twice;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -384,7 +389,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         if (j >= a.top) break;
         const bool ok = id[i] >= 0 && id[i] < V;
         if (!ok) id[i] = -1;
-        list.p[j] = t[i];
+        list.t[j] = t[i];
         list.ids[j] = id[i];
         if (ok) {
             s_any = 1;
@@ -406,8 +411,9 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     }
     if (ctas > 1) cluster_arrive();
     if (warp == 0) {
-        const double sum_p = distill_teacher<TAIL>(a, list, teacher_lse), rest = sum_p != sum_p ? sum_p : fmax(0.0, 1.0 - sum_p);
-        if (lane == 0) s_rest = rest, s_sum_p = (float)sum_p, s_p_rest = (float)rest;
+        const float max_t = TAIL ? 0.0f : distill_teacher_max(a, list);
+        const double z = distill_teacher(a, list, DistillTeacher{a.inv_tau, TAIL ? (double)teacher_lse : (double)max_t * a.inv_tau});
+        if (lane == 0) s_z = z, s_max_t = max_t;
     }
     ExpSum out = ExpSum::none();
     float m = -INFINITY;
@@ -452,9 +458,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
         row_sync(cluster, ctas);
     }
     if (!GRAD && (warp != 0 || rank != 0)) return;
-    const DistillRow whole = DistillRow::of<TAIL>(parts, ctas, DistillScale{0.0f, m, far}, s_list_max, a.scale, s_sum_p, s_p_rest);
+    const double z = s_z;  // (a list of nothing but minus infinity has no mass)
+    const float sum_p = TAIL || z == 0 || z != z ? (float)z : 1.0f, p_rest = !TAIL ? 0.0f : z != z ? (float)z : (float)fmax(0.0, 1 - z);
+    const DistillRow whole = DistillRow::of<TAIL>(parts, ctas, DistillScale{0.0f, m, far}, s_list_max, a.scale, sum_p, p_rest);
     if (a.loss && rank == 0 && warp == 0) {
-        const float l = whole.loss(a, list, s_rest);
+        const float l = whole.loss<TAIL>(a, list, DistillTeacher{a.inv_tau, TAIL ? (double)teacher_lse : (double)s_max_t * a.inv_tau}, z);
         if (lane == 0) a.loss[r] = l;
     }
     if (!GRAD) return;
@@ -465,7 +473,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_distill(DistillArgs a)
     });
     if (weight == 0.0f) return;
     __syncthreads();
-    distill_put_list<T>(grad, a, list, v0, v1, twice, f, whole.in_scale, tid, threads);
+    distill_put_list<T>(grad, a, list, v0, v1, twice, f, whole.in_scale, TAIL || z == 0 ? 1.0f : (float)z, tid, threads);
 }
 
 template <typename T>

@@ -594,6 +594,27 @@ def test_distill_rows_far_from_zero_in_steps_of_their_type(dtype):
     check_apart(x, ids, values, lse, tau)
 
 
+@pytest.mark.parametrize("top", [300, 512, 37])
+@pytest.mark.parametrize("tail", [False, True], ids=["list", "tail"])
+def test_distill_student_that_has_learnt_its_teacher(tail, top):
+    """All words alike on both sides: the student's exponentials and sums are exact, and so are the list's e^0; what is left is the
+    logarithms', in 64 bits.  With a tail p is expf's, two units of the last place off at most (2^-22), and P by as much the other way:
+    with both ratios next to 1 the loss moves by that, its own derivative, and by its square."""
+    V = top if not tail else 2 * top
+    x = torch.zeros(2, V, device="cuda")
+    ids = torch.arange(top, dtype=torch.int32, device="cuda").repeat(2, 1)
+    values = torch.zeros(2, top, device="cuda")
+    lse = torch.full((2,), math.log(V), device="cuda") if tail else None
+    want, bound = 0.0, 1e-12
+    if tail:
+        a = -float(lse[0])
+        p = top * math.exp(a)
+        want = p * (a + math.log(V)) + (1 - p) * (math.log(1 - p) + math.log(2))
+        bound += p * 2.0**-22 * (1 + 2.0**-20)
+    got = rows.distill_loss(x, ids, values, lse).cpu().double()
+    assert bool(((got - want).abs() <= bound + 2.0**-24 * abs(want)).all()), (got, want)
+
+
 # --- verification of drafts --------------------------------------------------------------------------------------------------
 
 def verify_reference(offsets, drafts, target, probs, au, du):
