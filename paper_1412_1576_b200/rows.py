@@ -9,6 +9,7 @@ the current stream of the tensors' device.  There is no fallback: tensors that a
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as _b
 
@@ -166,11 +167,14 @@ def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
     ids, values: the teacher's lists, as ``top_logits`` gives them; an id outside the vocabulary is padding.  lse None: the
     teacher's distribution is the softmax over the list.  With the teacher's log-sum-exp (taken at the same temperature) it
     is that of its whole row, and all words outside the list make one bucket more, unless the student has them all masked, with
-    minus infinity (a large negative number is a logit like any other).  Differentiable once, with respect to
+    minus infinity (a large negative number is a logit like any other).  Differentiable once, in reverse mode, with respect to
     ``logits`` alone (the teacher is a constant); a row that gets the gradient 0 passes 0 on, whatever it holds.  A backward pass that is
     captured into a CUDA graph needs, as always with torch, that no eager graph of the same leaves is alive;
     ``distill_loss_and_grad`` does not.
     """
+    # (a tangent is lost outside of autograd's function, which has no forward mode and says so)
+    if forward_ad.unpack_dual(logits).tangent is not None:
+        raise NotImplementedError("distill_loss: forward-mode differentiation is not offered")
     if torch.is_grad_enabled() and logits.requires_grad:
         return _Distill.apply(logits, ids, values, lse, temperature)
     return _loss(logits, ids, values, lse, temperature)

@@ -1,6 +1,7 @@
 """What the operators on rows refuse, before anything reaches a GPU (the statuses of the C ABI, the binding's checks)."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_1412_1576_b200 import binding as b
 from paper_1412_1576_b200 import rows
@@ -129,3 +130,18 @@ def test_drafts_that_are_no_vector_are_refused(monkeypatch, shape):
     n = drafts.numel()
     with pytest.raises(ValueError, match="drafts"):
         rows.verify_drafts(torch.tensor([0, n]), drafts, torch.zeros(n + 1, 10), None, torch.zeros(n), torch.zeros(1))
+
+
+def test_forward_mode_is_refused(monkeypatch):
+    # (a tensor with a tangent need not require a gradient; no GPU: the library's calls are left out)
+    monkeypatch.setattr(rows, "_cuda", lambda x, name: x.device)
+    monkeypatch.setattr(rows, "_call", lambda name, device, *args: None)
+    x, ids, values = torch.zeros(2, 10), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3)
+    with forward_ad.dual_level():
+        for primal in (x, x.clone().requires_grad_()):
+            dual = forward_ad.make_dual(primal, torch.ones(2, 10))
+            with pytest.raises(NotImplementedError):
+                rows.distill_loss(dual, ids, values)
+            with torch.no_grad(), pytest.raises(NotImplementedError):
+                rows.distill_loss(dual, ids, values)
+        assert rows.distill_loss(x, ids, values).shape == (2,)      # without a tangent nothing is lost
