@@ -3,16 +3,21 @@
 What a neural model of the sampler's words needs beside the sampler: a teacher's lists (``top_logits``), a drafter's loss
 against them (``distill_loss``, ``distill_loss_and_grad``), and the test that accepts the drafter's tokens (``verify_drafts``).
 Argument checks and outputs only: the work is done by the entry points of the same purpose in ``include/lda_b200.h``, queued on
-the current stream of the tensors' device.  There is no fallback: tensors that are not on a GPU are refused.
+the current stream of the tensors' device.  There is no fallback: tensors that are not on a GPU are refused, and so is tracing
+(``torch.compile`` leaves the calls outside of its graphs).
 """
 
 from __future__ import annotations
 
 import torch
 from torch.autograd import forward_ad
+from torch.fx.experimental.proxy_tensor import get_proxy_mode
 
 from . import binding as _b
 
+# (whether torch.jit or a dispatch mode, a tracer's among them, is at work: a third of a microsecond together)
+_jit_tracing, _modes = torch._C._is_tracing, torch._C._len_torch_dispatch_stack
+_modes_before_dispatch = torch._ops._len_torch_dispatch_stack_pre_dispatch
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 _DTYPES = {torch.float32: _b.LDA_F32, torch.float16: _b.LDA_F16, torch.bfloat16: _b.LDA_BF16}
 
@@ -49,6 +54,9 @@ def _here(x, name, device):
 
 
 def _cuda(x, name):
+    # (a tracer sees the outputs' allocation, not the library's call that fills them)
+    if _jit_tracing() or (_modes() or _modes_before_dispatch()) and get_proxy_mode() is not None:
+        raise RuntimeError(f"{name}: operators on rows cannot be traced")
     if not x.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed (there is no CPU fallback)")
     return x.device
@@ -173,7 +181,7 @@ def distill_loss(logits, ids, values, lse=None, temperature: float = 1.0):
     ``distill_loss_and_grad`` does not.
     """
     # (a tangent is lost outside of autograd's function, which has no forward mode and says so)
-    if forward_ad.unpack_dual(logits).tangent is not None:
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(logits).tangent is not None:
         raise NotImplementedError("distill_loss: forward-mode differentiation is not offered")
     if torch.is_grad_enabled() and logits.requires_grad:
         return _Distill.apply(logits, ids, values, lse, temperature)

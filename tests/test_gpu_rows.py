@@ -884,6 +884,29 @@ def test_a_captured_training_step(through):
     assert eager is None or eager.requires_grad
 
 
+def test_calls_from_compiled_functions():
+    """The calls stay outside of a compiled function's graphs: other inputs, another stream, and a backward pass through them."""
+    x, ids, values, lse, w, args = inputs(13, V=5_003, dtype=F32)
+    top = torch.compile(lambda t: rows.top_logits(t * 1.0, 48), backend="eager")
+    learn = torch.compile(lambda t: rows.distill_loss(t * 1.0, ids, values, lse), backend="eager")
+    both = torch.compile(lambda t: rows.distill_loss_and_grad(t * 1.0, ids, values, lse, weights=w), backend="eager")
+    verify = torch.compile(lambda p: rows.verify_drafts(args[0], args[1], p * 1.0, *args[3:]), backend="eager")
+    for k in range(3):
+        fresh = make(9, 5_003, F32, 14 + k)
+        target = torch.softmax(make(10, 5_003, F32, 24 + k), 1)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side if k else torch.cuda.current_stream()):
+            got = (*top(fresh), learn(fresh), *both(fresh), *verify(target))
+        torch.cuda.synchronize()
+        want = (*rows.top_logits(fresh, 48), rows.distill_loss(fresh, ids, values, lse),
+                *rows.distill_loss_and_grad(fresh, ids, values, lse, weights=w), *rows.verify_drafts(args[0], args[1], target, *args[3:]))
+        assert all(torch.equal(a, c) for a, c in zip(got, want))
+    student = x.clone().requires_grad_()
+    (learn(student) * w).sum().backward()
+    assert torch.equal(student.grad, rows.distill_loss_and_grad(x, ids, values, lse, weights=w)[1])
+
+
 FIRST_IN_A_CAPTURE = """
 import sys
 sys.path[:0] = [{root!r}, {tests!r}]

@@ -2,6 +2,7 @@
 import pytest
 import torch
 from torch.autograd import forward_ad
+from torch.fx.experimental.proxy_tensor import make_fx
 
 from paper_1412_1576_b200 import binding as b
 from paper_1412_1576_b200 import rows
@@ -145,3 +146,25 @@ def test_forward_mode_is_refused(monkeypatch):
             with torch.no_grad(), pytest.raises(NotImplementedError):
                 rows.distill_loss(dual, ids, values)
         assert rows.distill_loss(x, ids, values).shape == (2,)      # without a tangent nothing is lost
+
+
+def calls():
+    """Each entry point as a function of one matrix of the host."""
+    ids, values = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3)
+    offsets, drafts, u = torch.tensor([0, 1]), torch.zeros(1, dtype=torch.int32), torch.zeros(1)
+    return [lambda x: rows.top_logits(x, 3), lambda x: rows.distill_loss(x, ids, values),
+            lambda x: rows.distill_loss(x.detach().requires_grad_(), ids, values),
+            lambda x: rows.distill_loss_and_grad(x, ids, values), lambda x: rows.verify_drafts(offsets, drafts, x, None, u, u)]
+
+
+@pytest.mark.parametrize("which", range(5))
+def test_tracing_is_refused(which):
+    """A traced graph would hold the outputs' allocation alone."""
+    call, x = calls()[which], torch.zeros(2, 10)
+    with pytest.raises(RuntimeError, match="traced"):
+        torch.jit.trace(call, x, check_trace=False)
+    for before in (False, True):
+        with pytest.raises(RuntimeError, match="traced"):
+            make_fx(call, pre_dispatch=before)(x)
+    with pytest.raises(ValueError, match="CUDA"):      # (and nothing of it is left)
+        call(x)
