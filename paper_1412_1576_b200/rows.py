@@ -36,10 +36,18 @@ def _rows(x, name):
     return code, shape[0], shape[1], between if shape[0] > 1 else shape[1]
 
 
+def _address(x, name):
+    """Address of a tensor of some elements; torch's functional wrappers have 0, which the library takes for `not given`."""
+    address = x.data_ptr()
+    if not address:
+        raise ValueError(f"{name}: a tensor without memory of its own")
+    return address
+
+
 def _vector(x, name, dtype, n, device):
     """Checks a contiguous vector; returns its address."""
     if x.dtype is dtype and x.shape == (n,) and x.device == device and x.is_contiguous():
-        return x.data_ptr()
+        return _address(x, name) if n else None
     if x.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {x.dtype}")
     if x.shape != (n,):
@@ -226,7 +234,7 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
         _, _, _, probs_stride = _rows(draft_probs, "draft_probs")
         _here(draft_probs, "draft_probs", device)
         # (without drafts there is nothing to point at; sequences then have one row each, of the target)
-        probs_ptr = draft_probs.data_ptr() if n_drafts else None
+        probs_ptr = _address(draft_probs, "draft_probs") if n_drafts else None
     accept_ptr = _vector(accept_u, "accept_u", torch.float32, n_drafts, device)
     draw_ptr = _vector(draw_u, "draw_u", torch.float32, n_seqs, device)
     if tokens is None:

@@ -168,3 +168,18 @@ def test_tracing_is_refused(which):
             make_fx(call, pre_dispatch=before)(x)
     with pytest.raises(ValueError, match="CUDA"):      # (and nothing of it is left)
         call(x)
+
+
+@pytest.mark.parametrize("which", ["lse", "weights", "draft_probs"])
+def test_tensors_without_memory_are_refused(monkeypatch, which):
+    """What functionalize hands on has the address 0, which stands for `not given` in the library."""
+    monkeypatch.setattr(rows, "_cuda", lambda x, name: x.device)
+    monkeypatch.setattr(rows, "_call", lambda name, device, *args: None)
+    x, ids, values = torch.zeros(2, 10), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3)
+    offsets, drafts, u = torch.tensor([0, 1]), torch.zeros(1, dtype=torch.int32), torch.zeros(1)
+    call, given = {"lse": (lambda t: rows.distill_loss(x, ids, values, t), torch.zeros(2)),
+                   "weights": (lambda t: rows.distill_loss_and_grad(x, ids, values, weights=t), torch.zeros(2)),
+                   "draft_probs": (lambda t: rows.verify_drafts(offsets, drafts, x, t, u, u), torch.zeros(1, 10))}[which]
+    call(given)
+    with pytest.raises(ValueError, match="memory"):
+        torch.func.functionalize(call)(given)
