@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.graph import increment_version
 from torch.fx.experimental.proxy_tensor import get_proxy_mode
 
 from . import binding as _b
@@ -173,7 +174,7 @@ def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
     _call("lda_distill_grad", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
           None if loss is None else loss.data_ptr(), grad.data_ptr(), grad_stride)
     if given:
-        torch.autograd.graph.increment_version(grad)  # (a graph that has saved what was there finds out)
+        increment_version(grad)  # (a graph that has saved what was there finds out)
     return grad
 
 
@@ -237,6 +238,7 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
         probs_ptr = _address(draft_probs, "draft_probs") if n_drafts else None
     accept_ptr = _vector(accept_u, "accept_u", torch.float32, n_drafts, device)
     draw_ptr = _vector(draw_u, "draw_u", torch.float32, n_seqs, device)
+    given = [x for x in (tokens, accepted) if x is not None]
     if tokens is None:
         tokens = torch.full((rows,), -1, dtype=torch.int32, device=device)
     if accepted is None:
@@ -245,4 +247,6 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
     accepted_ptr = _vector(accepted, "accepted", torch.int32, n_seqs, device)
     _call("lda_verify_drafts", device, offsets_ptr, n_seqs, drafts_ptr, n_drafts, target.data_ptr(), stride, probs_ptr,
           probs_stride, code, V, accept_ptr, draw_ptr, tokens_ptr, accepted_ptr)
+    if given:
+        increment_version(given)  # (a graph that has saved them, as an embedding's indices, finds out)
     return tokens, accepted

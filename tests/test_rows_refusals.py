@@ -183,3 +183,20 @@ def test_tensors_without_memory_are_refused(monkeypatch, which):
     call(given)
     with pytest.raises(ValueError, match="memory"):
         torch.func.functionalize(call)(given)
+
+
+def test_tokens_over_a_saved_index_are_noticed(monkeypatch):
+    monkeypatch.setattr(rows, "_cuda", lambda x, name: x.device)
+    monkeypatch.setattr(rows, "_call", lambda name, device, *args: None)
+    table = torch.ones(5, 4, requires_grad=True)
+    target, u = torch.zeros(3, 10), torch.zeros(3)
+    offsets, drafts = torch.tensor([0, 1, 2]), torch.zeros(2, dtype=torch.int32)
+    for name, n in (("tokens", 4), ("accepted", 2)):
+        given = torch.zeros(n, dtype=torch.int32)
+        kept = torch.nn.functional.embedding(given, table)
+        rows.verify_drafts(offsets, drafts, torch.zeros(4, 10), None, u[:2], u[:2])
+        kept.sum().backward()
+        lost = torch.nn.functional.embedding(given, table)
+        rows.verify_drafts(offsets, drafts, torch.zeros(4, 10), None, u[:2], u[:2], **{name: given})
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            lost.sum().backward()
