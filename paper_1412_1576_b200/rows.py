@@ -16,9 +16,9 @@ from torch.fx.experimental.proxy_tensor import get_proxy_mode
 
 from . import binding as _b
 
-# (whether torch.jit or a dispatch mode, a tracer's among them, is at work: a third of a microsecond together)
+# (whether torch.jit, a dispatch mode or a tracer before dispatch is at work: a quarter of a microsecond together)
 _jit_tracing, _modes = torch._C._is_tracing, torch._C._len_torch_dispatch_stack
-_modes_before_dispatch = torch._ops._len_torch_dispatch_stack_pre_dispatch
+_before_dispatch = torch._ops.mode_stack_state_for_pre_dispatch().get
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 _DTYPES = {torch.float32: _b.LDA_F32, torch.float16: _b.LDA_F16, torch.bfloat16: _b.LDA_BF16}
 
@@ -37,24 +37,26 @@ def _rows(x, name):
     return code, shape[0], shape[1], between if shape[0] > 1 else shape[1]
 
 
-def _address(x, name):
-    """Address of a tensor of some elements; torch's functional wrappers have 0, which the library takes for `not given`."""
-    address = x.data_ptr()
-    if not address:
-        raise ValueError(f"{name}: a tensor without memory of its own")
-    return address
-
-
 def _vector(x, name, dtype, n, device):
     """Checks a contiguous vector; returns its address."""
     if x.dtype is dtype and x.shape == (n,) and x.device == device and x.is_contiguous():
-        return _address(x, name) if n else None
+        return x.data_ptr()
     if x.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {x.dtype}")
     if x.shape != (n,):
         raise ValueError(f"{name}: {n} values are needed, not {tuple(x.shape)}")
     _here(x, name, device)
     raise ValueError(f"{name}: must be contiguous")
+
+
+def _optional(x, name, n, device):
+    """The same of a float32 vector that may be None, as NULL."""
+    if x is None:
+        return None
+    address = _vector(x, name, torch.float32, n, device)
+    if not address and n:  # (torch's functional wrappers; the library would take it for `not given`)
+        raise ValueError(f"{name}: a tensor without memory of its own")
+    return address
 
 
 def _here(x, name, device):
@@ -64,7 +66,7 @@ def _here(x, name, device):
 
 def _cuda(x, name):
     # (a tracer sees the outputs' allocation, not the library's call that fills them)
-    if _jit_tracing() or (_modes() or _modes_before_dispatch()) and get_proxy_mode() is not None:
+    if _jit_tracing() or (_modes() or _before_dispatch(0)) and get_proxy_mode() is not None:
         raise RuntimeError(f"{name}: operators on rows cannot be traced")
     if not x.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed (there is no CPU fallback)")
@@ -127,8 +129,7 @@ def _list(ids, values, lse, rows, device):
     if ids.device != device or values.device != device:
         _here(ids, "ids", device)
         _here(values, "values", device)
-    teacher_lse = None if lse is None else _vector(lse, "lse", torch.float32, rows, device)
-    return ids.data_ptr(), values.data_ptr(), code, top, between[0] if rows > 1 else top, teacher_lse
+    return ids.data_ptr(), values.data_ptr(), code, top, between[0] if rows > 1 else top, _optional(lse, "lse", rows, device)
 
 
 class _Distill(torch.autograd.Function):
@@ -170,7 +171,7 @@ def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
             raise ValueError("grad: a tensor that autograd follows cannot be written to (detach it)")
         grad_stride = _rows(grad, "grad")[3]
         _here(grad, "grad", device)
-    w = None if weights is None else _vector(weights, "weights", torch.float32, rows, device)
+    w = _optional(weights, "weights", rows, device)
     _call("lda_distill_grad", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
           None if loss is None else loss.data_ptr(), grad.data_ptr(), grad_stride)
     if given:
@@ -235,10 +236,12 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
         _, _, _, probs_stride = _rows(draft_probs, "draft_probs")
         _here(draft_probs, "draft_probs", device)
         # (without drafts there is nothing to point at; sequences then have one row each, of the target)
-        probs_ptr = _address(draft_probs, "draft_probs") if n_drafts else None
+        probs_ptr = draft_probs.data_ptr() if n_drafts else None
+        if probs_ptr == 0:
+            raise ValueError("draft_probs: a tensor without memory of its own")
     accept_ptr = _vector(accept_u, "accept_u", torch.float32, n_drafts, device)
     draw_ptr = _vector(draw_u, "draw_u", torch.float32, n_seqs, device)
-    given = [x for x in (tokens, accepted) if x is not None]
+    given = tokens is not None or accepted is not None
     if tokens is None:
         tokens = torch.full((rows,), -1, dtype=torch.int32, device=device)
     if accepted is None:
@@ -248,5 +251,5 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
     _call("lda_verify_drafts", device, offsets_ptr, n_seqs, drafts_ptr, n_drafts, target.data_ptr(), stride, probs_ptr,
           probs_stride, code, V, accept_ptr, draw_ptr, tokens_ptr, accepted_ptr)
     if given:
-        increment_version(given)  # (a graph that has saved them, as an embedding's indices, finds out)
+        increment_version((tokens, accepted))  # (a graph that has saved them, as an embedding's indices, finds out)
     return tokens, accepted
