@@ -31,10 +31,14 @@ def _rows(x, name):
         if code is None:
             raise TypeError(f"{name}: float32, float16 or bfloat16 is needed, not {x.dtype}")
         raise ValueError(f"{name}: a matrix with at least one column is needed, not {tuple(shape)}")
+    return code, shape[0], shape[1], _row_stride(x, shape, name)
+
+
+def _row_stride(x, shape, name):
     between, step = x.stride()
     if step != 1 and shape[1] > 1:
         raise ValueError(f"{name}: the words of a row must be consecutive in memory")
-    return code, shape[0], shape[1], between if shape[0] > 1 else shape[1]
+    return between if shape[0] > 1 else shape[1]
 
 
 def _vector(x, name, dtype, n, device):
@@ -222,18 +226,20 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
     """
     device = _cuda(target, "target")
     code, rows, V, stride = _rows(target, "target")
-    if draft_offsets.dim() != 1 or draft_offsets.shape[0] < 1:
+    shape = draft_offsets.shape
+    if len(shape) != 1 or shape[0] < 1:
         raise ValueError("draft_offsets: one more than there are sequences is needed")
-    n_seqs, n_drafts = draft_offsets.shape[0] - 1, drafts.numel()
+    n_seqs, n_drafts = shape[0] - 1, drafts.numel()
     if rows != n_drafts + n_seqs:
         raise ValueError(f"target: {n_drafts} drafts of {n_seqs} sequences need {n_drafts + n_seqs} rows, not {rows}")
     offsets_ptr = _vector(draft_offsets, "draft_offsets", torch.int64, n_seqs + 1, device)
     drafts_ptr = _vector(drafts, "drafts", torch.int32, n_drafts, device)
     probs_ptr, probs_stride = None, 0
     if draft_probs is not None:
-        if draft_probs.dtype != target.dtype or draft_probs.shape != (n_drafts, V):
+        shape = draft_probs.shape
+        if draft_probs.dtype is not target.dtype or shape != (n_drafts, V):
             raise ValueError(f"draft_probs: [{n_drafts}, {V}] of {target.dtype} is needed")
-        _, _, _, probs_stride = _rows(draft_probs, "draft_probs")
+        probs_stride = _row_stride(draft_probs, shape, "draft_probs")
         _here(draft_probs, "draft_probs", device)
         # (without drafts there is nothing to point at; sequences then have one row each, of the target)
         probs_ptr = draft_probs.data_ptr() if n_drafts else None
