@@ -101,6 +101,7 @@ __host__ __device__ constexpr int distill_bits(int chunks) { return chunks * (32
 struct DistillTeacher {
     double inv_tau, shift;  // shift: the teacher's log-sum-exp, or the largest of the list
     __device__ __forceinline__ double log_of(float t) const { return (double)t * inv_tau - shift; }
+    // (e above 0 or NaN: where the logarithm is beyond single precision, what its rounding takes away is no number)
     static __device__ __forceinline__ double exact(float e, double log_e) { return (double)e * (1.0 + (log_e - (double)(float)log_e)); }
 };
 
@@ -111,10 +112,9 @@ __device__ __forceinline__ double distill_teacher(const DistillArgs& a, const Di
     for (int j = threadIdx.x & 31; j < a.top; j += 32) {
         const float t = list.t[j];
         const double l = teacher.log_of(t);
-        const bool none = list.ids[j] < 0 || t == -INFINITY;
-        const float e = none ? 0.0f : expf((float)l);
+        const float e = list.ids[j] < 0 || t == -INFINITY ? 0.0f : expf((float)l);
         list.p[j] = e;
-        if (!none) z += DistillTeacher::exact(e, l);
+        if (e != 0.0f) z += DistillTeacher::exact(e, l);
     }
     return warp_reduce_sum(z);
 }
@@ -332,9 +332,11 @@ __device__ __forceinline__ void distill_put_list(T* grad, const DistillArgs& a, 
 // part, so that one pass adds up the exponentials of the others; those of the list come from its own places.  The CTAs exchange
 // their sums; each works out the gradient of its part from a second read, which L2 answers, and puts the list's words over it.
 // 2048 rows of 141 000 words of bf16, lists of 64, loss and gradient: 254 us, 4.5 TB/s of the logits' one read and the gradient's
-// write (DRAM sees 10 % more).  Both exponentials per word keep the multifunction units 54 % busy, the issue slots are 54 % full; a
-// CTA (half a row) spends 14 of 24 us on the two passes, the rest on the list, the exchange and the sums, three CTAs at a time.
-// The loss alone, 4096 rows of 100 000 of fp16, lists of 128: 148 us, 5.5 TB/s.
+// write (DRAM sees 10 % more), in a replayed graph of ten calls, as all times here (calls one by one on a warm card: 277).  Both
+// exponentials per word keep the multifunction units 53 % busy, the issue slots are 54 % full: what bounds it is latency.  A CTA (half a
+// row) spends 14 of 24 us on the two passes, the rest on the list, the exchange and the sums, three CTAs at a time.
+// The loss alone, 4096 rows of 100 000 of fp16, lists of 128: 148 us, 5.5 TB/s (calls: 168).
+// The loss worked out behind the second pass by all warps, from exponentials of 64 bits: 259 us, and 13 % more for 16 rows.
 // Tried: a cluster that goes from row to row with the row held in shared memory and the list worked on by a warp of its own (759 us:
 // 2 KB of a row to a thread do not pay for an exchange), rows in clusters of eight held in shared memory (414 us).
 template <typename T, bool TAIL, bool GRAD>

@@ -615,6 +615,21 @@ def test_distill_student_that_has_learnt_its_teacher(tail, top):
     assert bool(((got - want).abs() <= bound + 2.0**-24 * abs(want)).all()), (got, want)
 
 
+@pytest.mark.parametrize("tau", [0.5, 1e-3, 2.0])
+@pytest.mark.parametrize("values_dtype", [F32, F16, BF16], ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("tail", [False, True], ids=["list", "tail"])
+def test_distill_teacher_with_words_at_the_lowest_value(tail, values_dtype, tau):
+    """Some places of the list, or (without a tail) all of one, at the lowest value: t / tau is beyond single precision then."""
+    x = make(3, 2_000, F32, 83)
+    ids, values, lse = lists_of(make(3, 2_000, F32, 84, spread=3.0 * min(tau, 1.0)).cpu(), 40, tau, tail, values_dtype)
+    values = values.clone()
+    values[0, 20:] = torch.finfo(values_dtype).min
+    values[1, ::2] = torch.finfo(values_dtype).min
+    if not tail:
+        values[2] = torch.finfo(values_dtype).min
+    check_distill(x, ids, values, lse, tau=tau)
+
+
 # --- verification of drafts --------------------------------------------------------------------------------------------------
 
 def verify_reference(offsets, drafts, target, probs, au, du):
