@@ -346,7 +346,8 @@ int lda_distill_grad(const void* logits_dev, int dtype, int64_t rows, int32_t V,
  *   - one token follows, drawn with draw_u[b] from the masses max(p - q, 0) of the first draft that was not accepted (draft_probs
  *     NULL: p without that draft), or from p of the last row.  A mass is floor(2^42 x), x cut to [0, 1], NaN as 0; masses are
  *     added up as whole numbers, and the token is the first whose running sum exceeds floor(total floor(2^32 u) / 2^32).  Rows
- *     without any such mass are drawn from p itself, and where p has none either the token is -1.  (u: cut to [0, 1 - 2^-32].)
+ *     without any such mass are drawn from p itself, and where p has none either the token is -1.  (u: cut to [0, 1 - 2^-32].  The draw is as fine as u: with
+ *     uniforms that are multiples of 2^-24, words of much less than 2^-24 of the mass are drawn too often or never.)
  * tokens[n_drafts + n_seqs]: at the places of the sequence's target rows, the accepted drafts, the drawn token, then -1.
  * accepted[n_seqs]: how many drafts stood.  Offsets that do not run upwards inside [0, n_drafts] give accepted = -1 and leave
  * the sequence's tokens as they were; so are places that belong to no sequence. */

@@ -24,7 +24,9 @@ constexpr int TOP_GROUPS = 4;     // groups of a lane in a chunk (two: 242 us fo
 constexpr int TOP_DEPTH = 2;      // chunks on their way (three: the same time)
 constexpr int TOP_VALUES = 1024;  // groups of pieces whose largest keys give the border, at most
 constexpr uint32_t TOP_LOWEST = (KEY_NEG_INF >> 16) + 1;  // first half-key above minus infinity
-// Words and pieces that may be left for lists of `top`: about four times what is expected.
+// Words and pieces that may be left for lists of `top`: about four times what rows in no order leave (95 words for lists of 64 of 131 072).
+// Rows in order of their words' frequency and long ties may leave more (534 with a normal part of 0.7 beside the logarithm of the rank, all
+// of a row all alike) and then go by top_by_bytes: 4096 such rows of bf16 take 9.6 and 10.0 ms.
 __host__ __device__ constexpr int top_room(int top) { return top <= 64 ? 512 : top <= 256 ? 1024 : 2048; }
 
 // What takes the ring's place behind the pass.
@@ -428,7 +430,8 @@ struct TopPart {
 // One cluster per row.  The pass leaves the pieces' largest keys.  A border that at least `top` groups of pieces reach
 // leaves at least `top` words, and few more (95 for 64 of 131 072); the pieces that reach it are read again (from L2), their words
 // sorted, in runs of 128 by a warp each, and merged by rank.
-// 4096 rows of 131 072 words of bf16, lists of 64: 214 us, 5.0 TB/s; no unit is full (of what they can, the multifunction units do
+// 4096 rows of 131 072 words of bf16, lists of 64: 214 us, 5.0 TB/s, in a replayed graph of ten calls, as all times here (calls one by
+// one on a warm card: 229); no unit is full (of what they can, the multifunction units do
 // 59 %, the issue slots 59 %, DRAM 75 %): a row's CTA spends 35 of 53 us on the pass and the rest on its list, eight CTAs at a time.
 // 777 rows of 100 003 of fp16, lists of 301: 64 us, 25 of them the pass, 13 the second read of 430 pieces (17 with the border
 // compared to a key per element).

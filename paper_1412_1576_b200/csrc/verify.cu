@@ -3,7 +3,8 @@
 // A sequence of n drafts x_1..x_n has rows p_0..p_n of the target (p_i: before draft i+1) and rows q_0..q_{n-1} of the drafter.
 // Draft i is accepted iff u_i q(x_i) < p(x_i): the Metropolis-Hastings test of an independence proposal with the ratio's
 // denominator on the left, as the sweep's own accept pass has it.  Behind the leading accepted drafts one token is drawn, from the
-// masses max(p - q, 0) where a draft was refused and from p behind the last draft; accepted and drawn tokens together follow p.
+// masses max(p - q, 0) where a draft was refused and from p behind the last draft; accepted and drawn tokens together follow p, as finely
+// as the uniforms do: a float32 uniform has 2^24 values as generators give it, so that of 10^6 words of equal mass some answer to 16 of them and some to 17.
 // Decisions are exact: the test compares products of 24 by 24 bits in doubles, and the draw is the inverse CDF over masses that
 // are whole multiples of 2^-42, added up as integers, so that no order of summation and no split of the row changes a token.
 #include "lda_device.cuh"
