@@ -274,6 +274,8 @@ __device__ __forceinline__ void unpack(uint4 g, float (&x)[PER<T>])
 // 2^(x c - R) is added up with R the largest x c met so far, rounded down.  With R whole, moving a sum from one R to another
 // is exact, and x c - R is rounded once (a fused multiply-add).  |R| <= 2^22 keeps R c's rounding out; rows whose maximum lies
 // beyond that (the type's lowest value as a mask, say) are added up again as 2^((x - maximum) c): `far`.
+// In 32 bits: a chunk's terms are added in a tree and a thread has few chunks, which leaves chains of some tens of additions, off
+// by 2^-24 each at most.
 constexpr float REF_MOST = 4194304.0f;
 __device__ __forceinline__ float exp_ref(float max, float c)
 {
