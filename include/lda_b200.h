@@ -356,6 +356,62 @@ int lda_verify_drafts(const int64_t* draft_offsets_dev, int64_t n_seqs, const in
                       int dtype, int32_t V, const float* accept_u_dev, const float* draw_u_dev, int32_t* tokens_dev,
                       int32_t* accepted_dev, void* cuda_stream);
 
+/* Operators on a paged cache of keys and values: what the target model of drafted tokens needs beside the operators on rows -- the
+ * drafts' keys and values into the cache, and their attention over it, one token per sequence or a tree of them.  As above: no context,
+ * DEVICE pointers of the current GPU, queued on `cuda_stream`, nothing allocated and no state kept; a call may be captured into a graph.
+ *
+ * The cache lies in pages of `page_size` slots; slot s of sequence b is place s % page_size of page table[b][s / page_size].  Entries outside
+ * [0, pages) are no pages: nothing is written there, and attention leaves their keys out, as it does all behind the table's end.
+ *   dtype      LDA_F16 or LDA_BF16, of the cache and of all rows of heads
+ *   keys, values   element (page, place, head, 0) lies at page strides[0] + place strides[1] + head strides[2]; a head's `dim` elements
+ *              are consecutive.  Addresses are multiples of 16 bytes and strides of 8 elements, here and in all rows of heads
+ *   dim        a multiple of 8, up to LDA_HEAD_MAX_DIM; heads and kv_heads up to LDA_HEADS_MAX; table_width page_size < 2^31
+ *   starts     [n_seqs]: how many slots the sequence has before its new tokens (below 0: 0)
+ *   offsets    [n_seqs + 1]: sequence b has the new tokens offsets[b] .. offsets[b+1] - 1 of the call's `tokens`, in the slots
+ *              from starts[b] on.  Offsets that do not run upwards inside [0, tokens] leave the sequence out; rows of outputs that belong
+ *              to no sequence stay as they are
+ * Rows of heads (keys, values, queries, outputs) are [tokens, heads, dim] with two strides. */
+#define LDA_HEAD_MAX_DIM 256
+#define LDA_HEADS_MAX 1024
+#define LDA_MASK_MAX_WORDS 64
+typedef struct lda_paged_cache {
+    void *keys, *values;
+    int32_t dtype, kv_heads, dim, page_size;
+    int64_t pages, key_strides[3], value_strides[3];
+    const int32_t* table;
+    int64_t table_stride, n_seqs;
+    const int32_t* starts;
+    const int64_t* offsets;
+    int32_t table_width;
+} lda_paged_cache;
+
+/* New tokens' keys and values into the cache; keys, and the queries q[tokens][heads] (heads 0: none) into q_out (q itself is allowed), are rotated
+ * on the way: of the first `rotated` elements of a head, pair i (elements i and i + rotated / 2; interleaved: 2 i and 2 i + 1) by the
+ * angle positions[token] inv_freq[i], worked out in 64 bits (positions NULL: the token's slot).  rotated 0: nothing is. */
+int lda_append_cache(const lda_paged_cache* cache, int64_t tokens, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
+                     const void* v_dev, int64_t v_token_stride, int64_t v_head_stride, const int32_t* positions_dev,
+                     const float* inv_freq_dev, int32_t rotated, int interleaved, const void* q_dev, int64_t q_token_stride,
+                     int64_t q_head_stride, int32_t heads, void* q_out_dev, int64_t out_token_stride, int64_t out_head_stride,
+                     void* cuda_stream);
+
+/* Who sees whom in trees of new tokens.  parents[tokens]: a token's parent by its place in its sequence; parents stand before their
+ * children, and anything else marks a root.  mask[tokens][words]: bit j % 64 of word j / 64 is set for the token itself (place j) and all above
+ * it; places from 64 words on have no bits.  positions[tokens] (may be NULL): starts[b] (NULL: 0) + how many are above it. */
+int lda_tree_mask(const int32_t* parents_dev, const int64_t* offsets_dev, int64_t n_seqs, int64_t tokens, const int32_t* starts_dev,
+                  int32_t words, int64_t* mask_dev, int32_t* positions_dev, void* cuda_stream);
+
+/* Attention of the new tokens, whose keys and values are in the cache, over the cache: out = softmax(scale q k) v over the sequence's slots
+ * before its new tokens and over the new tokens j whose bit is set in the token's words of mask[tokens] (mask_stride words apart;
+ * NULL: those up to itself).  Query head h reads head h / (heads / kv_heads) of the cache.  What a token does not see
+ * does not touch it, NaN and infinities among it; a token that sees nothing gets zeros.  scale: 1e-6 .. 1e6.
+ * The workspace (a multiple of 16 bytes; its size by lda_tree_attention_workspace, or a negative status; no less for the same cache,
+ * tokens and heads) holds nothing between calls: calls that may overlap need one each. */
+int64_t lda_tree_attention_workspace(const lda_paged_cache* cache, int64_t tokens, int32_t heads);
+int lda_tree_attention(const lda_paged_cache* cache, int64_t tokens, const void* q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                       int32_t heads, const int64_t* mask_dev, int64_t mask_stride, int32_t mask_words, double scale, void* out_dev,
+                       int64_t out_token_stride, int64_t out_head_stride, void* workspace_dev, int64_t workspace_bytes,
+                       void* cuda_stream);
+
 int lda_get_stats(lda_ctx* ctx, lda_stats* out);
 
 /* Message of the last failure on this context (library-owned, valid until the next call). */

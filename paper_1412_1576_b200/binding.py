@@ -20,6 +20,7 @@ LDA_OK, LDA_EINVAL, LDA_ERANGE, LDA_ESTATE, LDA_ENOMEM, LDA_ECUDA, LDA_EINTERNAL
 LDA_NK, LDA_NWK, LDA_NDK = 0, 1, 2
 LDA_F32, LDA_F16, LDA_BF16 = 0, 1, 2
 LDA_ROW_MAX_V, LDA_TOP_MAX = 1048576, 512
+LDA_HEAD_MAX_DIM, LDA_HEADS_MAX, LDA_MASK_MAX_WORDS = 256, 1024, 64
 
 EXPORTS = [
     "lda_create", "lda_set_stream", "lda_set_allocator", "lda_set_option", "lda_set_proposals", "lda_load_corpus", "lda_load_corpus_device",
@@ -27,6 +28,7 @@ EXPORTS = [
     "lda_get_assignments", "lda_get_assignments_u16", "lda_get_assignments_async", "lda_get_assignments_u16_async", "lda_wait", "lda_get_tables", "lda_get_stats", "lda_last_error", "lda_destroy",
     "lda_dense_table_noalloc",
     "lda_top_logits", "lda_distill_loss", "lda_distill_grad", "lda_verify_drafts",
+    "lda_append_cache", "lda_tree_mask", "lda_tree_attention_workspace", "lda_tree_attention",
 ]
 
 
@@ -45,6 +47,15 @@ class lda_stats(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class lda_paged_cache(C.Structure):
+    _fields_ = [
+        ("keys", C.c_void_p), ("values", C.c_void_p), ("dtype", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+        ("page_size", C.c_int32), ("pages", C.c_int64), ("key_strides", C.c_int64 * 3), ("value_strides", C.c_int64 * 3),
+        ("table", C.c_void_p), ("table_stride", C.c_int64), ("n_seqs", C.c_int64), ("starts", C.c_void_p), ("offsets", C.c_void_p),
+        ("table_width", C.c_int32),
+    ]
 
 
 # lda_alloc_fn / lda_free_fn of the header
@@ -107,6 +118,11 @@ def load_library(path: str | None = None):
     L.lda_distill_loss.argtypes = lists + [vp, vp]
     L.lda_distill_grad.argtypes = lists + [vp, vp, vp, i64, vp]
     L.lda_verify_drafts.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, C.c_int, i32, vp, vp, vp, vp, vp]
+    cache = C.POINTER(lda_paged_cache)
+    L.lda_append_cache.argtypes = [cache, i64, vp, i64, i64, vp, i64, i64, vp, vp, i32, C.c_int, vp, i64, i64, i32, vp, i64, i64, vp]
+    L.lda_tree_mask.argtypes = [vp, vp, i64, i64, vp, i32, vp, vp, vp]
+    L.lda_tree_attention_workspace.argtypes = [cache, i64, i32]
+    L.lda_tree_attention.argtypes = [cache, i64, vp, i64, i64, i32, vp, i64, i32, dbl, vp, i64, i64, vp, i64, vp]
     L.lda_last_error.argtypes = [vp]
     L.lda_last_error.restype = C.c_char_p
     L.lda_destroy.argtypes = [vp]
@@ -114,6 +130,7 @@ def load_library(path: str | None = None):
     for name in EXPORTS:
         if name not in ("lda_last_error", "lda_destroy"):
             getattr(L, name).restype = C.c_int
+    L.lda_tree_attention_workspace.restype = i64
     if path == library_path():
         _lib = L
     return L
@@ -315,6 +332,31 @@ def lda_verify_drafts(offsets_ptr, n_seqs, drafts_ptr, n_drafts, target_ptr, tar
                       accept_u_ptr, draw_u_ptr, tokens_ptr, accepted_ptr, cuda_stream=None):
     return load_library().lda_verify_drafts(offsets_ptr, n_seqs, drafts_ptr, n_drafts, target_ptr, target_stride, probs_ptr,
                                             probs_stride, dtype, V, accept_u_ptr, draw_u_ptr, tokens_ptr, accepted_ptr, cuda_stream)
+
+
+# Operators on a paged cache (``cache``: an ``lda_paged_cache``; raw DEVICE pointers or None, as above).  The module ``cache`` has them for
+# torch tensors.
+
+def lda_append_cache(cache, tokens, k_ptr, k_token_stride, k_head_stride, v_ptr, v_token_stride, v_head_stride, positions_ptr, inv_freq_ptr,
+                     rotated, interleaved, q_ptr=None, q_token_stride=0, q_head_stride=0, heads=0, q_out_ptr=None, out_token_stride=0,
+                     out_head_stride=0, cuda_stream=None):
+    return load_library().lda_append_cache(cache, tokens, k_ptr, k_token_stride, k_head_stride, v_ptr, v_token_stride, v_head_stride,
+                                           positions_ptr, inv_freq_ptr, rotated, interleaved, q_ptr, q_token_stride, q_head_stride,
+                                           heads, q_out_ptr, out_token_stride, out_head_stride, cuda_stream)
+
+
+def lda_tree_mask(parents_ptr, offsets_ptr, n_seqs, tokens, starts_ptr, words, mask_ptr, positions_ptr=None, cuda_stream=None):
+    return load_library().lda_tree_mask(parents_ptr, offsets_ptr, n_seqs, tokens, starts_ptr, words, mask_ptr, positions_ptr, cuda_stream)
+
+
+def lda_tree_attention_workspace(cache, tokens, heads):
+    return load_library().lda_tree_attention_workspace(cache, tokens, heads)
+
+
+def lda_tree_attention(cache, tokens, q_ptr, q_token_stride, q_head_stride, heads, mask_ptr, mask_stride, mask_words, scale, out_ptr,
+                       out_token_stride, out_head_stride, workspace_ptr, workspace_bytes, cuda_stream=None):
+    return load_library().lda_tree_attention(cache, tokens, q_ptr, q_token_stride, q_head_stride, heads, mask_ptr, mask_stride, mask_words,
+                                             scale, out_ptr, out_token_stride, out_head_stride, workspace_ptr, workspace_bytes, cuda_stream)
 
 
 def lda_get_stats(h):

@@ -1,0 +1,72 @@
+// Shared pieces of the operators on a paged cache of keys and values (cache.cu, attend.cu).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/lda_b200.h"
+
+namespace lda {
+
+// Division of numbers below 2^31 by a number that a launch knows: n d^-1 as a product by a 33-bit reciprocal rounded up (off by less
+// than 2^-31 / d, which no quotient of such numbers notices).
+struct Divider {
+    uint32_t d, magic, shift;
+    Divider() = default;
+    explicit Divider(uint32_t by) : d(by), shift(0)
+    {
+        while (shift < 31 && (1u << shift) < by) ++shift;
+        magic = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - by)) / by + 1);
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (uint32_t)(((uint64_t)__umulhi(n, magic) + n) >> shift); }
+};
+
+// A sequence's part of the call: its new tokens' first row, their number, and the keys in the cache before them.
+struct CacheSeq {
+    int64_t first;
+    int n, start;
+};
+
+struct CacheView {
+    char *keys, *values;
+    int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;  // strides in elements
+    const int32_t* table;
+    int64_t table_stride, pages, tokens;
+    const int32_t* starts;
+    const int64_t* offsets;
+    int32_t seqs, width, kv_heads, dim;
+    Divider page_size;
+
+    // Offsets that do not run upwards inside [0, tokens] leave the sequence out; a start below 0 counts as 0.
+    __device__ __forceinline__ CacheSeq seq(int b) const
+    {
+        const int64_t lo = offsets[b], hi = offsets[b + 1];
+        const int start = starts[b];
+        const bool ok = lo >= 0 && hi >= lo && hi <= tokens;
+        return CacheSeq{lo, ok ? (int)(hi - lo) : 0, start > 0 ? start : 0};
+    }
+    // The page of a slot of sequence b, or -1 where the table has none, and the slot's place in it.
+    __device__ __forceinline__ int page(int b, uint32_t slot, int& place) const
+    {
+        const uint32_t i = page_size.quotient(slot);
+        place = (int)(slot - i * page_size.d);
+        if (i >= (uint32_t)width) return -1;
+        const int p = table[b * table_stride + i];
+        return p >= 0 && p < pages ? p : -1;
+    }
+};
+
+// What both entry points refuse of a cache, and its view.
+int cache_view(const lda_paged_cache* cache, int64_t tokens, CacheView& view);
+
+// Strides of rows of heads in elements, and where they start: multiples of 16 bytes.
+inline bool heads_ok(const void* p, int64_t token_stride, int64_t head_stride)
+{
+    return p && (uintptr_t)p % 16 == 0 && token_stride % 8 == 0 && head_stride % 8 == 0 && token_stride >= 0 && head_stride >= 0;
+}
+
+__device__ __forceinline__ float cache_value(__half x) { return __half2float(x); }
+__device__ __forceinline__ float cache_value(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+}  // namespace lda

@@ -68,10 +68,10 @@ def _here(x, name, device):
         raise ValueError(f"{name}: on {x.device}, the rows are on {device}")
 
 
-def _cuda(x, name):
+def _cuda(x, name, what="operators on rows"):
     # (a tracer sees the outputs' allocation, not the library's call that fills them)
     if _jit_tracing() or (_modes() or _before_dispatch(0)) and get_proxy_mode() is not None:
-        raise RuntimeError(f"{name}: operators on rows cannot be traced")
+        raise RuntimeError(f"{name}: {what} cannot be traced")
     if not x.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor is needed (there is no CPU fallback)")
     return x.device
