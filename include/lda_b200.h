@@ -356,6 +356,23 @@ int lda_verify_drafts(const int64_t* draft_offsets_dev, int64_t n_seqs, const in
                       int dtype, int32_t V, const float* accept_u_dev, const float* draw_u_dev, int32_t* tokens_dev,
                       int32_t* accepted_dev, void* cuda_stream);
 
+/* Log probabilities of given tokens and the rows' entropies: with q = softmax(x / temperature), logprobs[r] = log q of tokens[r] and
+ * entropy[r] = -sum q log q, in natural units.  A token outside [0, V) has log probability 0; a row that is masked whole has entropy 0 and
+ * log probabilities minus infinity; a NaN or plus infinity in a row makes its numbers NaN.  Both are exact to their last places where a
+ * row is nearly sure, too.  stats[rows][3] (may be NULL): what the gradient needs -- the largest logit m, log sum exp((x - m) / temperature),
+ * sum q (m - x) / temperature.  top 1..LDA_TOP_MAX: ids[rows][top] as lda_top_logits gives them, and alternatives[rows][top],
+ * their log probabilities (minus infinity where no word is left); top 0: neither is looked at. */
+int lda_token_logprobs(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride, const int32_t* tokens_dev,
+                       int32_t top, double temperature, float* logprobs_dev, float* entropy_dev, float* stats_dev,
+                       int32_t* ids_dev, float* alternatives_dev, void* cuda_stream);
+
+/* Gradient of sum_r (logprob_weights[r] logprobs[r] + entropy_weights[r] entropy[r]) with respect to the logits (weights NULL: 0), in
+ * their element type, from the same logits, tokens and temperature and the stats of the call above.  Rows of weights 0 and 0 and rows that
+ * are masked whole have gradient 0; a token outside [0, V) has weight 0.  grad may be the logits themselves (same stride). */
+int lda_token_logprobs_grad(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride, const int32_t* tokens_dev,
+                            const float* stats_dev, const float* logprob_weights_dev, const float* entropy_weights_dev,
+                            double temperature, void* grad_dev, int64_t grad_stride, void* cuda_stream);
+
 /* Operators on a paged cache of keys and values: what the target model of drafted tokens needs beside the operators on rows -- the
  * drafts' keys and values into the cache, and their attention over it, one token per sequence or a tree of them.  As above: no context,
  * DEVICE pointers of the current GPU, queued on `cuda_stream`, nothing allocated and no state kept; a call may be captured into a graph.

@@ -28,7 +28,7 @@ EXPORTS = [
     "lda_get_assignments", "lda_get_assignments_u16", "lda_get_assignments_async", "lda_get_assignments_u16_async", "lda_wait", "lda_get_tables", "lda_get_stats", "lda_last_error", "lda_destroy",
     "lda_dense_table_noalloc",
     "lda_top_logits", "lda_distill_loss", "lda_distill_grad", "lda_verify_drafts",
-    "lda_append_cache", "lda_tree_mask", "lda_tree_attention_workspace", "lda_tree_attention",
+    "lda_token_logprobs", "lda_token_logprobs_grad", "lda_append_cache", "lda_tree_mask", "lda_tree_attention_workspace", "lda_tree_attention",
 ]
 
 
@@ -118,6 +118,8 @@ def load_library(path: str | None = None):
     L.lda_distill_loss.argtypes = lists + [vp, vp]
     L.lda_distill_grad.argtypes = lists + [vp, vp, vp, i64, vp]
     L.lda_verify_drafts.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, C.c_int, i32, vp, vp, vp, vp, vp]
+    L.lda_token_logprobs.argtypes = [vp, C.c_int, i64, i32, i64, vp, i32, dbl, vp, vp, vp, vp, vp, vp]
+    L.lda_token_logprobs_grad.argtypes = [vp, C.c_int, i64, i32, i64, vp, vp, vp, vp, dbl, vp, i64, vp]
     cache = C.POINTER(lda_paged_cache)
     L.lda_append_cache.argtypes = [cache, i64, vp, i64, i64, vp, i64, i64, vp, vp, i32, C.c_int, vp, i64, i64, i32, vp, i64, i64, vp]
     L.lda_tree_mask.argtypes = [vp, vp, i64, i64, vp, i32, vp, vp, vp]
@@ -332,6 +334,18 @@ def lda_verify_drafts(offsets_ptr, n_seqs, drafts_ptr, n_drafts, target_ptr, tar
                       accept_u_ptr, draw_u_ptr, tokens_ptr, accepted_ptr, cuda_stream=None):
     return load_library().lda_verify_drafts(offsets_ptr, n_seqs, drafts_ptr, n_drafts, target_ptr, target_stride, probs_ptr,
                                             probs_stride, dtype, V, accept_u_ptr, draw_u_ptr, tokens_ptr, accepted_ptr, cuda_stream)
+
+
+def lda_token_logprobs(logits_ptr, dtype, rows, V, row_stride, tokens_ptr, top, temperature, logprobs_ptr, entropy_ptr, stats_ptr=None,
+                       ids_ptr=None, alternatives_ptr=None, cuda_stream=None):
+    return load_library().lda_token_logprobs(logits_ptr, dtype, rows, V, row_stride, tokens_ptr, top, temperature, logprobs_ptr,
+                                             entropy_ptr, stats_ptr, ids_ptr, alternatives_ptr, cuda_stream)
+
+
+def lda_token_logprobs_grad(logits_ptr, dtype, rows, V, row_stride, tokens_ptr, stats_ptr, logprob_weights_ptr, entropy_weights_ptr,
+                            temperature, grad_ptr, grad_stride, cuda_stream=None):
+    return load_library().lda_token_logprobs_grad(logits_ptr, dtype, rows, V, row_stride, tokens_ptr, stats_ptr, logprob_weights_ptr,
+                                                  entropy_weights_ptr, temperature, grad_ptr, grad_stride, cuda_stream)
 
 
 # Operators on a paged cache (``cache``: an ``lda_paged_cache``; raw DEVICE pointers or None, as above).  The module ``cache`` has them for

@@ -1,4 +1,4 @@
-// Shared pieces of the operators on rows of logits or probabilities (toplogits.cu, distill.cu, verify.cu): element types,
+// Shared pieces of the operators on rows of logits or probabilities (toplogits.cu, distill.cu, verify.cu, logprobs.cu): element types,
 // 2^x, keys that order values, a row split over CTAs and walked over, sums of exponentials, launches.
 #pragma once
 #include <cooperative_groups.h>
@@ -398,6 +398,138 @@ __device__ __forceinline__ void add_groups(ExpSum& s, const uint4 (&raw)[N], flo
     for (int r = 1; r < N; ++r) part[0] = add_two(part[0], part[r]);
     s.sum += part[0].x + part[0].y;
 }
+
+// Sums of exponentials and of how far they lie below the largest, for log probabilities and entropies.  The words at the largest value met
+// so far (`max`, the same in all lanes of a warp) are counted and stay out of the sums: beside their ones the rest of a row that is nearly
+// sure, which is all that its entropy and its likely word's log probability consist of, would lose its digits.  What is left is
+//   sum = sum 2^(x c - R),   spread = sum 2^(x c - R) (x c - R)     over the words below it, R as in ExpSum
+struct SpreadSum {
+    float max, ref, sum, spread;
+    int most;
+    static __device__ __forceinline__ SpreadSum none() { return SpreadSum{-INFINITY, -REF_MOST, 0.0f, 0.0f, 0}; }
+    __device__ __forceinline__ void raise(float to)
+    {
+        if (to > ref) {
+            const float by = ref - to, f = exp2_whole(by);
+            spread = __fmaf_rn(by, sum, spread) * f;
+            sum *= f;
+            ref = to;
+        }
+    }
+    // A larger value (or NaN) has been met: the counted words go into the sums.
+    __device__ __forceinline__ void top(float to, float c)
+    {
+        if (to == max || max != max) return;  // (NaN stays)
+        raise(exp_ref(to, c));
+        if (most && max > -INFINITY) {
+            const float y = __fmaf_rn(max, c, -ref), e = exp2_unit(y) * (float)most;
+            sum += e;
+            spread = __fmaf_rn(e, y > -200.0f ? y : -200.0f, spread);
+        }
+        most = 0;
+        max = to;
+    }
+    // Adds N groups of each lane of a warp, of which `lane_max` is the largest value (NaN if there is one).
+    template <typename T, int N>
+    __device__ __forceinline__ void add(const uint4 (&raw)[N], float lane_max, float c)
+    {
+        const float to = key_value(__reduce_max_sync(0xffffffffu, order_key(lane_max)));
+        const bool has = !(to < max);
+        if (has) top(to, c);
+        if (has) add_groups<T, N, true>(raw, c);
+        else add_groups<T, N, false>(raw, c);
+    }
+    // The same with what the exponent is relative to given: 2^((x - max) c) (rows far from zero, `exp_far`).
+    template <typename T, int N, bool HAS, bool FAR = false>
+    __device__ __forceinline__ void add_groups(const uint4 (&raw)[N], float c)
+    {
+        const float2 cc = make_float2(c, c), from = FAR ? make_float2(-max, -max) : make_float2(-ref, -ref);
+        float2 part[N], far_off[N];
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            float x[PER<T>];
+            unpack<T>(raw[r], x);
+            float2 e[PER<T> / 2];
+            far_off[r] = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < PER<T> / 2; ++i) {
+                const float2 two = make_float2(x[2 * i], x[2 * i + 1]);
+                float2 y = FAR ? mul_two(add_two(two, from), cc) : fma_two(two, cc, from);
+                // (a masked word's minus infinity times its zero)
+                y.x = max_nan(y.x, -200.0f), y.y = max_nan(y.y, -200.0f);
+                e[i] = make_float2(exp2_unit(y.x), exp2_unit(y.y));
+                if (HAS) {
+                    if (two.x == max) e[i].x = 0.0f, ++most;
+                    if (two.y == max) e[i].y = 0.0f, ++most;
+                }
+                far_off[r] = fma_two(e[i], y, far_off[r]);
+            }
+#pragma unroll
+            for (int w = PER<T> / 4; w > 0; w /= 2)
+#pragma unroll
+                for (int i = 0; i < w; ++i) e[i] = add_two(e[i], e[i + w]);
+            part[r] = e[0];
+        }
+#pragma unroll
+        for (int r = 1; r < N; ++r) part[0] = add_two(part[0], part[r]), far_off[0] = add_two(far_off[0], far_off[r]);
+        sum += part[0].x + part[0].y;
+        spread += far_off[0].x + far_off[0].y;
+    }
+    // Of the lanes of a warp, whose largest values and R are the same; every lane has it.
+    __device__ __forceinline__ void lanes()
+    {
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            spread += __shfl_xor_sync(0xffffffffu, spread, o);
+        }
+        most = (int)__reduce_add_sync(0xffffffffu, (unsigned)most);
+    }
+    // Those of other words (not of rows far from zero).
+    __device__ __forceinline__ void join(SpreadSum o, float c)
+    {
+        const float m = max_nan(max, o.max);
+        top(m, c);
+        o.top(m, c);
+        raise(exp_ref(m, c));
+        o.raise(ref);
+        sum += o.sum, spread += o.spread, most += o.most;
+    }
+    // Of the lanes of a warp; every lane has it.
+    __device__ __forceinline__ void warp_reduce(float c)
+    {
+        top(key_value(__reduce_max_sync(0xffffffffu, order_key(max))), c);
+        raise(exp_ref(max, c));
+        lanes();
+    }
+};
+
+// What the sums say of a row (by one thread): in natural units, relative to the largest value.
+struct SpreadRow {
+    float max;
+    double log_z, mean;  // logarithm of the sum of exponentials; mean of (max - x) / tau
+    static __device__ __forceinline__ SpreadRow of(const SpreadSum& s, bool far, float c)
+    {
+        const double phi = far ? 0.0 : (double)__fmaf_rn(s.max, c, -s.ref), to = exp2(-phi);
+        const double rest = (double)s.sum * to, z = rest + s.most;
+        SpreadRow r;
+        r.max = s.max;
+        if (s.max == -INFINITY) {  // masked whole
+            r.log_z = r.mean = 0;
+            return r;
+        }
+        r.log_z = s.max < INFINITY ? log1p(rest + (s.most - 1)) : NAN;  // (NaN too, and infinity, of which nothing is left)
+        const double mean = (phi * s.sum - s.spread) * to * LN2 / z;
+        r.mean = !(s.max < INFINITY) ? NAN : mean < 0 ? 0.0 : mean;
+        return r;
+    }
+    __device__ __forceinline__ double entropy() const { return log_z + mean; }
+    // Of a word with logit x.
+    __device__ __forceinline__ double logprob(float x, double inv_tau) const
+    {
+        return max == -INFINITY ? -INFINITY : ((double)x - (double)max) * inv_tau - log_z;
+    }
+};
 
 // A group of values, each rounded once.
 template <typename T>

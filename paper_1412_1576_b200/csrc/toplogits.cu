@@ -5,20 +5,9 @@
 
 #include "lda_device.cuh"
 #include "rows.cuh"
+#include "toplogits.cuh"
 
 namespace lda {
-
-struct TopArgs {
-    const void* logits;
-    int64_t stride;
-    int32_t V, top;
-    float scale;     // log2(e) / temperature
-    double inv_tau;
-    int32_t* ids;
-    void* values;
-    float* lse;
-    int ring;  // bytes of the walk's ring, or of the lists that take its place
-};
 
 constexpr int TOP_GROUPS = 4;     // groups of a lane in a chunk (two: 242 us for 229)
 constexpr int TOP_DEPTH = 2;      // chunks on their way (three: the same time)
@@ -167,9 +156,9 @@ __device__ __noinline__ int top_by_bytes(const T* row, int V, int top, TopCounts
 // What the pass over a row does with a thread's chunk number `turn`: its values into the sum, the largest of every piece (a lane's groups
 // of the chunk; FINE: each group) as the upper half of its key, and of every group of pieces (`tops`: this thread's of the first
 // groups; it has turns + 1 of them, `threads` places apart).
-template <typename T, bool FINE>
+template <typename T, bool FINE, typename Sum>
 __device__ __forceinline__ void top_chunk(const uint4 (&raw)[TOP_GROUPS], uint16_t* keys, uint16_t* tops, int turn, int turns, int threads,
-                                          float c, float& m, ExpSum& sum)
+                                          float c, float& m, Sum& sum)
 {
     constexpr int PIECES = FINE ? TOP_GROUPS : 1;
     float top = -INFINITY;
@@ -188,7 +177,8 @@ __device__ __forceinline__ void top_chunk(const uint4 (&raw)[TOP_GROUPS], uint16
         top = FINE ? max_nan(top, x) : x;
     }
     m = fmaxf(m, top);
-    add_groups<T, TOP_GROUPS>(sum, raw, top, c);
+    if constexpr (std::is_same_v<Sum, ExpSum>) add_groups<T, TOP_GROUPS>(sum, raw, top, c);
+    else sum.template add<T, TOP_GROUPS>(raw, top, c);
 }
 
 // Groups of pieces: a power of two of them per thread, so that a fourth at most will reach the border where that is possible.
@@ -365,10 +355,20 @@ __device__ __forceinline__ void top_collect(const T* row, const RowSplit& split,
 }
 
 // The row's outputs from its n candidates (room + 1 or more: they did not fit).
-template <typename T>
+template <typename T, typename Sum>
 __device__ __forceinline__ void top_finish(const TopArgs& a, int64_t r, const T* row, int room, int n,
-                                           unsigned long long* list, TopCounts& sh, ExpSum sum, float m, bool far)
+                                           unsigned long long* list, TopCounts& sh, Sum sum, float m, bool far)
 {
+    constexpr bool LOGP = std::is_same_v<Sum, SpreadSum>;
+    __shared__ SpreadRow of;  // (LOGP)
+    if constexpr (LOGP)
+        if (threadIdx.x == 0) {
+            of = SpreadRow::of(sum, far, a.scale);
+            const int token = a.tokens[r];
+            a.logprobs[r] = token < 0 || token >= a.V ? 0.0f : (float)of.logprob(row_value(row[token]), a.inv_tau);
+            a.entropy[r] = (float)of.entropy();
+            if (a.stats) a.stats[3 * r] = of.max, a.stats[3 * r + 1] = (float)of.log_z, a.stats[3 * r + 2] = (float)of.mean;
+        }
     if (n > room) n = top_by_bytes<T>(row, a.V, a.top, sh, list);
     top_sort_runs(list, n);
     __syncthreads();
@@ -382,23 +382,27 @@ __device__ __forceinline__ void top_finish(const TopArgs& a, int64_t r, const T*
         if (place >= want) continue;
         const int v = (int)(0xFFFFFFFFu - (uint32_t)x);
         a.ids[r * a.top + place] = v;
-        ((T*)a.values)[r * a.top + place] = row[v];
+        if constexpr (LOGP) a.alternatives[r * a.top + place] = (float)of.logprob(row_value(row[v]), a.inv_tau);
+        else ((T*)a.values)[r * a.top + place] = row[v];
         if (place == 0) sh.prefix = (uint32_t)(x >> 32);
     }
     for (int i = want + tid; i < a.top; i += threads) {
         a.ids[r * a.top + i] = -1;
-        ((T*)a.values)[r * a.top + i] = row_element<T>(-INFINITY);
+        if constexpr (LOGP) a.alternatives[r * a.top + i] = -INFINITY;
+        else ((T*)a.values)[r * a.top + i] = row_element<T>(-INFINITY);
     }
-    if (!a.lse) return;
-    __syncthreads();
-    if (tid == 0) {
-        const uint32_t first = sh.prefix;
-        // (log2 of the largest exponential: x c - R, or 0 when far)
-        const double largest = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
-        a.lse[r] = want == 0 ? -INFINITY
-                   : first == KEY_NAN ? NAN
-                   : m == INFINITY ? INFINITY
-                                   : (float)((double)m * a.inv_tau + ((double)log2f(sum.sum) - largest) * LN2);
+    if constexpr (!LOGP) {
+        if (!a.lse) return;
+        __syncthreads();
+        if (tid == 0) {
+            const uint32_t first = sh.prefix;
+            // (log2 of the largest exponential: x c - R, or 0 when far)
+            const double largest = far ? 0.0 : (double)m * (double)a.scale - (double)sum.ref;
+            a.lse[r] = want == 0 ? -INFINITY
+                       : first == KEY_NAN ? NAN
+                       : m == INFINITY ? INFINITY
+                                       : (float)((double)m * a.inv_tau + ((double)log2f(sum.sum) - largest) * LN2);
+        }
     }
 }
 
@@ -420,9 +424,26 @@ __device__ __noinline__ float top_far_sum(const T* row, const RowSplit& split, i
     return warp_reduce_sum(o);
 }
 
+// The same of the words below m, with what an entropy needs, of the warp's lanes together.
+template <typename T>
+__device__ __noinline__ SpreadSum top_far_spread(const T* row, const RowSplit& split, int V, float m, float c, int warp, int warps)
+{
+    constexpr int R = TOP_GROUPS;
+    SpreadSum o = SpreadSum::none();
+    o.max = m;
+    for (int chunk = split.chunk0 + warp; chunk < split.chunk1; chunk += warps) {
+        uint4 raw[R];
+        load_chunk<T, R>(row, chunk_first<T, R>(chunk, split.pre), V, row_element<T>(-INFINITY), raw);
+        o.add_groups<T, R, true, true>(raw, c);
+    }
+    o.lanes();
+    return o;
+}
+
 // What a CTA knows of its part of the row.
+template <typename Sum>
 struct TopPart {
-    ExpSum sum;
+    Sum sum;
     float max;
     uint32_t share, alone;  // borders
 };
@@ -437,13 +458,14 @@ struct TopPart {
 // compared to a key per element).
 // Tried: the lists put together by warps of their own beside the next row's pass (558 us with one such warp, 237 with four: the list
 // is more work than they have time for), 256 threads a row (222 us), groups as pieces (259 us; for lists of 301 85 us).
-template <typename T, bool FINE>
+template <typename T, bool FINE, typename Sum>
 __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
 {
     constexpr int R = TOP_GROUPS, PIECES = FINE ? R : 1;
+    constexpr bool LOGP = std::is_same_v<Sum, SpreadSum>;
     extern __shared__ __align__(16) uint8_t dynamic[];  // the walk's ring and, later, the lists; the groups' and the pieces' largest keys
-    __shared__ TopPart parts[2][ROW_CTAS];
-    __shared__ ExpSum ered[ROW_THREADS / 32];
+    __shared__ TopPart<Sum> parts[2][ROW_CTAS];
+    __shared__ Sum ered[ROW_THREADS / 32];
     __shared__ float fred[ROW_THREADS / 32];
     __shared__ int counts[2][ROW_THREADS / 32], valids[ROW_THREADS / 32];
     __shared__ TopCounts sh;
@@ -465,12 +487,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     if (tid == 0) sh.n = sh.queued = 0;
     for (int g = tid; g < groups; g += threads) tops[g] = 0;  // (a thread's own)
     int turn = 0;
-    ExpSum sum = ExpSum::none();
+    Sum sum = Sum::none();
     float m = -INFINITY;
     walk.each(row, split, V, row_element<T>(-INFINITY), [&](int c, int, uint4(&raw)[R]) {
         top_chunk<T, FINE>(raw, keys + (c - split.chunk0) * 32 * PIECES + lane, tops + tid, turn++, turns, threads, a.scale, m, sum);
     });
-    sum.warp_reduce();
+    if constexpr (LOGP) sum.lanes();
+    else sum.warp_reduce();
     m = warp_reduce_max(m);
     // the groups that are not masked whole: their number, their least and largest key
     uint32_t most = 0, least = 0xFFFFu;
@@ -500,12 +523,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
         __syncthreads();
     }
     if (warp == 0) {
-        sum = lane < warps ? ered[lane] : ExpSum::none();
-        sum.warp_reduce();
+        sum = lane < warps ? ered[lane] : Sum::none();
+        if constexpr (LOGP) sum.warp_reduce(a.scale);
+        else sum.warp_reduce();
         m = warp_reduce_max(lane < warps ? fred[lane] : -INFINITY);
     }
     if (ctas > 1) cluster_wait();
-    if (tid < ctas) *row_peer(cluster, &parts[0][rank], tid, ctas) = TopPart{sum, m, share, alone};
+    if (tid < ctas) *row_peer(cluster, &parts[0][rank], tid, ctas) = TopPart<Sum>{sum, m, share, alone};
     row_sync(cluster, ctas);
     uint32_t border = 0, lowest = 0xFFFFFFFFu;
     m = -INFINITY;
@@ -517,11 +541,23 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     border = max(border, lowest);
     const bool far = exp_far(m, a.scale);
     if (far) {  // (the same in every CTA of the cluster)
-        float o = top_far_sum<T>(row, split, V, m, a.scale, warp, warps);
-        if (lane == 0) fred[warp] = o;
-        __syncthreads();
-        if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
-        if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = TopPart{{0.0f, o}, m, 0, 0};
+        if constexpr (LOGP) {
+            sum = top_far_spread<T>(row, split, V, m, a.scale, warp, warps);
+            if (lane == 0) ered[warp] = sum;
+            __syncthreads();
+            if (warp == 0) {
+                sum = lane < warps ? ered[lane] : Sum::none();
+                sum.max = m;
+                sum.lanes();
+            }
+            if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = TopPart<Sum>{sum, m, 0, 0};
+        } else {
+            float o = top_far_sum<T>(row, split, V, m, a.scale, warp, warps);
+            if (lane == 0) fred[warp] = o;
+            __syncthreads();
+            if (warp == 0) o = warp_reduce_sum(lane < warps ? fred[lane] : 0.0f);
+            if (tid < ctas) *row_peer(cluster, &parts[1][rank], tid, ctas) = TopPart<Sum>{{0.0f, o}, m, 0, 0};
+        }
         row_sync(cluster, ctas);
     }
     top_collect<T, FINE>(row, split, V, keys, pieces, border, room, lists.queue, &sh.queued,
@@ -529,11 +565,15 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) k_top(TopArgs a)
     row_sync(cluster, ctas);
     if (rank != 0) return;
     sum = parts[far][0].sum;
-    for (int k = 1; k < ctas; ++k) sum.add(parts[far][k].sum);
+    for (int k = 1; k < ctas; ++k) {
+        if constexpr (!LOGP) sum.add(parts[far][k].sum);
+        else if (far) sum.sum += parts[1][k].sum.sum, sum.spread += parts[1][k].sum.spread, sum.most += parts[1][k].sum.most;
+        else sum.join(parts[0][k].sum, a.scale);
+    }
     top_finish<T>(a, r, row, room, sh.n, lists.list, sh, sum, m, far);
 }
 
-template <typename T>
+template <typename T, typename Sum>
 static cudaError_t run_top(TopArgs a, int64_t rows, cudaStream_t st)
 {
     constexpr int CHUNK = 32 * TOP_GROUPS * PER<T>;
@@ -549,8 +589,16 @@ static cudaError_t run_top(TopArgs a, int64_t rows, cudaStream_t st)
     const bool fine = per / TOP_GROUPS / shape.ctas < 4 * a.top;
     a.ring = std::max(ChunkWalk<T, TOP_GROUPS, TOP_DEPTH>::bytes(shape, a.V), TopLists::bytes(room));
     const size_t smem = a.ring + 2 * (size_t)(top_groups(shape.threads, a.top) + pieces(shape.ctas, fine));
-    return fine ? launch_rows<k_top<T, true>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st)
-                : launch_rows<k_top<T, false>>(a, rows, shape, smem, sizeof(TopCounts) + 1024, st);
+    constexpr size_t fixed = sizeof(TopCounts) + 1024 + (sizeof(Sum) - sizeof(ExpSum)) * (ROW_THREADS / 32 + 2 * ROW_CTAS);
+    return fine ? launch_rows<k_top<T, true, Sum>>(a, rows, shape, smem, fixed, st)
+                : launch_rows<k_top<T, false, Sum>>(a, rows, shape, smem, fixed, st);
+}
+
+cudaError_t top_logprobs(const TopArgs& a, int dtype, int64_t rows, cudaStream_t st)
+{
+    return dtype == LDA_F32 ? run_top<float, SpreadSum>(a, rows, st)
+           : dtype == LDA_F16 ? run_top<__half, SpreadSum>(a, rows, st)
+                              : run_top<__nv_bfloat16, SpreadSum>(a, rows, st);
 }
 
 }  // namespace lda
@@ -567,11 +615,11 @@ extern "C" int lda_top_logits(const void* logits_dev, int dtype, int64_t rows, i
     if (!ids_dev || !values_dev) return LDA_EINVAL;
     if (!aligned(ids_dev, 4) || !aligned(values_dev, dtype == LDA_F32 ? 4 : 2) || !aligned(lse_dev, 4)) return LDA_EINVAL;
     TopArgs a{logits_dev, row_stride, V, top, (float)(1.4426950408889634 / temperature), 1.0 / temperature, ids_dev, values_dev,
-              lse_dev, 0};
+              lse_dev, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = dtype == LDA_F32 ? run_top<float>(a, rows, st)
-                          : dtype == LDA_F16 ? run_top<__half>(a, rows, st)
-                                             : run_top<__nv_bfloat16>(a, rows, st);
+    const cudaError_t e = dtype == LDA_F32 ? run_top<float, ExpSum>(a, rows, st)
+                          : dtype == LDA_F16 ? run_top<__half, ExpSum>(a, rows, st)
+                                             : run_top<__nv_bfloat16, ExpSum>(a, rows, st);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return LDA_ECUDA;

@@ -1,13 +1,16 @@
 """Operators on rows of logits or probabilities, for callers that hold torch tensors.
 
 What a neural model of the sampler's words needs beside the sampler: a teacher's lists (``top_logits``), a drafter's loss
-against them (``distill_loss``, ``distill_loss_and_grad``), and the test that accepts the drafter's tokens (``verify_drafts``).
+against them (``distill_loss``, ``distill_loss_and_grad``), the test that accepts the drafter's tokens (``verify_drafts``), and what is
+reported of tokens, or learnt from them (``token_logprobs``, ``token_logprobs_grad``).
 Argument checks and outputs only: the work is done by the entry points of the same purpose in ``include/lda_b200.h``, queued on
 the current stream of the tensors' device.  There is no fallback: tensors that are not on a GPU are refused, and so is tracing
 (``torch.compile`` leaves the calls outside of its graphs).
 """
 
 from __future__ import annotations
+
+from typing import NamedTuple
 
 import torch
 from torch.autograd import forward_ad
@@ -160,6 +163,17 @@ def _loss(logits, ids, values, lse, temperature):
     return loss
 
 
+def _given_grad(grad, logits):
+    """Checks a tensor that a gradient goes to; returns its row stride."""
+    if grad.dtype != logits.dtype or grad.shape != logits.shape:
+        raise ValueError("grad: must have the logits' type and shape")
+    if grad.requires_grad:
+        raise ValueError("grad: a tensor that autograd follows cannot be written to (detach it)")
+    stride = _rows(grad, "grad")[3]
+    _here(grad, "grad", logits.device)
+    return stride
+
+
 def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
     """Queues the gradient; grad None: into a new tensor.  Returns it."""
     device = _cuda(logits, "logits")
@@ -169,12 +183,7 @@ def _grad(logits, ids, values, lse, temperature, weights, loss, grad):
     if not given:
         grad, grad_stride = torch.empty_like(logits, memory_format=torch.contiguous_format), V
     else:
-        if grad.dtype != logits.dtype or grad.shape != logits.shape:
-            raise ValueError("grad: must have the logits' type and shape")
-        if grad.requires_grad:
-            raise ValueError("grad: a tensor that autograd follows cannot be written to (detach it)")
-        grad_stride = _rows(grad, "grad")[3]
-        _here(grad, "grad", device)
+        grad_stride = _given_grad(grad, logits)
     w = _optional(weights, "weights", rows, device)
     _call("lda_distill_grad", device, logits.data_ptr(), code, rows, V, stride, *lists, temperature, w,
           None if loss is None else loss.data_ptr(), grad.data_ptr(), grad_stride)
@@ -259,3 +268,99 @@ def verify_drafts(draft_offsets, drafts, target, draft_probs, accept_u, draw_u, 
     if given:
         increment_version((tokens, accepted))  # (a graph that has saved them, as an embedding's indices, finds out)
     return tokens, accepted
+
+
+class TokenLogprobs(NamedTuple):
+    logprobs: torch.Tensor
+    entropy: torch.Tensor
+    stats: torch.Tensor
+    ids: torch.Tensor | None
+    alternatives: torch.Tensor | None
+
+
+class _Logprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, top, temperature):
+        logprobs, entropy, stats, ids, alternatives = _logprobs(logits, tokens, top, temperature)
+        ctx.save_for_backward(logits, tokens, stats)
+        ctx.temperature = temperature
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*(x for x in (stats, ids, alternatives) if x is not None))
+        return logprobs, entropy, stats, ids, alternatives
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_logprobs, d_entropy, *_):
+        logits, tokens, stats = ctx.saved_tensors
+        weights = (None if d is None else d.contiguous() for d in (d_logprobs, d_entropy))
+        return _logprobs_grad(logits.detach(), tokens, stats, *weights, ctx.temperature, None), None, None, None
+
+
+def _logprobs(logits, tokens, top, temperature):
+    device = _cuda(logits, "logits")
+    code, rows, V, stride = _rows(logits, "logits")
+    tokens_ptr = _vector(tokens, "tokens", torch.int32, rows, device)
+    logprobs = logits.new_empty(rows, dtype=torch.float32)
+    entropy = logits.new_empty(rows, dtype=torch.float32)
+    stats = logits.new_empty((rows, 3), dtype=torch.float32)
+    ids = alternatives = ids_ptr = alternatives_ptr = None
+    if top:
+        ids = logits.new_empty((rows, top), dtype=torch.int32)
+        alternatives = logits.new_empty((rows, top), dtype=torch.float32)
+        ids_ptr, alternatives_ptr = ids.data_ptr(), alternatives.data_ptr()
+    _call("lda_token_logprobs", device, logits.data_ptr(), code, rows, V, stride, tokens_ptr, top, temperature, logprobs.data_ptr(),
+          entropy.data_ptr(), stats.data_ptr(), ids_ptr, alternatives_ptr)
+    return logprobs, entropy, stats, ids, alternatives
+
+
+def _logprobs_grad(logits, tokens, stats, logprob_weights, entropy_weights, temperature, grad):
+    device = _cuda(logits, "logits")
+    code, rows, V, stride = _rows(logits, "logits")
+    tokens_ptr = _vector(tokens, "tokens", torch.int32, rows, device)
+    if stats.shape != (rows, 3):
+        raise ValueError(f"stats: [{rows}, 3] is needed, not {tuple(stats.shape)}")
+    stats_ptr = _vector(stats.view(-1), "stats", torch.float32, 3 * rows, device) if stats.is_contiguous() else 0
+    if not stats_ptr and rows:
+        raise ValueError("stats: as token_logprobs gives them, and contiguous")
+    given = grad is not None
+    if not given:
+        grad, grad_stride = torch.empty_like(logits, memory_format=torch.contiguous_format), V
+    else:
+        grad_stride = _given_grad(grad, logits)
+    _call("lda_token_logprobs_grad", device, logits.data_ptr(), code, rows, V, stride, tokens_ptr, stats_ptr,
+          _optional(logprob_weights, "logprob_weights", rows, device), _optional(entropy_weights, "entropy_weights", rows, device), temperature,
+          grad.data_ptr(), grad_stride)
+    if given:
+        increment_version(grad)  # (a graph that has saved what was there finds out)
+    return grad
+
+
+def token_logprobs(logits, tokens, top: int = 0, temperature: float = 1.0):
+    """Log probabilities of given tokens under softmax(logits / temperature), and the rows' entropies, in one pass over the logits.
+
+    tokens: int32 [rows]; one outside the vocabulary is padding, of log probability 0.  Returns (logprobs, entropy, stats, ids, alternatives):
+    float32 [rows] each, in natural units; stats float32 [rows, 3]: the largest logit, the logarithm of the sum of exponentials relative to it,
+    and the mean distance from it over the temperature, which ``token_logprobs_grad`` needs; with top > 0 the `top` largest
+    words and their log probabilities, int32 and float32 [rows, top], as ``top_logits`` orders them (else None).  logprobs and entropy are
+    differentiable once, in reverse mode, with respect to ``logits``; the rest is not followed by autograd.  Of a backward pass that
+    is captured into a CUDA graph the same holds as for ``distill_loss``; ``token_logprobs_grad`` needs no autograd.
+    """
+    if not 0 <= top <= _b.LDA_TOP_MAX:
+        raise ValueError(f"top: 0 to {_b.LDA_TOP_MAX}, not {top}")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(logits).tangent is not None:
+        raise NotImplementedError("token_logprobs: forward-mode differentiation is not offered")
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return TokenLogprobs(*_Logprobs.apply(logits, tokens, top, temperature))
+    return TokenLogprobs(*_logprobs(logits, tokens, top, temperature))
+
+
+def token_logprobs_grad(logits, tokens, stats, logprob_weights=None, entropy_weights=None, temperature: float = 1.0, grad=None):
+    """Gradient of sum(logprob_weights * logprobs + entropy_weights * entropy) with respect to the logits, without autograd.
+
+    logits, tokens, temperature: those of a call of ``token_logprobs``, stats: what it returned.  Weights: float32 [rows], None for 0; a row of
+    weights 0 has gradient 0, whatever it holds.  grad: where it goes, None for a new tensor; the logits themselves are allowed and are
+    overwritten then.
+    """
+    if logits.requires_grad:
+        logits = logits.detach()
+    return _logprobs_grad(logits, tokens, stats, logprob_weights, entropy_weights, temperature, grad)
