@@ -4,154 +4,11 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax.  The rows that share a head of the cache (the new tokens of a
 // sequence times the query heads of a group) are taken together, so that a key is read once for all of them.
-#include "cache.cuh"
-#include "rows.cuh"
+#include "attend.cuh"
 
 namespace lda {
 
 constexpr int KEYS = 64;  // of a tile
-
-struct AttendArgs {
-    CacheView cache;
-    const void* q;
-    void* out;
-    int64_t q_token, q_head, out_token, out_head, mask_stride;
-    const int64_t* mask;  // null: a token sees those before it and itself
-    int32_t mask_words, heads, group;
-    float scale;  // by which a score becomes a power of two's exponent
-    int ctas;
-    float* part;   // [2 ctas][rows of a tile][padded dim]: sums of parts of an item
-    float2* ml;    // [2 ctas][rows of a tile]: their maxima and norms
-    int4* desc;    // [ctas]: the item that a CTA begins and others go on with: sequence (-1: none), head, row tile, how many others
-};
-
-// --- how the work is shared out -------------------------------------------------------------------------------------------------
-// An item is a row tile of a head of a sequence; it has a unit for every tile of keys.  All units stand in one line (by sequence, head, row
-// tile, keys), and every CTA takes an equal run of them.  So contexts of any lengths keep all CTAs busy to the end, few long ones too; an item
-// that does not lie within one run leaves parts that k_attend_join puts together.
-struct AttendShare {
-    int64_t total, lo, hi;  // units in all, and of this CTA
-    int ctas;               // that take part
-    __device__ __forceinline__ int64_t begin(int c) const { return total * c / ctas; }
-    // The CTA that has unit u.
-    __device__ __forceinline__ int owner(int64_t u) const { return (int)(((u + 1) * ctas - 1) / total); }
-};
-
-struct AttendItem {
-    CacheSeq seq;
-    int b, keys, row_tiles, tiles, head, row_tile, tile;
-    template <int ROWS>
-    __device__ __forceinline__ void load(const AttendArgs& a, int b_)
-    {
-        b = b_;
-        seq = a.cache.seq(b);
-        const int64_t most = (int64_t)a.cache.width * a.cache.page_size.d;
-        keys = (int)min((int64_t)seq.start + seq.n, most);
-        row_tiles = (int)(((int64_t)seq.n * a.group + ROWS - 1) / ROWS);
-        tiles = max(1, (int)(((int64_t)keys + KEYS - 1) / KEYS));  // (rows without keys are written too)
-    }
-    __device__ __forceinline__ int64_t units(const AttendArgs& a) const { return (int64_t)row_tiles * tiles * a.cache.kv_heads; }
-    __device__ __forceinline__ void at(int64_t unit)
-    {
-        const int64_t item = unit / tiles;
-        tile = (int)(unit - item * tiles);
-        head = (int)(item / row_tiles);
-        row_tile = (int)(item - (int64_t)head * row_tiles);
-    }
-    // The next unit of the line; there is one.
-    template <int ROWS>
-    __device__ __forceinline__ void next(const AttendArgs& a)
-    {
-        if (++tile < tiles) return;
-        tile = 0;
-        if (++row_tile < row_tiles) return;
-        row_tile = 0;
-        if (++head < a.cache.kv_heads) return;
-        head = 0;
-        do load<ROWS>(a, b + 1);
-        while (row_tiles == 0 && b + 1 < a.cache.seqs);
-    }
-};
-
-// Units that a CTA takes at least: what joining a part costs is about what a few tiles cost.
-constexpr int LEAST_UNITS = 4;
-
-// This CTA's share, and its first unit's item.  `red`: 34 numbers in shared memory.  False: it has none.
-template <int ROWS>
-__device__ __forceinline__ bool attend_share(const AttendArgs& a, int cta, AttendShare& s, AttendItem& item, unsigned long long* red)
-{
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
-    __shared__ int s_b;
-    __shared__ unsigned long long s_before;
-    AttendItem own;
-    unsigned long long sum = 0, mine = 0;
-    for (int b = tid; b < a.cache.seqs; b += threads) {
-        own.load<ROWS>(a, b);
-        mine = own.units(a);
-        sum += mine;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) red[warp] = sum;
-    __syncthreads();
-    s.total = 0;
-    for (int w = 0; w < warps; ++w) s.total += red[w];
-    s.ctas = (int)min((int64_t)a.ctas, max((int64_t)1, s.total / LEAST_UNITS));
-    if (s.total == 0 || cta >= s.ctas) return false;
-    s.lo = s.begin(cta), s.hi = s.begin(cta + 1);
-    // the sequence that has unit lo
-    unsigned long long before = 0;
-    for (int base = 0; base < a.cache.seqs; base += threads) {
-        if (a.cache.seqs > threads) {
-            mine = 0;
-            if (base + tid < a.cache.seqs) {
-                own.load<ROWS>(a, base + tid);
-                mine = own.units(a);
-            }
-        }
-        unsigned long long upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
-        }
-        __syncthreads();
-        if (lane == 31) red[warp] = upto;
-        __syncthreads();
-        unsigned long long all = 0, start = before;
-        for (int w = 0; w < warps; ++w) {
-            if (w < warp) start += red[w];
-            all += red[w];
-        }
-        start += upto - mine;
-        if (mine && start <= (unsigned long long)s.lo && (unsigned long long)s.lo < start + mine) s_b = base + tid, s_before = start;
-        before += all;
-    }
-    __syncthreads();
-    item.load<ROWS>(a, s_b);
-    item.at(s.lo - (int64_t)s_before);
-    return true;
-}
-
-// --- masks -----------------------------------------------------------------------------------------------------------------------
-
-// Which keys of a tile (bit j: key KEYS tile + j) a new token, number `place` of its sequence, sees.
-__device__ __forceinline__ unsigned long long attend_window(const AttendArgs& a, const CacheSeq& seq, int place, int tile)
-{
-    const int64_t from = (int64_t)tile * KEYS - seq.start;  // the new token that the tile's first key belongs to
-    if (from <= -KEYS) return ~0ull;
-    const auto word = [&](int64_t i) -> unsigned long long {
-        if (!a.mask) {
-            const int64_t left = place - 64 * i;  // bits 0..left
-            return left >= 63 ? ~0ull : left < 0 ? 0ull : (2ull << left) - 1;
-        }
-        return i < a.mask_words ? (unsigned long long)a.mask[(seq.first + place) * a.mask_stride + i] : 0ull;
-    };
-    if (from < 0) return word(0) << -from | ((1ull << -from) - 1);
-    const int64_t i = from >> 6;
-    const int shift = (int)(from & 63);
-    return word(i) >> shift | (shift ? word(i + 1) << (64 - shift) : 0ull);
-}
 
 // --- matrix products -------------------------------------------------------------------------------------------------------------
 
@@ -175,39 +32,6 @@ __device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t 
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-template <typename T>
-__device__ __forceinline__ uint32_t pack_two(float x, float y)
-{
-    if constexpr (T_is_bf16<T>) {
-        const __nv_bfloat162 two = __floats2bfloat162_rn(x, y);
-        return *reinterpret_cast<const uint32_t*>(&two);
-    } else {
-        const __half2 two = __floats2half2_rn(x, y);
-        return *reinterpret_cast<const uint32_t*>(&two);
-    }
-}
-
-// Exponent that is added to all of a row's probabilities before they are rounded for the second product: fp16 has full precision
-// only down to 2^-14, which a row of a hundred thousand keys reaches; up to 2^14 it has as much room above 1.
-template <typename T>
-constexpr float RAISE = T_is_bf16<T> ? 0.0f : 14.0f;
-
-// Whether one of a group's eight values is infinite or no number; such values become zero.
-template <typename T>
-__device__ __forceinline__ bool drop_wild(uint4& g)
-{
-    constexpr uint32_t EXP = T_is_bf16<T> ? 0x7F80u : 0x7C00u;
-    uint32_t w[4] = {g.x, g.y, g.z, g.w};
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if ((w[i] & EXP) == EXP) w[i] &= 0xFFFF0000u, any = true;
-        if ((w[i] >> 16 & EXP) == EXP) w[i] &= 0x0000FFFFu, any = true;
-    }
-    g = make_uint4(w[0], w[1], w[2], w[3]);
-    return any;
-}
-
 template <int DIM, int ROWS>
 struct AttendShape {
     static constexpr int THREADS = 128;
@@ -229,7 +53,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
     using S = AttendShape<DIM, ROWS>;
     constexpr int NK = KEYS / S::KEY_GROUPS / 8, ND = DIM / 8, CH = DIM / 8;  // blocks of 8 keys of a warp, of 8 columns; groups of a row
     extern __shared__ __align__(128) uint8_t dynamic[];
-    __shared__ unsigned long long red[34], wild[S::STAGES];
+    __shared__ unsigned long long red[4], wild[S::STAGES];
     __shared__ __align__(8) uint16_t valid[S::STAGES][4];
     __shared__ float s_m[4][16], s_l[4][16];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rg = warp % S::ROW_GROUPS, kg = warp / S::ROW_GROUPS;
@@ -240,7 +64,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
     AttendShare share;
     AttendItem item, ahead;
     int4 begun = make_int4(-1, 0, 0, 0);
-    if (!attend_share<ROWS>(a, blockIdx.x, share, item, red)) {
+    if (!attend_share<ROWS, KEYS>(a, blockIdx.x, share, item, red)) {
         if (tid == 0) a.desc[blockIdx.x] = begun;
         return;
     }
@@ -277,7 +101,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(k), "r"(size) : "memory");
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + S::TILE_BYTES), "l"(v), "r"(size) : "memory");
             }
-            if (++to_copy < share.hi) ahead.next<ROWS>(a);
+            if (++to_copy < share.hi) ahead.next<ROWS, KEYS>(a);
             look();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -533,7 +357,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
         if (!ends && item_begin >= share.lo)
             begun = make_int4(item.b, item.head, item.row_tile, share.owner(item_begin + item.tiles - 1) - (int)blockIdx.x);
         if (unit + 1 < share.hi) {
-            item.next<ROWS>(a);
+            item.next<ROWS, KEYS>(a);
             item_begin = unit + 1;
             __syncthreads();
             begin_item();
@@ -545,7 +369,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
 // The parts of items that several CTAs have worked on, by a warp per row: in the order of the keys, so that the same call gives the same
 // bits.  Every such item begins in one CTA, which has said so.
 constexpr int JOIN_WARPS = 4;
-template <typename T, int DIM, int ROWS>
+template <typename T, int DIM>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_constant__ AttendArgs a)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -553,26 +377,26 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_co
     if (item.x < 0) return;
     const CacheSeq seq = a.cache.seq(item.x);
     const int lane = threadIdx.x & 31, r = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
-    const int64_t row = (int64_t)item.z * ROWS + r;
+    const int64_t row = (int64_t)item.z * a.rows + r;
     if (row >= (int64_t)seq.n * a.group) return;
     const int parts = item.w + 1;
     const auto slot = [&](int i) { return i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i); };
     float most = -INFINITY;
-    for (int i = lane; i < parts; i += 32) most = fmaxf(most, a.ml[slot(i) * ROWS + r].x);
+    for (int i = lane; i < parts; i += 32) most = fmaxf(most, a.ml[slot(i) * a.rows + r].x);
     most = warp_reduce_max(most);
     constexpr int EACH = DIM / 32;
     float acc[EACH] = {}, norm = 0.0f;
     for (int base = 0; base < parts; base += 32) {
         float w = 0.0f;
         if (base + lane < parts) {
-            const float2 ml = a.ml[slot(base + lane) * ROWS + r];
+            const float2 ml = a.ml[slot(base + lane) * a.rows + r];
             w = ml.x == most ? 1.0f : exp2_unit(ml.x - most);
             norm += ml.y * w;
         }
         const int n = min(32, parts - base);
         for (int i = 0; i < n; ++i) {
             const float f = __shfl_sync(0xffffffffu, w, i);
-            const float* from = a.part + ((int64_t)slot(base + i) * ROWS + r) * DIM + lane * EACH;
+            const float* from = a.part + ((int64_t)slot(base + i) * a.rows + r) * DIM + lane * EACH;
             if (lane * EACH < a.cache.dim)
 #pragma unroll
                 for (int e = 0; e < EACH; e += 2) {
@@ -594,19 +418,19 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_co
 
 // --- host ------------------------------------------------------------------------------------------------------------------------
 
-// Rows of a tile: those that a sequence has on average share a key's read from shared memory.
-static int attend_rows(int64_t tokens, int64_t seqs, int group)
-{
-    const int64_t rows = (tokens + seqs - 1) / seqs * group;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-}
-static int attend_dim(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
-static int attend_ctas(int dim) { return 148 * (dim == 64 ? 3 : dim == 128 ? 2 : 1); }
-
-struct AttendSpace {
+struct AttendPlan {
+    bool tc;
+    int rows, dim, ctas;          // of a tile; padded; CTAs
     int64_t part, ml, desc, all;  // bytes up to each
-    AttendSpace(int ctas, int rows, int dim)
+    AttendPlan(const lda_paged_cache& cache, int64_t tokens, int32_t heads)
     {
+        tc = attend_tc_takes(cache);
+        dim = cache.dim <= 64 ? 64 : cache.dim <= 128 ? 128 : 256;
+        // those that a sequence has on average share what is read from shared memory
+        const int64_t most = (tokens + cache.n_seqs - 1) / cache.n_seqs * (heads / cache.kv_heads);
+        if (tc) rows = most <= 32 ? 32 : most <= 64 ? 64 : 256;
+        else rows = most <= 16 ? 16 : most <= 32 || dim == 256 ? 32 : 64;
+        ctas = 148 * (tc || dim == 256 ? 1 : dim == 128 ? 2 : 3);
         part = 0;
         ml = (int64_t)2 * ctas * rows * dim * 4;
         desc = ml + (int64_t)2 * ctas * rows * 8;
@@ -615,7 +439,7 @@ struct AttendSpace {
 };
 
 template <typename T, int DIM, int ROWS>
-static cudaError_t launch_attend(AttendArgs a, cudaStream_t st)
+static cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st)
 {
     using S = AttendShape<DIM, ROWS>;
     static std::atomic<bool> allowed[64];
@@ -628,10 +452,20 @@ static cudaError_t launch_attend(AttendArgs a, cudaStream_t st)
         if (dev < 64) allowed[dev].store(true, std::memory_order_release);
     }
     k_attend<T, DIM, ROWS><<<a.ctas, S::THREADS, S::SHARED, st>>>(a);
-    e = cudaGetLastError();
+    return cudaGetLastError();
+}
+
+template <typename T, int DIM>
+static cudaError_t attend_by_rows(const AttendArgs& a, const AttendPlan& plan, const lda_paged_cache& cache, cudaStream_t st)
+{
+    cudaError_t e;
+    if (plan.tc) e = attend_tc(a, cache, st);
+    else if (plan.rows == 16) e = launch_attend<T, DIM, 16>(a, st);
+    else if (plan.rows == 32 || DIM == 256) e = launch_attend<T, DIM, 32>(a, st);
+    else e = launch_attend<T, DIM, DIM == 256 ? 32 : 64>(a, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)a.ctas, ROWS / JOIN_WARPS);
+    c.gridDim = dim3((unsigned)a.ctas, (unsigned)(a.rows / JOIN_WARPS));
     c.blockDim = dim3(32 * JOIN_WARPS);
     c.stream = st;
     cudaLaunchAttribute at{};
@@ -639,22 +473,15 @@ static cudaError_t launch_attend(AttendArgs a, cudaStream_t st)
     at.val.programmaticStreamSerializationAllowed = 1;
     c.attrs = &at;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, k_attend_join<T, DIM, ROWS>, a);
-}
-
-template <typename T, int DIM>
-static cudaError_t attend_by_rows(const AttendArgs& a, int rows, cudaStream_t st)
-{
-    if (rows == 16) return launch_attend<T, DIM, 16>(a, st);
-    if (rows == 32 || DIM == 256) return launch_attend<T, DIM, 32>(a, st);
-    if constexpr (DIM < 256) return launch_attend<T, DIM, 64>(a, st);
-    return cudaErrorInvalidValue;
+    return cudaLaunchKernelEx(&c, k_attend_join<T, DIM>, a);
 }
 
 template <typename T>
-static cudaError_t attend_by_dim(const AttendArgs& a, int dim, int rows, cudaStream_t st)
+static cudaError_t attend_by_dim(const AttendArgs& a, const AttendPlan& plan, const lda_paged_cache& cache, cudaStream_t st)
 {
-    return dim == 64 ? attend_by_rows<T, 64>(a, rows, st) : dim == 128 ? attend_by_rows<T, 128>(a, rows, st) : attend_by_rows<T, 256>(a, rows, st);
+    return plan.dim == 64    ? attend_by_rows<T, 64>(a, plan, cache, st)
+           : plan.dim == 128 ? attend_by_rows<T, 128>(a, plan, cache, st)
+                             : attend_by_rows<T, 256>(a, plan, cache, st);
 }
 
 static int attend_check(const lda_paged_cache* cache, int64_t tokens, int32_t heads, CacheView& view)
@@ -663,14 +490,6 @@ static int attend_check(const lda_paged_cache* cache, int64_t tokens, int32_t he
     if (rc != LDA_OK) return rc;
     if (heads < 1 || heads % cache->kv_heads) return LDA_EINVAL;
     return heads > LDA_HEADS_MAX ? LDA_ERANGE : LDA_OK;
-}
-
-// Rows of a tile and the padded dimension of a call.
-static void attend_shape(const lda_paged_cache* cache, int64_t tokens, int32_t heads, int& rows, int& dim)
-{
-    dim = attend_dim(cache->dim);
-    rows = attend_rows(tokens, cache->n_seqs, heads / cache->kv_heads);
-    if (dim == 256 && rows > 32) rows = 32;
 }
 
 }  // namespace lda
@@ -682,9 +501,7 @@ extern "C" int64_t lda_tree_attention_workspace(const lda_paged_cache* cache, in
     const int rc = attend_check(cache, tokens, heads, view);
     if (rc != LDA_OK) return rc;
     if (tokens == 0 || cache->n_seqs == 0) return 0;
-    int rows, dim;
-    attend_shape(cache, tokens, heads, rows, dim);
-    return AttendSpace(attend_ctas(dim), rows, dim).all;
+    return AttendPlan(*cache, tokens, heads).all;
 }
 
 extern "C" int lda_tree_attention(const lda_paged_cache* cache, int64_t tokens, const void* q_dev, int64_t q_token_stride,
@@ -703,21 +520,19 @@ extern "C" int lda_tree_attention(const lda_paged_cache* cache, int64_t tokens, 
     if (!heads_ok(q_dev, q_token_stride, q_head_stride) || !heads_ok(out_dev, out_token_stride, out_head_stride)) return LDA_EINVAL;
     const int64_t most = 1ll << 31;
     if (q_token_stride > most || q_head_stride > most || out_token_stride > most || out_head_stride > most) return LDA_ERANGE;
-    int rows, dim;
-    attend_shape(cache, tokens, heads, rows, dim);
-    a.ctas = attend_ctas(dim);
-    const AttendSpace space(a.ctas, rows, dim);
-    if (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < space.all) return LDA_EINVAL;
+    const AttendPlan plan(*cache, tokens, heads);
+    if (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < plan.all) return LDA_EINVAL;
+    a.ctas = plan.ctas, a.rows = plan.rows;
     a.q = q_dev, a.out = out_dev;
     a.q_token = q_token_stride, a.q_head = q_head_stride, a.out_token = out_token_stride, a.out_head = out_head_stride;
     a.mask = mask_dev, a.mask_stride = mask_stride, a.mask_words = mask_words;
     a.heads = heads, a.group = heads / cache->kv_heads;
     a.scale = (float)(scale * 1.4426950408889634);
-    a.part = (float*)((char*)workspace_dev + space.part);
-    a.ml = (float2*)((char*)workspace_dev + space.ml);
-    a.desc = (int4*)((char*)workspace_dev + space.desc);
-    const cudaError_t e = cache->dtype == LDA_F16 ? attend_by_dim<__half>(a, dim, rows, (cudaStream_t)cuda_stream)
-                                                  : attend_by_dim<__nv_bfloat16>(a, dim, rows, (cudaStream_t)cuda_stream);
+    a.part = (float*)((char*)workspace_dev + plan.part);
+    a.ml = (float2*)((char*)workspace_dev + plan.ml);
+    a.desc = (int4*)((char*)workspace_dev + plan.desc);
+    const cudaError_t e = cache->dtype == LDA_F16 ? attend_by_dim<__half>(a, plan, *cache, (cudaStream_t)cuda_stream)
+                                                  : attend_by_dim<__nv_bfloat16>(a, plan, *cache, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return LDA_ECUDA;

@@ -1,0 +1,714 @@
+// Attention over a paged cache on the tensor cores' own memory: heads of up to 128 values, pages of a multiple of 8 slots.
+//
+// A tile has 128 keys and 128 rows.  S = Q K^T and O += P V are matrix products of a whole tile, issued by one thread: K and V from shared
+// memory, where tensor copies bring them page by page, S, P and O in tensor memory (P in S's place).  There are two teams of four warps, each
+// with an S and an O of its own; a thread has a row: it reads the row's scores, makes probabilities of them and writes these back, while the
+// products of the other team run.
+//   items of more than 128 rows  the teams have 128 rows each, and every tile of keys serves both
+//   others                       the teams take the tiles of keys in turn, and the two O are added up at the item's end.  Of 64 or 32 rows
+//                                (ROWS) every one stands in the tile twice or four times, and each of its copies has the probabilities of
+//                                its own half or fourth of the keys (zeros for the others), so that all warps work.
+// The products cost the same, 128 rows or 4: 1024 cycles of the tensor cores for a tile of 128 values a head, whose keys and values take 2800
+// cycles to come from memory.
+#include <cuda.h>
+
+#include "attend.cuh"
+
+namespace lda {
+
+constexpr int TC_KEYS = 128, TC_ROWS = 128;
+constexpr int TC_TEAM = 128, TC_THREADS = 2 * TC_TEAM + 96;  // two teams; a warp that issues products, two that copy
+constexpr uint32_t TC_S = 0, TC_O = 256;                // columns of tensor memory: S twice, O twice
+
+template <int DIM, int ROWS>
+struct TcShape {
+    static constexpr bool PAIR = ROWS == 256;                    // the teams may have rows of their own
+    static constexpr int HALVES = DIM / 64;                      // 128 bytes of every row at a time
+    static constexpr int TILE = TC_KEYS * DIM * 2;               // bytes of keys, values or queries
+    static constexpr int K_STAGES = DIM == 128 ? 2 : 4, V_STAGES = DIM == 128 ? (PAIR ? 2 : 3) : 4;  // (a tile's values are needed later and longer)
+    static constexpr int COLS = PAIR ? 128 : ROWS;               // of S that a thread looks at
+    static constexpr int GROUPS = TC_ROWS / COLS;                // of keys
+    static constexpr int TOGETHER = 16 / GROUPS, PITCH = DIM + 4;  // rows whose parts are added up at a time
+    static constexpr int K_AT = 0, V_AT = K_STAGES * TILE, Q_AT = V_AT + V_STAGES * TILE, REGION_AT = Q_AT + (PAIR ? 2 : 1) * TILE;
+    static constexpr int SHARED = REGION_AT + 2 * GROUPS * TOGETHER * PITCH * 4 + 1024;  // (its start is moved up to a multiple of 1024)
+};
+
+struct TcBars {
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_full[2], o_done[2], q_full, q_empty;
+};
+
+__device__ __forceinline__ uint32_t tc_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void tc_init(uint64_t& bar, uint32_t arrivals)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(tc_smem(&bar)), "r"(arrivals) : "memory");
+}
+__device__ __forceinline__ void tc_arrive(uint64_t& bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(tc_smem(&bar)) : "memory"); }
+__device__ __forceinline__ void tc_expect(uint64_t& bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc_smem(&bar)), "r"(bytes) : "memory");
+}
+// Waits for a phase.  Every wait here ends by itself; one that has not after some seconds gives up and tells the others, which then do
+// not wait any more.
+constexpr int TC_POLLS = 1 << 22;
+__device__ __forceinline__ bool tc_wait(uint64_t& bar, uint32_t parity, volatile int* failed)
+{
+    const uint32_t at = tc_smem(&bar);
+    for (int i = 0; i < TC_POLLS; ++i) {
+        uint32_t done;
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                     : "=r"(done)
+                     : "r"(at), "r"(parity)
+                     : "memory");
+        if (done) return true;
+        if (*failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
+// What a product reads or has written, seen by the other side of a barrier.
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint64_t& bar, bool leads)
+{
+    asm volatile("{ .reg .pred q; setp.ne.u32 q, %1, 0; @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(tc_smem(&bar)),
+                 "r"((uint32_t)leads)
+                 : "memory");
+}
+// An operand in shared memory, rows of 128 bytes swizzled among eight, in units of 16 bytes: its place, and what is the same for all places.
+// `across`: bytes from one group of 64 elements to the next where the contiguous dimension is not the one that is summed over.
+__device__ __forceinline__ uint32_t tc_operand_at(uint32_t at) { return at >> 4; }
+__device__ __forceinline__ constexpr uint32_t tc_operand_low(uint32_t across) { return across >> 4 << 16; }
+constexpr uint32_t TC_OPERAND_HIGH = 1024 >> 4 | 1u << 14 | 2u << 29;
+// Types (fp16 0, bf16 1; sums of single precision), whether B is contiguous in the columns, columns; 128 rows.
+__device__ __forceinline__ constexpr uint32_t tc_kind(bool bf16, bool turned, uint32_t columns)
+{
+    return 1u << 4 | (uint32_t)bf16 << 7 | (uint32_t)bf16 << 10 | (uint32_t)turned << 16 | columns / 8 << 17 | (uint32_t)(TC_ROWS / 16) << 24;
+}
+// By a whole warp, of which the lane `leads` issues: what the product needs is the same in all lanes then, and stays in uniform registers.
+__device__ __forceinline__ void tc_product_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t kind, bool add, bool leads)
+{
+    asm volatile("{ .reg .pred p, q; .reg .b64 x, y; setp.ne.u32 p, %5, 0; setp.ne.u32 q, %6, 0; mov.b64 x, {%1, %4}; mov.b64 y, {%2, %4}; "
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p; }" ::"r"(d),
+                 "r"(a), "r"(b), "r"(kind), "r"(TC_OPERAND_HIGH), "r"((uint32_t)add), "r"((uint32_t)leads)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_product_tensor(uint32_t d, uint32_t a, uint32_t b, uint32_t kind, bool add, bool leads)
+{
+    asm volatile("{ .reg .pred p, q; .reg .b64 y; setp.ne.u32 p, %5, 0; setp.ne.u32 q, %6, 0; mov.b64 y, {%2, %4}; "
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p; }" ::"r"(d),
+                 "r"(a), "r"(b), "r"(kind), "r"(TC_OPERAND_HIGH), "r"((uint32_t)add), "r"((uint32_t)leads)
+                 : "memory");
+}
+// 32 columns of a thread's row of tensor memory.
+__device__ __forceinline__ void tc_load(uint32_t (&r)[32], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+                   "=r"(r[31])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tc_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_store(uint32_t at, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+                 "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tc_store(uint32_t at, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tc_load(uint32_t (&r)[8], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tc_store(uint32_t at, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t tc_load(uint32_t at)
+{
+    uint32_t r;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
+    return r;
+}
+// 64 columns of `rows` slots of a page's head; every coordinate is inside the cache, the first one a multiple of 64.
+__device__ __forceinline__ void tc_copy(uint32_t to, const CUtensorMap* map, int column, int slot, int head, int page, uint64_t& bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+                 "l"(map), "r"(column), "r"(slot), "r"(head), "r"(page), "r"(tc_smem(&bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tc_team_sync(int team) { asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory"); }
+__device__ __forceinline__ void tc_rows_sync() { asm volatile("bar.sync 3, 256;" ::: "memory"); }
+__device__ __forceinline__ uint4 tc_shared16(uint32_t at)
+{
+    uint4 x;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at) : "memory");
+    return x;
+}
+__device__ __forceinline__ void tc_put16(uint32_t at, uint4 x)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+
+struct TcMaps {
+    CUtensorMap k, v;
+    int32_t group_bits;  // 2^group_bits slots come in a copy: a power of two that divides a page, 8 to 128
+};
+
+// How far a row's largest exponent may rise above what its probabilities are relative to before its sums are moved: they need no more
+// digits up to there (2^8 times the probability, fp16 2^15), and most rows never do it after their first tile.
+constexpr float TC_SLACK = 8.0f;
+template <typename T>
+constexpr float TC_RAISE = T_is_bf16<T> ? 0.0f : 7.0f;
+
+// A copying warp's walk over its CTA's units, for keys or for values: a lane has one of the tile's groups of slots.
+template <int DIM, int ROWS, int STAGES>
+__device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap* map, int bits, AttendItem item, int n_units, uint32_t to,
+                                          uint64_t* full, uint64_t* empty, uint32_t* valid, unsigned long long (*wild)[2], volatile int* failed)
+{
+    const int lane = threadIdx.x & 31, groups = TC_KEYS >> bits;
+    int page = -1, place = 0;
+    const auto look = [&] {
+        const int key = item.tile * TC_KEYS + (lane << bits);
+        page = lane < groups && key < item.keys ? a.cache.page(item.b, (uint32_t)key, place) : -1;
+    };
+    look();
+    int it = 0;
+#pragma unroll 1
+    for (; it < n_units; ++it) {
+        const int p = page, at = place, head = item.head, s = it % STAGES;
+        const uint32_t there = __ballot_sync(0xffffffffu, p >= 0);
+        const bool ok = tc_wait(empty[s], it / STAGES & 1 ^ 1, failed);
+        if (__any_sync(0xffffffffu, !ok)) break;
+        if (lane == 0) {
+            if (valid) valid[it & 15] = there;
+            if (wild) wild[s][0] = wild[s][1] = 0;
+            tc_expect(full[s], (__popc(there) << bits) * DIM * 2);
+        }
+        __syncwarp();
+        if (p >= 0)
+#pragma unroll
+            for (int h = 0; h < DIM / 64; ++h)
+                tc_copy(to + s * (TC_KEYS * DIM * 2) + h * (TC_KEYS * 128) + (lane << bits) * 128, map, 64 * h, at, head, p, full[s]);
+        if (it + 1 < n_units) {
+            item.template next<ROWS, TC_KEYS>(a);
+            look();
+        }
+    }
+    if (it < n_units) {  // gave up: what is under way still lands
+        int quit = 0;
+        for (int i = max(0, it - STAGES); i < it; ++i) tc_wait(full[i % STAGES], i / STAGES & 1, (volatile int*)&quit);
+    }
+}
+
+template <typename T, int DIM, int ROWS>
+__global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ TcMaps maps)
+{
+    using S = TcShape<DIM, ROWS>;
+    constexpr bool PAIR = S::PAIR;
+    constexpr int GROUPS = S::GROUPS, COLS = S::COLS;
+    extern __shared__ uint8_t dynamic[];
+    __shared__ TcBars bars;
+    __shared__ unsigned long long red[TC_THREADS / 32], wild[4][2];  // (wild: of a stage's keys, those whose values are not all finite)
+    __shared__ uint32_t s_tmem, valid[16];
+    __shared__ int s_failed;
+    __shared__ float s_m[2 * TC_ROWS], s_l[2 * TC_ROWS];
+    const uint32_t base = (tc_smem(dynamic) + 1023) & ~1023u;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const CacheView& c = a.cache;
+    volatile int* failed = &s_failed;
+    if (tid == 0) {
+        for (int i = 0; i < 4; ++i) tc_init(bars.k_full[i], 1), tc_init(bars.k_empty[i], 1), tc_init(bars.v_full[i], 1), tc_init(bars.v_empty[i], 1);
+        for (int i = 0; i < 2; ++i) tc_init(bars.s_full[i], 1), tc_init(bars.p_full[i], TC_TEAM), tc_init(bars.o_done[i], 1);
+        tc_init(bars.q_full, 2 * TC_TEAM), tc_init(bars.q_empty, 1);
+        s_failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    AttendShare share;
+    AttendItem item;
+    int4 begun = make_int4(-1, 0, 0, 0);
+    if (!attend_share<ROWS, TC_KEYS>(a, blockIdx.x, share, item, red)) {
+        if (tid == 0) a.desc[blockIdx.x] = begun;
+        return;
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tc_smem(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc_before();
+    }
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = s_tmem;
+    const int n_units = (int)(share.hi - share.lo);
+    // whether the teams have rows of their own of an item
+    const auto splits = [&](const AttendItem& of) { return PAIR && (int64_t)of.seq.n * a.group - (int64_t)of.row_tile * ROWS > TC_ROWS; };
+
+    if (warp >= 8) {
+        if (warp == 9) {
+            tc_copies<DIM, ROWS, S::K_STAGES>(a, &maps.k, maps.group_bits, item, n_units, base + S::K_AT, bars.k_full, bars.k_empty, valid, nullptr,
+                                                  failed);
+        } else if (warp == 10) {
+            tc_copies<DIM, ROWS, S::V_STAGES>(a, &maps.v, maps.group_bits, item, n_units, base + S::V_AT, bars.v_full, bars.v_empty, nullptr, wild,
+                                                  failed);
+        } else if (warp == 8) {
+            // --- products, a tile's for a team at a time (a job): a job's scores ahead of the outputs of the job before it
+            constexpr uint32_t KIND_S = tc_kind(T_is_bf16<T>, false, TC_KEYS), KIND_O = tc_kind(T_is_bf16<T>, true, DIM);
+            const bool leads = lane == 0;
+            const uint32_t at = __shfl_sync(0xffffffffu, base, 0), tensor = __shfl_sync(0xffffffffu, tmem, 0);
+            const int n = __shfl_sync(0xffffffffu, n_units, 0);
+            bool ok = true;
+            uint32_t waited = 0, n_q = 0;  // phases waited for: of p_full, a bit for each team; of q_full
+            const auto scores = [&](int it, int team, bool first, bool last, bool new_q) {
+                const int ks = it % S::K_STAGES;
+                if (new_q) ok = ok && tc_wait(bars.q_full, n_q++ & 1, failed);
+                if (first) ok = ok && tc_wait(bars.k_full[ks], it / S::K_STAGES & 1, failed);
+                if (!__all_sync(0xffffffffu, ok)) return;
+                tc_after();
+                const uint32_t q = tc_operand_low(16) + tc_operand_at(at + S::Q_AT) + (PAIR ? team * (S::TILE / 16) : 0),
+                               k = tc_operand_low(16) + tc_operand_at(at + S::K_AT) + ks * (S::TILE / 16);
+#pragma unroll
+                for (int i = 0; i < DIM / 16; ++i) {
+                    const uint32_t step = (i / 4 * (TC_KEYS * 128) + i % 4 * 32) / 16;
+                    tc_product_shared(tensor + TC_S + team * TC_KEYS, q + step, k + step, KIND_S, i > 0, leads);
+                }
+                tc_commit(bars.s_full[team], leads);
+                if (last) tc_commit(bars.k_empty[ks], leads);
+            };
+            const auto outputs = [&](int it, int team, bool first, bool last, bool fresh) {
+                const int vs = it % S::V_STAGES;
+                ok = ok && tc_wait(bars.p_full[team], waited >> team & 1, failed);
+                waited ^= 1u << team;
+                if (first) ok = ok && tc_wait(bars.v_full[vs], it / S::V_STAGES & 1, failed);
+                if (!__all_sync(0xffffffffu, ok)) return;
+                tc_after();
+                const uint32_t v = tc_operand_low(TC_KEYS * 128) + tc_operand_at(at + S::V_AT) + vs * (S::TILE / 16);
+#pragma unroll
+                for (int i = 0; i < TC_KEYS / 16; ++i)
+                    tc_product_tensor(tensor + TC_O + team * 128, tensor + TC_S + team * TC_KEYS + 8 * i, v + i * (2048 / 16), KIND_O, i > 0 || !fresh, leads);
+                if (last) tc_commit(bars.v_empty[vs], leads);
+                tc_commit(bars.o_done[team], leads);
+            };
+            int nth = 0, left = item.tiles - item.tile;  // the unit's number in its item here, and how many the item still has
+            bool split = __any_sync(0xffffffffu, splits(item)), fresh_before = false, split_before = false;
+#pragma unroll 1
+            for (int it = 0; it < n && ok; ++it) {
+                const bool begins = nth == 0, fresh = split ? nth == 0 : nth < 2;
+                const int team = split ? 0 : it & 1, team_before = split_before ? 1 : (it - 1) & 1;
+                // (an item's first scores need queries that the rows put down when they are through with the item before it)
+                if (begins && it > 0) outputs(it - 1, team_before, !split_before, true, fresh_before);
+                scores(it, team, true, !split, begins);
+                if (!begins) outputs(it - 1, team_before, !split_before, true, fresh_before);
+                if (split) {
+                    scores(it, 1, false, true, false);
+                    outputs(it, 0, true, false, fresh);
+                }
+                fresh_before = fresh, split_before = split;
+                ++nth;
+                if (--left == 0) {
+                    if (ok) tc_commit(bars.q_empty, leads);
+                    if (it + 1 < n) {
+                        item.tile = item.tiles - 1;
+                        item.template next<ROWS, TC_KEYS>(a);
+                        nth = 0, left = __shfl_sync(0xffffffffu, item.tiles, 0);
+                        split = __any_sync(0xffffffffu, splits(item));
+                    }
+                }
+            }
+            outputs(n - 1, split_before ? 1 : (n - 1) & 1, !split_before, true, fresh_before);
+        }
+        __syncwarp();
+    } else {
+        // --- rows (they go on where a wait gave up, so that all of them meet at their barriers; outputs are undefined then)
+        const int team = warp >> 2, kg = tid % TC_TEAM / COLS;
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+        const uint32_t at_s = tmem + lanes + TC_S + team * TC_KEYS, at_o = tmem + lanes + TC_O + team * 128;
+        const uint32_t at_q = base + S::Q_AT + (PAIR ? team * S::TILE : 0) + tid % TC_TEAM * 128;
+        // a thread's row of an item
+        const auto row_of = [&](const AttendItem& of) { return splits(of) ? tid : tid % COLS; };
+        // a row's queries, once for each of its copies, a half by each team (PAIR: each team has a place for its own)
+        constexpr int Q_EACH = PAIR ? DIM / 8 : DIM / 16;
+        const int q_from = PAIR ? 0 : team * Q_EACH;
+        uint4 q[Q_EACH];
+        const auto get_q = [&](const AttendItem& of) {
+            const int64_t row = (int64_t)of.row_tile * ROWS + row_of(of);
+            const bool there = row < (int64_t)of.seq.n * a.group;
+            const int token = there ? (int)attend_quotient(row, a.group) : 0, h = there ? (int)(row - (int64_t)token * a.group) : 0;
+            const T* from = (const T*)a.q + (of.seq.first + token) * a.q_token + (of.head * a.group + h) * a.q_head + q_from * 8;
+#pragma unroll
+            for (int i = 0; i < Q_EACH; ++i) q[i] = there && (q_from + i) * 8 < c.dim ? __ldg((const uint4*)(from + i * 8)) : make_uint4(0, 0, 0, 0);
+        };
+        const auto put_q = [&] {
+#pragma unroll
+            for (int i = 0; i < Q_EACH; ++i) {
+                const int ch = q_from + i;
+                tc_put16(at_q + ch / 8 * (TC_KEYS * 128) + ((ch % 8 ^ tid % 8) << 4), q[i]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tc_arrive(bars.q_full);
+        };
+        get_q(item);
+        put_q();
+        int it = 0;
+        uint32_t n_s = 0, n_q = 0;  // tiles of the team, queries put down
+#pragma unroll 1
+        while (it < n_units) {
+            const int count = min(item.tiles - item.tile, n_units - it), end = it + count;
+            const bool ends = item.tile + count == item.tiles, last = end == n_units, split = splits(item);
+            const int r = row_of(item);
+            const int64_t item_begin = share.lo + it - item.tile, row0 = (int64_t)item.row_tile * ROWS, all_rows = (int64_t)item.seq.n * a.group - row0;
+            const int rows = (int)min((int64_t)ROWS, all_rows), place = r < rows ? (int)attend_quotient(row0 + r, a.group) : -1;
+            float m = -INFINITY, l = 0.0f;
+            bool any = false;
+#pragma unroll 1
+            for (int u = split ? it : it + ((it ^ team) & 1); u < end; u += split ? 1 : 2) {
+                const int tile = item.tile + u - it;
+                tc_wait(bars.s_full[team], n_s & 1, failed);
+                tc_after();
+                const uint32_t there = *(volatile uint32_t*)&valid[u & 15];
+                const bool full = there == (uint32_t)((1ull << (TC_KEYS >> maps.group_bits)) - 1);
+                unsigned long long bad[2] = {0, 0}, see[2] = {~0ull, ~0ull};
+                const bool masked = !full || (int64_t)(tile + 1) * TC_KEYS > item.seq.start;
+                if (masked) {
+                    // what the row sees of the keys
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int left = item.keys - (tile * TC_KEYS + 64 * i);
+                        see[i] = place < 0 || left <= 0 ? 0ull : attend_window(a, item.seq, place, 2 * tile + i) & (left >= 64 ? ~0ull : (1ull << left) - 1);
+                        if (!full)
+#pragma unroll 1
+                            for (int g = 0; g < 64; g += 8)
+                                if (!(there >> ((64 * i + g) >> maps.group_bits) & 1)) see[i] &= ~(0xFFull << g);
+                    }
+                    // a value that a row does not see must not touch it, whatever it is: infinities and NaN are taken out and added apart
+                    const int vs = u % S::V_STAGES;
+                    tc_wait(bars.v_full[vs], u / S::V_STAGES & 1, failed);
+                    const int from = full ? max(0, (int)min((int64_t)TC_KEYS, (int64_t)item.seq.start - (int64_t)tile * TC_KEYS)) : 0;
+#pragma unroll 2
+                    for (int key = from + tid % TC_TEAM / 8; key < TC_KEYS; key += TC_TEAM / 8)
+#pragma unroll
+                        for (int h = 0; h < S::HALVES; ++h) {
+                            const uint32_t at = base + S::V_AT + vs * S::TILE + (h * TC_KEYS + key) * 128 + tid % 8 * 16;
+                            uint4 g = tc_shared16(at);
+                            if (drop_wild<T>(g)) {
+                                // (where there is no key, what is left of others is not looked at again; said before it is taken out: PAIR's teams
+                                // both look)
+                                if (tile * TC_KEYS + key < item.keys && (there >> (key >> maps.group_bits) & 1)) atomicOr(&wild[vs][key / 64], 1ull << (key & 63));
+                                __threadfence_block();
+                                tc_put16(at, g);
+                            }
+                        }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    tc_team_sync(team);
+                    bad[0] = *(volatile unsigned long long*)&wild[vs][0], bad[1] = *(volatile unsigned long long*)&wild[vs][1];
+                }
+                // the scores are read twice, 32 columns at a time (of 128 in one go the code and the registers would be four times as many)
+                const auto scores = [&](uint32_t (&s)[32], int from) {
+                    tc_load(s, at_s + kg * COLS + from);
+                    tc_loaded();
+                    if (masked) {
+                        const int k = kg * COLS + from;
+                        const uint32_t w = (uint32_t)((k & 64 ? see[1] : see[0]) >> (k & 32));
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (!(w >> j & 1)) s[j] = 0xFF800000u;  // minus infinity
+                    }
+                };
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int from = 0; from < COLS; from += 32) {
+                    uint32_t s[32];
+                    scores(s, from);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[j]), __uint_as_float(s[j + 1])));
+                }
+                top *= a.scale;
+                // (minus infinity is no reason; the first number is)
+                const bool raise = top > (m == -INFINITY ? -INFINITY : m + TC_SLACK);
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float to = fmaxf(m, top), f = to == m ? 1.0f : exp2_unit(m - to);
+                    m = to;
+                    l *= f;
+                    if (any) {  // (O holds something)
+                        tc_wait(bars.o_done[team], (n_s & 1) ^ 1, failed);
+                        tc_after();
+#pragma unroll 1
+                        for (int d = 0; d < DIM; d += 32) {
+                            uint32_t o[32];
+                            tc_load(o, at_o + d);
+                            tc_loaded();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tc_store(at_o + d, o);
+                        }
+                    }
+                }
+                const float shift = (m == -INFINITY ? 0.0f : -m) + TC_RAISE<T>;
+                // the probabilities are rounded to the values' type, which the product takes: half a step each, as much as the output's own
+                // rounding; the norm is that of the unrounded ones
+                float sum[2] = {0.0f, 0.0f};
+#pragma unroll 1
+                for (int from = 0; from < COLS; from += 32) {
+                    uint32_t s[32], p[16];
+                    scores(s, from);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        const float x = exp2_unit(__fmaf_rn(__uint_as_float(s[j]), a.scale, shift)), y = exp2_unit(__fmaf_rn(__uint_as_float(s[j + 1]), a.scale, shift));
+                        sum[0] += x, sum[1] += y;
+                        p[j / 2] = pack_two<T>(x, y);
+                    }
+                    // (of the scores only those are overwritten that have been read for the second time)
+                    tc_store(at_s + (kg * COLS + from) / 2, p);
+                }
+                if (GROUPS > 1) {
+                    const uint32_t zero[16] = {};
+#pragma unroll
+                    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+                        for (int from = 0; from < COLS; from += 32) tc_store(at_s + (((kg + g) % GROUPS) * COLS + from) / 2, zero);
+                }
+                l += sum[0] + sum[1];
+                tc_stored();
+                tc_before();
+                tc_arrive(bars.p_full[team]);
+                any = true;
+                if (bad[0] | bad[1]) {
+                    tc_wait(bars.o_done[team], n_s & 1, failed);
+                    tc_after();
+#pragma unroll 1
+                    for (int k = kg * COLS; k < (kg + 1) * COLS; ++k) {
+                        if (!((k < 64 ? bad[0] : bad[1]) >> (k & 63) & 1)) continue;  // (the same in the warp)
+                        const uint32_t two = tc_load(at_s + k / 2);
+                        tc_loaded();
+                        const uint16_t half = (uint16_t)(k & 1 ? two >> 16 : two);
+                        const float p = cache_value(*reinterpret_cast<const T*>(&half));
+                        int slot = 0;
+                        const int64_t pg = c.page(item.b, (uint32_t)(tile * TC_KEYS + k), slot);
+                        const T* v = (const T*)c.values + pg * c.v_page + slot * c.v_slot + item.head * c.v_head;
+#pragma unroll 1
+                        for (int d = 0; d < c.dim && pg >= 0; d += 8) {
+                            float x[8];
+                            unpack<T>(*(const uint4*)(v + d), x);
+                            uint32_t o[8];
+                            tc_load(o, at_o + d);
+                            tc_loaded();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (p != 0.0f && !(fabsf(x[e]) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + p * x[e]);
+                            tc_store(at_o + d, o);
+                            tc_stored();
+                        }
+                    }
+                    tc_before();
+                }
+                ++n_s;
+            }
+            // --- the item's end, or the share's: the next item's queries, then the sums out or to the parts
+            AttendItem after = item;
+            if (!last) {
+                after.tile = after.tiles - 1;
+                after.template next<ROWS, TC_KEYS>(a);
+                get_q(after);
+                tc_wait(bars.q_empty, n_q++ & 1, failed);  // (the queries before these have been read)
+                put_q();
+            }
+            if (any) tc_wait(bars.o_done[team], (n_s & 1) ^ 1, failed);
+            tc_after();
+            const bool whole = ends && item_begin >= share.lo;
+            const int slot = 2 * blockIdx.x + (item_begin < share.lo ? 0 : 1);
+            const auto out_at = [&](int row) {
+                const int64_t token = attend_quotient(row0 + row, a.group);
+                const int h = (int)(row0 + row - token * a.group);
+                return (T*)a.out + (item.seq.first + token) * a.out_token + (item.head * a.group + h) * a.out_head;
+            };
+            if (split) {
+                const float f = !whole ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;  // (a row that sees nothing is zero)
+                if (!whole) a.ml[(int64_t)slot * ROWS + r] = make_float2(m, l);
+                T* to = r < rows ? out_at(r) : nullptr;
+                float* part = a.part + ((int64_t)slot * ROWS + r) * DIM;
+#pragma unroll 1
+                for (int d = 0; d < c.dim; d += 32) {
+                    uint32_t o[32];
+                    tc_load(o, at_o + d);
+                    tc_loaded();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8)
+                        if (r < rows && d + i < c.dim) {
+                            float x[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(o[i + e]) * f;
+                            if (whole) *(uint4*)(to + d + i) = pack<T>(x);
+                            else {
+                                *(float4*)(part + d + i) = make_float4(x[0], x[1], x[2], x[3]);
+                                *(float4*)(part + d + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
+                            }
+                        }
+                    __syncwarp();
+                }
+            } else {
+                // the teams' and key groups' parts of a few rows at a time
+                s_m[tid] = m, s_l[tid] = l;
+                tc_rows_sync();
+                float most = -INFINITY, norm = 0.0f;
+#pragma unroll
+                for (int g = 0; g < 2 * GROUPS; ++g) most = fmaxf(most, s_m[g * COLS + r]);
+#pragma unroll
+                for (int g = 0; g < 2 * GROUPS; ++g) {
+                    const float x = s_m[g * COLS + r];
+                    norm += x == most ? s_l[g * COLS + r] : s_l[g * COLS + r] * exp2_unit(x - most);
+                }
+                float f = m == most ? 1.0f : exp2_unit(m - most);
+                if (whole) f = norm == 0.0f ? 0.0f : f / norm;  // (a row that sees nothing is zero)
+                if (!whole && tid < COLS) a.ml[(int64_t)slot * ROWS + r] = make_float2(most, norm);
+                const uint32_t region = base + S::REGION_AT;
+#pragma unroll 1
+                for (int first = 0; first < rows; first += S::TOGETHER) {
+                    const bool here = r >= first && r < first + S::TOGETHER && r < rows;
+                    if (first > 0) tc_rows_sync();
+                    if (__any_sync(0xffffffffu, here))
+#pragma unroll 1
+                        for (int d = 0; d < c.dim; d += 32) {
+                            uint32_t o[32];
+                            tc_load(o, at_o + d);
+                            tc_loaded();
+                            const uint32_t to = region + ((tid / COLS * S::TOGETHER + r - first) * S::PITCH + d) * 4;
+                            if (here)
+#pragma unroll
+                                for (int i = 0; i < 32; i += 4)
+                                    tc_put16(to + 4 * i, any ? make_uint4(__float_as_uint(__uint_as_float(o[i]) * f), __float_as_uint(__uint_as_float(o[i + 1]) * f),
+                                                                          __float_as_uint(__uint_as_float(o[i + 2]) * f), __float_as_uint(__uint_as_float(o[i + 3]) * f))
+                                                             : make_uint4(0, 0, 0, 0));
+                            __syncwarp();
+                        }
+                    tc_rows_sync();
+#pragma unroll 1
+                    for (int t = tid; t < S::TOGETHER * (DIM / 4); t += 2 * TC_TEAM) {
+                        const int rr = t / (DIM / 4), col = t % (DIM / 4) * 4;
+                        if (first + rr >= rows || col >= c.dim) continue;
+                        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                        for (int g = 0; g < 2 * GROUPS; ++g) {
+                            const uint4 y = tc_shared16(region + ((g * S::TOGETHER + rr) * S::PITCH + col) * 4);
+                            x.x += __uint_as_float(y.x), x.y += __uint_as_float(y.y), x.z += __uint_as_float(y.z), x.w += __uint_as_float(y.w);
+                        }
+                        if (whole) *(uint2*)(out_at(first + rr) + col) = make_uint2(pack_two<T>(x.x, x.y), pack_two<T>(x.z, x.w));
+                        else *(float4*)(a.part + ((int64_t)slot * ROWS + first + rr) * DIM + col) = x;
+                    }
+                }
+            }
+            tc_before();
+            if (!ends && item_begin >= share.lo)
+                begun = make_int4(item.b, item.head, item.row_tile, share.owner(item_begin + item.tiles - 1) - (int)blockIdx.x);
+            it = end;
+            item = after;
+        }
+        if (tid == 0) a.desc[blockIdx.x] = begun;
+    }
+    tc_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// --- host ------------------------------------------------------------------------------------------------------------------------
+
+// The largest power of two that divides a page, 128 at most.
+static int tc_group(int page_size)
+{
+    const int g = page_size & -page_size;
+    return g < TC_KEYS ? g : TC_KEYS;
+}
+
+// Whether a tensor map can describe one side of the cache: a dimension that is stepped over has a stride.
+static bool tc_strides_ok(const int64_t (&s)[3], const lda_paged_cache& c)
+{
+    return (s[0] > 0 || c.pages <= 1) && (s[1] > 0 || c.page_size == 1) && (s[2] > 0 || c.kv_heads == 1);
+}
+
+bool attend_tc_takes(const lda_paged_cache& c)
+{
+    return c.dim <= 128 && c.pages > 0 && tc_group(c.page_size) >= 8 && tc_strides_ok(c.key_strides, c) && tc_strides_ok(c.value_strides, c);
+}
+
+using TcEncode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static TcEncode tc_encode()
+{
+    static std::atomic<void*> known;
+    void* fn = known.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        known.store(fn, std::memory_order_release);
+    }
+    return (TcEncode)fn;
+}
+
+static bool tc_map(CUtensorMap& map, void* at, const int64_t (&strides)[3], const lda_paged_cache& c, int group)
+{
+    const TcEncode encode = tc_encode();
+    if (!encode) return false;
+    const auto bytes = [](int64_t stride) { return (cuuint64_t)(stride > 0 ? 2 * stride : 16); };  // (of a dimension of one: never taken)
+    const cuuint64_t sizes[4] = {(cuuint64_t)c.dim, (cuuint64_t)c.page_size, (cuuint64_t)c.kv_heads, (cuuint64_t)c.pages};
+    const cuuint64_t steps[3] = {bytes(strides[1]), bytes(strides[2]), bytes(strides[0])};
+    const cuuint32_t box[4] = {64, (cuuint32_t)group, 1, 1}, each[4] = {1, 1, 1, 1};
+    return encode(&map, c.dtype == LDA_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, at, sizes, steps, box, each,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DIM, int ROWS>
+static cudaError_t launch_tc(const AttendArgs& a, const TcMaps& maps, cudaStream_t st)
+{
+    using S = TcShape<DIM, ROWS>;
+    static std::atomic<bool> allowed[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev].load(std::memory_order_acquire)) {
+        e = cudaFuncSetAttribute(k_attend_tc<T, DIM, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SHARED);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev].store(true, std::memory_order_release);
+    }
+    k_attend_tc<T, DIM, ROWS><<<a.ctas, TC_THREADS, S::SHARED, st>>>(a, maps);
+    return cudaGetLastError();
+}
+
+template <typename T, int DIM>
+static cudaError_t tc_by_rows(const AttendArgs& a, const TcMaps& maps, cudaStream_t st)
+{
+    return a.rows == 32 ? launch_tc<T, DIM, 32>(a, maps, st) : a.rows == 64 ? launch_tc<T, DIM, 64>(a, maps, st) : launch_tc<T, DIM, 256>(a, maps, st);
+}
+
+cudaError_t attend_tc(const AttendArgs& a, const lda_paged_cache& cache, cudaStream_t st)
+{
+    TcMaps maps;
+    const int group = tc_group(cache.page_size);
+    maps.group_bits = 0;
+    while (1 << maps.group_bits < group) ++maps.group_bits;
+    if (!tc_map(maps.k, cache.keys, cache.key_strides, cache, group) || !tc_map(maps.v, cache.values, cache.value_strides, cache, group))
+        return cudaErrorInvalidValue;
+    if (cache.dtype == LDA_F16) return cache.dim <= 64 ? tc_by_rows<__half, 64>(a, maps, st) : tc_by_rows<__half, 128>(a, maps, st);
+    return cache.dim <= 64 ? tc_by_rows<__nv_bfloat16, 64>(a, maps, st) : tc_by_rows<__nv_bfloat16, 128>(a, maps, st);
+}
+
+}  // namespace lda
