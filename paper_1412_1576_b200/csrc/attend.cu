@@ -200,9 +200,9 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
             for (int i = tid; i < KEYS * CH; i += S::THREADS) {
                 const int row = i / CH, ch = i % CH;
                 uint4* at = (uint4*)(dynamic + stage * 2 * S::TILE_BYTES + S::TILE_BYTES + row * S::ROW_BYTES + ((ch ^ (row & 7)) << 4));
-                uint4 g = *at;
-                if (drop_wild<T>(g)) {
-                    *at = g;
+                const uint4 g = *at;
+                if (has_wild<T>(g)) {
+                    *at = without_wild<T>(g);
                     atomicOr(&wild[stage], 1ull << row);
                 }
             }
@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
             }
         }
         if (!ends && item_begin >= share.lo)
-            begun = make_int4(item.b, item.head, item.row_tile, share.owner(item_begin + item.tiles - 1) - (int)blockIdx.x);
+            begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + item.tiles, 1) - (int)blockIdx.x);
         if (unit + 1 < share.hi) {
             item.next<ROWS, KEYS>(a);
             item_begin = unit + 1;
@@ -366,9 +366,9 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
     if (tid == 0) a.desc[blockIdx.x] = begun;
 }
 
-// The parts of items that several CTAs have worked on, by a warp per row: in the order of the keys, so that the same call gives the same
+// The parts of items that several CTAs have worked on, two rows by a warp: in the order of the keys, so that the same call gives the same
 // bits.  Every such item begins in one CTA, which has said so.
-constexpr int JOIN_WARPS = 4;
+constexpr int JOIN_WARPS = 4, JOIN_ROWS = 2, JOIN_PARTS = 32 / JOIN_ROWS;  // rows of a warp, parts that its lanes look at together
 template <typename T, int DIM>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_constant__ AttendArgs a)
 {
@@ -376,44 +376,63 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_co
     const int4 item = a.desc[blockIdx.x];
     if (item.x < 0) return;
     const CacheSeq seq = a.cache.seq(item.x);
-    const int lane = threadIdx.x & 31, r = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
-    const int64_t row = (int64_t)item.z * a.rows + r;
-    if (row >= (int64_t)seq.n * a.group) return;
-    const int parts = item.w + 1;
-    const auto slot = [&](int i) { return i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i); };
+    const int lane = threadIdx.x & 31, first = (blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5)) * JOIN_ROWS;
+    const int64_t row0 = (int64_t)item.z * a.rows, rows = min((int64_t)a.rows, (int64_t)seq.n * a.group - row0);
+    if (first >= rows) return;
+    const int parts = item.w + 1, mine = lane / JOIN_PARTS, part = lane % JOIN_PARTS;
+    const auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i)); };
+    const auto load = [&](int i) {
+        return i < parts && first + mine < rows ? __ldcg(&a.ml[slot(i) * a.rows + first + mine]) : make_float2(-INFINITY, 0.0f);
+    };
     float most = -INFINITY;
-    for (int i = lane; i < parts; i += 32) most = fmaxf(most, a.ml[slot(i) * a.rows + r].x);
-    most = warp_reduce_max(most);
-    constexpr int EACH = DIM / 32;
-    float acc[EACH] = {}, norm = 0.0f;
-    for (int base = 0; base < parts; base += 32) {
-        float w = 0.0f;
-        if (base + lane < parts) {
-            const float2 ml = a.ml[slot(base + lane) * a.rows + r];
-            w = ml.x == most ? 1.0f : exp2_unit(ml.x - most);
-            norm += ml.y * w;
-        }
-        const int n = min(32, parts - base);
-        for (int i = 0; i < n; ++i) {
-            const float f = __shfl_sync(0xffffffffu, w, i);
-            const float* from = a.part + ((int64_t)slot(base + i) * a.rows + r) * DIM + lane * EACH;
-            if (lane * EACH < a.cache.dim)
+    for (int base = 0; base < parts; base += JOIN_PARTS) most = fmaxf(most, load(base + part).x);
 #pragma unroll
-                for (int e = 0; e < EACH; e += 2) {
-                    const float2 x = *(const float2*)(from + e);
-                    acc[e] += x.x * f, acc[e + 1] += x.y * f;
+    for (int o = JOIN_PARTS / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    constexpr int EACH = DIM / 32;
+    float acc[JOIN_ROWS][EACH] = {}, norm = 0.0f;
+    const bool there = lane * EACH < a.cache.dim;
+    for (int base = 0; base < parts; base += JOIN_PARTS) {
+        const float2 ml = load(base + part);
+        const float w = ml.x == most ? 1.0f : exp2_unit(ml.x - most);
+        norm += ml.y * w;
+        const int n = min(JOIN_PARTS, parts - base);
+        constexpr int AHEAD = 4;  // parts on their way together
+#pragma unroll 1
+        for (int i = 0; i < n; i += AHEAD) {
+            float2 x[AHEAD][JOIN_ROWS][EACH / 2];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const float* from = a.part + (slot(base + min(i + k, n - 1)) * a.rows + first) * DIM + lane * EACH;
+#pragma unroll
+                for (int j = 0; j < JOIN_ROWS; ++j)
+#pragma unroll
+                    for (int e = 0; e < EACH; e += 2)
+                        x[k][j][e / 2] = there && first + j < rows ? __ldcg((const float2*)(from + j * DIM + e)) : make_float2(0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int j = 0; j < JOIN_ROWS; ++j) {
+                    const float f = __shfl_sync(0xffffffffu, w, j * JOIN_PARTS + min(i + k, n - 1));
+                    if (i + k < n)
+#pragma unroll
+                        for (int e = 0; e < EACH; e += 2) acc[j][e] += x[k][j][e / 2].x * f, acc[j][e + 1] += x[k][j][e / 2].y * f;
                 }
         }
     }
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) norm += __shfl_xor_sync(0xffffffffu, norm, s);
+    for (int o = JOIN_PARTS / 2; o > 0; o >>= 1) norm += __shfl_xor_sync(0xffffffffu, norm, o);
     const float inv = norm == 0.0f ? 0.0f : 1.0f / norm;
-    if (lane * EACH >= a.cache.dim) return;
-    const int64_t token = row / a.group;
-    const int h = (int)(row - token * a.group);
-    T* to = (T*)a.out + (seq.first + token) * a.out_token + (item.y * a.group + h) * a.out_head + lane * EACH;
 #pragma unroll
-    for (int e = 0; e < EACH; e += 2) *(uint32_t*)(to + e) = pack_two<T>(acc[e] * inv, acc[e + 1] * inv);
+    for (int j = 0; j < JOIN_ROWS; ++j) {
+        const float f = __shfl_sync(0xffffffffu, inv, j * JOIN_PARTS);
+        if (!there || first + j >= rows) continue;
+        const int64_t token = attend_quotient(row0 + first + j, a.group);
+        const int h = (int)(row0 + first + j - token * a.group);
+        T* to = (T*)a.out + (seq.first + token) * a.out_token + (item.y * a.group + h) * a.out_head + lane * EACH;
+#pragma unroll
+        for (int e = 0; e < EACH; e += 2) *(uint32_t*)(to + e) = pack_two<T>(acc[j][e] * f, acc[j][e + 1] * f);
+    }
 }
 
 // --- host ------------------------------------------------------------------------------------------------------------------------
@@ -428,7 +447,7 @@ struct AttendPlan {
         dim = cache.dim <= 64 ? 64 : cache.dim <= 128 ? 128 : 256;
         // those that a sequence has on average share what is read from shared memory
         const int64_t most = (tokens + cache.n_seqs - 1) / cache.n_seqs * (heads / cache.kv_heads);
-        if (tc) rows = most <= 32 ? 32 : most <= 64 ? 64 : 256;
+        if (tc) rows = most <= 16 ? 32 : most <= 32 ? 64 : 256;
         else rows = most <= 16 ? 16 : most <= 32 || dim == 256 ? 32 : 64;
         ctas = 148 * (tc || dim == 256 ? 1 : dim == 128 ? 2 : 3);
         part = 0;
@@ -465,7 +484,7 @@ static cudaError_t attend_by_rows(const AttendArgs& a, const AttendPlan& plan, c
     else e = launch_attend<T, DIM, DIM == 256 ? 32 : 64>(a, st);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3((unsigned)a.ctas, (unsigned)(a.rows / JOIN_WARPS));
+    c.gridDim = dim3((unsigned)a.ctas, (unsigned)(a.rows / (JOIN_WARPS * JOIN_ROWS)));
     c.blockDim = dim3(32 * JOIN_WARPS);
     c.stream = st;
     cudaLaunchAttribute at{};

@@ -20,7 +20,8 @@ struct AttendArgs {
 };
 
 // --- how the work is shared out -------------------------------------------------------------------------------------------------
-// An item is a row tile of a head of a sequence; it has a unit for every tile of keys.  All units stand in one line (by sequence, head, row
+// An item is a row tile of a head of a sequence; it has a unit for every tile of keys (`weight` units where it has 256 rows, as that many
+// cost twice as much as 128).  All units stand in one line (by sequence, head, row
 // tile, keys), and every CTA takes an equal run of them.  So contexts of any lengths keep all CTAs busy to the end, few long ones too; an item
 // that does not lie within one run leaves parts that k_attend_join puts together.
 __device__ __forceinline__ int64_t attend_quotient(int64_t n, int64_t d)
@@ -30,111 +31,149 @@ __device__ __forceinline__ int64_t attend_quotient(int64_t n, int64_t d)
 }
 struct AttendShare {
     int64_t total, lo, hi;  // units in all, and of this CTA
-    int ctas;               // that take part
+    int ctas, near;         // that take part; how near to an item's end a share's moves there
     __device__ __forceinline__ int64_t begin(int c) const { return attend_quotient(total * c, ctas); }
-    // The CTA that has unit u.
-    __device__ __forceinline__ int owner(int64_t u) const { return (int)attend_quotient((u + 1) * ctas - 1, total); }
+    // A part of an item costs its CTAs and the join about as much as two tiles: a share's border that is as near to its item's begin or end
+    // as that is moved there, and else to a tile's begin.  `from`, `left`: units of the item before the border and behind it;
+    // returns by how many it moves.
+    __device__ __forceinline__ int64_t moved(int64_t from, int64_t left, int weight) const
+    {
+        return from <= near * weight && from <= left ? -from : left <= near * weight ? left : -(from & (weight - 1));
+    }
+    // The last CTA that has units of an item, first .. end - 1, that several have.
+    __device__ __forceinline__ int last_of(int64_t first, int64_t end, int weight) const
+    {
+        int c = (int)attend_quotient(end * ctas - 1, total);
+        while (begin(c) > first && begin(c) + moved(begin(c) - first, end - begin(c), weight) >= end) --c;
+        return c;
+    }
 };
 
 struct AttendItem {
     CacheSeq seq;
     int b, keys, row_tiles, tiles, head, row_tile, tile;
+    int parts, weight;  // units of a tile of keys for all rows of a head, and for the item's
     template <int ROWS, int KEYS>
     __device__ __forceinline__ void load(const AttendArgs& a, int b_)
     {
         b = b_;
         seq = a.cache.seq(b);
         keys = (int)min((int64_t)seq.start + seq.n, (int64_t)(a.cache.width * (int)a.cache.page_size.d));
-        row_tiles = (int)(((int64_t)seq.n * a.group + ROWS - 1) / ROWS);
+        const int64_t rows = (int64_t)seq.n * a.group;
+        row_tiles = (int)((rows + ROWS - 1) / ROWS);
+        parts = ROWS == 256 ? (int)((rows + 127) / 128) : row_tiles;
         tiles = max(1, (int)(((int64_t)keys + KEYS - 1) / KEYS));  // (rows without keys are written too)
     }
-    __device__ __forceinline__ int64_t units(const AttendArgs& a) const { return (int64_t)row_tiles * tiles * a.cache.kv_heads; }
-    __device__ __forceinline__ void at(int64_t unit)
+    template <int ROWS>
+    __device__ __forceinline__ void weigh()
     {
-        const int64_t item = attend_quotient(unit, tiles);
-        tile = (int)(unit - item * tiles);
-        head = (int)attend_quotient(item, row_tiles);
-        row_tile = (int)(item - (int64_t)head * row_tiles);
+        weight = ROWS == 256 && 2 * row_tile + 2 <= parts ? 2 : 1;
     }
-    // The next unit of the line; there is one.
+    __device__ __forceinline__ int64_t units(const AttendArgs& a) const { return (int64_t)parts * tiles * a.cache.kv_heads; }
+    // To the tile that has a unit of the sequence; returns how many units of the tile stand before it.
+    template <int ROWS>
+    __device__ __forceinline__ int at(int64_t unit)
+    {
+        constexpr int EACH = ROWS == 256 ? 2 : 1;  // units of a tile of a whole item
+        const int64_t of_head = (int64_t)parts * tiles;
+        head = (int)attend_quotient(unit, of_head);
+        const int64_t u = unit - head * of_head;
+        row_tile = (int)attend_quotient(u, EACH * (int64_t)tiles);
+        weigh<ROWS>();
+        const int off = (int)(u - row_tile * (EACH * (int64_t)tiles));
+        tile = off >> (weight - 1);
+        return off & (weight - 1);
+    }
+    // The next tile of the line; there is one.
     template <int ROWS, int KEYS>
     __device__ __forceinline__ void next(const AttendArgs& a)
     {
         if (++tile < tiles) return;
         tile = 0;
-        if (++row_tile < row_tiles) return;
-        row_tile = 0;
-        if (++head < a.cache.kv_heads) return;
-        head = 0;
-        do load<ROWS, KEYS>(a, b + 1);
-        while (row_tiles == 0 && b + 1 < a.cache.seqs);
+        if (++row_tile >= row_tiles) {
+            row_tile = 0;
+            if (++head >= a.cache.kv_heads) {
+                head = 0;
+                do load<ROWS, KEYS>(a, b + 1);
+                while (row_tiles == 0 && b + 1 < a.cache.seqs);
+            }
+        }
+        weigh<ROWS>();
     }
 };
-
-// Units that a CTA takes at least: what joining a part costs is about what a few tiles cost.
-constexpr int LEAST_UNITS = 2;
 
 // This CTA's share, and its first unit's item.  `red`: a number for each warp in shared memory.  False: it has none.
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool attend_share(const AttendArgs& a, int cta, AttendShare& s, AttendItem& item, unsigned long long* red)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5, seqs = a.cache.seqs;
-    __shared__ int s_b;
-    __shared__ unsigned long long s_before;
-    AttendItem own;
-    unsigned long long mine = 0;
-    const auto look = [&](int b) {
-        mine = 0;
-        if (b < seqs) {
-            own.load<ROWS, KEYS>(a, b);
-            mine = own.units(a);
-        }
-    };
-    // units before this thread's sequence and in all of the threads'
-    const auto scan = [&](unsigned long long& all) {
-        unsigned long long upto = mine;
+    __shared__ int s_b[2];
+    __shared__ unsigned long long s_before[2];
+    // (one copy of the code for both rounds: a CTA runs it once, and waits for every line of it to be fetched)
+    unsigned long long mine = 0, start = 0, before = 0;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+#pragma unroll 1
+        for (int base = 0; base < seqs; base += threads) {
+            if (round == 0 || seqs > threads) {  // (else the first round's scan says it)
+                AttendItem own;
+                mine = 0;
+                if (base + tid < seqs) {
+                    own.load<ROWS, KEYS>(a, base + tid);
+                    mine = own.units(a);
+                }
+                unsigned long long upto = mine;
+#pragma unroll 1
+                for (int o = 1; o < 32; o <<= 1) {
+                    const unsigned long long x = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += x;
+                }
+                if (base > 0 || round > 0) __syncthreads();
+                if (lane == 31) red[warp] = upto;
+                __syncthreads();
+                start = before + upto - mine;
+#pragma unroll 1
+                for (int w = 0; w < warps; ++w) {
+                    if (w < warp) start += red[w];
+                    before += red[w];
+                }
+            }
+            if (round > 0)
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
+                for (int i = 0; i < 2; ++i) {
+                    const unsigned long long at = (unsigned long long)(i ? s.hi : s.lo);
+                    if (mine && start <= at && at < start + mine) s_b[i] = base + tid, s_before[i] = start;
+                }
         }
-        if (lane == 31) red[warp] = upto;
-        __syncthreads();
-        unsigned long long start = upto - mine;
-        all = 0;
-        for (int w = 0; w < warps; ++w) {
-            if (w < warp) start += red[w];
-            all += red[w];
-        }
-        return start;
-    };
-    unsigned long long all, start = 0;
-    s.total = 0;
-    for (int base = 0; base < seqs; base += threads) {
-        if (base > 0) __syncthreads();
-        look(base + tid);
-        start = scan(all);
-        s.total += all;
-    }
-    s.ctas = (int)min((int64_t)a.ctas, max((int64_t)1, s.total / LEAST_UNITS));
-    if (s.total == 0 || cta >= s.ctas) return false;
-    s.lo = s.begin(cta), s.hi = s.begin(cta + 1);
-    // the sequence that has unit lo
-    const unsigned long long lo = (unsigned long long)s.lo;
-    unsigned long long before = 0;
-    for (int base = 0; base < seqs; base += threads) {
-        if (seqs > threads) {  // (else the one scan there was says it)
-            __syncthreads();
-            look(base + tid);
-            start = before + scan(all);
-            before += all;
-        }
-        if (mine && start <= lo && lo < start + mine) s_b = base + tid, s_before = start;
+        if (round > 0) break;
+        s.total = (int64_t)before;
+        s.ctas = (int)min((int64_t)a.ctas, max((int64_t)1, s.total / (ROWS == 256 ? 2 : 1)));
+        if (s.total == 0 || cta >= s.ctas) return false;
+        s.lo = s.begin(cta), s.hi = s.begin(cta + 1);
+        s.near = s.total > s.ctas ? (s.total >= 2ll * s.ctas && s.total < 8ll * s.ctas ? 2 : 1) : 0;
+        before = 0;
     }
     __syncthreads();
-    item.load<ROWS, KEYS>(a, s_b);
-    item.at(s.lo - (int64_t)s_before);
-    return true;
+    // the borders, moved; the first unit's item stays
+#pragma unroll 1
+    for (int i = 1; i >= 0; --i) {
+        if (i == 1 && s.hi == s.total) continue;
+        const int64_t at = i ? s.hi : s.lo;
+        item.load<ROWS, KEYS>(a, s_b[i]);
+        const int part = item.at<ROWS>(at - (int64_t)s_before[i]);
+        if (at == 0) continue;
+        const int64_t from = (int64_t)item.tile * item.weight + part, by = s.moved(from, (int64_t)item.tiles * item.weight - from, item.weight);
+        if (i == 1) s.hi += by;
+        else {
+            s.lo += by;
+            if (by <= 0) item.tile = (int)((from + by) >> (item.weight - 1));
+            else if (s.lo < s.total) {
+                item.tile = item.tiles - 1;
+                item.next<ROWS, KEYS>(a);
+            }
+        }
+    }
+    return s.lo < s.hi;
 }
 
 // --- masks -----------------------------------------------------------------------------------------------------------------------
@@ -176,20 +215,30 @@ __device__ __forceinline__ uint32_t pack_two(float x, float y)
 template <typename T>
 constexpr float RAISE = T_is_bf16<T> ? 0.0f : 14.0f;
 
-// Whether one of a group's eight values is infinite or no number; such values become zero.
+// Whether one of a group's eight values is infinite or no number: times zero it is NaN.
 template <typename T>
-__device__ __forceinline__ bool drop_wild(uint4& g)
+__device__ __forceinline__ bool has_wild(uint4 g)
+{
+    using T2 = std::conditional_t<T_is_bf16<T>, __nv_bfloat162, __half2>;
+    const uint32_t none = 0;
+    const auto zero = [&](uint32_t w) {
+        const T2 x = __hmul2(*reinterpret_cast<const T2*>(&w), *reinterpret_cast<const T2*>(&none));
+        return *reinterpret_cast<const uint32_t*>(&x);
+    };
+    return ((zero(g.x) | zero(g.y) | zero(g.z) | zero(g.w)) & 0x7FFF7FFFu) != 0;
+}
+// The group without such values.
+template <typename T>
+__device__ __noinline__ uint4 without_wild(uint4 g)
 {
     constexpr uint32_t EXP = T_is_bf16<T> ? 0x7F80u : 0x7C00u;
     uint32_t w[4] = {g.x, g.y, g.z, g.w};
-    bool any = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if ((w[i] & EXP) == EXP) w[i] &= 0xFFFF0000u, any = true;
-        if ((w[i] >> 16 & EXP) == EXP) w[i] &= 0x0000FFFFu, any = true;
+        if ((w[i] & EXP) == EXP) w[i] &= 0xFFFF0000u;
+        if ((w[i] >> 16 & EXP) == EXP) w[i] &= 0x0000FFFFu;
     }
-    g = make_uint4(w[0], w[1], w[2], w[3]);
-    return any;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // The other kernel (attend_tc.cu): whether it takes a cache, and its launch (the parts are joined by the caller).

@@ -179,7 +179,7 @@ constexpr float TC_RAISE = T_is_bf16<T> ? 0.0f : 7.0f;
 
 // A copying warp's walk over its CTA's units, for keys or for values: a lane has one of the tile's groups of slots.
 template <int DIM, int ROWS, int STAGES>
-__device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap* map, int bits, AttendItem item, int n_units, uint32_t to,
+__device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap* map, int bits, AttendItem item, int64_t units, uint32_t to,
                                           uint64_t* full, uint64_t* empty, uint32_t* valid, unsigned long long (*wild)[2], volatile int* failed)
 {
     const int lane = threadIdx.x & 31, groups = TC_KEYS >> bits;
@@ -191,7 +191,7 @@ __device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap
     look();
     int it = 0;
 #pragma unroll 1
-    for (; it < n_units; ++it) {
+    for (; units > 0; ++it) {
         const int p = page, at = place, head = item.head, s = it % STAGES;
         const uint32_t there = __ballot_sync(0xffffffffu, p >= 0);
         const bool ok = tc_wait(empty[s], it / STAGES & 1 ^ 1, failed);
@@ -206,12 +206,13 @@ __device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap
 #pragma unroll
             for (int h = 0; h < DIM / 64; ++h)
                 tc_copy(to + s * (TC_KEYS * DIM * 2) + h * (TC_KEYS * 128) + (lane << bits) * 128, map, 64 * h, at, head, p, full[s]);
-        if (it + 1 < n_units) {
+        units -= item.weight;
+        if (units > 0) {
             item.template next<ROWS, TC_KEYS>(a);
             look();
         }
     }
-    if (it < n_units) {  // gave up: what is under way still lands
+    if (units > 0) {  // gave up: what is under way still lands
         int quit = 0;
         for (int i = max(0, it - STAGES); i < it; ++i) tc_wait(full[i % STAGES], i / STAGES & 1, (volatile int*)&quit);
     }
@@ -256,23 +257,24 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
     __syncthreads();
     tc_after();
     const uint32_t tmem = s_tmem;
-    const int n_units = (int)(share.hi - share.lo);
+    const int64_t units = share.hi - share.lo;
     // whether the teams have rows of their own of an item
-    const auto splits = [&](const AttendItem& of) { return PAIR && (int64_t)of.seq.n * a.group - (int64_t)of.row_tile * ROWS > TC_ROWS; };
+    const auto splits = [&](const AttendItem& of) { return PAIR && of.weight == 2; };
 
     if (warp >= 8) {
         if (warp == 9) {
-            tc_copies<DIM, ROWS, S::K_STAGES>(a, &maps.k, maps.group_bits, item, n_units, base + S::K_AT, bars.k_full, bars.k_empty, valid, nullptr,
+            tc_copies<DIM, ROWS, S::K_STAGES>(a, &maps.k, maps.group_bits, item, units, base + S::K_AT, bars.k_full, bars.k_empty, valid, nullptr,
                                                   failed);
         } else if (warp == 10) {
-            tc_copies<DIM, ROWS, S::V_STAGES>(a, &maps.v, maps.group_bits, item, n_units, base + S::V_AT, bars.v_full, bars.v_empty, nullptr, wild,
+            tc_copies<DIM, ROWS, S::V_STAGES>(a, &maps.v, maps.group_bits, item, units, base + S::V_AT, bars.v_full, bars.v_empty, nullptr, wild,
                                                   failed);
         } else if (warp == 8) {
             // --- products, a tile's for a team at a time (a job): a job's scores ahead of the outputs of the job before it
             constexpr uint32_t KIND_S = tc_kind(T_is_bf16<T>, false, TC_KEYS), KIND_O = tc_kind(T_is_bf16<T>, true, DIM);
             const bool leads = lane == 0;
             const uint32_t at = __shfl_sync(0xffffffffu, base, 0), tensor = __shfl_sync(0xffffffffu, tmem, 0);
-            const int n = __shfl_sync(0xffffffffu, n_units, 0);
+            int64_t units_left = units;
+            int it = 0;
             bool ok = true;
             uint32_t waited = 0, n_q = 0;  // phases waited for: of p_full, a bit for each team; of q_full
             const auto scores = [&](int it, int team, bool first, bool last, bool new_q) {
@@ -291,7 +293,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 tc_commit(bars.s_full[team], leads);
                 if (last) tc_commit(bars.k_empty[ks], leads);
             };
-            const auto outputs = [&](int it, int team, bool first, bool last, bool fresh) {
+            // (of a tile's keys the sixteens that there are)
+            const auto steps_of = [&] { return __shfl_sync(0xffffffffu, min(TC_KEYS / 16, max(1, (item.keys - item.tile * TC_KEYS + 15) / 16)), 0); };
+            const auto outputs = [&](int it, int team, bool first, bool last, bool fresh, int steps) {
                 const int vs = it % S::V_STAGES;
                 ok = ok && tc_wait(bars.p_full[team], waited >> team & 1, failed);
                 waited ^= 1u << team;
@@ -301,37 +305,39 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 const uint32_t v = tc_operand_low(TC_KEYS * 128) + tc_operand_at(at + S::V_AT) + vs * (S::TILE / 16);
 #pragma unroll
                 for (int i = 0; i < TC_KEYS / 16; ++i)
-                    tc_product_tensor(tensor + TC_O + team * 128, tensor + TC_S + team * TC_KEYS + 8 * i, v + i * (2048 / 16), KIND_O, i > 0 || !fresh, leads);
+                    if (i < steps) tc_product_tensor(tensor + TC_O + team * 128, tensor + TC_S + team * TC_KEYS + 8 * i, v + i * (2048 / 16), KIND_O, i > 0 || !fresh, leads);
                 if (last) tc_commit(bars.v_empty[vs], leads);
                 tc_commit(bars.o_done[team], leads);
             };
             int nth = 0, left = item.tiles - item.tile;  // the unit's number in its item here, and how many the item still has
             bool split = __any_sync(0xffffffffu, splits(item)), fresh_before = false, split_before = false;
+            int steps_before = 0;
 #pragma unroll 1
-            for (int it = 0; it < n && ok; ++it) {
+            for (; ok; ++it) {
                 const bool begins = nth == 0, fresh = split ? nth == 0 : nth < 2;
+                const int steps = left > 1 ? TC_KEYS / 16 : steps_of();
                 const int team = split ? 0 : it & 1, team_before = split_before ? 1 : (it - 1) & 1;
                 // (an item's first scores need queries that the rows put down when they are through with the item before it)
-                if (begins && it > 0) outputs(it - 1, team_before, !split_before, true, fresh_before);
+                if (begins && it > 0) outputs(it - 1, team_before, !split_before, true, fresh_before, steps_before);
                 scores(it, team, true, !split, begins);
-                if (!begins) outputs(it - 1, team_before, !split_before, true, fresh_before);
+                if (!begins) outputs(it - 1, team_before, !split_before, true, fresh_before, steps_before);
                 if (split) {
                     scores(it, 1, false, true, false);
-                    outputs(it, 0, true, false, fresh);
+                    outputs(it, 0, true, false, fresh, steps);
                 }
-                fresh_before = fresh, split_before = split;
+                fresh_before = fresh, split_before = split, steps_before = steps;
                 ++nth;
-                if (--left == 0) {
-                    if (ok) tc_commit(bars.q_empty, leads);
-                    if (it + 1 < n) {
-                        item.tile = item.tiles - 1;
-                        item.template next<ROWS, TC_KEYS>(a);
-                        nth = 0, left = __shfl_sync(0xffffffffu, item.tiles, 0);
-                        split = __any_sync(0xffffffffu, splits(item));
-                    }
+                units_left -= item.weight;
+                if (--left == 0 && ok) tc_commit(bars.q_empty, leads);
+                if (!__any_sync(0xffffffffu, units_left > 0)) break;
+                if (left > 0) ++item.tile;
+                else {
+                    item.template next<ROWS, TC_KEYS>(a);
+                    nth = 0, left = __shfl_sync(0xffffffffu, item.tiles, 0);
+                    split = __any_sync(0xffffffffu, splits(item));
                 }
             }
-            outputs(n - 1, split_before ? 1 : (n - 1) & 1, !split_before, true, fresh_before);
+            outputs(it, split_before ? 1 : it & 1, !split_before, true, fresh_before, steps_before);
         }
         __syncwarp();
     } else {
@@ -366,13 +372,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
         get_q(item);
         put_q();
         int it = 0;
+        int64_t unit = share.lo;
         uint32_t n_s = 0, n_q = 0;  // tiles of the team, queries put down
 #pragma unroll 1
-        while (it < n_units) {
-            const int count = min(item.tiles - item.tile, n_units - it), end = it + count;
-            const bool ends = item.tile + count == item.tiles, last = end == n_units, split = splits(item);
+        while (unit < share.hi) {
+            const int count = (int)min((int64_t)(item.tiles - item.tile), (share.hi - unit) >> (item.weight - 1)), end = it + count;
+            const bool ends = item.tile + count == item.tiles, last = unit + (int64_t)count * item.weight == share.hi, split = splits(item);
             const int r = row_of(item);
-            const int64_t item_begin = share.lo + it - item.tile, row0 = (int64_t)item.row_tile * ROWS, all_rows = (int64_t)item.seq.n * a.group - row0;
+            const int64_t item_begin = unit - (int64_t)item.tile * item.weight, row0 = (int64_t)item.row_tile * ROWS, all_rows = (int64_t)item.seq.n * a.group - row0;
             const int rows = (int)min((int64_t)ROWS, all_rows), place = r < rows ? (int)attend_quotient(row0 + r, a.group) : -1;
             float m = -INFINITY, l = 0.0f;
             bool any = false;
@@ -382,38 +389,48 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 tc_wait(bars.s_full[team], n_s & 1, failed);
                 tc_after();
                 const uint32_t there = *(volatile uint32_t*)&valid[u & 15];
-                const bool full = there == (uint32_t)((1ull << (TC_KEYS >> maps.group_bits)) - 1);
+                // the tile's keys, and whether all their pages have come
+                const int keys = min(TC_KEYS, item.keys - tile * TC_KEYS), groups = (keys + (1 << maps.group_bits) - 1) >> maps.group_bits;
+                const bool full = there == (uint32_t)((1ull << groups) - 1);
                 unsigned long long bad[2] = {0, 0}, see[2] = {~0ull, ~0ull};
-                const bool masked = !full || (int64_t)(tile + 1) * TC_KEYS > item.seq.start;
+                const bool masked = !full || tile * TC_KEYS + keys > item.seq.start || keys < TC_KEYS;
                 if (masked) {
-                    // what the row sees of the keys
-#pragma unroll
+                    // what the row sees of the keys (in loops that stay loops: this runs once or twice in a call)
+#pragma unroll 1
                     for (int i = 0; i < 2; ++i) {
-                        const int left = item.keys - (tile * TC_KEYS + 64 * i);
-                        see[i] = place < 0 || left <= 0 ? 0ull : attend_window(a, item.seq, place, 2 * tile + i) & (left >= 64 ? ~0ull : (1ull << left) - 1);
+                        const int left = keys - 64 * i;
+                        unsigned long long w = place < 0 || left <= 0 ? 0ull : attend_window(a, item.seq, place, 2 * tile + i);
+                        if (left < 64 && left > 0) w &= (1ull << left) - 1;
                         if (!full)
 #pragma unroll 1
                             for (int g = 0; g < 64; g += 8)
-                                if (!(there >> ((64 * i + g) >> maps.group_bits) & 1)) see[i] &= ~(0xFFull << g);
+                                if (!(there >> ((64 * i + g) >> maps.group_bits) & 1)) w &= ~(0xFFull << g);
+                        if (i == 0) see[0] = w;
+                        else see[1] = w;
                     }
-                    // a value that a row does not see must not touch it, whatever it is: infinities and NaN are taken out and added apart
+                    // a value that a row does not see must not touch it, whatever it is: infinities and NaN are taken out and added apart, and
+                    // what stands where no key is, up to the last sixteen that the product takes, becomes zero
                     const int vs = u % S::V_STAGES;
                     tc_wait(bars.v_full[vs], u / S::V_STAGES & 1, failed);
-                    const int from = full ? max(0, (int)min((int64_t)TC_KEYS, (int64_t)item.seq.start - (int64_t)tile * TC_KEYS)) : 0;
-#pragma unroll 2
-                    for (int key = from + tid % TC_TEAM / 8; key < TC_KEYS; key += TC_TEAM / 8)
+                    const int from = full ? max(0, min(keys, item.seq.start - tile * TC_KEYS)) : 0, to = max(16, (keys + 15) & ~15);
+#pragma unroll 1
+                    for (int key = from + tid % TC_TEAM / 8; key < to; key += TC_TEAM / 8) {
+                        const bool known = key < keys && (there >> (key >> maps.group_bits) & 1);
 #pragma unroll
                         for (int h = 0; h < S::HALVES; ++h) {
                             const uint32_t at = base + S::V_AT + vs * S::TILE + (h * TC_KEYS + key) * 128 + tid % 8 * 16;
-                            uint4 g = tc_shared16(at);
-                            if (drop_wild<T>(g)) {
-                                // (where there is no key, what is left of others is not looked at again; said before it is taken out: PAIR's teams
-                                // both look)
-                                if (tile * TC_KEYS + key < item.keys && (there >> (key >> maps.group_bits) & 1)) atomicOr(&wild[vs][key / 64], 1ull << (key & 63));
+                            uint4 g = make_uint4(0, 0, 0, 0);
+                            if (known) {
+                                g = tc_shared16(at);
+                                if (!has_wild<T>(g)) continue;
+                                g = without_wild<T>(g);
+                                // (said before it is taken out: where the teams have the same tile, both look)
+                                atomicOr(&wild[vs][key / 64], 1ull << (key & 63));
                                 __threadfence_block();
-                                tc_put16(at, g);
                             }
+                            tc_put16(at, g);
                         }
+                    }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tc_team_sync(team);
                     bad[0] = *(volatile unsigned long long*)&wild[vs][0], bad[1] = *(volatile unsigned long long*)&wild[vs][1];
@@ -562,7 +579,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     __syncwarp();
                 }
             } else {
-                // the teams' and key groups' parts of a few rows at a time
+                // the teams' and key groups' parts: of a few rows at a time, or, behind the CTA's last unit, of all of them, where its keys and
+                // values were
+                constexpr int ALL = COLS < (S::K_STAGES + S::V_STAGES + (PAIR ? 2 : 1)) * S::TILE / (2 * GROUPS * S::PITCH * 4)
+                                        ? COLS
+                                        : (S::K_STAGES + S::V_STAGES + (PAIR ? 2 : 1)) * S::TILE / (2 * GROUPS * S::PITCH * 4);
+                const int together = last ? ALL : S::TOGETHER;
                 s_m[tid] = m, s_l[tid] = l;
                 tc_rows_sync();
                 float most = -INFINITY, norm = 0.0f;
@@ -576,10 +598,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 float f = m == most ? 1.0f : exp2_unit(m - most);
                 if (whole) f = norm == 0.0f ? 0.0f : f / norm;  // (a row that sees nothing is zero)
                 if (!whole && tid < COLS) a.ml[(int64_t)slot * ROWS + r] = make_float2(most, norm);
-                const uint32_t region = base + S::REGION_AT;
+                const uint32_t region = base + (last ? S::K_AT : S::REGION_AT);
 #pragma unroll 1
-                for (int first = 0; first < rows; first += S::TOGETHER) {
-                    const bool here = r >= first && r < first + S::TOGETHER && r < rows;
+                for (int first = 0; first < rows; first += together) {
+                    const bool here = r >= first && r < first + together && r < rows;
                     if (first > 0) tc_rows_sync();
                     if (__any_sync(0xffffffffu, here))
 #pragma unroll 1
@@ -587,7 +609,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                             uint32_t o[32];
                             tc_load(o, at_o + d);
                             tc_loaded();
-                            const uint32_t to = region + ((tid / COLS * S::TOGETHER + r - first) * S::PITCH + d) * 4;
+                            const uint32_t to = region + ((tid / COLS * together + r - first) * S::PITCH + d) * 4;
                             if (here)
 #pragma unroll
                                 for (int i = 0; i < 32; i += 4)
@@ -598,13 +620,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         }
                     tc_rows_sync();
 #pragma unroll 1
-                    for (int t = tid; t < S::TOGETHER * (DIM / 4); t += 2 * TC_TEAM) {
+                    for (int t = tid; t < together * (DIM / 4); t += 2 * TC_TEAM) {
                         const int rr = t / (DIM / 4), col = t % (DIM / 4) * 4;
                         if (first + rr >= rows || col >= c.dim) continue;
                         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
                         for (int g = 0; g < 2 * GROUPS; ++g) {
-                            const uint4 y = tc_shared16(region + ((g * S::TOGETHER + rr) * S::PITCH + col) * 4);
+                            const uint4 y = tc_shared16(region + ((g * together + rr) * S::PITCH + col) * 4);
                             x.x += __uint_as_float(y.x), x.y += __uint_as_float(y.y), x.z += __uint_as_float(y.z), x.w += __uint_as_float(y.w);
                         }
                         if (whole) *(uint2*)(out_at(first + rr) + col) = make_uint2(pack_two<T>(x.x, x.y), pack_two<T>(x.z, x.w));
@@ -614,8 +636,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             }
             tc_before();
             if (!ends && item_begin >= share.lo)
-                begun = make_int4(item.b, item.head, item.row_tile, share.owner(item_begin + item.tiles - 1) - (int)blockIdx.x);
+                begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + (int64_t)item.tiles * item.weight, item.weight) - (int)blockIdx.x);
             it = end;
+            unit += (int64_t)count * item.weight;
             item = after;
         }
         if (tid == 0) a.desc[blockIdx.x] = begun;
