@@ -18,7 +18,7 @@ namespace lda {
 
 constexpr int TC_KEYS = 128, TC_ROWS = 128;
 constexpr int TC_TEAM = 128, TC_THREADS = 2 * TC_TEAM + 96;  // two teams; a warp that issues products, two that copy
-constexpr uint32_t TC_S = 0, TC_O = 256;                // columns of tensor memory: S twice, O twice
+constexpr uint32_t TC_S = 0, TC_O = 256, TC_P = 64;     // columns of tensor memory: S twice, O twice; P's behind S's
 
 template <int DIM, int ROWS>
 struct TcShape {
@@ -110,7 +110,20 @@ __device__ __forceinline__ void tc_load(uint32_t (&r)[32], uint32_t at)
                    "=r"(r[31])
                  : "r"(at));
 }
-__device__ __forceinline__ void tc_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The registers of a load may be looked at behind this only.
+__device__ __forceinline__ void tc_loaded(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
+                   "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]),
+                   "+r"(r[31])::"memory");
+}
+__device__ __forceinline__ void tc_loaded(uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
+}
 __device__ __forceinline__ void tc_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_store(uint32_t at, const uint32_t (&r)[32])
 {
@@ -144,6 +157,7 @@ __device__ __forceinline__ uint32_t tc_load(uint32_t at)
 {
     uint32_t r;
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r)::"memory");
     return r;
 }
 // 64 columns of `rows` slots of a page's head; every coordinate is inside the cache, the first one a multiple of 64.
@@ -275,69 +289,80 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             const uint32_t at = __shfl_sync(0xffffffffu, base, 0), tensor = __shfl_sync(0xffffffffu, tmem, 0);
             int64_t units_left = units;
             int it = 0;
-            bool ok = true;
-            uint32_t waited = 0, n_q = 0;  // phases waited for: of p_full, a bit for each team; of q_full
-            const auto scores = [&](int it, int team, bool first, bool last, bool new_q) {
-                const int ks = it % S::K_STAGES;
-                if (new_q) ok = ok && tc_wait(bars.q_full, n_q++ & 1, failed);
-                if (first) ok = ok && tc_wait(bars.k_full[ks], it / S::K_STAGES & 1, failed);
-                if (!__all_sync(0xffffffffu, ok)) return;
+            bool go = leads;  // (products and barriers are this lane's; none where a wait gave up)
+            const auto wait = [&](uint64_t& bar, uint32_t parity) { go = tc_wait(bar, parity, failed) && go; };
+            uint32_t k_at = 0, k_round = 0, v_at = 0, v_round = 0, p_rounds = 0, q_round = 0;  // stages, and parities of the next phases
+            const uint32_t q_operand = tc_operand_low(16) + tc_operand_at(at + S::Q_AT), k_operand = tc_operand_low(16) + tc_operand_at(at + S::K_AT),
+                           v_operand = tc_operand_low(TC_KEYS * 128) + tc_operand_at(at + S::V_AT);
+            const auto scores = [&](int team, bool first, bool last) {
+                if (first) wait(bars.k_full[k_at], k_round);
                 tc_after();
-                const uint32_t q = tc_operand_low(16) + tc_operand_at(at + S::Q_AT) + (PAIR ? team * (S::TILE / 16) : 0),
-                               k = tc_operand_low(16) + tc_operand_at(at + S::K_AT) + ks * (S::TILE / 16);
+                const uint32_t q = q_operand + (PAIR ? team * (S::TILE / 16) : 0), k = k_operand + k_at * (S::TILE / 16), to = tensor + TC_S + team * TC_KEYS;
 #pragma unroll
                 for (int i = 0; i < DIM / 16; ++i) {
                     const uint32_t step = (i / 4 * (TC_KEYS * 128) + i % 4 * 32) / 16;
-                    tc_product_shared(tensor + TC_S + team * TC_KEYS, q + step, k + step, KIND_S, i > 0, leads);
+                    tc_product_shared(to, q + step, k + step, KIND_S, i > 0, go);
                 }
-                tc_commit(bars.s_full[team], leads);
-                if (last) tc_commit(bars.k_empty[ks], leads);
+                tc_commit(bars.s_full[team], go);
+                if (!last) return;
+                tc_commit(bars.k_empty[k_at], go);
+                if (++k_at == S::K_STAGES) k_at = 0, k_round ^= 1;
             };
-            // (of a tile's keys the sixteens that there are)
-            const auto steps_of = [&] { return __shfl_sync(0xffffffffu, min(TC_KEYS / 16, max(1, (item.keys - item.tile * TC_KEYS + 15) / 16)), 0); };
-            const auto outputs = [&](int it, int team, bool first, bool last, bool fresh, int steps) {
-                const int vs = it % S::V_STAGES;
-                ok = ok && tc_wait(bars.p_full[team], waited >> team & 1, failed);
-                waited ^= 1u << team;
-                if (first) ok = ok && tc_wait(bars.v_full[vs], it / S::V_STAGES & 1, failed);
-                if (!__all_sync(0xffffffffu, ok)) return;
+            const auto outputs = [&](int team, bool first, bool last, bool fresh, int steps) {
+                wait(bars.p_full[team], p_rounds >> team & 1);
+                p_rounds ^= 1u << team;
+                if (first) wait(bars.v_full[v_at], v_round);
                 tc_after();
-                const uint32_t v = tc_operand_low(TC_KEYS * 128) + tc_operand_at(at + S::V_AT) + vs * (S::TILE / 16);
+                const uint32_t v = v_operand + v_at * (S::TILE / 16), from = tensor + TC_S + team * TC_KEYS + TC_P, to = tensor + TC_O + team * 128;
+                tc_product_tensor(to, from, v, KIND_O, !fresh, go);
+                if (steps == TC_KEYS / 16) {
 #pragma unroll
-                for (int i = 0; i < TC_KEYS / 16; ++i)
-                    if (i < steps) tc_product_tensor(tensor + TC_O + team * 128, tensor + TC_S + team * TC_KEYS + 8 * i, v + i * (2048 / 16), KIND_O, i > 0 || !fresh, leads);
-                if (last) tc_commit(bars.v_empty[vs], leads);
-                tc_commit(bars.o_done[team], leads);
-            };
-            int nth = 0, left = item.tiles - item.tile;  // the unit's number in its item here, and how many the item still has
-            bool split = __any_sync(0xffffffffu, splits(item)), fresh_before = false, split_before = false;
-            int steps_before = 0;
+                    for (int i = 1; i < TC_KEYS / 16; ++i) tc_product_tensor(to, from + 8 * i, v + i * (2048 / 16), KIND_O, true, go);
+                } else
 #pragma unroll 1
-            for (; ok; ++it) {
-                const bool begins = nth == 0, fresh = split ? nth == 0 : nth < 2;
-                const int steps = left > 1 ? TC_KEYS / 16 : steps_of();
-                const int team = split ? 0 : it & 1, team_before = split_before ? 1 : (it - 1) & 1;
+                    for (int i = 1; i < steps; ++i) tc_product_tensor(to, from + 8 * i, v + i * (2048 / 16), KIND_O, true, go);
+                tc_commit(bars.o_done[team], go);
+                if (!last) return;
+                tc_commit(bars.v_empty[v_at], go);
+                if (++v_at == S::V_STAGES) v_at = 0, v_round ^= 1;
+            };
+            int64_t unit = share.lo;
+            int turn = 0, before = -1, steps_before = 0;  // the team of the next tile that one team has; that of the job before (-1: none), its sixteens
+            bool first_before = false, fresh_before = false;
+            const auto finish = [&] { outputs(before, first_before, true, fresh_before, steps_before); };
+            while (true) {
+                const int tiles = __shfl_sync(0xffffffffu, (int)min((int64_t)(item.tiles - item.tile), (share.hi - unit) >> (item.weight - 1)), 0);
+                const bool split = __any_sync(0xffffffffu, splits(item)), ends = __any_sync(0xffffffffu, item.tile + tiles == item.tiles);
+                // of the item's last tile the sixteens of keys that there are
+                const int last_steps = ends ? __shfl_sync(0xffffffffu, max(1, (item.keys - (item.tiles - 1) * TC_KEYS + 15) / 16), 0) : TC_KEYS / 16;
                 // (an item's first scores need queries that the rows put down when they are through with the item before it)
-                if (begins && it > 0) outputs(it - 1, team_before, !split_before, true, fresh_before, steps_before);
-                scores(it, team, true, !split, begins);
-                if (!begins) outputs(it - 1, team_before, !split_before, true, fresh_before, steps_before);
-                if (split) {
-                    scores(it, 1, false, true, false);
-                    outputs(it, 0, true, false, fresh, steps);
+                if (before >= 0) finish();
+                wait(bars.q_full, q_round);
+                q_round ^= 1;
+#pragma unroll 1
+                for (int i = 0; i < tiles; ++i) {
+                    const int steps = i + 1 < tiles ? TC_KEYS / 16 : last_steps;
+                    if (split) {
+                        scores(0, true, false);
+                        if (i > 0) finish();
+                        scores(1, false, true);
+                        outputs(0, true, false, i == 0, steps);
+                        before = 1, first_before = false, fresh_before = i == 0;
+                    } else {
+                        scores(turn, true, true);
+                        if (i > 0) finish();
+                        before = turn, first_before = true, fresh_before = i < 2;
+                    }
+                    steps_before = steps;
+                    turn ^= 1;
                 }
-                fresh_before = fresh, split_before = split, steps_before = steps;
-                ++nth;
-                units_left -= item.weight;
-                if (--left == 0 && ok) tc_commit(bars.q_empty, leads);
-                if (!__any_sync(0xffffffffu, units_left > 0)) break;
-                if (left > 0) ++item.tile;
-                else {
-                    item.template next<ROWS, TC_KEYS>(a);
-                    nth = 0, left = __shfl_sync(0xffffffffu, item.tiles, 0);
-                    split = __any_sync(0xffffffffu, splits(item));
-                }
+                if (ends) tc_commit(bars.q_empty, go);
+                unit += (int64_t)tiles * item.weight;
+                if (!__any_sync(0xffffffffu, unit < share.hi)) break;
+                item.tile = item.tiles - 1;
+                item.template next<ROWS, TC_KEYS>(a);
             }
-            outputs(it, split_before ? 1 : it & 1, !split_before, true, fresh_before, steps_before);
+            finish();
         }
         __syncwarp();
     } else {
@@ -348,29 +373,33 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
         const uint32_t at_q = base + S::Q_AT + (PAIR ? team * S::TILE : 0) + tid % TC_TEAM * 128;
         // a thread's row of an item
         const auto row_of = [&](const AttendItem& of) { return splits(of) ? tid : tid % COLS; };
-        // a row's queries, once for each of its copies, a half by each team (PAIR: each team has a place for its own)
-        constexpr int Q_EACH = PAIR ? DIM / 8 : DIM / 16;
-        const int q_from = PAIR ? 0 : team * Q_EACH;
-        uint4 q[Q_EACH];
-        const auto get_q = [&](const AttendItem& of) {
+        // a row's queries, once for each of its copies, a half by each team (PAIR: each team has a place for its own); an item's first are put down
+        // where the last one's have been read, which `ready` waits for
+        constexpr int Q_EACH = DIM / 16;
+        const auto put_q = [&](const AttendItem& of, auto ready) {
             const int64_t row = (int64_t)of.row_tile * ROWS + row_of(of);
             const bool there = row < (int64_t)of.seq.n * a.group;
             const int token = there ? (int)attend_quotient(row, a.group) : 0, h = there ? (int)(row - (int64_t)token * a.group) : 0;
-            const T* from = (const T*)a.q + (of.seq.first + token) * a.q_token + (of.head * a.group + h) * a.q_head + q_from * 8;
+            const T* from = (const T*)a.q + (of.seq.first + token) * a.q_token + (of.head * a.group + h) * a.q_head;
+#pragma unroll 1
+            for (int half = PAIR ? 0 : team; half < (PAIR ? 2 : team + 1); ++half) {
+                uint4 q[Q_EACH];
 #pragma unroll
-            for (int i = 0; i < Q_EACH; ++i) q[i] = there && (q_from + i) * 8 < c.dim ? __ldg((const uint4*)(from + i * 8)) : make_uint4(0, 0, 0, 0);
-        };
-        const auto put_q = [&] {
+                for (int i = 0; i < Q_EACH; ++i) {
+                    const int ch = half * Q_EACH + i;
+                    q[i] = there && ch * 8 < c.dim ? __ldg((const uint4*)(from + ch * 8)) : make_uint4(0, 0, 0, 0);
+                }
+                if (!PAIR || half == 0) ready();
 #pragma unroll
-            for (int i = 0; i < Q_EACH; ++i) {
-                const int ch = q_from + i;
-                tc_put16(at_q + ch / 8 * (TC_KEYS * 128) + ((ch % 8 ^ tid % 8) << 4), q[i]);
+                for (int i = 0; i < Q_EACH; ++i) {
+                    const int ch = half * Q_EACH + i;
+                    tc_put16(at_q + ch / 8 * (TC_KEYS * 128) + ((ch % 8 ^ tid % 8) << 4), q[i]);
+                }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_arrive(bars.q_full);
         };
-        get_q(item);
-        put_q();
+        put_q(item, [] {});
         int it = 0;
         int64_t unit = share.lo;
         uint32_t n_s = 0, n_q = 0;  // tiles of the team, queries put down
@@ -435,25 +464,40 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     tc_team_sync(team);
                     bad[0] = *(volatile unsigned long long*)&wild[vs][0], bad[1] = *(volatile unsigned long long*)&wild[vs][1];
                 }
-                // the scores are read twice, 32 columns at a time (of 128 in one go the code and the registers would be four times as many)
-                const auto scores = [&](uint32_t (&s)[32], int from) {
-                    tc_load(s, at_s + kg * COLS + from);
-                    tc_loaded();
-                    if (masked) {
-                        const int k = kg * COLS + from;
-                        const uint32_t w = (uint32_t)((k & 64 ? see[1] : see[0]) >> (k & 32));
+                // the scores come 32 columns at a time, the next ones while the last are worked on, and of 128 the first half twice (all at
+                // once would be more registers than there are); the probabilities go behind them, from the last to the first: over scores
+                // that have been read
+                constexpr int CHUNKS = COLS / 32;
+                uint32_t even[32], odd[32];
+                const auto fetch = [&](uint32_t (&s)[32], int chunk) { tc_load(s, at_s + kg * COLS + 32 * chunk); };
+                const auto hide = [&](uint32_t (&s)[32], int chunk) {
+                    if (!masked) return;
+                    const int k = kg * COLS + 32 * chunk;
+                    const uint32_t w = (uint32_t)((k & 64 ? see[1] : see[0]) >> (k & 32));
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (!(w >> j & 1)) s[j] = 0xFF800000u;  // minus infinity
-                    }
+                    for (int j = 0; j < 32; ++j)
+                        if (!(w >> j & 1)) s[j] = 0xFF800000u;  // minus infinity
                 };
                 float top = -INFINITY;
-#pragma unroll 1
-                for (int from = 0; from < COLS; from += 32) {
-                    uint32_t s[32];
-                    scores(s, from);
+                const auto largest = [&](const uint32_t (&s)[32]) {
+                    float x[4] = {top, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[j]), __uint_as_float(s[j + 1])));
+                    for (int j = 0; j < 32; j += 8)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + 2 * i]), __uint_as_float(s[j + 2 * i + 1])));
+                    top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                };
+                fetch(even, 0);
+#pragma unroll
+                for (int chunk = 0; chunk < CHUNKS; ++chunk) {
+                    if (chunk & 1) tc_loaded(odd);
+                    else tc_loaded(even);
+                    if (chunk + 1 < CHUNKS) {
+                        if (chunk & 1) fetch(even, chunk + 1);
+                        else fetch(odd, chunk + 1);
+                    }
+                    if (chunk & 1) hide(odd, chunk), largest(odd);
+                    else hide(even, chunk), largest(even);
                 }
                 top *= a.scale;
                 // (minus infinity is no reason; the first number is)
@@ -469,7 +513,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         for (int d = 0; d < DIM; d += 32) {
                             uint32_t o[32];
                             tc_load(o, at_o + d);
-                            tc_loaded();
+                            tc_loaded(o);
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                             tc_store(at_o + d, o);
@@ -479,28 +523,42 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 const float shift = (m == -INFINITY ? 0.0f : -m) + TC_RAISE<T>;
                 // the probabilities are rounded to the values' type, which the product takes: half a step each, as much as the output's own
                 // rounding; the norm is that of the unrounded ones
-                float sum[2] = {0.0f, 0.0f};
-#pragma unroll 1
-                for (int from = 0; from < COLS; from += 32) {
-                    uint32_t s[32], p[16];
-                    scores(s, from);
+                float2 sum = make_float2(0.0f, 0.0f);
+                const auto put = [&](const uint32_t (&s)[32], int chunk) {
+                    uint32_t p[16];
+                    const float2 by = make_float2(a.scale, a.scale), plus = make_float2(shift, shift);
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) {
-                        const float x = exp2_unit(__fmaf_rn(__uint_as_float(s[j]), a.scale, shift)), y = exp2_unit(__fmaf_rn(__uint_as_float(s[j + 1]), a.scale, shift));
-                        sum[0] += x, sum[1] += y;
-                        p[j / 2] = pack_two<T>(x, y);
+                        const float2 y = fma_two(make_float2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), by, plus);
+                        const float2 x = make_float2(exp2_unit(y.x), exp2_unit(y.y));
+                        sum = add_two(sum, x);
+                        p[j / 2] = pack_two<T>(x.x, x.y);
                     }
-                    // (of the scores only those are overwritten that have been read for the second time)
-                    tc_store(at_s + (kg * COLS + from) / 2, p);
+                    tc_store(at_s + TC_P + (kg * COLS + 32 * chunk) / 2, p);
+                };
+                if constexpr (CHUNKS == 4) {
+                    put(odd, 3);
+                    fetch(odd, 1);
+                    put(even, 2);
+                    tc_loaded(odd);
+                    fetch(even, 0);
+                    hide(odd, 1);
+                    put(odd, 1);
+                    tc_loaded(even);
+                    hide(even, 0);
+                    put(even, 0);
+                } else {
+                    if constexpr (CHUNKS == 2) put(odd, 1);
+                    put(even, 0);
                 }
                 if (GROUPS > 1) {
                     const uint32_t zero[16] = {};
 #pragma unroll
                     for (int g = 1; g < GROUPS; ++g)
 #pragma unroll
-                        for (int from = 0; from < COLS; from += 32) tc_store(at_s + (((kg + g) % GROUPS) * COLS + from) / 2, zero);
+                        for (int from = 0; from < COLS; from += 32) tc_store(at_s + TC_P + (((kg + g) % GROUPS) * COLS + from) / 2, zero);
                 }
-                l += sum[0] + sum[1];
+                l += sum.x + sum.y;
                 tc_stored();
                 tc_before();
                 tc_arrive(bars.p_full[team]);
@@ -511,8 +569,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll 1
                     for (int k = kg * COLS; k < (kg + 1) * COLS; ++k) {
                         if (!((k < 64 ? bad[0] : bad[1]) >> (k & 63) & 1)) continue;  // (the same in the warp)
-                        const uint32_t two = tc_load(at_s + k / 2);
-                        tc_loaded();
+                        const uint32_t two = tc_load(at_s + TC_P + k / 2);
                         const uint16_t half = (uint16_t)(k & 1 ? two >> 16 : two);
                         const float p = cache_value(*reinterpret_cast<const T*>(&half));
                         int slot = 0;
@@ -524,7 +581,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                             unpack<T>(*(const uint4*)(v + d), x);
                             uint32_t o[8];
                             tc_load(o, at_o + d);
-                            tc_loaded();
+                            tc_loaded(o);
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 if (p != 0.0f && !(fabsf(x[e]) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + p * x[e]);
@@ -541,9 +598,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             if (!last) {
                 after.tile = after.tiles - 1;
                 after.template next<ROWS, TC_KEYS>(a);
-                get_q(after);
-                tc_wait(bars.q_empty, n_q++ & 1, failed);  // (the queries before these have been read)
-                put_q();
+                put_q(after, [&] { tc_wait(bars.q_empty, n_q++ & 1, failed); });
             }
             if (any) tc_wait(bars.o_done[team], (n_s & 1) ^ 1, failed);
             tc_after();
@@ -563,7 +618,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 for (int d = 0; d < c.dim; d += 32) {
                     uint32_t o[32];
                     tc_load(o, at_o + d);
-                    tc_loaded();
+                    tc_loaded(o);
 #pragma unroll
                     for (int i = 0; i < 32; i += 8)
                         if (r < rows && d + i < c.dim) {
@@ -608,7 +663,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         for (int d = 0; d < c.dim; d += 32) {
                             uint32_t o[32];
                             tc_load(o, at_o + d);
-                            tc_loaded();
+                            tc_loaded(o);
                             const uint32_t to = region + ((tid / COLS * together + r - first) * S::PITCH + d) * 4;
                             if (here)
 #pragma unroll
