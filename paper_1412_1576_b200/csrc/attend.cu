@@ -101,7 +101,8 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(k), "r"(size) : "memory");
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + S::TILE_BYTES), "l"(v), "r"(size) : "memory");
             }
-            if (++to_copy < share.hi) ahead.next<ROWS, KEYS>(a);
+            to_copy += ahead.tile + 1 == ahead.tiles ? 1 + ahead.extra_units() : 1;
+            if (to_copy < share.hi) ahead.next<ROWS, KEYS>(a);
             look();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
 
     int stage = 0;
 #pragma unroll 1
-    for (int64_t unit = share.lo; unit < share.hi; ++unit) {
+    for (int64_t unit = share.lo; unit < share.hi;) {
         asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
         __syncthreads();
         copy(stage == 0 ? S::STAGES - 1 : stage - 1);  // (the stage that the last unit has left)
@@ -291,7 +292,8 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
         stage = stage + 1 == S::STAGES ? 0 : stage + 1;
 
         const bool ends = item.tile + 1 == item.tiles;
-        if (!ends && unit + 1 < share.hi) {
+        unit += ends ? 1 + item.extra_units() : 1;
+        if (!ends && unit < share.hi) {
             ++item.tile;
             continue;
         }
@@ -355,10 +357,10 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
             }
         }
         if (!ends && item_begin >= share.lo)
-            begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + item.tiles, 1) - (int)blockIdx.x);
-        if (unit + 1 < share.hi) {
+            begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + item.own_units(), 1) - (int)blockIdx.x);
+        if (unit < share.hi) {
             item.next<ROWS, KEYS>(a);
-            item_begin = unit + 1;
+            item_begin = unit;
             __syncthreads();
             begin_item();
         }
@@ -540,7 +542,7 @@ extern "C" int lda_tree_attention(const lda_paged_cache* cache, int64_t tokens, 
     const int64_t most = 1ll << 31;
     if (q_token_stride > most || q_head_stride > most || out_token_stride > most || out_head_stride > most) return LDA_ERANGE;
     const AttendPlan plan(*cache, tokens, heads);
-    if (!workspace_dev || !aligned(workspace_dev, 16) || workspace_bytes < plan.all) return LDA_EINVAL;
+    if (!workspace_dev || !aligned(workspace_dev, 32) || workspace_bytes < plan.all) return LDA_EINVAL;
     a.ctas = plan.ctas, a.rows = plan.rows;
     a.q = q_dev, a.out = out_dev;
     a.q_token = q_token_stride, a.q_head = q_head_stride, a.out_token = out_token_stride, a.out_head = out_head_stride;

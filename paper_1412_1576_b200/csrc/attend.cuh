@@ -21,9 +21,10 @@ struct AttendArgs {
 
 // --- how the work is shared out -------------------------------------------------------------------------------------------------
 // An item is a row tile of a head of a sequence; it has a unit for every tile of keys (`weight` units where it has 256 rows, as that many
-// cost twice as much as 128).  All units stand in one line (by sequence, head, row
+// cost twice as much as 128), and ITEM_EXTRA tiles' worth behind them, without work, for what an item costs besides: queries, and sums out.  All units stand in one line (by sequence, head, row
 // tile, keys), and every CTA takes an equal run of them.  So contexts of any lengths keep all CTAs busy to the end, few long ones too; an item
 // that does not lie within one run leaves parts that k_attend_join puts together.
+constexpr int ITEM_EXTRA = 2;
 __device__ __forceinline__ int64_t attend_quotient(int64_t n, int64_t d)
 {
     // (a division of 64 bits is a call of its own)
@@ -33,12 +34,12 @@ struct AttendShare {
     int64_t total, lo, hi;  // units in all, and of this CTA
     int ctas, near;         // that take part; how near to an item's end a share's moves there
     __device__ __forceinline__ int64_t begin(int c) const { return attend_quotient(total * c, ctas); }
-    // A part of an item costs its CTAs and the join about as much as two tiles: a share's border that is as near to its item's begin or end
-    // as that is moved there, and else to a tile's begin.  `from`, `left`: units of the item before the border and behind it;
-    // returns by how many it moves.
+    // A part of an item costs its CTAs and the join about as much as two tiles: a share's border that is as near to the item's first tile or
+    // behind its last is moved there, and else to a tile's begin.  `from`, `left`: units of the item before the border and behind
+    // it; returns by how many it moves.
     __device__ __forceinline__ int64_t moved(int64_t from, int64_t left, int weight) const
     {
-        return from <= near * weight && from <= left ? -from : left <= near * weight ? left : -(from & (weight - 1));
+        return from <= near * weight && from <= left ? -from : left <= (near + ITEM_EXTRA) * weight ? left : -(from & (weight - 1));
     }
     // The last CTA that has units of an item, first .. end - 1, that several have.
     __device__ __forceinline__ int last_of(int64_t first, int64_t end, int weight) const
@@ -69,18 +70,21 @@ struct AttendItem {
     {
         weight = ROWS == 256 && 2 * row_tile + 2 <= parts ? 2 : 1;
     }
-    __device__ __forceinline__ int64_t units(const AttendArgs& a) const { return (int64_t)parts * tiles * a.cache.kv_heads; }
-    // To the tile that has a unit of the sequence; returns how many units of the tile stand before it.
+    __device__ __forceinline__ int64_t units(const AttendArgs& a) const { return (int64_t)parts * (tiles + ITEM_EXTRA) * a.cache.kv_heads; }
+    // Of the item, and of what stands behind its last tile.
+    __device__ __forceinline__ int64_t own_units() const { return (int64_t)(tiles + ITEM_EXTRA) * weight; }
+    __device__ __forceinline__ int extra_units() const { return ITEM_EXTRA * weight; }
+    // To the tile that has a unit of the sequence (from `tiles` on: none has); returns how many units of the tile stand before it.
     template <int ROWS>
     __device__ __forceinline__ int at(int64_t unit)
     {
         constexpr int EACH = ROWS == 256 ? 2 : 1;  // units of a tile of a whole item
-        const int64_t of_head = (int64_t)parts * tiles;
+        const int64_t of_tile = tiles + ITEM_EXTRA, of_head = parts * of_tile;
         head = (int)attend_quotient(unit, of_head);
         const int64_t u = unit - head * of_head;
-        row_tile = (int)attend_quotient(u, EACH * (int64_t)tiles);
+        row_tile = (int)attend_quotient(u, EACH * of_tile);
         weigh<ROWS>();
-        const int off = (int)(u - row_tile * (EACH * (int64_t)tiles));
+        const int off = (int)(u - row_tile * (EACH * of_tile));
         tile = off >> (weight - 1);
         return off & (weight - 1);
     }
@@ -162,7 +166,7 @@ __device__ __forceinline__ bool attend_share(const AttendArgs& a, int cta, Atten
         item.load<ROWS, KEYS>(a, s_b[i]);
         const int part = item.at<ROWS>(at - (int64_t)s_before[i]);
         if (at == 0) continue;
-        const int64_t from = (int64_t)item.tile * item.weight + part, by = s.moved(from, (int64_t)item.tiles * item.weight - from, item.weight);
+        const int64_t from = (int64_t)item.tile * item.weight + part, by = s.moved(from, item.own_units() - from, item.weight);
         if (i == 1) s.hi += by;
         else {
             s.lo += by;

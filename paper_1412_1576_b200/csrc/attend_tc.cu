@@ -220,7 +220,7 @@ __device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap
 #pragma unroll
             for (int h = 0; h < DIM / 64; ++h)
                 tc_copy(to + s * (TC_KEYS * DIM * 2) + h * (TC_KEYS * 128) + (lane << bits) * 128, map, 64 * h, at, head, p, full[s]);
-        units -= item.weight;
+        units -= item.tile + 1 == item.tiles ? item.weight + item.extra_units() : item.weight;
         if (units > 0) {
             item.template next<ROWS, TC_KEYS>(a);
             look();
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     turn ^= 1;
                 }
                 if (ends) tc_commit(bars.q_empty, go);
-                unit += (int64_t)tiles * item.weight;
+                unit += (int64_t)tiles * item.weight + (ends ? item.extra_units() : 0);
                 if (!__any_sync(0xffffffffu, unit < share.hi)) break;
                 item.tile = item.tiles - 1;
                 item.template next<ROWS, TC_KEYS>(a);
@@ -406,7 +406,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll 1
         while (unit < share.hi) {
             const int count = (int)min((int64_t)(item.tiles - item.tile), (share.hi - unit) >> (item.weight - 1)), end = it + count;
-            const bool ends = item.tile + count == item.tiles, last = unit + (int64_t)count * item.weight == share.hi, split = splits(item);
+            const bool ends = item.tile + count == item.tiles, split = splits(item);
+            const int64_t unit_after = unit + (int64_t)count * item.weight + (ends ? item.extra_units() : 0);
+            const bool last = unit_after == share.hi;
             const int r = row_of(item);
             const int64_t item_begin = unit - (int64_t)item.tile * item.weight, row0 = (int64_t)item.row_tile * ROWS, all_rows = (int64_t)item.seq.n * a.group - row0;
             const int rows = (int)min((int64_t)ROWS, all_rows), place = r < rows ? (int)attend_quotient(row0 + r, a.group) : -1;
@@ -626,10 +628,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll
                             for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(o[i + e]) * f;
                             if (whole) *(uint4*)(to + d + i) = pack<T>(x);
-                            else {
-                                *(float4*)(part + d + i) = make_float4(x[0], x[1], x[2], x[3]);
-                                *(float4*)(part + d + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                            }
+                            else  // (32 bytes at a time: a thread's row lies by itself)
+                                asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(part + d + i), "f"(x[0]), "f"(x[1]), "f"(x[2]),
+                                             "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                                             : "memory");
                         }
                     __syncwarp();
                 }
@@ -691,9 +693,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             }
             tc_before();
             if (!ends && item_begin >= share.lo)
-                begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + (int64_t)item.tiles * item.weight, item.weight) - (int)blockIdx.x);
+                begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + item.own_units(), item.weight) - (int)blockIdx.x);
             it = end;
-            unit += (int64_t)count * item.weight;
+            unit = unit_after;
             item = after;
         }
         if (tid == 0) a.desc[blockIdx.x] = begun;
