@@ -63,9 +63,9 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
     const uint32_t q_shared = stages + S::STAGES * 2 * S::TILE_BYTES + 64 * S::PITCH * 4;
     AttendShare share;
     AttendItem item, ahead;
-    int4 begun = make_int4(-1, 0, 0, 0);
+    AttendBegun begun{};
     if (!attend_share<ROWS, KEYS>(a, blockIdx.x, share, item, red)) {
-        if (tid == 0) a.desc[blockIdx.x] = begun;
+        if (tid == 0) a.begun[blockIdx.x] = begun;
         return;
     }
 
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
             }
         }
         if (!ends && item_begin >= share.lo)
-            begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + item.own_units(), 1) - (int)blockIdx.x);
+            begun = AttendBegun{row0, item.seq.first, item.head, (int)rows, share.last_of(item_begin, item_begin + item.own_units(), 1) - (int)blockIdx.x, 0};
         if (unit < share.hi) {
             item.next<ROWS, KEYS>(a);
             item_begin = unit;
@@ -365,62 +365,64 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
             begin_item();
         }
     }
-    if (tid == 0) a.desc[blockIdx.x] = begun;
+    if (tid == 0) a.begun[blockIdx.x] = begun;
 }
 
 // The parts of items that several CTAs have worked on, two rows by a warp: in the order of the keys, so that the same call gives the same
-// bits.  Every such item begins in one CTA, which has said so.
+// bits.  Every such item begins in one CTA, which has said so.  Bound by reads that need each other, three of them: the item; its parts' maxima
+// and first sums; the other sums.
 constexpr int JOIN_WARPS = 4, JOIN_ROWS = 2, JOIN_PARTS = 32 / JOIN_ROWS;  // rows of a warp, parts that its lanes look at together
 template <typename T, int DIM>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_constant__ AttendArgs a)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int4 item = a.desc[blockIdx.x];
-    if (item.x < 0) return;
-    const CacheSeq seq = a.cache.seq(item.x);
+    const AttendBegun item = a.begun[blockIdx.x];
     const int lane = threadIdx.x & 31, first = (blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5)) * JOIN_ROWS;
-    const int64_t row0 = (int64_t)item.z * a.rows, rows = min((int64_t)a.rows, (int64_t)seq.n * a.group - row0);
-    if (first >= rows) return;
-    const int parts = item.w + 1, mine = lane / JOIN_PARTS, part = lane % JOIN_PARTS;
+    if (first >= item.rows) return;
+    constexpr int EACH = DIM / 32, AHEAD = 4;  // columns of a lane, parts on their way together
+    const int parts = item.others + 1, mine = lane / JOIN_PARTS, part = lane % JOIN_PARTS;
+    const bool there = lane * EACH < a.cache.dim;
     const auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i)); };
     const auto load = [&](int i) {
-        return i < parts && first + mine < rows ? __ldcg(&a.ml[slot(i) * a.rows + first + mine]) : make_float2(-INFINITY, 0.0f);
+        return i < parts && first + mine < item.rows ? __ldcg(&a.ml[slot(i) * a.rows + first + mine]) : make_float2(-INFINITY, 0.0f);
     };
-    float most = -INFINITY;
-    for (int base = 0; base < parts; base += JOIN_PARTS) most = fmaxf(most, load(base + part).x);
+    float2 x[AHEAD][JOIN_ROWS][EACH / 2];
+    const auto fetch = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const float* from = a.part + (slot(min(i + k, parts - 1)) * a.rows + first) * DIM + lane * EACH;
+#pragma unroll
+            for (int j = 0; j < JOIN_ROWS; ++j)
+#pragma unroll
+                for (int e = 0; e < EACH; e += 2)
+                    x[k][j][e / 2] = there && first + j < item.rows ? __ldcg((const float2*)(from + j * DIM + e)) : make_float2(0.0f, 0.0f);
+        }
+    };
+    fetch(0);
+    const float2 near = load(part), next = load(JOIN_PARTS + part);
+    float most = fmaxf(near.x, next.x);
+#pragma unroll 1
+    for (int base = 2 * JOIN_PARTS; base < parts; base += JOIN_PARTS) most = fmaxf(most, load(base + part).x);
 #pragma unroll
     for (int o = JOIN_PARTS / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    constexpr int EACH = DIM / 32;
-    float acc[JOIN_ROWS][EACH] = {}, norm = 0.0f;
-    const bool there = lane * EACH < a.cache.dim;
-    for (int base = 0; base < parts; base += JOIN_PARTS) {
-        const float2 ml = load(base + part);
-        const float w = ml.x == most ? 1.0f : exp2_unit(ml.x - most);
-        norm += ml.y * w;
-        const int n = min(JOIN_PARTS, parts - base);
-        constexpr int AHEAD = 4;  // parts on their way together
+    float acc[JOIN_ROWS][EACH] = {}, norm = 0.0f, w = 0.0f;
 #pragma unroll 1
-        for (int i = 0; i < n; i += AHEAD) {
-            float2 x[AHEAD][JOIN_ROWS][EACH / 2];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const float* from = a.part + (slot(base + min(i + k, n - 1)) * a.rows + first) * DIM + lane * EACH;
-#pragma unroll
-                for (int j = 0; j < JOIN_ROWS; ++j)
-#pragma unroll
-                    for (int e = 0; e < EACH; e += 2)
-                        x[k][j][e / 2] = there && first + j < rows ? __ldcg((const float2*)(from + j * DIM + e)) : make_float2(0.0f, 0.0f);
-            }
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-                for (int j = 0; j < JOIN_ROWS; ++j) {
-                    const float f = __shfl_sync(0xffffffffu, w, j * JOIN_PARTS + min(i + k, n - 1));
-                    if (i + k < n)
-#pragma unroll
-                        for (int e = 0; e < EACH; e += 2) acc[j][e] += x[k][j][e / 2].x * f, acc[j][e + 1] += x[k][j][e / 2].y * f;
-                }
+    for (int i = 0; i < parts; i += AHEAD) {
+        if (i % JOIN_PARTS == 0) {
+            const float2 ml = i == 0 ? near : i == JOIN_PARTS ? next : load(i + part);
+            w = ml.x == most ? 1.0f : exp2_unit(ml.x - most);
+            norm += ml.y * w;
         }
+        if (i > 0) fetch(i);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int j = 0; j < JOIN_ROWS; ++j) {
+                const float f = __shfl_sync(0xffffffffu, w, j * JOIN_PARTS + (i + k) % JOIN_PARTS);
+                if (i + k < parts)
+#pragma unroll
+                    for (int e = 0; e < EACH; e += 2) acc[j][e] += x[k][j][e / 2].x * f, acc[j][e + 1] += x[k][j][e / 2].y * f;
+            }
     }
 #pragma unroll
     for (int o = JOIN_PARTS / 2; o > 0; o >>= 1) norm += __shfl_xor_sync(0xffffffffu, norm, o);
@@ -428,10 +430,9 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_co
 #pragma unroll
     for (int j = 0; j < JOIN_ROWS; ++j) {
         const float f = __shfl_sync(0xffffffffu, inv, j * JOIN_PARTS);
-        if (!there || first + j >= rows) continue;
-        const int64_t token = attend_quotient(row0 + first + j, a.group);
-        const int h = (int)(row0 + first + j - token * a.group);
-        T* to = (T*)a.out + (seq.first + token) * a.out_token + (item.y * a.group + h) * a.out_head + lane * EACH;
+        if (!there || first + j >= item.rows) continue;
+        const int64_t row = item.row0 + first + j, token = attend_quotient(row, a.group);
+        T* to = (T*)a.out + (item.first + token) * a.out_token + (item.head * a.group + (int)(row - token * a.group)) * a.out_head + lane * EACH;
 #pragma unroll
         for (int e = 0; e < EACH; e += 2) *(uint32_t*)(to + e) = pack_two<T>(acc[j][e] * f, acc[j][e + 1] * f);
     }
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_attend_join(const __grid_co
 struct AttendPlan {
     bool tc;
     int rows, dim, ctas;          // of a tile; padded; CTAs
-    int64_t part, ml, desc, all;  // bytes up to each
+    int64_t part, ml, begun, all;  // bytes up to each
     AttendPlan(const lda_paged_cache& cache, int64_t tokens, int32_t heads)
     {
         tc = attend_tc_takes(cache);
@@ -454,8 +455,8 @@ struct AttendPlan {
         ctas = 148 * (tc || dim == 256 ? 1 : dim == 128 ? 2 : 3);
         part = 0;
         ml = (int64_t)2 * ctas * rows * dim * 4;
-        desc = ml + (int64_t)2 * ctas * rows * 8;
-        all = desc + (int64_t)ctas * 16;
+        begun = ml + (int64_t)2 * ctas * rows * 8;
+        all = begun + (int64_t)ctas * sizeof(AttendBegun);
     }
 };
 
@@ -551,7 +552,7 @@ extern "C" int lda_tree_attention(const lda_paged_cache* cache, int64_t tokens, 
     a.scale = (float)(scale * 1.4426950408889634);
     a.part = (float*)((char*)workspace_dev + plan.part);
     a.ml = (float2*)((char*)workspace_dev + plan.ml);
-    a.desc = (int4*)((char*)workspace_dev + plan.desc);
+    a.begun = (AttendBegun*)((char*)workspace_dev + plan.begun);
     const cudaError_t e = cache->dtype == LDA_F16 ? attend_by_dim<__half>(a, plan, *cache, (cudaStream_t)cuda_stream)
                                                   : attend_by_dim<__nv_bfloat16>(a, plan, *cache, (cudaStream_t)cuda_stream);
     if (e != cudaSuccess) {

@@ -5,6 +5,12 @@
 
 namespace lda {
 
+struct AttendBegun {
+    int64_t row0, first;  // the item's first row, and its sequence's first token
+    int head, rows;       // rows: of the tile; 0: there is no such item
+    int others, unused;   // how many CTAs go on with it
+};
+
 struct AttendArgs {
     CacheView cache;
     const void* q;
@@ -16,7 +22,7 @@ struct AttendArgs {
     int ctas, rows;  // rows of a tile
     float* part;   // [2 ctas][rows][padded dim]: sums of parts of an item
     float2* ml;    // [2 ctas][rows]: their maxima and norms
-    int4* desc;    // [ctas]: the item that a CTA begins and others go on with: sequence (-1: none), head, row tile, how many others
+    AttendBegun* begun;  // [ctas]: the item that a CTA begins and others go on with
 };
 
 // --- how the work is shared out -------------------------------------------------------------------------------------------------

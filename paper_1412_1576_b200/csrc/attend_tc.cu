@@ -258,9 +258,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
     }
     AttendShare share;
     AttendItem item;
-    int4 begun = make_int4(-1, 0, 0, 0);
+    AttendBegun begun{};
     if (!attend_share<ROWS, TC_KEYS>(a, blockIdx.x, share, item, red)) {
-        if (tid == 0) a.desc[blockIdx.x] = begun;
+        if (tid == 0) a.begun[blockIdx.x] = begun;
         return;
     }
     if (warp == 8) {
@@ -693,12 +693,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             }
             tc_before();
             if (!ends && item_begin >= share.lo)
-                begun = make_int4(item.b, item.head, item.row_tile, share.last_of(item_begin, item_begin + item.own_units(), item.weight) - (int)blockIdx.x);
+                begun = AttendBegun{row0, item.seq.first, item.head, rows, share.last_of(item_begin, item_begin + item.own_units(), item.weight) - (int)blockIdx.x, 0};
             it = end;
             unit = unit_after;
             item = after;
         }
-        if (tid == 0) a.desc[blockIdx.x] = begun;
+        if (tid == 0) a.begun[blockIdx.x] = begun;
     }
     tc_before();
     __syncthreads();
