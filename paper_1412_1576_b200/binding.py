@@ -120,7 +120,7 @@ def load_library(path: str | None = None):
     L.lda_verify_drafts.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, C.c_int, i32, vp, vp, vp, vp, vp]
     L.lda_token_logprobs.argtypes = [vp, C.c_int, i64, i32, i64, vp, i32, dbl, vp, vp, vp, vp, vp, vp]
     L.lda_token_logprobs_grad.argtypes = [vp, C.c_int, i64, i32, i64, vp, vp, vp, vp, dbl, vp, i64, vp]
-    cache = C.POINTER(lda_paged_cache)
+    cache = vp  # an lda_paged_cache by reference, or its bytes
     L.lda_append_cache.argtypes = [cache, i64, vp, i64, i64, vp, i64, i64, vp, vp, i32, C.c_int, vp, i64, i64, i32, vp, i64, i64, vp]
     L.lda_tree_mask.argtypes = [vp, vp, i64, i64, vp, i32, vp, vp, vp]
     L.lda_tree_attention_workspace.argtypes = [cache, i64, i32]
@@ -348,13 +348,17 @@ def lda_token_logprobs_grad(logits_ptr, dtype, rows, V, row_stride, tokens_ptr, 
                                                   entropy_weights_ptr, temperature, grad_ptr, grad_stride, cuda_stream)
 
 
+def _by_reference(cache):
+    return C.byref(cache) if isinstance(cache, lda_paged_cache) else cache
+
+
 # Operators on a paged cache (``cache``: an ``lda_paged_cache``; raw DEVICE pointers or None, as above).  The module ``cache`` has them for
 # torch tensors.
 
 def lda_append_cache(cache, tokens, k_ptr, k_token_stride, k_head_stride, v_ptr, v_token_stride, v_head_stride, positions_ptr, inv_freq_ptr,
                      rotated, interleaved, q_ptr=None, q_token_stride=0, q_head_stride=0, heads=0, q_out_ptr=None, out_token_stride=0,
                      out_head_stride=0, cuda_stream=None):
-    return load_library().lda_append_cache(cache, tokens, k_ptr, k_token_stride, k_head_stride, v_ptr, v_token_stride, v_head_stride,
+    return load_library().lda_append_cache(_by_reference(cache), tokens, k_ptr, k_token_stride, k_head_stride, v_ptr, v_token_stride, v_head_stride,
                                            positions_ptr, inv_freq_ptr, rotated, interleaved, q_ptr, q_token_stride, q_head_stride,
                                            heads, q_out_ptr, out_token_stride, out_head_stride, cuda_stream)
 
@@ -364,12 +368,12 @@ def lda_tree_mask(parents_ptr, offsets_ptr, n_seqs, tokens, starts_ptr, words, m
 
 
 def lda_tree_attention_workspace(cache, tokens, heads):
-    return load_library().lda_tree_attention_workspace(cache, tokens, heads)
+    return load_library().lda_tree_attention_workspace(_by_reference(cache), tokens, heads)
 
 
 def lda_tree_attention(cache, tokens, q_ptr, q_token_stride, q_head_stride, heads, mask_ptr, mask_stride, mask_words, scale, out_ptr,
                        out_token_stride, out_head_stride, workspace_ptr, workspace_bytes, cuda_stream=None):
-    return load_library().lda_tree_attention(cache, tokens, q_ptr, q_token_stride, q_head_stride, heads, mask_ptr, mask_stride, mask_words,
+    return load_library().lda_tree_attention(_by_reference(cache), tokens, q_ptr, q_token_stride, q_head_stride, heads, mask_ptr, mask_stride, mask_words,
                                              scale, out_ptr, out_token_stride, out_head_stride, workspace_ptr, workspace_bytes, cuda_stream)
 
 
