@@ -119,15 +119,16 @@ struct LogprobGradArgs {
 
 constexpr int LOGPROB_GRAD_THREADS = 256, LOGPROB_GRAD_CHUNKS = 4;  // chunks of a warp
 
-// A CTA has a run of a row's chunks; a warp loads a chunk of 16-byte groups and writes its gradient.
+// A CTA has a run of a row's chunks; a warp loads a chunk of 16-byte groups and writes its gradient.  The last rows come first: of what
+// the forward pass has read last, L2 still holds some.
 template <typename T>
 __global__ void __launch_bounds__(LOGPROB_GRAD_THREADS) k_logprobs_grad(LogprobGradArgs a)
 {
     constexpr int R = LOGPROB_GROUPS, WARPS = LOGPROB_GRAD_THREADS / 32;
     __shared__ uint4 stage[WARPS][R * 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, V = a.V;
-    const int64_t r = blockIdx.x / a.parts;
-    const int part = (int)(blockIdx.x - r * a.parts);
+    const int64_t block = gridDim.x - 1 - blockIdx.x, r = block / a.parts;
+    const int part = (int)(block - r * a.parts);
     const T* row = (const T*)a.logits + r * a.stride;
     T* grad = (T*)a.grad + r * a.grad_stride;
     const int pre = (int)((uintptr_t)row % 16 / sizeof(T));
