@@ -522,7 +522,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         }
                     }
                 }
-                const float shift = (m == -INFINITY ? 0.0f : -m) + TC_RAISE<T>;
+                // (places of no row have no probabilities: products with zeros take less power, and a long call is bound by that)
+                const float shift = place < 0 ? -INFINITY : (m == -INFINITY ? 0.0f : -m) + TC_RAISE<T>;
                 // the probabilities are rounded to the values' type, which the product takes: half a step each, as much as the output's own
                 // rounding; the norm is that of the unrounded ones
                 float2 sum = make_float2(0.0f, 0.0f);
