@@ -17,8 +17,8 @@
 namespace lda {
 
 constexpr int TC_KEYS = 128, TC_ROWS = 128;
-constexpr int TC_TEAM = 128, TC_THREADS = 2 * TC_TEAM + 96;  // two teams; a warp that issues products, two that copy
-constexpr uint32_t TC_S = 0, TC_O = 256, TC_P = 64;     // columns of tensor memory: S twice, O twice; P's behind S's
+constexpr int TC_TEAM = 128, TC_THREADS = 3 * TC_TEAM;  // two teams; two warps that issue products, two that copy
+constexpr uint32_t TC_S = 0, TC_O = 256;                     // columns of tensor memory: S twice, O twice
 
 template <int DIM, int ROWS>
 struct TcShape {
@@ -26,15 +26,19 @@ struct TcShape {
     static constexpr int HALVES = DIM / 64;                      // 128 bytes of every row at a time
     static constexpr int TILE = TC_KEYS * DIM * 2;               // bytes of keys, values or queries
     static constexpr int K_STAGES = DIM == 128 ? 2 : 4, V_STAGES = DIM == 128 ? (PAIR ? 2 : 3) : 4;  // (a tile's values are needed later and longer)
-    static constexpr int COLS = PAIR ? 128 : ROWS;               // of S that a thread looks at
-    static constexpr int GROUPS = TC_ROWS / COLS;                // of keys
+    static constexpr int RT = PAIR ? 128 : ROWS;                 // rows of a team
+    static constexpr int GROUPS = TC_ROWS / RT;                  // of keys
+    // A tile's scores come and its probabilities go in one piece, or (PAIR) in two of 64 keys, so that a team has one to work on while the products
+    // of its other one run.  A piece's probabilities stand in the second half of its scores' columns.
+    static constexpr int PIECES = PAIR ? 2 : 1, PIECE = TC_KEYS / PIECES;
+    static constexpr int COLS = PAIR ? 64 : ROWS;                // of a piece that a thread looks at
     static constexpr int TOGETHER = 16 / GROUPS, PITCH = DIM + 4;  // rows whose parts are added up at a time
     static constexpr int K_AT = 0, V_AT = K_STAGES * TILE, Q_AT = V_AT + V_STAGES * TILE, REGION_AT = Q_AT + (PAIR ? 2 : 1) * TILE;
     static constexpr int SHARED = REGION_AT + 2 * GROUPS * TOGETHER * PITCH * 4 + 1024;  // (its start is moved up to a multiple of 1024)
 };
 
 struct TcBars {
-    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_full[2], o_done[2], q_full, q_empty;
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[4], p_full[4], o_done[4], q_full, q_empty;  // (S, P and O: of a team's piece)
 };
 
 __device__ __forceinline__ uint32_t tc_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
 {
     using S = TcShape<DIM, ROWS>;
     constexpr bool PAIR = S::PAIR;
-    constexpr int GROUPS = S::GROUPS, COLS = S::COLS;
+    constexpr int GROUPS = S::GROUPS, COLS = S::COLS, RT = S::RT, PIECES = S::PIECES, PIECE = S::PIECE;
     extern __shared__ uint8_t dynamic[];
     __shared__ TcBars bars;
     __shared__ unsigned long long red[TC_THREADS / 32], wild[4][2];  // (wild: of a stage's keys, those whose values are not all finite)
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
     volatile int* failed = &s_failed;
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) tc_init(bars.k_full[i], 1), tc_init(bars.k_empty[i], 1), tc_init(bars.v_full[i], 1), tc_init(bars.v_empty[i], 1);
-        for (int i = 0; i < 2; ++i) tc_init(bars.s_full[i], 1), tc_init(bars.p_full[i], TC_TEAM), tc_init(bars.o_done[i], 1);
+        for (int i = 0; i < 4; ++i) tc_init(bars.s_full[i], 1), tc_init(bars.p_full[i], TC_TEAM), tc_init(bars.o_done[i], 1);
         tc_init(bars.q_full, 2 * TC_TEAM), tc_init(bars.q_empty, 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -282,97 +286,98 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
         } else if (warp == 10) {
             tc_copies<DIM, ROWS, S::V_STAGES>(a, &maps.v, maps.group_bits, item, units, base + S::V_AT, bars.v_full, bars.v_empty, nullptr, wild,
                                                   failed);
-        } else if (warp == 8) {
-            // --- products, a tile's for a team at a time (a job): a job's scores ahead of the outputs of the job before it
-            constexpr uint32_t KIND_S = tc_kind(T_is_bf16<T>, false, TC_KEYS), KIND_O = tc_kind(T_is_bf16<T>, true, DIM);
+        } else {
+            // --- products, a piece's for a team at a time (a job): one warp issues those of the scores, as soon as the outputs of the job before
+            // in the same place are done, another those of the outputs (one alone is the slowest part of a tile: an issue takes it as long
+            // as the tensor cores take for the product)
+            constexpr uint32_t KIND_S = tc_kind(T_is_bf16<T>, false, PIECE), KIND_O = tc_kind(T_is_bf16<T>, true, DIM);
+            constexpr uint32_t JOB_PIECE = 1, JOB_TEAM = 2, JOB_FIRST = 4, JOB_LAST = 8, JOB_FRESH = 16, JOB_STEPS = 32;  // (first, last: of its tile)
             const bool leads = lane == 0;
             const uint32_t at = __shfl_sync(0xffffffffu, base, 0), tensor = __shfl_sync(0xffffffffu, tmem, 0);
-            int64_t units_left = units;
-            int it = 0;
             bool go = leads;  // (products and barriers are this lane's; none where a wait gave up)
             const auto wait = [&](uint64_t& bar, uint32_t parity) { go = tc_wait(bar, parity, failed) && go; };
-            uint32_t k_at = 0, k_round = 0, v_at = 0, v_round = 0, p_rounds = 0, q_round = 0;  // stages, and parities of the next phases
+            uint32_t stage = 0, round = 0, rounds = 0, q_round = 0;  // of keys or values, and parities of the next phases
             const uint32_t q_operand = tc_operand_low(16) + tc_operand_at(at + S::Q_AT), k_operand = tc_operand_low(16) + tc_operand_at(at + S::K_AT),
                            v_operand = tc_operand_low(TC_KEYS * 128) + tc_operand_at(at + S::V_AT);
-            const auto scores = [&](int team, bool first, bool last) {
-                if (first) wait(bars.k_full[k_at], k_round);
+            const auto scores = [&](uint32_t job) {
+                const uint32_t piece = job & 1, team = job >> 1 & 1, place = team * PIECES + piece;
+                if (job & JOB_FIRST) wait(bars.k_full[stage], round);
+                wait(bars.o_done[place], rounds >> place & 1 ^ 1);
+                rounds ^= 1u << place;
                 tc_after();
-                const uint32_t q = q_operand + (PAIR ? team * (S::TILE / 16) : 0), k = k_operand + k_at * (S::TILE / 16), to = tensor + TC_S + team * TC_KEYS;
+                const uint32_t q = q_operand + (PAIR ? team * (S::TILE / 16) : 0), k = k_operand + stage * (S::TILE / 16) + piece * (PIECE * 128 / 16),
+                               to = tensor + TC_S + team * TC_KEYS + piece * PIECE;
 #pragma unroll
                 for (int i = 0; i < DIM / 16; ++i) {
                     const uint32_t step = (i / 4 * (TC_KEYS * 128) + i % 4 * 32) / 16;
                     tc_product_shared(to, q + step, k + step, KIND_S, i > 0, go);
                 }
-                tc_commit(bars.s_full[team], go);
-                if (!last) return;
-                tc_commit(bars.k_empty[k_at], go);
-                if (++k_at == S::K_STAGES) k_at = 0, k_round ^= 1;
+                tc_commit(bars.s_full[place], go);
+                if (!(job & JOB_LAST)) return;
+                tc_commit(bars.k_empty[stage], go);
+                if (++stage == S::K_STAGES) stage = 0, round ^= 1;
             };
-            const auto outputs = [&](int team, bool first, bool last, bool fresh, int steps) {
-                wait(bars.p_full[team], p_rounds >> team & 1);
-                p_rounds ^= 1u << team;
-                if (first) wait(bars.v_full[v_at], v_round);
+            const auto outputs = [&](uint32_t job) {
+                const uint32_t piece = job & 1, team = job >> 1 & 1, place = team * PIECES + piece;
+                const int steps = (int)(job / JOB_STEPS);
+                if (job & JOB_FIRST) wait(bars.v_full[stage], round);
+                wait(bars.p_full[place], rounds >> place & 1);
+                rounds ^= 1u << place;
                 tc_after();
-                const uint32_t v = v_operand + v_at * (S::TILE / 16), from = tensor + TC_S + team * TC_KEYS + TC_P, to = tensor + TC_O + team * 128;
-                tc_product_tensor(to, from, v, KIND_O, !fresh, go);
-                if (steps == TC_KEYS / 16) {
+                const uint32_t v = v_operand + stage * (S::TILE / 16) + piece * (PIECE * 128 / 16),
+                               from = tensor + TC_S + team * TC_KEYS + piece * PIECE + PIECE / 2, to = tensor + TC_O + team * 128;
+                if (steps == PIECE / 16) {
 #pragma unroll
-                    for (int i = 1; i < TC_KEYS / 16; ++i) tc_product_tensor(to, from + 8 * i, v + i * (2048 / 16), KIND_O, true, go);
+                    for (int i = 0; i < PIECE / 16; ++i) tc_product_tensor(to, from + 8 * i, v + i * (2048 / 16), KIND_O, i > 0 || !(job & JOB_FRESH), go);
                 } else
 #pragma unroll 1
-                    for (int i = 1; i < steps; ++i) tc_product_tensor(to, from + 8 * i, v + i * (2048 / 16), KIND_O, true, go);
-                tc_commit(bars.o_done[team], go);
-                if (!last) return;
-                tc_commit(bars.v_empty[v_at], go);
-                if (++v_at == S::V_STAGES) v_at = 0, v_round ^= 1;
+                    for (int i = 0; i < steps; ++i) tc_product_tensor(to, from + 8 * i, v + i * (2048 / 16), KIND_O, i > 0 || !(job & JOB_FRESH), go);
+                tc_commit(bars.o_done[place], go);
+                if (!(job & JOB_LAST)) return;
+                tc_commit(bars.v_empty[stage], go);
+                if (++stage == S::V_STAGES) stage = 0, round ^= 1;
             };
             int64_t unit = share.lo;
-            int turn = 0, before = -1, steps_before = 0;  // the team of the next tile that one team has; that of the job before (-1: none), its sixteens
-            bool first_before = false, fresh_before = false;
-            const auto finish = [&] { outputs(before, first_before, true, fresh_before, steps_before); };
+            uint32_t turn = 0;  // the team of the next tile that one team has
             while (true) {
                 const int tiles = __shfl_sync(0xffffffffu, (int)min((int64_t)(item.tiles - item.tile), (share.hi - unit) >> (item.weight - 1)), 0);
                 const bool split = __any_sync(0xffffffffu, splits(item)), ends = __any_sync(0xffffffffu, item.tile + tiles == item.tiles);
                 // of the item's last tile the sixteens of keys that there are
                 const int last_steps = ends ? __shfl_sync(0xffffffffu, max(1, (item.keys - (item.tiles - 1) * TC_KEYS + 15) / 16), 0) : TC_KEYS / 16;
-                // (an item's first scores need queries that the rows put down when they are through with the item before it)
-                if (before >= 0) finish();
-                wait(bars.q_full, q_round);
-                q_round ^= 1;
+                if (warp == 8) {
+                    wait(bars.q_full, q_round);
+                    q_round ^= 1;
+                }
 #pragma unroll 1
                 for (int i = 0; i < tiles; ++i) {
-                    const int steps = i + 1 < tiles ? TC_KEYS / 16 : last_steps;
-                    if (split) {
-                        scores(0, true, false);
-                        if (i > 0) finish();
-                        scores(1, false, true);
-                        outputs(0, true, false, i == 0, steps);
-                        before = 1, first_before = false, fresh_before = i == 0;
-                    } else {
-                        scores(turn, true, true);
-                        if (i > 0) finish();
-                        before = turn, first_before = true, fresh_before = i < 2;
+                    const int steps = i + 1 < tiles ? TC_KEYS / 16 : last_steps, n = split ? 2 * PIECES : PIECES;
+                    const bool fresh = i < (split ? 1 : 2);
+#pragma unroll 1
+                    for (int x = 0; x < n; ++x) {
+                        const int piece = split ? x >> 1 : x, here = min(PIECE / 16, max(0, steps - piece * (PIECE / 16)));
+                        const uint32_t job = piece * JOB_PIECE | (split ? x & 1 : turn) * JOB_TEAM | (x == 0) * JOB_FIRST | (x + 1 == n) * JOB_LAST |
+                                             (fresh && piece == 0) * JOB_FRESH | here * JOB_STEPS;
+                        if (warp == 8) scores(job);
+                        else outputs(job);
                     }
-                    steps_before = steps;
                     turn ^= 1;
                 }
-                if (ends) tc_commit(bars.q_empty, go);
+                if (ends && warp == 8) tc_commit(bars.q_empty, go);
                 unit += (int64_t)tiles * item.weight + (ends ? item.extra_units() : 0);
                 if (!__any_sync(0xffffffffu, unit < share.hi)) break;
                 item.tile = item.tiles - 1;
                 item.template next<ROWS, TC_KEYS>(a);
             }
-            finish();
         }
         __syncwarp();
     } else {
         // --- rows (they go on where a wait gave up, so that all of them meet at their barriers; outputs are undefined then)
-        const int team = warp >> 2, kg = tid % TC_TEAM / COLS;
+        const int team = warp >> 2, kg = tid % TC_TEAM / RT;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const uint32_t at_s = tmem + lanes + TC_S + team * TC_KEYS, at_o = tmem + lanes + TC_O + team * 128;
         const uint32_t at_q = base + S::Q_AT + (PAIR ? team * S::TILE : 0) + tid % TC_TEAM * 128;
         // a thread's row of an item
-        const auto row_of = [&](const AttendItem& of) { return splits(of) ? tid : tid % COLS; };
+        const auto row_of = [&](const AttendItem& of) { return splits(of) ? tid : tid % RT; };
         // a row's queries, once for each of its copies, a half by each team (PAIR: each team has a place for its own); an item's first are put down
         // where the last one's have been read, which `ready` waits for
         constexpr int Q_EACH = DIM / 16;
@@ -402,7 +407,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
         put_q(item, [] {});
         int it = 0;
         int64_t unit = share.lo;
-        uint32_t n_s = 0, n_q = 0;  // tiles of the team, queries put down
+        uint32_t n_s = 0, n_q = 0;  // pieces of the team, queries put down
+        // barrier and parity of a piece of the team by its number
+        const auto place_of = [&](uint32_t n) { return team * PIECES + (PIECES == 2 ? n & 1 : 0); };
+        const auto phase_of = [&](uint32_t n) { return (PIECES == 2 ? n >> 1 : n) & 1; };
 #pragma unroll 1
         while (unit < share.hi) {
             const int count = (int)min((int64_t)(item.tiles - item.tile), (share.hi - unit) >> (item.weight - 1)), end = it + count;
@@ -417,7 +425,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
 #pragma unroll 1
             for (int u = split ? it : it + ((it ^ team) & 1); u < end; u += split ? 1 : 2) {
                 const int tile = item.tile + u - it;
-                tc_wait(bars.s_full[team], n_s & 1, failed);
+                tc_wait(bars.s_full[place_of(n_s)], phase_of(n_s), failed);
                 tc_after();
                 const uint32_t there = *(volatile uint32_t*)&valid[u & 15];
                 // the tile's keys, and whether all their pages have come
@@ -466,15 +474,21 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     tc_team_sync(team);
                     bad[0] = *(volatile unsigned long long*)&wild[vs][0], bad[1] = *(volatile unsigned long long*)&wild[vs][1];
                 }
-                // the scores come 32 columns at a time, the next ones while the last are worked on, and of 128 the first half twice (all at
-                // once would be more registers than there are); the probabilities go behind them, from the last to the first: over scores
-                // that have been read
+#pragma unroll 1
+                for (int piece = 0; piece < PIECES; ++piece) {
+                if (piece > 0) {
+                    tc_wait(bars.s_full[place_of(n_s)], phase_of(n_s), failed);
+                    tc_after();
+                }
+                const uint32_t at_piece = at_s + piece * PIECE;
+                // the scores come 32 columns at a time; the probabilities go behind them, from the last to the first: over scores that have
+                // been read
                 constexpr int CHUNKS = COLS / 32;
                 uint32_t even[32], odd[32];
-                const auto fetch = [&](uint32_t (&s)[32], int chunk) { tc_load(s, at_s + kg * COLS + 32 * chunk); };
+                const auto fetch = [&](uint32_t (&s)[32], int chunk) { tc_load(s, at_piece + kg * COLS + 32 * chunk); };
                 const auto hide = [&](uint32_t (&s)[32], int chunk) {
                     if (!masked) return;
-                    const int k = kg * COLS + 32 * chunk;
+                    const int k = piece * PIECE + kg * COLS + 32 * chunk;
                     const uint32_t w = (uint32_t)((k & 64 ? see[1] : see[0]) >> (k & 32));
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
@@ -509,7 +523,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     m = to;
                     l *= f;
                     if (any) {  // (O holds something)
-                        tc_wait(bars.o_done[team], (n_s & 1) ^ 1, failed);
+                        tc_wait(bars.o_done[place_of(n_s - 1)], phase_of(n_s - 1), failed);
                         tc_after();
 #pragma unroll 1
                         for (int d = 0; d < DIM; d += 32) {
@@ -537,42 +551,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         sum = add_two(sum, x);
                         p[j / 2] = pack_two<T>(x.x, x.y);
                     }
-                    tc_store(at_s + TC_P + (kg * COLS + 32 * chunk) / 2, p);
+                    tc_store(at_piece + PIECE / 2 + (kg * COLS + 32 * chunk) / 2, p);
                 };
-                if constexpr (CHUNKS == 4) {
-                    put(odd, 3);
-                    fetch(odd, 1);
-                    put(even, 2);
-                    tc_loaded(odd);
-                    fetch(even, 0);
-                    hide(odd, 1);
-                    put(odd, 1);
-                    tc_loaded(even);
-                    hide(even, 0);
-                    put(even, 0);
-                } else {
-                    if constexpr (CHUNKS == 2) put(odd, 1);
-                    put(even, 0);
-                }
+                if constexpr (CHUNKS == 2) put(odd, 1);
+                put(even, 0);
                 if (GROUPS > 1) {
                     const uint32_t zero[16] = {};
 #pragma unroll
                     for (int g = 1; g < GROUPS; ++g)
 #pragma unroll
-                        for (int from = 0; from < COLS; from += 32) tc_store(at_s + TC_P + (((kg + g) % GROUPS) * COLS + from) / 2, zero);
+                        for (int from = 0; from < COLS; from += 32) tc_store(at_piece + PIECE / 2 + (((kg + g) % GROUPS) * COLS + from) / 2, zero);
                 }
                 l += sum.x + sum.y;
                 tc_stored();
                 tc_before();
-                tc_arrive(bars.p_full[team]);
+                tc_arrive(bars.p_full[place_of(n_s)]);
                 any = true;
                 if (bad[0] | bad[1]) {
-                    tc_wait(bars.o_done[team], n_s & 1, failed);
+                    tc_wait(bars.o_done[place_of(n_s)], phase_of(n_s), failed);
                     tc_after();
 #pragma unroll 1
-                    for (int k = kg * COLS; k < (kg + 1) * COLS; ++k) {
+                    for (int k = piece * PIECE + kg * COLS, end_k = k + COLS; k < end_k; ++k) {
                         if (!((k < 64 ? bad[0] : bad[1]) >> (k & 63) & 1)) continue;  // (the same in the warp)
-                        const uint32_t two = tc_load(at_s + TC_P + k / 2);
+                        const uint32_t two = tc_load(at_piece + PIECE / 2 + k % PIECE / 2);
                         const uint16_t half = (uint16_t)(k & 1 ? two >> 16 : two);
                         const float p = cache_value(*reinterpret_cast<const T*>(&half));
                         int slot = 0;
@@ -595,6 +596,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     tc_before();
                 }
                 ++n_s;
+                }
             }
             // --- the item's end, or the share's: the next item's queries, then the sums out or to the parts
             AttendItem after = item;
@@ -603,7 +605,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 after.template next<ROWS, TC_KEYS>(a);
                 put_q(after, [&] { tc_wait(bars.q_empty, n_q++ & 1, failed); });
             }
-            if (any) tc_wait(bars.o_done[team], (n_s & 1) ^ 1, failed);
+            if (any) tc_wait(bars.o_done[place_of(n_s - 1)], phase_of(n_s - 1), failed);
             tc_after();
             const bool whole = ends && item_begin >= share.lo;
             const int slot = 2 * blockIdx.x + (item_begin < share.lo ? 0 : 1);
@@ -639,23 +641,23 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             } else {
                 // the teams' and key groups' parts: of a few rows at a time, or, behind the CTA's last unit, of all of them, where its keys and
                 // values were
-                constexpr int ALL = COLS < (S::K_STAGES + S::V_STAGES + (PAIR ? 2 : 1)) * S::TILE / (2 * GROUPS * S::PITCH * 4)
-                                        ? COLS
+                constexpr int ALL = RT < (S::K_STAGES + S::V_STAGES + (PAIR ? 2 : 1)) * S::TILE / (2 * GROUPS * S::PITCH * 4)
+                                        ? RT
                                         : (S::K_STAGES + S::V_STAGES + (PAIR ? 2 : 1)) * S::TILE / (2 * GROUPS * S::PITCH * 4);
                 const int together = last ? ALL : S::TOGETHER;
                 s_m[tid] = m, s_l[tid] = l;
                 tc_rows_sync();
                 float most = -INFINITY, norm = 0.0f;
 #pragma unroll
-                for (int g = 0; g < 2 * GROUPS; ++g) most = fmaxf(most, s_m[g * COLS + r]);
+                for (int g = 0; g < 2 * GROUPS; ++g) most = fmaxf(most, s_m[g * RT + r]);
 #pragma unroll
                 for (int g = 0; g < 2 * GROUPS; ++g) {
-                    const float x = s_m[g * COLS + r];
-                    norm += x == most ? s_l[g * COLS + r] : s_l[g * COLS + r] * exp2_unit(x - most);
+                    const float x = s_m[g * RT + r];
+                    norm += x == most ? s_l[g * RT + r] : s_l[g * RT + r] * exp2_unit(x - most);
                 }
                 float f = m == most ? 1.0f : exp2_unit(m - most);
                 if (whole) f = norm == 0.0f ? 0.0f : f / norm;  // (a row that sees nothing is zero)
-                if (!whole && tid < COLS) a.ml[(int64_t)slot * ROWS + r] = make_float2(most, norm);
+                if (!whole && tid < RT) a.ml[(int64_t)slot * ROWS + r] = make_float2(most, norm);
                 const uint32_t region = base + (last ? S::K_AT : S::REGION_AT);
 #pragma unroll 1
                 for (int first = 0; first < rows; first += together) {
@@ -667,7 +669,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                             uint32_t o[32];
                             tc_load(o, at_o + d);
                             tc_loaded(o);
-                            const uint32_t to = region + ((tid / COLS * together + r - first) * S::PITCH + d) * 4;
+                            const uint32_t to = region + ((tid / RT * together + r - first) * S::PITCH + d) * 4;
                             if (here)
 #pragma unroll
                                 for (int i = 0; i < 32; i += 4)
