@@ -44,9 +44,13 @@ struct AttendShape {
     static constexpr int SHARED = STAGES * 2 * TILE_BYTES + 64 * PITCH * 4 + (Q_SHARED ? ROWS * ROW_BYTES : 0);
 };
 
+// The kernel for caches that the tensor cores' own memory does not suit: heads of more than 128 values, pages that are no multiple of 8 slots.
 // A CTA of four warps walks over its units; a warp has 16 rows and, with fewer than four groups of rows, a share of every tile's keys.
 // Tiles of keys and values come by asynchronous copies of 16 bytes into a ring of stages (a warp brings 16 keys of each; pages may lie
 // anywhere), two or three tiles ahead, across the ends of items; what lies behind the last key is filled with zeros.
+// 64 sequences of up to 8192 slots in pages of 4, one token each, 32 query heads on 8 of 128 values: 314 us, 4.3 TB/s (in pages of 16 277, for the
+// 213 of the other kernel).  Bound by latency: eight warps of a multiprocessor go through copies, products and exponentials one after the other
+// (issue slots 36 % full).
 template <typename T, int DIM, int ROWS>
 __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendArgs a)
 {

@@ -25,7 +25,9 @@ struct LogprobArgs {
 
 constexpr int LOGPROB_GROUPS = 4, LOGPROB_DEPTH = 4;  // groups of a lane in a chunk, chunks on their way
 
-// One cluster per row: one pass, then the CTAs' sums.
+// One cluster per row: one pass, then the CTAs' sums.  2048 rows of 141 000 words of bf16: 101 us, 5.7 TB/s; 777 rows of 100 003 of fp16: 38 us (six rows
+// on some multiprocessors, five on others: 740 rows take 34).  Multifunction units 58 %, issue slots 55 % full.
+// Tried: 256 threads a row (101 and 40 us), rings of three and two chunks (99 to 100), rows of the second kind in clusters of two or four (40, 46).
 template <typename T>
 __global__ void __launch_bounds__(ROW_THREADS, 2) k_logprobs(LogprobArgs a)
 {
@@ -120,7 +122,7 @@ struct LogprobGradArgs {
 constexpr int LOGPROB_GRAD_THREADS = 256, LOGPROB_GRAD_CHUNKS = 4;  // chunks of a warp
 
 // A CTA has a run of a row's chunks; a warp loads a chunk of 16-byte groups and writes its gradient.  The last rows come first: of what
-// the forward pass has read last, L2 still holds some.
+// the forward pass has read last, L2 still holds some (both together 300 -> 296 us).  2048 rows of 141 000 words of bf16: 188 us, 6.15 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(LOGPROB_GRAD_THREADS) k_logprobs_grad(LogprobGradArgs a)
 {
