@@ -386,7 +386,7 @@ int lda_token_logprobs_grad(const void* logits_dev, int dtype, int64_t rows, int
  *   starts     [n_seqs]: how many slots the sequence has before its new tokens (below 0: 0)
  *   offsets    [n_seqs + 1]: sequence b has the new tokens offsets[b] .. offsets[b+1] - 1 of the call's `tokens`, in the slots
  *              from starts[b] on.  Offsets that do not run upwards inside [0, tokens] leave the sequence out; rows of outputs that belong
- *              to no sequence stay as they are
+ *              to no sequence stay as they are, and what several sequences claim is undefined, as are slots that several tokens get
  * Rows of heads (keys, values, queries, outputs) are [tokens, heads, dim] with two strides. */
 #define LDA_HEAD_MAX_DIM 256
 #define LDA_HEADS_MAX 1024

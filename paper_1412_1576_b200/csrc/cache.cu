@@ -203,11 +203,56 @@ struct MaskArgs {
     int32_t* positions;  // may be null
 };
 
-// One CTA per tree.  Of up to 256 nodes a thread has one, and what it knows of the way up doubles from round to round: its bits and those of
-// the node where they end, eight rounds for a chain of 256 (2048 trees of up to 255 nodes, every fourth a chain: 13.5 us, walking node by
-// node 41).
-// Larger trees are walked from each node to the root.  Parents stand before their children, so that the places on the way go down and a
-// node's words are done one after the other, from the last to the first.
+// One tree of up to 256 nodes in W words: a thread has a node, and what it knows of the way up doubles from round to round: its bits and
+// those of the node where they end, eight rounds for a chain of 256.  Shared memory bounds it, so a node's words behind its own are neither
+// written nor read, a node that has reached the root is written once more and then no longer, and a node's place and count are one word.
+// Rows go out by 16 bytes where they can.  2048 trees of up to 255 nodes, every fourth a chain: 10.4 us, without these 13.3, and walking
+// node by node 41.  Up to 64 nodes have W = 1 (32 trees of 48 nodes: 2.8 us, with W = 4 3.1).
+template <int W>
+__device__ __forceinline__ void mask_doubling(const MaskArgs& a, int64_t lo, int n, int start, int32_t* near,
+                                              unsigned long long (*s_bits)[MASK_THREADS])
+{
+    const int i = threadIdx.x;
+    int up = i < n ? a.parents[lo + i] : -1, above = 1;  // where the bits end, and how many there are
+    if (up < 0 || up >= i) up = -1;
+    bool fresh = i < n;  // not yet as it is in shared memory
+    unsigned long long bits[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) bits[w] = W == 1 || w == i >> 6 ? 1ull << (i & 63) : 0ull;
+    while (__syncthreads_or(up >= 0)) {
+        if (fresh) {
+            near[i] = above << 16 | (up + 1);
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                if (W == 1 || w <= i >> 6) s_bits[w][i] = bits[w];
+        }
+        __syncthreads();
+        fresh = up >= 0;
+        if (fresh) {
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                if (W == 1 || w <= up >> 6) bits[w] |= s_bits[w][up];
+            const int there = near[up];
+            above += there >> 16, up = (there & 0xffff) - 1;
+        }
+    }
+    if (i >= n) return;
+    int64_t* row = a.mask + (lo + i) * a.words;
+    if (W > 1 && a.words % 2 == 0 && (uintptr_t)a.mask % 16 == 0) {
+#pragma unroll
+        for (int w = 0; w + 1 < W; w += 2)
+            if (w < a.words) *(ulonglong2*)(row + w) = make_ulonglong2(bits[w], bits[w + 1]);
+    } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (w < a.words) row[w] = (int64_t)bits[w];
+    }
+    for (int w = W; w < a.words; ++w) row[w] = 0;
+    if (a.positions) a.positions[lo + i] = start + above - 1;
+}
+
+// One CTA per tree.  More than 256 nodes are walked from each to the root.  Parents stand before their children, so that the places on the
+// way go down and a node's words are done one after the other, from the last to the first.
 __global__ void __launch_bounds__(MASK_THREADS) k_tree_mask(MaskArgs a)
 {
     __shared__ int32_t near[MASK_PARENTS];
@@ -216,37 +261,9 @@ __global__ void __launch_bounds__(MASK_THREADS) k_tree_mask(MaskArgs a)
     const int64_t lo = a.offsets[b], hi = a.offsets[b + 1];
     if (lo < 0 || hi < lo || hi > a.tokens) return;
     const int n = (int)(hi - lo), start = a.starts ? a.starts[b] : 0;
+    if (n <= 64) return mask_doubling<1>(a, lo, n, start, near, s_bits);
+    if (n <= MASK_THREADS) return mask_doubling<MASK_THREADS / 64>(a, lo, n, start, near, s_bits);
     const int32_t* parents = a.parents + lo;
-    if (n <= MASK_THREADS) {
-        const int i = threadIdx.x, words = min(a.words, MASK_THREADS / 64), used = (n + 63) / 64;
-        int up = i < n ? parents[i] : -1, above = 1;  // where the bits end, and how many there are
-        if (up < 0 || up >= i) up = -1;
-        unsigned long long bits[MASK_THREADS / 64];
-#pragma unroll
-        for (int w = 0; w < MASK_THREADS / 64; ++w) bits[w] = w == i >> 6 ? 1ull << (i & 63) : 0ull;
-        while (__syncthreads_or(up >= 0)) {
-            near[i] = up, near[MASK_THREADS + i] = above;
-#pragma unroll
-            for (int w = 0; w < MASK_THREADS / 64; ++w)
-                if (w < used) s_bits[w][i] = bits[w];
-            __syncthreads();
-            if (up >= 0) {
-#pragma unroll
-                for (int w = 0; w < MASK_THREADS / 64; ++w)
-                    if (w < used) bits[w] |= s_bits[w][up];
-                above += near[MASK_THREADS + up];
-                up = near[up];
-            }
-        }
-        if (i >= n) return;
-        int64_t* row = a.mask + (lo + i) * a.words;
-#pragma unroll
-        for (int w = 0; w < MASK_THREADS / 64; ++w)
-            if (w < words) row[w] = (int64_t)bits[w];
-        for (int w = MASK_THREADS / 64; w < a.words; ++w) row[w] = 0;
-        if (a.positions) a.positions[lo + i] = start + above - 1;
-        return;
-    }
     if (n <= MASK_PARENTS) {
         for (int i = threadIdx.x; i < n; i += MASK_THREADS) near[i] = parents[i];
         __syncthreads();

@@ -168,6 +168,22 @@ def test_tree_mask(new, nodes, deep):
         x.starts, x.offsets[1:] - x.offsets[:-1]))
 
 
+@pytest.mark.parametrize("skip", [0, 1])
+@pytest.mark.parametrize("words", [1, 2, 3, 4, 5, 6, 64])
+def test_tree_mask_of_any_number_of_words(words, skip):
+    """More words than a tree needs, and fewer; rows that begin on 8 bytes and not on 16."""
+    new = [63, 64, 65, 128, 129, 255, 256, 257, 0, 1]
+    x = Batch([0] * len(new), new, 1, 8, 16, BF16, width=1)
+    parents = trees(x, 257)
+    n = sum(new)
+    out = torch.full((skip + n * words + 1,), 9, dtype=torch.int64).cuda()
+    assert b.lda_tree_mask(parents.data_ptr(), x.offsets.data_ptr(), len(new), n, None, words, out.data_ptr() + 8 * skip, None) == b.LDA_OK
+    torch.cuda.synchronize()
+    want, _ = mask_reference(parents.tolist(), x.offsets.tolist(), [0] * len(new), max(words, 5))
+    assert out[skip:-1].view(n, words).tolist() == [want[i][:words] for i in range(n)]
+    assert out[:skip].tolist() == [9] * skip and int(out[-1]) == 9
+
+
 def test_tree_mask_of_strange_parents_and_offsets():
     parents = torch.tensor([0, 5, -7, 2, 2**31 - 1, -(2**31), 4, 1], dtype=torch.int32).cuda()
     offsets = torch.tensor([0, 7, 7, 8], dtype=torch.int64).cuda()
