@@ -63,58 +63,61 @@ def _steps(x, name):
 
 
 def _heads(x, name, dtype, tokens, dim, device):
-    """Checks rows of heads; returns (address, token stride, head stride)."""
+    """Checks rows of heads; returns (their number, address, token stride, head stride)."""
     shape = x.shape
-    if x.dtype is dtype and len(shape) == 3 and shape[2] == dim and (tokens is None or shape[0] == tokens) and x.device == device:
-        # (what most calls bring)
-        address, (between, step, one) = x.data_ptr(), x.stride()
-        if one == 1 and not (between | step) & 7 and not address & 15 and address:
-            return address, between, step
+    if x.dtype is dtype and len(shape) == 3 and x.device == device:
+        n, heads, values = shape
+        if values == dim and (tokens is None or n == tokens):
+            # (what most calls bring)
+            address, (between, step, one) = x.data_ptr(), x.stride()
+            if one == 1 and not (between | step) & 7 and not address & 15 and address:
+                return heads, address, between, step
     if x.dtype is not dtype:
         raise TypeError(f"{name}: the cache's {dtype} is needed, not {x.dtype}")
     if len(shape) != 3 or shape[2] != dim or tokens is not None and shape[0] != tokens:
         raise ValueError(f"{name}: [{'tokens' if tokens is None else tokens}, heads, {dim}] is needed, not {tuple(shape)}")
     _here(x, name, device)
-    return (_memory(x, name), *_steps(x, name))
+    return (shape[1], _memory(x, name), *_steps(x, name))
 
 
 def _cache(k_cache, v_cache, table, starts, offsets, device):
-    """Checks a cache and its sequences; returns the library's description of them."""
-    code = _DTYPES.get(k_cache.dtype)
-    shape = k_cache.shape
+    """Checks a cache and its sequences; returns the library's description of them, and the cache's type, heads and their values."""
+    dtype, shape = k_cache.dtype, k_cache.shape
+    code = _DTYPES.get(dtype)
     if code is None:
-        raise TypeError(f"k_cache: float16 or bfloat16 is needed, not {k_cache.dtype}")
-    if v_cache.dtype is not k_cache.dtype:
-        raise TypeError(f"v_cache: {k_cache.dtype} is needed, not {v_cache.dtype}")
-    if len(shape) != 4 or v_cache.shape != shape or shape[1] < 1 or shape[2] < 1:
+        raise TypeError(f"k_cache: float16 or bfloat16 is needed, not {dtype}")
+    if v_cache.dtype is not dtype:
+        raise TypeError(f"v_cache: {dtype} is needed, not {v_cache.dtype}")
+    if len(shape) != 4 or v_cache.shape != shape or 0 in shape[1:3]:
         raise ValueError(f"k_cache and v_cache: [pages, page_size, kv_heads, dim] is needed, not {tuple(shape)} and {tuple(v_cache.shape)}")
-    if shape[3] < 8 or shape[3] % 8 or shape[3] > _b.LDA_HEAD_MAX_DIM:
-        raise ValueError(f"k_cache: heads of a multiple of 8 values up to {_b.LDA_HEAD_MAX_DIM} are needed, not {shape[3]}")
-    if shape[2] > _b.LDA_HEADS_MAX:
-        raise ValueError(f"k_cache: up to {_b.LDA_HEADS_MAX} heads, not {shape[2]}")
-    _here(k_cache, "k_cache", device)
-    _here(v_cache, "v_cache", device)
-    k, v = k_cache.stride(), v_cache.stride()
+    pages, page_size, heads, dim = shape
+    if dim < 8 or dim & 7 or dim > _b.LDA_HEAD_MAX_DIM:
+        raise ValueError(f"k_cache: heads of a multiple of 8 values up to {_b.LDA_HEAD_MAX_DIM} are needed, not {dim}")
+    if heads > _b.LDA_HEADS_MAX:
+        raise ValueError(f"k_cache: up to {_b.LDA_HEADS_MAX} heads, not {heads}")
+    if k_cache.device != device or v_cache.device != device or table.device != device:
+        _here(k_cache, "k_cache", device), _here(v_cache, "v_cache", device), _here(table, "table", device)
+    (k0, k1, k2, k3), (v0, v1, v2, v3) = k_cache.stride(), v_cache.stride()
     keys, values = k_cache.data_ptr(), v_cache.data_ptr()
-    if k[3] != 1 or v[3] != 1 or (k[0] | k[1] | k[2] | v[0] | v[1] | v[2]) & 7 or not keys or not values or (keys | values) & 15:
-        k, v = (*_steps(k_cache, "k_cache"), 1), (*_steps(v_cache, "v_cache"), 1)
+    if k3 != 1 or v3 != 1 or (k0 | k1 | k2 | v0 | v1 | v2) & 7 or not keys or not values or (keys | values) & 15:
+        (k0, k1, k2), (v0, v1, v2) = _steps(k_cache, "k_cache"), _steps(v_cache, "v_cache")
         keys, values = _memory(k_cache, "k_cache"), _memory(v_cache, "v_cache")
-    if offsets.dim() != 1 or offsets.shape[0] < 1:
+    n, grid = offsets.shape, table.shape
+    if len(n) != 1 or n[0] < 1:
         raise ValueError("offsets: one more than there are sequences is needed")
-    n = offsets.shape[0] - 1
+    n = n[0] - 1
     if table.dtype is not torch.int32:
         raise TypeError(f"table: int32 is needed, not {table.dtype}")
-    if table.dim() != 2 or table.shape[0] != n:
-        raise ValueError(f"table: a row for each of {n} sequences is needed, not {tuple(table.shape)}")
-    _here(table, "table", device)
-    width, (between, step) = table.shape[1], table.stride()
+    if len(grid) != 2 or grid[0] != n:
+        raise ValueError(f"table: a row for each of {n} sequences is needed, not {tuple(grid)}")
+    width, (between, step) = grid[1], table.stride()
     if width > 1 and step != 1:
         raise ValueError("table: the pages of a sequence must be consecutive in memory")
-    if width * shape[1] > 0x7FFFFFFF:
+    if width * page_size > 0x7FFFFFFF:
         raise ValueError("table: a sequence has less than 2^31 slots")
-    return _pack_cache(keys, values, code, shape[2], shape[3], shape[1], shape[0], k[0], k[1], k[2], v[0], v[1], v[2], table.data_ptr(),
-                       between if n > 1 else 0, n, _vector(starts, "starts", torch.int32, n, device),
-                       _vector(offsets, "offsets", torch.int64, n + 1, device), width)
+    return _pack_cache(keys, values, code, heads, dim, page_size, pages, k0, k1, k2, v0, v1, v2, table.data_ptr(), between if n > 1 else 0, n,
+                       _vector(starts, "starts", torch.int32, n, device), _vector(offsets, "offsets", torch.int64, n + 1, device),
+                       width), dtype, heads, dim
 
 
 def tree_mask(parents, offsets, starts, nodes: int):
@@ -157,22 +160,23 @@ def append_cache(k, v, k_cache, v_cache, table, starts, offsets, positions=None,
     _unfollowed(k=k, v=v, q=q)
     if k_cache.requires_grad or v_cache.requires_grad or q_out is not None and q_out.requires_grad:
         raise ValueError("k_cache, v_cache and q_out: tensors that autograd follows cannot be written to (detach them)")
-    cache = _cache(k_cache, v_cache, table, starts, offsets, device)
-    tokens, dtype, kv_heads, dim = k.shape[0] if k.dim() else 0, k_cache.dtype, k_cache.shape[2], k_cache.shape[3]
-    rows = (*_heads(k, "k", dtype, tokens, dim, device), *_heads(v, "v", dtype, tokens, dim, device))
-    if k.shape[1] != kv_heads or v.shape[1] != kv_heads:
-        raise ValueError(f"k and v: the cache's {kv_heads} heads are needed, not {k.shape[1]} and {v.shape[1]}")
+    cache, dtype, kv_heads, dim = _cache(k_cache, v_cache, table, starts, offsets, device)
+    k_heads, *from_k = _heads(k, "k", dtype, None, dim, device)
+    tokens = k.shape[0]
+    v_heads, *from_v = _heads(v, "v", dtype, tokens, dim, device)
+    if k_heads != kv_heads or v_heads != kv_heads:
+        raise ValueError(f"k and v: the cache's {kv_heads} heads are needed, not {k_heads} and {v_heads}")
     positions_ptr = inv_freq_ptr = None
     rotated = 0
     if positions is not None:
         positions_ptr = _vector(positions, "positions", torch.int32, tokens, device)
         if not positions_ptr and tokens:
             raise ValueError("positions: a tensor without memory of its own")
-    if inv_freq is not None and inv_freq.numel():
-        rotated = 2 * inv_freq.numel()
-        inv_freq_ptr = _vector(inv_freq, "inv_freq", torch.float32, rotated // 2, device)
+    if inv_freq is not None and (pairs := inv_freq.numel()):
+        inv_freq_ptr = _vector(inv_freq, "inv_freq", torch.float32, pairs, device)
+        rotated = 2 * pairs
         if rotated > dim:
-            raise ValueError(f"inv_freq: {dim // 2} values at most, not {rotated // 2}")
+            raise ValueError(f"inv_freq: {dim // 2} values at most, not {pairs}")
     queries = (None, 0, 0, 0, None, 0, 0)
     given = q_out is not None
     if q is None and given:
@@ -182,11 +186,12 @@ def append_cache(k, v, k_cache, v_cache, table, starts, offsets, positions=None,
             q_out = torch.empty_like(q)
         elif q_out.shape != q.shape:
             raise ValueError(f"q_out: must have the queries' shape, not {tuple(q_out.shape)}")
-        from_q, to = _heads(q, "q", dtype, tokens, dim, device), _heads(q_out, "q_out", dtype, tokens, dim, device)
-        if not 1 <= q.shape[1] <= _b.LDA_HEADS_MAX:
-            raise ValueError(f"q: 1 to {_b.LDA_HEADS_MAX} heads, not {q.shape[1]}")
-        queries = (*from_q, q.shape[1], *to)
-    _call("lda_append_cache", device, cache, tokens, *rows, positions_ptr, inv_freq_ptr, rotated, int(interleaved), *queries)
+        heads, *from_q = _heads(q, "q", dtype, tokens, dim, device)
+        _, *to = _heads(q_out, "q_out", dtype, tokens, dim, device)
+        if not 1 <= heads <= _b.LDA_HEADS_MAX:
+            raise ValueError(f"q: 1 to {_b.LDA_HEADS_MAX} heads, not {heads}")
+        queries = (*from_q, heads, *to)
+    _call("lda_append_cache", device, cache, tokens, *from_k, *from_v, positions_ptr, inv_freq_ptr, rotated, int(interleaved), *queries)
     increment_version((k_cache, v_cache, q_out) if given else (k_cache, v_cache))  # (a graph that has saved them finds out)
     return q_out
 
@@ -201,10 +206,9 @@ def tree_attention(q, k_cache, v_cache, table, starts, offsets, mask=None, scale
     """
     device = _cuda(q, "q")
     _unfollowed(q=q, k_cache=k_cache, v_cache=v_cache)
-    cache = _cache(k_cache, v_cache, table, starts, offsets, device)
-    dtype, kv_heads, dim = k_cache.dtype, k_cache.shape[2], k_cache.shape[3]
-    rows = _heads(q, "q", dtype, None, dim, device)
-    tokens, heads = q.shape[0], q.shape[1]
+    cache, dtype, kv_heads, dim = _cache(k_cache, v_cache, table, starts, offsets, device)
+    heads, *rows = _heads(q, "q", dtype, None, dim, device)
+    tokens = q.shape[0]
     if not 1 <= heads <= _b.LDA_HEADS_MAX or heads % kv_heads:
         raise ValueError(f"q: a multiple of the cache's {kv_heads} heads up to {_b.LDA_HEADS_MAX} is needed, not {heads}")
     if scale is None:
@@ -229,7 +233,7 @@ def tree_attention(q, k_cache, v_cache, table, starts, offsets, mask=None, scale
         out = torch.empty_like(q)
     elif out.shape != q.shape or out.requires_grad:
         raise ValueError("out: must have the queries' shape, and autograd must not follow it")
-    to = _heads(out, "out", dtype, tokens, dim, device)
+    _, *to = _heads(out, "out", dtype, tokens, dim, device)
     size = _b.load_library().lda_tree_attention_workspace(cache, tokens, heads)
     if size < 0:
         raise _b.LdaError(size, "lda_tree_attention_workspace")
