@@ -359,7 +359,7 @@ int lda_verify_drafts(const int64_t* draft_offsets_dev, int64_t n_seqs, const in
 /* Log probabilities of given tokens and the rows' entropies: with q = softmax(x / temperature), logprobs[r] = log q of tokens[r] and
  * entropy[r] = -sum q log q, in natural units.  A token outside [0, V) has log probability 0; a row that is masked whole has entropy 0 and
  * log probabilities minus infinity; a NaN or plus infinity in a row makes its numbers NaN.  Both are exact to their last places where a
- * row is nearly sure, too.  stats[rows][3] (may be NULL): what the gradient needs -- the largest logit m, log sum exp((x - m) / temperature),
+ * row is nearly sure, too; shares (and the gradient's values) below 2^-126 may count as 0.  stats[rows][3] (may be NULL): what the gradient needs -- the largest logit m, log sum exp((x - m) / temperature),
  * sum q (m - x) / temperature.  top 1..LDA_TOP_MAX: ids[rows][top] as lda_top_logits gives them, and alternatives[rows][top],
  * their log probabilities (minus infinity where no word is left); top 0: neither is looked at. */
 int lda_token_logprobs(const void* logits_dev, int dtype, int64_t rows, int32_t V, int64_t row_stride, const int32_t* tokens_dev,
