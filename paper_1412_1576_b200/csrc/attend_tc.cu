@@ -165,13 +165,6 @@ __device__ __forceinline__ void tc_store(uint32_t at, const uint32_t (&r)[8])
                  "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-__device__ __forceinline__ uint32_t tc_load(uint32_t at)
-{
-    uint32_t r;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r)::"memory");
-    return r;
-}
 // 64 columns of `rows` slots of a page's head; every coordinate is inside the cache, the first one a multiple of 64.
 __device__ __forceinline__ void tc_copy(uint32_t to, const CUtensorMap* map, int column, int slot, int head, int page, uint64_t& bar)
 {
@@ -572,6 +565,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 }
                 l += sum.x + sum.y;
                 tc_stored();
+                // (what is taken out below needs its probabilities when the outputs are done; the next scores may stand in their place by then,
+                // so they are read before the products may begin.  In local memory, which nothing else here uses)
+                uint32_t kept[COLS / 2];
+                if (bad[0] | bad[1])
+#pragma unroll 1
+                    for (int i = 0; i < COLS / 2; i += 8) {
+                        uint32_t x[8];
+                        tc_load(x, at_piece + PIECE / 2 + kg * COLS / 2 + i);
+                        tc_loaded(x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) kept[i + e] = x[e];
+                    }
                 tc_before();
                 tc_arrive(bars.p_full[place_of(n_s)]);
                 any = true;
@@ -579,9 +584,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     tc_wait(bars.o_done[place_of(n_s)], phase_of(n_s), failed);
                     tc_after();
 #pragma unroll 1
-                    for (int k = piece * PIECE + kg * COLS, end_k = k + COLS; k < end_k; ++k) {
+                    for (int i = 0; i < COLS; ++i) {
+                        const int k = piece * PIECE + kg * COLS + i;
                         if (!((k < 64 ? bad[0] : bad[1]) >> (k & 63) & 1)) continue;  // (the same in the warp)
-                        const uint32_t two = tc_load(at_piece + PIECE / 2 + k % PIECE / 2);
+                        const uint32_t two = kept[i / 2];
                         const uint16_t half = (uint16_t)(k & 1 ? two >> 16 : two);
                         const float p = cache_value(*reinterpret_cast<const T*>(&half));
                         int slot = 0;

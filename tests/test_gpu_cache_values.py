@@ -1,0 +1,59 @@
+"""Attention over a paged cache where values are infinite or no numbers: what a row does not see does not touch it, wherever it lies."""
+import pytest
+import torch
+
+from test_gpu_cache import BF16, F16, INF, NAN, Batch, check_attend, trees
+from paper_1412_1576_b200 import cache
+
+pytestmark = pytest.mark.gpu
+
+# (contexts, new tokens, heads of the cache, query heads, sequences without tokens behind them: rows of a tile go by the average).  So many heads
+# that each of 148 runs of tiles has more than one item's, and a tile with such values has others behind it.
+LONG = [([100, 70], [64, 64], 128, 512, 0),     # 256 rows, both teams have each tile of keys
+        ([37, 5], [400, 130], 64, 64, 0),       # the same, and items of fewer rows among them
+        ([37], [400], 64, 64, 15),              # 64 rows
+        ([37], [600], 64, 64, 40)]              # 32 rows
+
+
+def batch(starts, new, kv_heads, empty, dim, dtype, page=16):
+    return Batch(starts + [0] * empty, new + [0] * empty, kv_heads, dim, page, dtype, seed=dim + empty)
+
+
+def put(x, i, slot, column, value):
+    pages, places = x.slots(i)
+    x.v[pages[slot], places[slot], :, column] = value
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("tree", [False, True], ids=["chain", "tree"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("starts,new,kv_heads,heads,empty", LONG, ids=str)
+def test_values_in_any_of_several_tiles_of_new_tokens(starts, new, kv_heads, heads, empty, dim, tree, dtype):
+    """One kind in the first of the tiles, which rows behind it see, then all kinds in the first, a middle and the last one, some of them alone in
+    their column and some together."""
+    x = batch(starts, new, kv_heads, empty, dim, dtype)
+    mask = cache.tree_mask(trees(x, max(new)), x.offsets, None, max(new))[0] if tree else None
+    q = x.rows(heads, by=0.5)
+    put(x, 0, starts[0] + 3, 5, NAN)
+    check_attend(x, heads, mask, q=q)
+    for i, n in enumerate(new):
+        for j, (place, kind) in enumerate([(2, INF), (7, -INF), (n // 2, -INF), (n // 2 + 1, NAN), (n - 2, INF), (n - 1, NAN)]):
+            put(x, i, starts[i] + place, 8 + j, kind)
+            put(x, i, starts[i] + place, 40 + j % 3, kind)
+    got = check_attend(x, heads, mask, q=q)
+    # (of a chain, the first tokens see none of it)
+    assert tree or bool(torch.isfinite(got[:2]).all()) and bool(torch.isinf(got[3:7]).any())
+
+
+@pytest.mark.parametrize("empty,new", [(0, 40), (12, 300), (29, 300)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_values_beside_a_missing_page(empty, new, dim):
+    """A tile in the middle of a context, of which a page is missing."""
+    x = batch([1000], [new], 64, empty, dim, BF16)
+    x.table[0, 17] = -1                     # slots 272 .. 287
+    put(x, 0, 260, 3, INF)
+    put(x, 0, 300, 4, -INF)
+    put(x, 0, 383, 5, NAN)
+    heads = 64 if empty else 512
+    got = check_attend(x, heads, q=x.rows(heads, by=0.5))
+    assert bool((got[:, :, 3] == INF).all()) and bool((got[:, :, 4] == -INF).all()) and bool(torch.isnan(got[:, :, 5]).all())
