@@ -61,7 +61,7 @@ __device__ __forceinline__ float2 turn_of(int position, float freq)
     return cs;
 }
 
-// A CTA has up to four tokens: finds their sequences by counting offsets, their pages, and the angles of every pair once for all heads;
+// A CTA has up to four tokens: finds their sequences among all offsets, their pages, and the angles of every pair once for all heads;
 // then a thread moves 16 bytes of a head (VEC; or one pair), and of its other half where the pairs lie apart.
 // Bound by reading and writing each value once: four prompts of up to 8192 tokens, 32 query heads on 8 of 128 values, bf16: 87 us, 5.8 TB/s.  A call
 // for few tokens by four reads that need each other (offsets, start, table, keys): 32 tokens 7.5 us.
@@ -69,37 +69,30 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(APPEND_THREADS) k_append(AppendArgs a)
 {
     __shared__ float2 turns[APPEND_TOKENS][LDA_HEAD_MAX_DIM / 2];
-    __shared__ int before[APPEND_TOKENS], s_position[APPEND_TOKENS], s_page[APPEND_TOKENS], s_place[APPEND_TOKENS];
+    __shared__ int seqs[APPEND_TOKENS], s_position[APPEND_TOKENS], s_page[APPEND_TOKENS], s_place[APPEND_TOKENS];
     const CacheView& c = a.cache;
     const int tid = threadIdx.x;
     const int64_t first = (int64_t)blockIdx.x * APPEND_TOKENS;
     const int tokens = (int)min((int64_t)APPEND_TOKENS, c.tokens - first);
-    if (tid < APPEND_TOKENS) before[tid] = 0;
+    if (tid < APPEND_TOKENS) seqs[tid] = -1;
     __syncthreads();
-    // a token's sequence: as many as end at it or before
-    int ended[APPEND_TOKENS] = {};
+    // a token's sequence: every one is asked whether the token is its own, as offsets that run nowhere say nothing of the others
     for (int b = tid; b < c.seqs; b += APPEND_THREADS) {
-        const int64_t end = c.offsets[b + 1];
+        const int64_t lo = c.offsets[b], hi = c.offsets[b + 1];
+        if (lo < 0 || hi > c.tokens || hi <= first || lo >= first + tokens) continue;
 #pragma unroll
-        for (int j = 0; j < APPEND_TOKENS; ++j) ended[j] += end <= first + j;
-    }
-#pragma unroll
-    for (int j = 0; j < APPEND_TOKENS; ++j) {
-        const int n = __reduce_add_sync(0xffffffffu, ended[j]);
-        if (tid % 32 == 0 && n) atomicAdd(&before[j], n);
+        for (int j = 0; j < APPEND_TOKENS; ++j)
+            if (lo <= first + j && first + j < hi) atomicMax(&seqs[j], b);
     }
     __syncthreads();
     if (tid < tokens) {
-        const int b = before[tid];
+        const int b = seqs[tid];
         int page = -2, place = 0, position = 0;  // -2: a token of no sequence, which is left alone
-        if (b < c.seqs) {
+        if (b >= 0) {
             const CacheSeq s = c.seq(b);
-            const int64_t i = first + tid - s.first;
-            if (i >= 0 && i < s.n) {
-                const int64_t slot = s.start + i;
-                page = slot <= 0x7fffffffll ? c.page(b, (uint32_t)slot, place) : -1;
-                position = a.positions ? a.positions[first + tid] : (int)slot;
-            }
+            const int64_t slot = s.start + (first + tid - s.first);
+            page = slot <= 0x7fffffffll ? c.page(b, (uint32_t)slot, place) : -1;
+            position = a.positions ? a.positions[first + tid] : (int)slot;
         }
         s_page[tid] = page, s_place[tid] = place, s_position[tid] = position;
     }
