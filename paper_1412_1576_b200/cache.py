@@ -203,6 +203,7 @@ def tree_attention(q, k_cache, v_cache, table, starts, offsets, mask=None, scale
     makes it) names; mask None: those up to itself.  Head h of q reads head h // (heads // kv_heads) of the cache.  scale: of the scores,
     None for dim ** -0.5.  out: where to, None for a new tensor.  What a token does not see does not touch its row, whatever it
     holds; a token that sees nothing gets zeros.  Rows of tokens that belong to no sequence stay as they are (in a new tensor: undefined).
+    Waits inside the kernel are bounded; should one ever give up, the rows concerned are NaN.
     """
     device = _cuda(q, "q")
     _unfollowed(q=q, k_cache=k_cache, v_cache=v_cache)

@@ -46,7 +46,7 @@ struct TcShape {
 };
 
 struct TcBars {
-    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[4], p_full[4], o_done[4], q_full, q_empty;  // (S, P and O: of a team's piece)
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[4], p_full[4], o_done[4], q_full, q_empty, cleaned[2], last[2];  // (S, P and O: of a team's piece)
 };
 
 __device__ __forceinline__ uint32_t tc_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -59,13 +59,17 @@ __device__ __forceinline__ void tc_expect(uint64_t& bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(tc_smem(&bar)), "r"(bytes) : "memory");
 }
-// Waits for a phase.  Every wait here ends by itself; one that has not after some seconds gives up and tells the others, which then do
-// not wait any more.
-constexpr int TC_POLLS = 1 << 22;
-__device__ __forceinline__ bool tc_wait(uint64_t& bar, uint32_t parity, volatile int* failed)
+// Waits for a phase.  Every wait here ends by itself, within microseconds; one that has not after so many polls (how long the hardware holds each
+// of them is its own affair) gives up and tells the others, which then do not wait any more, and the rows concerned become NaN.  A build with 0 polls
+// shows that: every wait gives up at once.
+#ifndef LDA_WAIT_POLLS
+#define LDA_WAIT_POLLS (1 << 22)
+#endif
+constexpr int TC_POLLS = LDA_WAIT_POLLS, TC_POLLS_LAST = 1 << 22;  // (of what is under way at the end, in any build)
+__device__ __forceinline__ bool tc_wait(uint64_t& bar, uint32_t parity, volatile int* failed, int polls = TC_POLLS)
 {
     const uint32_t at = tc_smem(&bar);
-    for (int i = 0; i < TC_POLLS; ++i) {
+    for (int i = 0; i < polls; ++i) {
         uint32_t done;
         asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
                      : "=r"(done)
@@ -76,6 +80,21 @@ __device__ __forceinline__ bool tc_wait(uint64_t& bar, uint32_t parity, volatile
     }
     *failed = 1;
     return false;
+}
+// Arrives, and waits for all others of the phase.  A barrier that the threads of a team meet at wherever they are, and unlike bar.sync none that
+// hangs where a wait before it gave up in some of them only.  (The phase goes by what the arrival returns: a count of phases is one register
+// more in loops that have none left, 8 us of the trees' 127.)
+__device__ __forceinline__ void tc_meet(uint64_t& bar, volatile int* failed)
+{
+    const uint32_t at = tc_smem(&bar);
+    uint64_t phase;
+    asm volatile("mbarrier.arrive.shared::cta.b64 %0, [%1];" : "=l"(phase) : "r"(at) : "memory");
+    for (int i = 0; i < TC_POLLS; ++i) {
+        uint32_t done;
+        asm volatile("{ .reg .pred p; mbarrier.try_wait.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(done) : "r"(at), "l"(phase) : "memory");
+        if (done || *failed) break;
+        if (i + 1 == TC_POLLS) *failed = 1;
+    }
 }
 // What a product reads or has written, seen by the other side of a barrier.
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -172,7 +191,6 @@ __device__ __forceinline__ void tc_copy(uint32_t to, const CUtensorMap* map, int
                  "l"(map), "r"(column), "r"(slot), "r"(head), "r"(page), "r"(tc_smem(&bar))
                  : "memory");
 }
-__device__ __forceinline__ void tc_team_sync(int team) { asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory"); }
 __device__ __forceinline__ void tc_rows_sync() { asm volatile("bar.sync 3, 256;" ::: "memory"); }
 __device__ __forceinline__ uint4 tc_shared16(uint32_t at)
 {
@@ -233,7 +251,7 @@ __device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap
     }
     if (units > 0) {  // gave up: what is under way still lands
         int quit = 0;
-        for (int i = max(0, it - STAGES); i < it; ++i) tc_wait(full[i % STAGES], i / STAGES & 1, (volatile int*)&quit);
+        for (int i = max(0, it - STAGES); i < it; ++i) tc_wait(full[i % STAGES], i / STAGES & 1, (volatile int*)&quit, TC_POLLS_LAST);
     }
 }
 
@@ -257,6 +275,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
         for (int i = 0; i < 4; ++i) tc_init(bars.k_full[i], 1), tc_init(bars.k_empty[i], 1), tc_init(bars.v_full[i], 1), tc_init(bars.v_empty[i], 1);
         for (int i = 0; i < 4; ++i) tc_init(bars.s_full[i], 1), tc_init(bars.p_full[i], TC_TEAM), tc_init(bars.o_done[i], 1);
         tc_init(bars.q_full, 2 * TC_TEAM), tc_init(bars.q_empty, 1);
+        for (int i = 0; i < 2; ++i) tc_init(bars.cleaned[i], TC_TEAM), tc_init(bars.last[i], 1);
         s_failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -372,7 +391,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
         }
         __syncwarp();
     } else {
-        // --- rows (they go on where a wait gave up, so that all of them meet at their barriers; outputs are undefined then)
+        // --- rows (they go on where a wait gave up, so that all of them meet at an item's end; outputs are NaN then)
         const int team = warp >> 2, kg = tid % TC_TEAM / RT;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
         const uint32_t at_s = tmem + lanes + TC_S + team * TC_KEYS, at_o = tmem + lanes + TC_O + team * 128;
@@ -472,8 +491,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    tc_team_sync(team);
-                    bad[0] = *(volatile unsigned long long*)&wild[vs][0], bad[1] = *(volatile unsigned long long*)&wild[vs][1];
+                    tc_meet(bars.cleaned[team], failed);
+                    // (the same in the warp, also where a wait gave up)
+                    for (int i = 0; i < 2; ++i) bad[i] = __shfl_sync(0xffffffffu, *(volatile unsigned long long*)&wild[vs][i], 0);
                 }
 #pragma unroll 1
                 for (int piece = 0; piece < PIECES; ++piece) {
@@ -621,6 +641,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             }
             if (any) tc_wait(bars.o_done[place_of(n_s - 1)], phase_of(n_s - 1), failed);
             tc_after();
+            if (*failed) l = NAN;  // (and with the norm all of the row, here or where the parts are put together)
             const bool whole = ends && item_begin >= share.lo;
             const int slot = 2 * blockIdx.x + (item_begin < share.lo ? 0 : 1);
             const auto out_at = [&](int row) {
@@ -716,6 +737,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
             item = after;
         }
         if (tid == 0) a.begun[blockIdx.x] = begun;
+    }
+    // what the two warps have issued, arrivals among it, ends before the tensor memory is given back and the CTA goes (here, and not at the end of
+    // their branch: there it costs the products' loops registers, and trees take 8 us more)
+    if (const int issuer = threadIdx.x >> 5; issuer == 8 || issuer == 11) {
+        uint64_t& mine = bars.last[issuer & 1];
+        int quit = 0;
+        tc_commit(mine, threadIdx.x % 32 == 0);
+        tc_wait(mine, 0, (volatile int*)&quit, TC_POLLS_LAST);
     }
     tc_before();
     __syncthreads();
