@@ -214,6 +214,35 @@ constexpr float TC_SLACK = 8.0f;
 template <typename T>
 constexpr float TC_RAISE = T_is_bf16<T> ? 0.0f : 7.0f;
 
+// Of four columns of a row's sums, what is NaN although the row's norm is a number: what the infinities and NaN among the values of the keys
+// first .. end - 1 that the row sees make of it.  An infinity that all rows see stays in its tile, and times the zeros that a row's copies have for
+// each other's keys it is NaN.  (A function of its own: a call that needs it is rare, and the others do not fetch its code.)
+template <typename T>
+__device__ __noinline__ float4 tc_wild(const AttendArgs& a, float4 of, int b, int head, int64_t row, int first, int end, int column)
+{
+    const CacheView& c = a.cache;
+    const CacheSeq seq = c.seq(b);
+    const int place = (int)attend_quotient(row, a.group);
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+        float& x = i == 0 ? of.x : i == 1 ? of.y : i == 2 ? of.z : of.w;
+        if (!isnan(x)) continue;
+        const T* values = (const T*)c.values + head * c.v_head + column + i;
+        float sum = 0.0f;
+        unsigned long long see = 0;
+#pragma unroll 1
+        for (int key = first; key < end && sum == sum; ++key) {
+            if (key % 64 == 0) see = attend_window(a, seq, place, key / 64);  // (first: of a tile)
+            int slot = 0;
+            const int64_t page = see >> (key % 64) & 1 ? c.page(b, (uint32_t)key, slot) : -1;
+            const float v = page < 0 ? 0.0f : cache_value(values[page * c.v_page + slot * c.v_slot]);
+            if (!(fabsf(v) < INFINITY)) sum += v;
+        }
+        if (sum != 0.0f) x = sum;
+    }
+    return of;
+}
+
 // A copying warp's walk over its CTA's units, for keys or for values: a lane has one of the tile's groups of slots.
 template <int DIM, int ROWS, int STAGES>
 __device__ __forceinline__ void tc_copies(const AttendArgs& a, const CUtensorMap* map, int bits, AttendItem item, int64_t units, uint32_t to,
@@ -698,6 +727,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 for (int first = 0; first < rows; first += together) {
                     const bool here = r >= first && r < first + together && r < rows;
                     if (first > 0) tc_rows_sync();
+                    // (behind a row's sums of the first part, its norm)
+                    if (GROUPS > 1 && here && tid < RT)
+                        tc_put16(region + ((r - first) * S::PITCH + DIM) * 4, make_uint4(__float_as_uint(norm), 0, 0, 0));
                     if (__any_sync(0xffffffffu, here))
 #pragma unroll 1
                         for (int d = 0; d < c.dim; d += 32) {
@@ -723,6 +755,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         for (int g = 0; g < 2 * GROUPS; ++g) {
                             const uint4 y = tc_shared16(region + ((g * together + rr) * S::PITCH + col) * 4);
                             x.x += __uint_as_float(y.x), x.y += __uint_as_float(y.y), x.z += __uint_as_float(y.z), x.w += __uint_as_float(y.w);
+                        }
+                        if constexpr (GROUPS > 1) {
+                            const float all = x.x + x.y + x.z + x.w;
+                            if (all != all && !isnan(__uint_as_float(tc_shared16(region + (rr * S::PITCH + DIM) * 4).x)))
+                                x = tc_wild<T>(a, x, item.b, item.head, row0 + first + rr, item.tile * TC_KEYS, min((item.tile + count) * TC_KEYS, item.keys), col);
                         }
                         if (whole) *(uint2*)(out_at(first + rr) + col) = make_uint2(pack_two<T>(x.x, x.y), pack_two<T>(x.z, x.w));
                         else *(float4*)(a.part + ((int64_t)slot * ROWS + first + rr) * DIM + col) = x;

@@ -57,3 +57,24 @@ def test_values_beside_a_missing_page(empty, new, dim):
     heads = 64 if empty else 512
     got = check_attend(x, heads, q=x.rows(heads, by=0.5))
     assert bool((got[:, :, 3] == INF).all()) and bool((got[:, :, 4] == -INF).all()) and bool(torch.isnan(got[:, :, 5]).all())
+
+
+# (the same operator by other rows of a tile, and by the kernel for other pages and heads; one head of the cache, whose keys several CTAs share, and many)
+@pytest.mark.parametrize("new,empty,group,dim,page", [(40, 0, 8, 64, 16), (40, 0, 8, 128, 16), (40, 0, 2, 128, 16), (24, 0, 1, 128, 16), (24, 1, 2, 64, 16),
+                                                      (1, 0, 1, 64, 16), (1, 0, 8, 128, 16), (5, 0, 3, 80, 24), (1, 0, 8, 128, 4), (5, 0, 4, 256, 16), (40, 0, 8, 64, 4)])
+@pytest.mark.parametrize("kv_heads", [1, 48])
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+def test_infinities_in_a_context_that_all_see(new, empty, group, dim, page, kv_heads, dtype):
+    """In the context's tiles nothing is hidden; an infinity among the values is the row's output in its column, and not a NaN."""
+    x = batch([1500], [new], kv_heads, empty, dim, dtype, page)
+    heads = group * kv_heads
+    for slot, column, kind in [(0, 1, INF), (130, 2, -INF), (700, 3, INF), (1400, 3, INF), (64, 4, INF), (1000, 4, -INF), (900, 5, NAN), (901, 5, INF),
+                               (1407, 6, INF), (1408, 7, -INF), (1499, 7, -INF)]:
+        put(x, 0, slot, column, kind)
+    got = check_attend(x, heads, q=x.rows(heads, by=0.5))
+    assert bool((got[:, :, 1] == INF).all()) and bool((got[:, :, 2] == -INF).all()) and bool(torch.isnan(got[:, :, 4:6]).all())
+    put(x, 0, 1500, 9, -INF)               # with one among the new tokens, and a row of which nothing is a number
+    q = x.rows(heads, by=0.5)
+    q[0, 0, 0] = NAN
+    got = check_attend(x, heads, q=q)
+    assert bool(torch.isnan(got[0, 0]).all())
