@@ -387,7 +387,10 @@ int lda_token_logprobs_grad(const void* logits_dev, int dtype, int64_t rows, int
  *   offsets    [n_seqs + 1]: sequence b has the new tokens offsets[b] .. offsets[b+1] - 1 of the call's `tokens`, in the slots
  *              from starts[b] on.  Offsets that do not run upwards inside [0, tokens] leave the sequence out; rows of outputs that belong
  *              to no sequence stay as they are, and what several sequences claim is undefined, as are slots that several tokens get
- * Rows of heads (keys, values, queries, outputs) are [tokens, heads, dim] with two strides. */
+ * Rows of heads (keys, values, queries, outputs) are [tokens, heads, dim] with two strides.  Strides are at most 2^31 elements.
+ * What is written (the cache by lda_append_cache, rows of outputs) overlaps neither itself nor the inputs, but for rows of outputs in their queries'
+ * very places; strides of written tensors by which their elements share places (0, of an expanded tensor), and rows of outputs that lie
+ * across their queries, are refused. */
 #define LDA_HEAD_MAX_DIM 256
 #define LDA_HEADS_MAX 1024
 #define LDA_MASK_MAX_WORDS 64
@@ -402,7 +405,7 @@ typedef struct lda_paged_cache {
     int32_t table_width;
 } lda_paged_cache;
 
-/* New tokens' keys and values into the cache; keys, and the queries q[tokens][heads] (heads 0: none) into q_out (q itself is allowed), are rotated
+/* New tokens' keys and values into the cache; keys, and the queries q[tokens][heads] (heads 0: none) into q_out, are rotated
  * on the way: of the first `rotated` elements of a head, pair i (elements i and i + rotated / 2; interleaved: 2 i and 2 i + 1) by the
  * angle positions[token] inv_freq[i], worked out in 64 bits (positions NULL: the token's slot).  rotated 0: nothing is. */
 int lda_append_cache(const lda_paged_cache* cache, int64_t tokens, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,

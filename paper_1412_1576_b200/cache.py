@@ -153,7 +153,8 @@ def append_cache(k, v, k_cache, v_cache, table, starts, offsets, positions=None,
 
     k, v: [tokens, kv_heads, dim] in the cache's type.  inv_freq: float32 [n], None for no rotation: of a head's first 2 n values pair i is
     turned by positions[token] * inv_freq[i]; a pair lies n values apart, or side by side (interleaved).  positions: int32 [tokens], None
-    for the tokens' slots.  q: [tokens, heads, dim], rotated like the keys; q_out: where to, None for a new tensor, q itself is allowed.
+    for the tokens' slots.  q: [tokens, heads, dim], rotated like the keys; q_out: where to, None for a new tensor, q itself is allowed, any other
+    overlap is not.  Neither the cache nor q_out may be an expanded tensor, whose elements share their places.
     Returns the rotated queries (None without q).  Tokens of no sequence, and slots that the table has no page for, are left alone.
     """
     device = _cuda(k, "k")
@@ -201,8 +202,9 @@ def tree_attention(q, k_cache, v_cache, table, starts, offsets, mask=None, scale
 
     A token sees its sequence's slots before the new tokens, and of these the ones that its row of ``mask`` (int64 [tokens, words], as ``tree_mask``
     makes it) names; mask None: those up to itself.  Head h of q reads head h // (heads // kv_heads) of the cache.  scale: of the scores,
-    None for dim ** -0.5.  out: where to, None for a new tensor.  What a token does not see does not touch its row, whatever it
-    holds; a token that sees nothing gets zeros.  Rows of tokens that belong to no sequence stay as they are (in a new tensor: undefined).
+    None for dim ** -0.5.  out: where to, None for a new tensor; q itself is allowed, any other overlap and expanded tensors are not.  What a token
+    does not see does not touch its row, whatever it holds; a token that sees nothing gets zeros.  Rows of tokens that belong to no sequence
+    stay as they are (in a new tensor: undefined).
     Waits inside the kernel are bounded; should one ever give up, the rows concerned are NaN.
     """
     device = _cuda(q, "q")

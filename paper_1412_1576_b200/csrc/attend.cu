@@ -546,6 +546,7 @@ extern "C" int lda_tree_attention(const lda_paged_cache* cache, int64_t tokens, 
     if (!heads_ok(q_dev, q_token_stride, q_head_stride) || !heads_ok(out_dev, out_token_stride, out_head_stride)) return LDA_EINVAL;
     const int64_t most = 1ll << 31;
     if (q_token_stride > most || q_head_stride > most || out_token_stride > most || out_head_stride > most) return LDA_ERANGE;
+    if (!heads_apart(q_dev, q_token_stride, q_head_stride, out_dev, out_token_stride, out_head_stride, tokens, heads, cache->dim)) return LDA_EINVAL;
     const AttendPlan plan(*cache, tokens, heads);
     if (!workspace_dev || !aligned(workspace_dev, 32) || workspace_bytes < plan.all) return LDA_EINVAL;
     a.ctas = plan.ctas, a.rows = plan.rows;

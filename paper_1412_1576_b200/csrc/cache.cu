@@ -307,6 +307,9 @@ extern "C" int lda_append_cache(const lda_paged_cache* cache, int64_t tokens, co
     if (k_token_stride > most || k_head_stride > most || v_token_stride > most || v_head_stride > most || q_token_stride > most ||
         q_head_stride > most || out_token_stride > most || out_head_stride > most)
         return LDA_ERANGE;
+    const int64_t sizes[3] = {cache->pages, cache->page_size, cache->kv_heads};
+    if (!strides_apart(sizes, cache->key_strides, cache->dim) || !strides_apart(sizes, cache->value_strides, cache->dim)) return LDA_EINVAL;
+    if (heads > 0 && !heads_apart(q_dev, q_token_stride, q_head_stride, q_out_dev, out_token_stride, out_head_stride, tokens, heads, cache->dim)) return LDA_EINVAL;
     a.k = k_dev, a.v = v_dev, a.q = q_dev, a.q_out = q_out_dev;
     a.k_token = k_token_stride, a.k_head = k_head_stride, a.v_token = v_token_stride, a.v_head = v_head_stride;
     a.q_token = q_token_stride, a.q_head = q_head_stride, a.out_token = out_token_stride, a.out_head = out_head_stride;

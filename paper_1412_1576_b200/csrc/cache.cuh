@@ -66,6 +66,46 @@ inline bool heads_ok(const void* p, int64_t token_stride, int64_t head_stride)
     return p && (uintptr_t)p % 16 == 0 && token_stride % 8 == 0 && head_stride % 8 == 0 && token_stride >= 0 && head_stride >= 0;
 }
 
+// Whether no two elements of a tensor that is written to share their place, by dimensions of n values and a stride each, `width` consecutive elements in
+// the innermost: a stride passes over all that the smaller ones cover, as in any permuted or sliced tensor.
+template <int N>
+inline bool strides_apart(const int64_t (&n)[N], const int64_t (&stride)[N], int64_t width)
+{
+    uint64_t covered = (uint64_t)width;
+    bool done[N] = {};
+    for (int round = 0; round < N; ++round) {
+        int least = -1;
+        for (int i = 0; i < N; ++i)
+            if (!done[i] && n[i] > 1 && (least < 0 || stride[i] < stride[least])) least = i;
+        if (least < 0) break;
+        done[least] = true;
+        if ((uint64_t)stride[least] < covered) return false;
+        covered += (uint64_t)(n[least] - 1) * (uint64_t)stride[least];
+    }
+    return true;
+}
+
+// Whether rows of heads that are written (of 16-bit elements) share no place with each other, and none with those that are read but for lying in their
+// very places.
+inline bool heads_apart(const void* q, int64_t q_token, int64_t q_head, const void* out, int64_t out_token, int64_t out_head, int64_t tokens, int64_t heads,
+                        int64_t dim)
+{
+    if (!strides_apart({tokens, heads}, {out_token, out_head}, dim)) return false;
+    if (tokens == 1) q_token = out_token = 0;  // (never taken)
+    if (heads == 1) q_head = out_head = 0;
+    const int64_t delta = ((intptr_t)out - (intptr_t)q) / 2;
+    if (delta >= (tokens - 1) * q_token + (heads - 1) * q_head + dim || -delta >= (tokens - 1) * out_token + (heads - 1) * out_head + dim) return true;
+    if (q_token != out_token || q_head != out_head) return false;
+    if (delta == 0) return true;
+    // two parts of the same rows: is there a token and a head with |delta + token x stride + head x stride| < dim?
+    for (int64_t h = 1 - heads; h < heads; ++h) {
+        const int64_t at = delta + h * q_head, near = q_token ? -at / q_token : 0;
+        for (int64_t t = near - 1; t <= near + 1; ++t)
+            if (t > -tokens && t < tokens && at + t * q_token < dim && at + t * q_token > -dim) return false;
+    }
+    return true;
+}
+
 __device__ __forceinline__ float cache_value(__half x) { return __half2float(x); }
 __device__ __forceinline__ float cache_value(__nv_bfloat16 x) { return __bfloat162float(x); }
 
