@@ -214,15 +214,16 @@ constexpr float TC_SLACK = 8.0f;
 template <typename T>
 constexpr float TC_RAISE = T_is_bf16<T> ? 0.0f : 7.0f;
 
-// Of four columns of a row's sums, what is NaN although the row's norm is a number: what the infinities and NaN among the values of the keys
-// first .. end - 1 that the row sees make of it.  An infinity that all rows see stays in its tile, and times the zeros that a row's copies have for
+// Of four columns of a row's sums, what is NaN although the row's norm is a number: what the infinities and NaN among the values of the keys of
+// `count` tiles that the row sees make of it.  An infinity that all rows see stays in its tile, and times the zeros that a row's copies have for
 // each other's keys it is NaN.  (A function of its own: a call that needs it is rare, and the others do not fetch its code.)
 template <typename T>
-__device__ __noinline__ float4 tc_wild(const AttendArgs& a, float4 of, int b, int head, int64_t row, int first, int end, int column)
+__device__ __noinline__ float4 tc_wild(const AttendArgs& a, float4 of, int b, int head, int64_t row0, int row, int tile, int count, int keys, int column)
 {
     const CacheView& c = a.cache;
     const CacheSeq seq = c.seq(b);
-    const int place = (int)attend_quotient(row, a.group);
+    const int place = (int)attend_quotient(row0 + row, a.group);
+    const int64_t first = (int64_t)tile * TC_KEYS, end = min((int64_t)(tile + count) * TC_KEYS, (int64_t)keys);
 #pragma unroll 1
     for (int i = 0; i < 4; ++i) {
         float& x = i == 0 ? of.x : i == 1 ? of.y : i == 2 ? of.z : of.w;
@@ -231,12 +232,20 @@ __device__ __noinline__ float4 tc_wild(const AttendArgs& a, float4 of, int b, in
         float sum = 0.0f;
         unsigned long long see = 0;
 #pragma unroll 1
-        for (int key = first; key < end && sum == sum; ++key) {
-            if (key % 64 == 0) see = attend_window(a, seq, place, key / 64);  // (first: of a tile)
+        for (int64_t key = first; key < end && sum == sum; key += 8) {  // (eight slots of a page at a time)
+            if (key % 64 == 0) see = attend_window(a, seq, place, (int)(key / 64));
+            uint32_t bits = (uint32_t)(see >> (key % 64)) & 0xFFu;
+            if (end - key < 8) bits &= (1u << (end - key)) - 1;
             int slot = 0;
-            const int64_t page = see >> (key % 64) & 1 ? c.page(b, (uint32_t)key, slot) : -1;
-            const float v = page < 0 ? 0.0f : cache_value(values[page * c.v_page + slot * c.v_slot]);
-            if (!(fabsf(v) < INFINITY)) sum += v;
+            const int64_t page = bits ? c.page(b, (uint32_t)key, slot) : -1;
+            if (page < 0) continue;
+            const T* from = values + page * c.v_page + slot * c.v_slot;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = bits >> e & 1 ? cache_value(from[e * c.v_slot]) : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!(fabsf(v[e]) < INFINITY)) sum += v[e];
         }
         if (sum != 0.0f) x = sum;
     }
@@ -759,7 +768,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                         if constexpr (GROUPS > 1) {
                             const float all = x.x + x.y + x.z + x.w;
                             if (all != all && !isnan(__uint_as_float(tc_shared16(region + (rr * S::PITCH + DIM) * 4).x)))
-                                x = tc_wild<T>(a, x, item.b, item.head, row0 + first + rr, item.tile * TC_KEYS, min((item.tile + count) * TC_KEYS, item.keys), col);
+                                x = tc_wild<T>(a, x, item.b, item.head, row0, first + rr, item.tile, count, item.keys, col);
                         }
                         if (whole) *(uint2*)(out_at(first + rr) + col) = make_uint2(pack_two<T>(x.x, x.y), pack_two<T>(x.z, x.w));
                         else *(float4*)(a.part + ((int64_t)slot * ROWS + first + rr) * DIM + col) = x;

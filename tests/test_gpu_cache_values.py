@@ -78,3 +78,20 @@ def test_infinities_in_a_context_that_all_see(new, empty, group, dim, page, kv_h
     q[0, 0, 0] = NAN
     got = check_attend(x, heads, q=q)
     assert bool(torch.isnan(got[0, 0]).all())
+
+
+def test_an_infinity_at_the_end_of_the_longest_sequence():
+    """Numbers of keys up to 2^31 - 9: all entries of the table name one page, and a last one another, with the infinity."""
+    width = 2**28 - 1
+    k = torch.zeros(2, 8, 1, 8, dtype=F16, device="cuda")
+    v = torch.ones_like(k)
+    v[1, 3, 0, 2], v[1, 5, 0, 4] = INF, -INF
+    table = torch.zeros(1, width, dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    starts = torch.tensor([8 * width - 1], dtype=torch.int32).cuda()
+    got = cache.tree_attention(torch.ones(1, 4, 8, dtype=F16, device="cuda"), k, v, table, starts, torch.tensor([0, 1]).cuda())
+    want = torch.ones(8)
+    want[2], want[4] = INF, -INF
+    # (the norm's and the outputs' sums are of single precision, 2^31 / 148 terms each: the same terms in other orders)
+    assert torch.equal(torch.isinf(got[0].cpu()), torch.isinf(want).expand(4, 8)) and bool((got[0, :, 2] == INF).all()) and bool((got[0, :, 4] == -INF).all())
+    assert not bool(torch.isnan(got).any())
