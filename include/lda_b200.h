@@ -424,7 +424,7 @@ int lda_tree_mask(const int32_t* parents_dev, const int64_t* offsets_dev, int64_
  * before its new tokens and over the new tokens j whose bit is set in the token's words of mask[tokens] (mask_stride words apart;
  * NULL: those up to itself).  Query head h reads head h / (heads / kv_heads) of the cache.  What a token does not see
  * does not touch it, NaN and infinities among it; a token that sees nothing gets zeros, and one that sees an infinity among the values has it
- * in its output (a weight of 0 in single precision or in 16 bits may make NaN of it, or nothing).  scale: 1e-6 .. 1e6.  Weights are rounded to
+ * in its output (a weight of 0 in single precision or in 16 bits may make NaN of it).  scale: 1e-6 .. 1e6.  Weights are rounded to
  * the type of the values, sums are of single precision.  Waits inside the kernel are bounded: should one ever give up, the rows concerned are NaN.
  * The workspace (at a multiple of 32 bytes; its size by lda_tree_attention_workspace, or a negative status; no less for the same cache,
  * tokens and heads) holds nothing between calls: calls that may overlap need one each. */

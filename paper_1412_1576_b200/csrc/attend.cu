@@ -264,20 +264,14 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
                 mma_16x8x16<T>(o[2 * d + 1], p, b[2], b[3]);
             }
         }
+        // (what was taken out: a row that sees it has it, whatever the probability)
         for (unsigned long long left = bad; left; left &= left - 1) {
             const int row = __ffsll((long long)left) - 1, at = row - key0;
             if (at < 0 || at >= KEYS / S::KEY_GROUPS) continue;
-            float p[2] = {0.0f, 0.0f};
+            float sees[2];
 #pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (at == 8 * n + 2 * (lane & 3) + (e & 1)) p[e >> 1] += s[n][e];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                p[i] += __shfl_xor_sync(0xffffffffu, p[i], 1);
-                p[i] += __shfl_xor_sync(0xffffffffu, p[i], 2);
-            }
+            for (int i = 0; i < 2; ++i)
+                sees[i] = place_of[i] >= 0 && attend_window(a, item.seq, place_of[i], item.tile) >> row & 1 ? 1.0f : 0.0f;
             int slot = 0;
             const int64_t pg = c.page(item.b, (uint32_t)(item.tile * KEYS + row), slot);
             if (pg < 0) continue;
@@ -288,8 +282,8 @@ __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendAr
                 for (int e = 0; e < 2; ++e) {
                     const float x = 8 * n < c.dim ? cache_value(v[8 * n + e]) : 0.0f;
                     if (!(fabsf(x) < INFINITY)) {
-                        if (p[0] != 0.0f) o[n][e] += p[0] * x;
-                        if (p[1] != 0.0f) o[n][2 + e] += p[1] * x;
+                        if (sees[0] != 0.0f) o[n][e] += x;
+                        if (sees[1] != 0.0f) o[n][2 + e] += x;
                     }
                 }
         }

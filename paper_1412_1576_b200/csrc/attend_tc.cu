@@ -623,21 +623,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                 }
                 l += sum.x + sum.y;
                 tc_stored();
-                // (what is taken out below needs its probabilities when the outputs are done; the next scores may stand in their place by then,
-                // so they are read before the products may begin.  In local memory, which nothing else here uses)
-                uint32_t kept[COLS / 2];
-                if (bad[0] | bad[1])
-#pragma unroll 1
-                    for (int i = 0; i < COLS / 2; i += 8) {
-                        uint32_t x[8];
-                        tc_load(x, at_piece + PIECE / 2 + kg * COLS / 2 + i);
-                        tc_loaded(x);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) kept[i + e] = x[e];
-                    }
                 tc_before();
                 tc_arrive(bars.p_full[place_of(n_s)]);
                 any = true;
+                // (what was taken out: a row that sees it has it, whatever the probability, which cannot be read any more: the outputs being done, the
+                // next scores may stand in its place)
                 if (bad[0] | bad[1]) {
                     tc_wait(bars.o_done[place_of(n_s)], phase_of(n_s), failed);
                     tc_after();
@@ -645,9 +635,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                     for (int i = 0; i < COLS; ++i) {
                         const int k = piece * PIECE + kg * COLS + i;
                         if (!((k < 64 ? bad[0] : bad[1]) >> (k & 63) & 1)) continue;  // (the same in the warp)
-                        const uint32_t two = kept[i / 2];
-                        const uint16_t half = (uint16_t)(k & 1 ? two >> 16 : two);
-                        const float p = cache_value(*reinterpret_cast<const T*>(&half));
+                        const bool sees = (k < 64 ? see[0] : see[1]) >> (k & 63) & 1;
                         int slot = 0;
                         const int64_t pg = c.page(item.b, (uint32_t)(tile * TC_KEYS + k), slot);
                         const T* v = (const T*)c.values + pg * c.v_page + slot * c.v_slot + item.head * c.v_head;
@@ -660,7 +648,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_attend_tc(const __grid_consta
                             tc_loaded(o);
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                if (p != 0.0f && !(fabsf(x[e]) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + p * x[e]);
+                                if (sees && !(fabsf(x[e]) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + x[e]);
                             tc_store(at_o + d, o);
                             tc_stored();
                         }

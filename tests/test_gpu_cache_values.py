@@ -95,3 +95,17 @@ def test_an_infinity_at_the_end_of_the_longest_sequence():
     # (the norm's and the outputs' sums are of single precision, 2^31 / 148 terms each: the same terms in other orders)
     assert torch.equal(torch.isinf(got[0].cpu()), torch.isinf(want).expand(4, 8)) and bool((got[0, :, 2] == INF).all()) and bool((got[0, :, 4] == -INF).all())
     assert not bool(torch.isnan(got).any())
+
+
+@pytest.mark.parametrize("new,empty,heads,dim,page", [(300, 0, 64, 64, 16), (300, 15, 32, 128, 16), (300, 40, 32, 64, 16), (300, 0, 8, 64, 4), (40, 0, 8, 256, 16)])
+def test_an_infinity_of_next_to_no_weight(new, empty, heads, dim, page):
+    """Among the new tokens' values, at keys whose weights are far below what single precision has: those who see it have it, the others do not."""
+    x = batch([200], [new], heads, empty, dim, BF16, page)
+    q = x.rows(heads)
+    q[:] = 2.0
+    pages, places = x.slots(0)
+    x.k[:] = 1.0
+    x.k[pages[200 + 5], places[200 + 5]] = -6.0       # (scores lower by 14 times the head's values)
+    x.v[pages[200 + 5], places[200 + 5], :, 3] = INF
+    got = cache.tree_attention(q, x.k, x.v, *x.where(), scale=1.0)[:new]
+    assert bool((got[5:, :, 3] == INF).all()) and bool(torch.isfinite(got[:5]).all()) and bool(torch.isfinite(got[:, :, :3]).all())
