@@ -6,10 +6,10 @@ the cache (``tree_attention``), which is also that of an ordinary decoding step,
 work is done by the entry points of the same names in ``include/lda_b200.h``, queued on the current stream of the tensors' device.  There is no
 fallback: tensors that are not on a GPU are refused, and so are tracing and tensors that autograd follows (there is no backward pass).
 
-A cache is a pair of tensors [pages, page_size, kv_heads, dim] in float16 or bfloat16, of any strides that are multiples of 16 bytes (so one
-that lies head by head is handed over as a transposed view).  ``table``: int32 [sequences, most pages], the pages of each sequence in order;
-``starts``: int32 [sequences], the slots that a sequence has before its new tokens; ``offsets``: int64 [sequences + 1], where each
-sequence's new tokens begin among those of the call.
+A cache is a pair of tensors [pages, page_size, kv_heads, dim] in float16 or bfloat16, of any strides that are multiples of 16 bytes and at most
+2^31 elements (so one that lies head by head is handed over as a transposed view).  ``table``: int32 [sequences, most pages], the pages of each
+sequence in order; ``starts``: int32 [sequences], the slots that a sequence has before its new tokens; ``offsets``: int64 [sequences + 1], where
+each sequence's new tokens begin among those of the call (a sequence whose own two do not run upwards inside the tokens is left out).
 """
 
 from __future__ import annotations
@@ -200,8 +200,8 @@ def append_cache(k, v, k_cache, v_cache, table, starts, offsets, positions=None,
 def tree_attention(q, k_cache, v_cache, table, starts, offsets, mask=None, scale: float | None = None, out=None):
     """Attention of new tokens, whose keys and values ``append_cache`` has put into the cache, over the cache: [tokens, heads, dim].
 
-    A token sees its sequence's slots before the new tokens, and of these the ones that its row of ``mask`` (int64 [tokens, words], as ``tree_mask``
-    makes it) names; mask None: those up to itself.  Head h of q reads head h // (heads // kv_heads) of the cache.  scale: of the scores,
+    A token sees its sequence's slots before the new tokens, and of the new tokens those that its row of ``mask`` (int64 [tokens, words], as
+    ``tree_mask`` makes it) names; mask None: those up to itself.  Head h of q reads head h // (heads // kv_heads) of the cache.  scale: of the scores,
     None for dim ** -0.5.  out: where to, None for a new tensor; q itself is allowed, any other overlap and expanded tensors are not.  What a token
     does not see does not touch its row, whatever it holds; a token that sees nothing gets zeros.  Rows of tokens that belong to no sequence
     stay as they are (in a new tensor: undefined).

@@ -48,9 +48,9 @@ struct AttendShape {
 // A CTA of four warps walks over its units; a warp has 16 rows and, with fewer than four groups of rows, a share of every tile's keys.
 // Tiles of keys and values come by asynchronous copies of 16 bytes into a ring of stages (a warp brings 16 keys of each; pages may lie
 // anywhere), two or three tiles ahead, across the ends of items; what lies behind the last key is filled with zeros.
-// 64 sequences of up to 8192 slots in pages of 4, one token each, 32 query heads on 8 of 128 values: 314 us, 4.3 TB/s (in pages of 16 277, for the
-// 213 of the other kernel).  Bound by latency: eight warps of a multiprocessor go through copies, products and exponentials one after the other
-// (issue slots 36 % full).
+// 64 sequences of up to 8192 slots in pages of 4, one token each, 32 query heads on 8 of 128 values: 316 us, 4.3 TB/s (in pages of 16 277, for the
+// 212 to 230 of the other kernel); with heads of 256 872 us, 3.1 TB/s.  Bound by latency: eight warps of a multiprocessor, four with heads of 256, go
+// through copies, products and exponentials one after the other (issue slots 36 and 22 % full).
 template <typename T, int DIM, int ROWS>
 __global__ void __launch_bounds__(128) k_attend(const __grid_constant__ AttendArgs a)
 {
@@ -446,7 +446,11 @@ struct AttendPlan {
     {
         tc = attend_tc_takes(cache);
         dim = cache.dim <= 64 ? 64 : cache.dim <= 128 ? 128 : 256;
-        // those that a sequence has on average share what is read from shared memory
+        // Those that a sequence has on average share what is read from shared memory.  Of 32 sequences of up to 4096 slots, all with as many rows, heads of
+        // 128, in us: by 32 rows, 64 and 256 with 16 rows a sequence 75, 76, 89, with 24 82, 78, 93, with 40 140, 85, 96, with 96 235, 159, 116 (64 would
+        // do up to 64 rows where all have as many; where some have more than the average, 256 read their keys once).  Without tensor memory, pages of 4: by 16,
+        // 32 and 64 rows with 16 rows a sequence 95, 103, 121, with 20 170, 107, 124, with 40 248, 192, 125; heads of 256 by 16 and 32 with 16 154, 164, with
+        // 20 276, 171.
         const int64_t most = (tokens + cache.n_seqs - 1) / cache.n_seqs * (heads / cache.kv_heads);
         if (tc) rows = most <= 16 ? 32 : most <= 32 ? 64 : 256;
         else rows = most <= 16 ? 16 : most <= 32 || dim == 256 ? 32 : 64;

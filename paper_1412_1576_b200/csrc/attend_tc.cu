@@ -1,9 +1,9 @@
 // Attention over a paged cache on the tensor cores' own memory: heads of up to 128 values, pages of a multiple of 8 slots.
 //
-// A tile has 128 keys and 128 rows.  S = Q K^T and O += P V are matrix products of a whole tile, issued by one thread: K and V from shared
-// memory, where tensor copies bring them page by page, S, P and O in tensor memory (P in S's place).  There are two teams of four warps, each
-// with an S and an O of its own; a thread has a row: it reads the row's scores, makes probabilities of them and writes these back, while the
-// products of the other team run.
+// A tile has 128 keys and 128 rows.  S = Q K^T and O += P V are matrix products of a tile, or of half its keys (PIECES), each issued by one thread
+// of a warp of its own: K and V from shared memory, where tensor copies bring them page by page, S, P and O in tensor memory (P in S's place).
+// There are two teams of four warps, each with an S and an O of its own; a thread has a row: it reads the row's scores, makes probabilities of
+// them and writes these back, while the products of the other team run.
 //   items of more than 128 rows  the teams have 128 rows each, and every tile of keys serves both
 //   others                       the teams take the tiles of keys in turn, and the two O are added up at the item's end.  Of 64 or 32 rows
 //                                (ROWS) every one stands in the tile twice or four times, and each of its copies has the probabilities of
@@ -11,11 +11,11 @@
 // The products cost the same, 128 rows or 4: 1024 cycles of the tensor cores for a tile of 128 values a head, whose keys and values take 2800
 // cycles to come from memory.
 // Measured (bf16, heads of 128, 32 query heads on 8 of the cache; replayed graphs of five calls, a call being this kernel and the join):
-//   64 sequences of up to 8192 slots, one token each   213 to 217 us, 6.2 TB/s (the copy's rate is 6.5): memory.  A long run of calls draws 1000 W
-//                                                      and takes 232 to 252, at 1.5 to 1.6 GHz
-//   16 sequences of up to 8192, trees of up to 64      127 us, 425 TFLOP/s: the warps that issue products and their waits (a piece of 64 keys:
-//                                                      1200 cycles of its warp, 400 of the tensor cores), then starting up and the join
-//   one sequence of 32 768, 8 tokens                   39 us: 20 of memory, 9 to the first tile's end, 8 the join
+//   64 sequences of up to 8192 slots, one token each   212 to 230 us on different cards, 5.8 to 6.3 TB/s (the copy's rate is 6.5): memory.  A long
+//                                                      run of calls draws 1000 W and takes 229 to 252, at 1.5 to 1.6 GHz
+//   16 sequences of up to 8192, trees of up to 64      127 to 130 us, 420 TFLOP/s: the warps that issue products and their waits (a piece of 64
+//                                                      keys: 1200 cycles of its warp, 400 of the tensor cores), then starting up and the join
+//   one sequence of 32 768, 8 tokens                   40 us: 20 of memory, 9 to the first tile's end, 8 the join
 // With one warp for all products 44, 225 and 147 us; with one for each team's scores and outputs (four, 128 registers a thread) 48, 223 and
 // 137; the scores of a tile in one piece 153 (trees); the matrix instructions of the other kernel (attend.cu) 51, 277 and 297.
 #include <cuda.h>

@@ -9,8 +9,8 @@
 
 namespace lda {
 
-// Division of numbers below 2^31 by a number that a launch knows: n d^-1 as a product by a 33-bit reciprocal rounded up (off by less
-// than 2^-31 / d, which no quotient of such numbers notices).
+// Division of numbers below 2^31 by a number that a launch knows, after Granlund and Montgomery (Division by invariant integers using
+// multiplication, 1994): n d^-1 as a product by a 33-bit reciprocal rounded up (off by less than 2^-31 / d, which no quotient of such numbers notices).
 struct Divider {
     uint32_t d, magic, shift;
     Divider() = default;
